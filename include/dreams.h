@@ -82,6 +82,9 @@ typedef enum dreams_dtype { DREAMS_F32 = 0, DREAMS_BF16 = 1 } dreams_dtype_t;
 #define DREAMS_DATA_BAD_PAGE 0x8     /* page-table entry outside [0, num_pages) */
 #define DREAMS_DATA_BAD_PATH 0x10    /* path[0] != 0 or not strictly increasing */
 #define DREAMS_DATA_TIMEOUT 0x20     /* a kernel gave up waiting on its own pipeline (2 s) */
+#define DREAMS_DATA_NO_PAGES 0x40    /* the page pool has too few free pages for the call */
+#define DREAMS_DATA_SHARED_PAGE 0x80 /* a page that the call would write belongs to several sequences */
+#define DREAMS_DATA_BAD_INDEX 0x100  /* a row or slot index of the call is out of range or out of order */
 
 /*
  * One attention layer's K and V cache (bf16), or n_layers of them.
@@ -394,6 +397,141 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
                                          int64_t K, int64_t v0, int64_t n_vis, int32_t r, float *importance,
                                          int32_t *keep, void *workspace, size_t workspace_bytes,
                                          dreams_stream_t stream);
+
+/*
+ * Attention with a sliding window and sinks, for one layer: a target (or draft)
+ * whose queries see the last `window` positions and the first `sinks` ones.
+ * With L = kv_len[b] committed slots and q_len[b] queries whose K/V sit in slots
+ * L .. L + q_len[b] - 1 (prefill, a chunk on top of a cache, or one new token):
+ *   parent == NULL  query t is at position p = L + t and sees slot s (its
+ *                   position) when s <= p and (p - s < window or s < sinks);
+ *   parent != NULL  the queries are the nodes of a draft tree (parent [B, T_max],
+ *                   T_max <= 64, as in dreams_tree_t): node t at depth d(t) is at
+ *                   position p = L + d(t). It sees a committed slot s < L when
+ *                   p - s < window or s < sinks, and slot L + a when a is t or an
+ *                   ancestor of t and d(t) - d(a) < window or L + d(a) < sinks.
+ *     out[b, t, h, :] = sum_s softmax_s(scale * <q, K[b, s, g]>) V[b, s, g, :]
+ *     lse[b, t, h]    = log sum_s exp(scale * <q, K[b, s, g]>)    (may be NULL)
+ * over the slots s it sees; every query sees itself. window >= 1, sinks >= 0; a
+ * window of at least kv_len + q_len is plain causal (tree) attention. q, out,
+ * lse, layer and scale as for dreams_attention, 1 <= T_max <= 2^20. q_len[b] in
+ * [0, T_max]: 0 is an idle sequence (nothing is read or written). Rows
+ * t >= q_len[b] of out and lse are left untouched, as are the rows of a sequence
+ * with bad lengths or a bad tree.
+ * Slots that no query of the call sees are not used, whatever they hold: on a
+ * paged cache, pages that lie wholly between the sinks and the window of the
+ * first query may have been released (page-table entry -1). A page that holds a
+ * visible slot and whose entry is out of range is flagged DREAMS_DATA_BAD_PAGE,
+ * and its slots read as zeros. What a slot holds does not reach a query that does
+ * not see it, infinities and NaN included. Accumulation is fp32; probabilities
+ * enter the PV product as bf16, and the output is rounded to bf16 once.
+ */
+size_t dreams_window_attention_workspace_size(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max, int32_t Hq,
+                                              int32_t window, int32_t sinks, int32_t tree);
+dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
+                                        const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
+                                        const int32_t *q_len, const int32_t *kv_len, int32_t B, int32_t T_max,
+                                        int32_t Hq, float scale, int32_t window, int32_t sinks, void *out,
+                                        float *lse, void *workspace, size_t workspace_bytes, int32_t *status_word,
+                                        dreams_stream_t stream);
+
+/*
+ * The pages of a paged cache, kept on the device so that no call has to read
+ * lengths back. refcount[p] counts the page-table entries that hold page p; a
+ * page is free when it is 0. The calls keep the two consistent. Layers share the
+ * table: one page id stands for that page in every layer of the cache.
+ * Sequences may share pages that are full of committed slots; the page that the
+ * next slot goes to, and those after it, belong to one sequence (kv_fork sees to
+ * it), so that appending, compacting and pruning write to no other sequence.
+ * All arrays are device int32. kv->page_table is not const for these calls.
+ */
+typedef struct dreams_page_pool {
+  int32_t *page_table; /* [B, pages_per_seq], -1 = no page */
+  int32_t *refcount;   /* [num_pages] */
+  int32_t B;
+  int32_t pages_per_seq;
+  int32_t num_pages;
+} dreams_page_pool_t;
+
+/*
+ * Pages for the next slots: for every sequence, the table entries of slots
+ * kv_len[b] .. kv_len[b] + n_new[b] - 1 that have no page take free ones, the
+ * lowest page ids first, in the order of (sequence, entry). A sequence is skipped
+ * and flagged when its lengths are bad (BAD_KV_LEN), when an entry is out of
+ * range (BAD_PAGE) or belongs to several sequences (SHARED_PAGE), and when the
+ * free pages do not suffice for it and all sequences before it (NO_PAGES): it
+ * then gets none, as do all sequences after it that need any. Entries behind
+ * kv_len[b] are not looked at. One launch. The workspace holds no state.
+ */
+size_t dreams_kv_reserve_workspace_size(const dreams_page_pool_t *pool);
+dreams_status_t dreams_kv_reserve(const dreams_page_pool_t *pool, const int32_t *kv_len, const int32_t *n_new,
+                                  void *workspace, size_t workspace_bytes, int32_t *status_word,
+                                  dreams_stream_t stream);
+
+/*
+ * Gives back the pages that lie wholly inside slots begin[b] .. end[b] - 1:
+ * their entries become -1, their counts fall by one. Eviction behind a window
+ * (begin = sinks, end = kv_len - window + 1), the unused tail of a draft (begin =
+ * the new length, end = capacity) and the end of a sequence (0, capacity) are all
+ * this call. begin[b] >= end[b] gives nothing back; begin[b] < 0 or end[b] >
+ * capacity is flagged BAD_KV_LEN and skips the sequence, an entry outside
+ * [-1, num_pages) is flagged BAD_PAGE and stays. One launch.
+ */
+dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, const int32_t *begin, const int32_t *end,
+                                  int32_t *status_word, dreams_stream_t stream);
+
+/*
+ * Makes sequence i a copy of what sequence parent[i] was before the call, for
+ * all i at once (several samples of one prompt, beams reordered): pages full of
+ * the kv_len[parent[i]] committed slots are shared, and the last, partly filled
+ * page is copied in all layers of kv (the committed rows of it) to the lowest
+ * free pages, in the order of i. The lowest i of a parent takes over its last
+ * page, and the pages reserved after it, without a copy. parent[i] == -1 empties
+ * sequence i. Pages that no sequence holds any more are free afterwards, and may
+ * be taken for the copies. new_kv_len[i] = kv_len[parent[i]] (0 when emptied; may
+ * alias kv_len). kv is the cache of the pool (same table, page size 64). A call
+ * with a bad parent (BAD_INDEX), a bad length (BAD_KV_LEN), a table entry out of
+ * range or missing for a partly filled page (BAD_PAGE) or too few free pages
+ * (NO_PAGES) is flagged and changes nothing, with new_kv_len = kv_len. Two
+ * launches, chained by programmatic dependent launch. The workspace holds no
+ * state between calls.
+ */
+size_t dreams_kv_fork_workspace_size(const dreams_page_pool_t *pool);
+dreams_status_t dreams_kv_fork(const dreams_kv_cache_t *kv, const dreams_page_pool_t *pool, const int32_t *parent,
+                               const int32_t *kv_len, int32_t *new_kv_len, void *workspace,
+                               size_t workspace_bytes, int32_t *status_word, dreams_stream_t stream);
+
+/*
+ * Writes new K/V rows of one layer: slot kv_len[b] + t <- k_new[b, t], v_new[b, t]
+ * for t < n_new[b]. k_new, v_new: bf16, element (b, t, g, d) at b * stride_b +
+ * t * stride_t + g * D + d (so views of a fused projection; the same strides for
+ * both, multiples of 8 elements, stride_t >= Hkv * D; stride_b is ignored when
+ * B == 1), 16-byte aligned, n_new[b] in [0, T_max]. Bad lengths skip the sequence
+ * (BAD_KV_LEN), a slot whose page is missing is skipped (BAD_PAGE). The rows do
+ * not overlap the cache. One launch.
+ */
+dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t layer, const void *k_new, const void *v_new,
+                                 int64_t stride_b, int64_t stride_t, const int32_t *kv_len, const int32_t *n_new,
+                                 int32_t B, int32_t T_max, int32_t *status_word, dreams_stream_t stream);
+
+/*
+ * Drops visual tokens from the cache (Sec. 3.2 "Visual Token Compression"): of
+ * slots v0 .. v0 + n_vis - 1 the r slots keep[b] (strictly increasing, as
+ * dreams_visual_importance returns them) stay, and the cache closes up, in all
+ * layers:
+ *     slot v0 + i  <-  slot keep[b][i]                        for i < r
+ *     slot s - (n_vis - r)  <-  slot s                        for v0 + n_vis <= s < kv_len[b]
+ * as if all rows were read before any is written; new_kv_len[b] = kv_len[b] -
+ * (n_vis - r) (not the same array as kv_len). Other slots keep their bytes. A sequence is
+ * skipped and flagged, with new_kv_len = kv_len, when v0 + n_vis > kv_len[b] or
+ * kv_len[b] > capacity (BAD_KV_LEN), its list is not of that form (BAD_INDEX), a
+ * slot from v0 on has no page (BAD_PAGE), or, where refcount (of a paged cache,
+ * may be NULL) is given, its page is shared (SHARED_PAGE). 0 <= r <= n_vis.
+ * Pages past the new length stay with the sequence until kv_release. One launch.
+ */
+dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t B, const int32_t *keep, int32_t v0, int32_t n_vis,
+                                int32_t r, const int32_t *kv_len, const int32_t *refcount, int32_t *new_kv_len,
+                                int32_t *status_word, dreams_stream_t stream);
 
 /*
  * Row-wise argmax for callers that cannot allocate device memory. The paper

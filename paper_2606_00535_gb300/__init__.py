@@ -35,6 +35,7 @@ NOALLOC_ARGMAX_MAX_ROWS = 16384
 F32, BF16 = 0, 1
 DATA_BAD_PARENT, DATA_BAD_TREE_LEN, DATA_BAD_KV_LEN, DATA_BAD_PAGE, DATA_BAD_PATH = 1, 2, 4, 8, 16
 DATA_TIMEOUT = 0x20  # a kernel gave up waiting on its own pipeline
+DATA_NO_PAGES, DATA_SHARED_PAGE, DATA_BAD_INDEX = 0x40, 0x80, 0x100
 TEST_ATTENTION, TEST_LM_HEAD = 1, 2  # kernel families of test_set_stall
 
 
@@ -60,6 +61,11 @@ class _Tree(ctypes.Structure):
                 ("kv_len", ctypes.c_void_p), ("B", ctypes.c_int32), ("T_max", ctypes.c_int32)]
 
 
+class _PagePool(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("refcount", ctypes.c_void_p), ("B", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 _LOCK = threading.Lock()
 
@@ -75,7 +81,7 @@ def _lib() -> ctypes.CDLL:
                 lib = ctypes.CDLL(LIB_PATH)
                 p, i32, i64, sz, f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                                         ctypes.c_float)
-                pkv, ptr = ctypes.POINTER(_KVCache), ctypes.POINTER(_Tree)
+                pkv, ptr, ppl = ctypes.POINTER(_KVCache), ctypes.POINTER(_Tree), ctypes.POINTER(_PagePool)
                 sig = {
                     "dreams_tree_verify_attn_workspace_size": (sz, [pkv, ptr, i32]),
                     "dreams_tree_verify_attn_launches": (i32, [pkv, ptr, i32]),
@@ -104,6 +110,16 @@ def _lib() -> ctypes.CDLL:
                                                                   p, p, p, p, p, p, sz, p, p]),
                     "dreams_verify_step_speculative": (ctypes.c_int, [p, p, ctypes.c_int, i64, i64, ptr, pkv, i32,
                                                                       f32, p, p, p, p, p, p, p, p]),
+                    "dreams_window_attention_workspace_size": (sz, [pkv, i32, i32, i32, i32, i32, i32]),
+                    "dreams_window_attention": (ctypes.c_int, [p, i64, i64, pkv, i32, p, p, p, i32, i32, i32, f32,
+                                                               i32, i32, p, p, p, sz, p, p]),
+                    "dreams_kv_reserve_workspace_size": (sz, [ppl]),
+                    "dreams_kv_reserve": (ctypes.c_int, [ppl, p, p, p, sz, p, p]),
+                    "dreams_kv_release": (ctypes.c_int, [ppl, p, p, p, p]),
+                    "dreams_kv_fork_workspace_size": (sz, [ppl]),
+                    "dreams_kv_fork": (ctypes.c_int, [pkv, ppl, p, p, p, p, sz, p, p]),
+                    "dreams_kv_append": (ctypes.c_int, [pkv, i32, p, p, i64, i64, p, p, i32, i32, p, p]),
+                    "dreams_kv_prune": (ctypes.c_int, [pkv, i32, p, i32, i32, i32, p, p, p, p, p]),
                     "dreams_test_set_stall": (ctypes.c_int, [i32, i32, i64]),
                     "dreams_status_string": (ctypes.c_char_p, [ctypes.c_int]),
                     "dreams_version": (i32, []),
@@ -318,14 +334,14 @@ def _cache_covers(kv: "KVCache", B: int, D: Optional[int] = None) -> None:
         raise ValueError(f"q's head dim {D} differs from the cache's {kv.D}")
 
 
-def _q_strides(q: torch.Tensor) -> Tuple[int, int]:
+def _q_strides(q: torch.Tensor, name: str = "q", heads: str = "Hq") -> Tuple[int, int]:
     """(sequence stride, token stride) in elements of a bf16 [B, T, Hq, D]
     query tensor whose head rows are dense (a view into a fused QKV output
     qualifies)."""
     if not isinstance(q, torch.Tensor) or q.dtype != torch.bfloat16 or q.dim() != 4:
-        raise TypeError("q must be a 4-D bfloat16 tensor [B, T, Hq, D]")
+        raise TypeError(f"{name} must be a 4-D bfloat16 tensor [B, T, {heads}, D]")
     if q.stride(3) != 1 or q.stride(2) != q.shape[3]:
-        raise ValueError("q's head rows must be dense (strides [.., .., D, 1])")
+        raise ValueError(f"{name}'s head rows must be dense (strides [.., .., D, 1])")
     return int(q.stride(0)), int(q.stride(1))
 
 
@@ -651,6 +667,208 @@ def verify_step_speculative(target_logits: torch.Tensor, draft_logits: torch.Ten
           _ptr(u_accept), _ptr(u_resample), _ptr(acc), _ptr(path), _ptr(toks), _ptr(nkl), st,
           _stream(stream, dev))
     return {"accept_len": acc, "path": path, "out_tokens": toks, "new_kv_len": nkl}
+
+
+def _launch(name: str, dev: torch.device, stream, *args) -> None:
+    """_call for the calls a decode step makes many times: the device is
+    switched only when another one is current, and the raw handle of the
+    current stream is read without wrapping it. The stream comes last."""
+    if dev.type != "cuda":
+        raise ValueError(f"{name}: tensors must be on a CUDA device, got {dev}")
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(dev.index)
+    elif stream.device != dev:
+        raise ValueError(f"stream is on {stream.device}, the tensors on {dev}")
+    else:
+        s = stream.cuda_stream
+    fn = getattr(_LIB or _lib(), name)
+    if torch._C._cuda_getDevice() == dev.index:
+        st = fn(*args, s)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, s)
+    if st != OK:
+        raise DreamsError(name, st)
+
+
+def _scratch(kind: str, need: int, workspace: Optional[torch.Tensor], dev: torch.device, stream):
+    """(address, bytes) of the caller's workspace, or of one kept for this call,
+    device and stream; nothing where the call needs none."""
+    if workspace is not None:
+        ws, n = _ws(workspace, dev)
+        return ws, n
+    if need == 0 or dev.type != "cuda":  # off the GPU the launch refuses
+        return None, 0
+    ws = _workspace(kind, need, dev, stream)
+    return ws.data_ptr(), ws.numel()
+
+
+@dataclass
+class PagePool:
+    """The pages of a paged cache: its page table and ``refcount`` (int32
+    [num_pages]: how many table entries hold each page; 0 = free). The calls
+    below change both. ``PagePool.empty(kv)`` starts with every page free."""
+    kv: KVCache
+    refcount: torch.Tensor
+
+    def __post_init__(self):
+        if self.kv.page_table is None:
+            raise ValueError("a page pool needs a paged cache")
+        _need(self.refcount, "refcount", torch.int32, self.kv.k.device)
+        if self.refcount.numel() != self.kv.num_pages:
+            raise ValueError(f"refcount must hold one entry per page ({self.kv.num_pages})")
+        self.B = self.kv.B
+        self._c = _PagePool(self.kv.page_table.data_ptr(), self.refcount.data_ptr(), self.kv.B,
+                            self.kv.pages_per_seq, self.kv.num_pages)
+        self._reserve_bytes = int(_lib().dreams_kv_reserve_workspace_size(ctypes.byref(self._c)))
+        self._fork_bytes = int(_lib().dreams_kv_fork_workspace_size(ctypes.byref(self._c)))
+
+    @classmethod
+    def empty(cls, kv: KVCache) -> "PagePool":
+        if kv.page_table is None:
+            raise ValueError("a page pool needs a paged cache")
+        kv.page_table.fill_(-1)
+        return cls(kv, torch.zeros(kv.num_pages, dtype=torch.int32, device=kv.k.device))
+
+
+def _per_seq(t: torch.Tensor, name: str, B: int, dev) -> int:
+    """Address of an int32 array with an entry for each of B sequences."""
+    _need(t, name, torch.int32, dev)
+    if t.numel() < B:
+        raise ValueError(f"{name} holds {t.numel()} entries, the call addresses {B} sequences")
+    return t.data_ptr()
+
+
+def window_attention_workspace_size(kv: KVCache, B: int, T_max: int, Hq: int, window: int, sinks: int = 0,
+                                    tree: bool = False) -> int:
+    return int(_lib().dreams_window_attention_workspace_size(ctypes.byref(kv._c), B, T_max, Hq, window, sinks,
+                                                             int(tree)))
+
+
+def window_attention(q: torch.Tensor, kv: KVCache, q_len: torch.Tensor, kv_len: torch.Tensor, scale: float,
+                     window: int, sinks: int = 0, parent: Optional[torch.Tensor] = None, layer: int = 0,
+                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                     workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """Attention in which a query at position p sees the slots of the last
+    ``window`` positions (its own among them) and of the first ``sinks`` ones.
+    q: bf16 [B, T_max, Hq, D] (head rows dense, tokens and sequences may be
+    strided), the queries of slots kv_len .. kv_len + q_len - 1 (q_len 0: idle);
+    with ``parent`` (int32 [B, T_max]) they are the nodes of a draft tree.
+    Returns (out, lse or None); rows past q_len are left untouched."""
+    dev = q.device
+    sb, stt = _q_strides(q)
+    B, T_max, Hq, D = q.shape
+    ql, kl = _per_seq(q_len, "q_len", B, dev), _per_seq(kv_len, "kv_len", B, dev)
+    _cache_covers(kv, B, D)
+    if kv.k.device != dev:
+        raise ValueError(f"the KV cache is on {kv.k.device}, q on {dev}")
+    par = None
+    if parent is not None:
+        _need(parent, "parent", torch.int32, dev)
+        if tuple(parent.shape) != (B, T_max):
+            raise ValueError("parent must be [B, T_max]")
+        par = parent.data_ptr()
+    if out is None:
+        out = torch.empty((B, T_max, Hq, D), dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out, "out", torch.bfloat16, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((B, T_max, Hq), dtype=torch.float32, device=dev)
+    else:
+        _need(lse, "lse", torch.float32, dev)
+        if lse.shape != q.shape[:3]:
+            raise ValueError("lse must be [B, T_max, Hq]")
+    need = window_attention_workspace_size(kv, B, T_max, Hq, window, sinks, parent is not None)
+    ws, ws_bytes = _scratch("window", need, workspace, dev, stream)
+    _launch("dreams_window_attention", dev, stream, q.data_ptr(), sb, stt, ctypes.byref(kv._c), layer, par, ql, kl, B,
+            T_max, Hq, float(scale), window, sinks, out.data_ptr(), None if lse is None else lse.data_ptr(), ws, ws_bytes,
+            _status(status, dev))
+    return out, lse
+
+
+def kv_reserve(pool: PagePool, kv_len: torch.Tensor, n_new: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+               status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Pages for slots kv_len .. kv_len + n_new - 1 of every sequence, where
+    they have none: free pages, lowest ids first."""
+    dev = pool.refcount.device
+    kl, nn = _per_seq(kv_len, "kv_len", pool.B, dev), _per_seq(n_new, "n_new", pool.B, dev)
+    ws, ws_bytes = _scratch("reserve", pool._reserve_bytes, workspace, dev, stream)
+    _launch("dreams_kv_reserve", dev, stream, ctypes.byref(pool._c), kl, nn, ws, ws_bytes, _status(status, dev))
+
+
+def kv_release(pool: PagePool, begin: torch.Tensor, end: torch.Tensor, status: Optional[torch.Tensor] = None,
+               stream=None) -> None:
+    """Gives back the pages wholly inside slots begin .. end - 1 of every
+    sequence (eviction behind a window, an unused tail, a finished sequence)."""
+    dev = pool.refcount.device
+    _launch("dreams_kv_release", dev, stream, ctypes.byref(pool._c), _per_seq(begin, "begin", pool.B, dev),
+            _per_seq(end, "end", pool.B, dev), _status(status, dev))
+
+
+def kv_fork(pool: PagePool, parent: torch.Tensor, kv_len: torch.Tensor, new_kv_len: Optional[torch.Tensor] = None,
+            workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+            stream=None) -> torch.Tensor:
+    """Sequence i becomes a copy of what sequence parent[i] was (-1: empty),
+    for all at once: full pages are shared, the partly filled last page is copied
+    in all layers. Returns the new lengths."""
+    dev = pool.refcount.device
+    par, kl = _per_seq(parent, "parent", pool.B, dev), _per_seq(kv_len, "kv_len", pool.B, dev)
+    if new_kv_len is None:
+        new_kv_len = torch.empty(pool.B, dtype=torch.int32, device=dev)
+    ws, ws_bytes = _scratch("fork", pool._fork_bytes, workspace, dev, stream)
+    _launch("dreams_kv_fork", dev, stream, ctypes.byref(pool.kv._c), ctypes.byref(pool._c), par, kl,
+            _per_seq(new_kv_len, "new_kv_len", pool.B, dev), ws, ws_bytes, _status(status, dev))
+    return new_kv_len
+
+
+KV_FORK_LAUNCHES = 2  # the table and counts, then the copies of partly filled pages
+
+
+def kv_append(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, kv_len: torch.Tensor, n_new: torch.Tensor,
+              layer: int = 0, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Writes rows k_new, v_new (bf16 [B, T_max, Hkv, D], head rows dense, the
+    same strides; views of a fused projection qualify) to slots kv_len ..
+    kv_len + n_new - 1 of one layer."""
+    dev = kv.k.device
+    sb, stt = _q_strides(k_new, "k_new", "Hkv")
+    if k_new.shape != v_new.shape or v_new.dtype != torch.bfloat16 or k_new.stride() != v_new.stride() or \
+            k_new.device != dev or v_new.device != dev:
+        raise ValueError("k_new and v_new must share shape, strides, bfloat16 and the cache's device")
+    B, T_max, Hkv, D = k_new.shape
+    if Hkv != kv.Hkv:
+        raise ValueError(f"k_new has {Hkv} heads, the cache {kv.Hkv}")
+    _cache_covers(kv, B, D)
+    _launch("dreams_kv_append", dev, stream, ctypes.byref(kv._c), layer, k_new.data_ptr(), v_new.data_ptr(), sb, stt,
+            _per_seq(kv_len, "kv_len", B, dev), _per_seq(n_new, "n_new", B, dev), B, T_max, _status(status, dev))
+
+
+def kv_prune(kv: KVCache, keep: torch.Tensor, v0: int, n_vis: int, kv_len: torch.Tensor,
+             refcount: Optional[torch.Tensor] = None, new_kv_len: Optional[torch.Tensor] = None,
+             status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Keeps the slots ``keep`` (int32 [B, r], strictly increasing, as
+    visual_importance returns them) of the n_vis visual slots from v0 on and
+    closes the gap, in all layers. ``refcount`` (of a page pool): refuse to
+    write shared pages. Returns the new lengths, kv_len - (n_vis - r)."""
+    dev = kv.k.device
+    _need(keep, "keep", torch.int32, dev)
+    if keep.dim() != 2:
+        raise ValueError("keep must be [B, r]")
+    B, r = keep.shape
+    _cache_covers(kv, B)
+    kl = _per_seq(kv_len, "kv_len", B, dev)
+    if refcount is not None:
+        if kv.page_table is None:
+            raise ValueError("refcount goes with a paged cache")
+        _need_out(refcount, "refcount", torch.int32, dev, kv.num_pages)
+    if new_kv_len is None:
+        new_kv_len = torch.empty(B, dtype=torch.int32, device=dev)
+    _launch("dreams_kv_prune", dev, stream, ctypes.byref(kv._c), B, keep.data_ptr() if r else None, v0, n_vis, r, kl,
+            None if refcount is None else refcount.data_ptr(), _per_seq(new_kv_len, "new_kv_len", B, dev),
+            _status(status, dev))
+    return new_kv_len
 
 
 VERIFY_STEP_SPECULATIVE_LAUNCHES = 1  # one cluster per sequence: walk, residual sums, bonus, compaction
