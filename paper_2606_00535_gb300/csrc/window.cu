@@ -20,46 +20,12 @@
 
 #include <algorithm>
 
-#include "common.cuh"
-#include "tc.cuh"
+#include "window.cuh"
 
 namespace dreams {
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LN2 = 0.6931471805599453f;
-
-struct WinParams {
-  const __nv_bfloat16 *q;
-  int64_t sb, st;  // strides of q in elements
-  const __nv_bfloat16 *k, *v;
-  __nv_bfloat16 *out;
-  float *lse;
-  const int32_t *table;  // nullptr: contiguous cache
-  int32_t P, num_pages, capacity;
-  const int32_t *parent;  // nullptr: causal
-  const int32_t *q_len, *kv_len;
-  int32_t B, T_max, Hq, Hkv, G;
-  int32_t window, sinks;
-  float scale_log2;
-  int32_t nrb, nsplit;
-  int32_t *status;
-};
-
-// The key list of a block of rows: slots 0 .. S1-1, then lo .. hi-1.
-struct KeyList {
-  int lo, S1, n;
-  __device__ __forceinline__ int slot(int i) const { return i < S1 ? i : lo + (i - S1); }
-};
-
-__device__ __forceinline__ KeyList key_list(const WinParams &p, int L, int t_first, int t_last) {
-  KeyList kl;
-  const int p0 = L + (p.parent != nullptr ? 0 : t_first);  // no row of the block is before it
-  kl.lo = ::max(0, p0 - p.window + 1);
-  kl.S1 = ::min(p.sinks, kl.lo);
-  kl.n = kl.S1 + (L + t_last + 1 - kl.lo);
-  return kl;
-}
+using namespace win;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -87,18 +53,10 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t cta) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
-  return r;
-}
 __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
   float2 v;
   asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Does a pair of bf16 values hold an infinity or a NaN?
 __device__ __forceinline__ bool nonfinite2(uint32_t x) {
@@ -124,12 +82,6 @@ struct RowInfo {
   int off;                 // position - L; -1: no row
   unsigned long long anc;  // tree: bit a = sees slot L + a
 };
-
-__device__ __forceinline__ bool sees(const WinParams &p, int L, int off, unsigned long long anc, int slot) {
-  const bool near = int64_t(L) + off - slot < p.window || slot < p.sinks;
-  if (p.parent == nullptr) return near && slot <= L + off;
-  return slot < L ? near : ((anc >> (slot - L)) & 1ull) != 0;
-}
 
 template <int D>
 __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams p) {
@@ -180,14 +132,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
     RowInfo r{-1, 0ull};
     if (t < T) {
       r.off = t;
-      if (p.parent != nullptr) {
-        int depth = 0;
-        for (int a = t; a > 0; a = s_par[a]) ++depth;
-        r.off = depth;
-        int da = depth;
-        for (int a = t; a >= 0; a = s_par[a], --da)
-          if (depth - da < p.window || int64_t(L) + da < p.sinks) r.anc |= 1ull << a;
-      }
+      if (p.parent != nullptr) r.anc = tree_row(p, s_par, L, t, r.off);
     }
     s_row[tid] = r;
   }
@@ -506,6 +451,7 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
       kv->v == nullptr || !shapes_ok(kv, B, T_max, Hq, window, sinks, parent != nullptr))
     return DREAMS_ERR_INVALID_ARG;
   if (kv->D != 64 && kv->D != 128) return DREAMS_ERR_UNSUPPORTED;
+  if (kv->capacity > (1 << 30)) return DREAMS_ERR_UNSUPPORTED;
   if (layer < 0 || layer >= kv->n_layers || kv->layer_stride < 0) return DREAMS_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(kv->k) || !aligned16(kv->v) || (kv->layer_stride * 2) % 16 != 0 ||
       (reinterpret_cast<uintptr_t>(lse) & 3))
@@ -545,5 +491,6 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
   p.scale_log2 = scale * LOG2E;
   p.status = status_word;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (int64_t(T_max) * p.G > RB) return launch_tc(p, kv, s);
   return kv->D == 128 ? launch_rows<128>(p, s) : launch_rows<64>(p, s);
 }

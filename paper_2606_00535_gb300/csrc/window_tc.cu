@@ -1,0 +1,1099 @@
+// window_tc.cu -- windowed attention for blocks of 128 query rows on tcgen05
+// tensor cores (prefill, chunks, draft trees).
+//
+// A block is 128 / G tokens times the G query heads of a KV head. Its keys come in
+// tiles of 128: the sinks first, then the window of the block's first query up to
+// its last one (from the 64-slot page the window starts in). A tile at either end
+// is cut to the columns it needs (a multiple of 32), so the few sinks cost a
+// quarter of a tile or less.
+//
+// One CTA per SM holds two slots of tensor memory (256 columns each: S or P, and
+// O). S = Q K^T and O += P V are one M128 instruction group each; a slot's softmax
+// warpgroup (one row per thread) turns S into P while the tensor pipe works on the
+// other slot, which is what keeps the pipe busy.
+//   PAIR   the slots are two neighbouring blocks of a KV head: every K/V tile is
+//          loaded once for 256 rows. The CTAs are persistent: they walk over the
+//          items with a ring of K/V stages that runs on across them, so the next
+//          item's loads and first Q K^T overlap the epilogue of the last.
+//   !PAIR  both slots work on one block, alternate tiles; a block's tiles may be
+//          split over a cluster of CTAs, joined through distributed shared memory.
+//          For grids too small to fill the SMs with pairs.
+// The tensor pipe completes in order, so the commit that announces S of a tile
+// also says that everything issued before it is done: the softmax warps give the
+// stages read by it back to the producer, and the issuing thread needs no commits
+// of its own for that. Every mbarrier wait is bounded; a CTA that gives up flags
+// DREAMS_DATA_TIMEOUT, drains its copies and MMAs, frees its tensor memory and
+// leaves unfinished rows untouched.
+#include <cuda.h>
+#include <limits.h>
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "tmap.cuh"
+#include "window.cuh"
+
+namespace dreams {
+namespace win {
+namespace {
+
+constexpr int KT = 128;    // keys of a tile
+constexpr int ROWS = 128;  // query rows of a block
+constexpr int THREADS = 384;
+// Registers a thread: the kernel is launched with 168; the producer's warpgroup
+// gives some to the two softmax warpgroups, which hold 128 scores a thread.
+constexpr int LAUNCH_REGS = 168, SOFTMAX_REGS = 216, OTHER_REGS = 72;
+static_assert(256 * SOFTMAX_REGS + 128 * OTHER_REGS <= THREADS * LAUNCH_REGS, "the shares fit what the block is launched with");
+constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 10;
+constexpr int SEEN = 8;  // items whose scan results are kept (more than the ring can be ahead)
+constexpr uint32_t TMEM_COLS = 512;
+constexpr float RESCALE = 8.f;  // log2 headroom of the reference maximum
+
+template <int D, bool PAIR>
+struct Cfg {
+  static constexpr int NR = D / 64;  // 128-byte column regions of a row
+  static constexpr uint32_t Q_REGION = ROWS * 128, KV_REGION = KT * 128;
+  static constexpr uint32_t Q_BYTES = NR * Q_REGION;
+  static constexpr uint32_t STAGE = NR * KV_REGION;
+  static constexpr int NQ = PAIR ? 2 : 1;
+  static constexpr int NST = D == 64 ? 8 : 5;
+  static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + 1024, 120 * 1024);
+};
+
+struct TcParams {
+  CUtensorMap tmap_q, tmap_k, tmap_v;
+  WinParams p;
+  int32_t TB;      // tokens of a block
+  int32_t nblk;    // blocks (or pairs) per sequence and KV head
+  int32_t items;   // B * Hkv * nblk
+  int32_t stall_at;
+  uint64_t wait_ns;
+};
+
+// An item: a pair of blocks, or one block, of a sequence and KV head. Tiles are
+// numbered 0 .. n-1, the ns sink tiles first.
+struct Item {
+  int b, g, L, T;
+  int t00, t01, tl0, tl1;  // first and last token of each block
+  int nb;                  // blocks present (0: nothing to do)
+  int lo, lo64, S1, hi;
+  int ns, n;
+  int a0, a1, e0, e1;      // window tiles of each block: [a, e)
+  __device__ __forceinline__ int t0(int w) const { return w ? t01 : t00; }
+  __device__ __forceinline__ int tl(int w) const { return w ? tl1 : tl0; }
+  __device__ __forceinline__ int a(int w) const { return w ? a1 : a0; }
+  __device__ __forceinline__ int e(int w) const { return w ? e1 : e0; }
+  __device__ __forceinline__ bool need(int w, int j) const { return w < nb && j < e(w) && (j < ns || j >= a(w)); }
+  // the next tile of block w after j (n: none)
+  __device__ __forceinline__ int next(int w, int j) const {
+    int k = j + 1;
+    if (k >= ns) k = ::max(k, a(w));
+    return k < e(w) ? k : n;
+  }
+  __device__ __forceinline__ int first(int w) const { return w < nb ? next(w, -1) : n; }
+  __device__ __forceinline__ int slot0(int j) const { return j < ns ? j * KT : lo64 + (j - ns) * KT; }
+  __device__ __forceinline__ int beg(int j) const { return j < ns ? j * KT : ::max(lo, lo64 + (j - ns) * KT); }
+  __device__ __forceinline__ int end(int j) const { return j < ns ? ::min(S1, j * KT + KT) : ::min(hi, lo64 + (j - ns) * KT + KT); }
+  __device__ __forceinline__ int ncols(int j) const { return (end(j) - slot0(j) + 31) & ~31; }
+  // does every row of block w see the whole tile?
+  __device__ __forceinline__ bool whole(const WinParams &p, int w, int j) const {
+    const int s = slot0(j);
+    if (beg(j) != s || end(j) != s + KT) return false;
+    if (j < ns) return true;
+    const bool tree = p.parent != nullptr;
+    return s > L + tl(w) - p.window && s + KT <= (tree ? L : L + t0(w) + 1);
+  }
+};
+
+template <bool PAIR>
+__device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bool report) {
+  const WinParams &p = P.p;
+  // the last blocks first (they have the most keys), all heads of a block together
+  const int heads = p.B * p.Hkv;
+  const int blk = P.nblk - 1 - x / heads, bg = x % heads;
+  it.b = bg / p.Hkv;
+  it.g = bg - it.b * p.Hkv;
+  it.T = __ldg(p.q_len + it.b);
+  it.L = __ldg(p.kv_len + it.b);
+  it.nb = it.n = it.ns = 0;
+  report = report && it.g == 0 && blk == 0;
+  if (it.T < 0 || it.T > p.T_max) {
+    if (report) flag(p.status, DREAMS_DATA_BAD_TREE_LEN);
+    return;
+  }
+  if (it.L < 0 || int64_t(it.L) + it.T > p.capacity) {
+    if (report) flag(p.status, DREAMS_DATA_BAD_KV_LEN);
+    return;
+  }
+  it.t00 = blk * (PAIR ? 2 : 1) * P.TB;
+  it.t01 = it.t00 + P.TB;
+  if (it.t00 >= it.T) return;
+  it.nb = PAIR && it.t01 < it.T ? 2 : 1;
+  it.tl0 = ::min(it.T, it.t00 + P.TB) - 1;
+  it.tl1 = it.nb == 2 ? ::min(it.T, it.t01 + P.TB) - 1 : it.tl0;
+  const bool tree = p.parent != nullptr;
+  it.lo = ::max(0, it.L + (tree ? 0 : it.t00) - p.window + 1);
+  it.lo64 = it.lo & ~63;
+  it.S1 = ::min(p.sinks, it.lo);
+  it.ns = (it.S1 + KT - 1) / KT;
+  it.hi = it.L + it.tl1 + 1;
+  it.n = it.ns + (it.hi - it.lo64 + KT - 1) / KT;
+  // with more sinks than slots before the window, the first window tiles hold sinks too
+  const int lo1 = ::max(0, it.L + (tree ? 0 : it.t01) - p.window + 1);
+  it.a0 = it.ns;
+  it.a1 = p.sinks > it.lo ? it.ns : it.ns + (lo1 - it.lo64) / KT;
+  it.e0 = it.ns + (it.L + it.tl0 - it.lo64) / KT + 1;
+  it.e1 = it.n;
+}
+
+// A place in the ring of stages: index and phase.
+template <int N>
+struct Place {
+  int s;
+  uint32_t ph;
+  __device__ __forceinline__ Place plus(int d) const {  // d < N
+    Place q{s + d, ph};
+    if (q.s >= N) {
+      q.s -= N;
+      q.ph ^= 1u;
+    }
+    return q;
+  }
+  __device__ __forceinline__ void move(int64_t d) {  // any d >= 0
+    const int64_t at = s + d;
+    s = int(at % N);
+    ph ^= uint32_t(at / N) & 1u;
+  }
+};
+
+__device__ __forceinline__ float max3f(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float &lo, float &hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t ffma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+// tcgen05.mma of kind::f16 with the descriptors' low words in registers: the high
+// word (stride offset 1024 bytes, 128-byte swizzle) is the same for every operand.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "n"(DESC_HI)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b_lo), "r"(idesc), "r"(acc), "n"(DESC_HI)
+      : "memory");
+}
+// The low n bits of a word (n may be any integer).
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// What a query row sees, for the masks.
+struct Row {
+  int plow, phi;           // window slots [plow, phi) (tree: committed slots)
+  int sink;                // slots below it are seen too: min(sinks, phi)
+  unsigned long long anc;  // tree: the new slots
+  int L;
+  // allowed columns among slots base .. base + 31, inside the tile's [beg, end)
+  __device__ __forceinline__ uint32_t word(int base, int beg, int end) const {
+    uint32_t m = (low_bits(phi - base) & ~low_bits(plow - base)) | low_bits(sink - base);
+    if (anc != 0ull) {
+      const int sh = base - L;
+      m |= (sh >= 64 || sh <= -32) ? 0u : (sh >= 0 ? uint32_t(anc >> sh) : uint32_t(anc << (-sh)));
+    }
+    return m & low_bits(end - base) & ~low_bits(beg - base);
+  }
+};
+
+// One row by a whole warp, straight from the definition: used when a tile with
+// partly masked columns held an infinity or a NaN in V (0 x inf would reach rows
+// that do not see it). Slow, and rare.
+template <int D>
+__device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, int t, int h, int off, unsigned long long anc) {
+  const int lane = threadIdx.x & 31;
+  constexpr int E = D / 32;
+  float q[E], o[E];
+  const __nv_bfloat16 *src = p.q + b * p.sb + t * p.st + int64_t(h) * D + lane * E;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    q[i] = __bfloat162float(src[i]);
+    o[i] = 0.f;
+  }
+  const KeyList kl = key_list(p, L, p.parent != nullptr ? 0 : t, t);
+  float m = -INFINITY, l = 0.f;
+  for (int i = 0; i < kl.n; ++i) {
+    const int s = kl.slot(i);
+    if (!sees(p, L, off, anc, s)) continue;
+    int64_t at;
+    if (p.table == nullptr) {
+      at = (int64_t(b) * p.capacity + s) * p.Hkv + g;
+    } else {
+      const int pg = __ldg(p.table + int64_t(b) * p.P + (s >> 6));
+      at = pg >= 0 && pg < p.num_pages ? (int64_t(pg) * 64 + (s & 63)) * p.Hkv + g : -1;
+    }
+    float x = 0.f, v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      x += at >= 0 ? q[e] * __bfloat162float(p.k[at * D + lane * E + e]) : 0.f;
+      v[e] = at >= 0 ? __bfloat162float(p.v[at * D + lane * E + e]) : 0.f;
+    }
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
+    x *= p.scale_log2;
+    if (x > m) {
+      const float c = tc::ex2(m - x);
+      l *= c;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= c;
+      m = x;
+    }
+    const float w = tc::ex2(x - (m == -INFINITY ? 0.f : m));
+    l += w;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += w * v[e];
+  }
+  const int64_t row = (int64_t(b) * p.T_max + t) * p.Hq + h;
+#pragma unroll
+  for (int e = 0; e < E; ++e) p.out[row * D + lane * E + e] = __float2bfloat16(o[e] / l);
+  if (lane == 0 && p.lse != nullptr) p.lse[row] = (m + log2f(l)) * LN2;
+}
+
+
+template <int D, bool PAIR>
+__global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_constant__ TcParams P) {
+  using C = Cfg<D, PAIR>;
+  using Pos = Place<C::NST>;
+  const WinParams &p = P.p;
+  constexpr int NST = C::NST, NR = C::NR;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST];
+  __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain, bar_never;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort, s_zero, s_dirty[SEEN];
+  __shared__ int8_t s_par[8][64];
+  __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
+  __shared__ struct { int off, t; unsigned long long anc; } s_row[PAIR ? 1 : ROWS];
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t base = smem_u32(smem);
+  auto q_s = [&](int w) { return base + uint32_t(PAIR ? w : 0) * C::Q_BYTES; };
+  const uint32_t ring = base + C::NQ * C::Q_BYTES;
+  const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty);
+  const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
+                 o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain = smem_u32(&bar_drain), never = smem_u32(&bar_never);
+  if (tid == TMA_WARP * 32) {
+    for (int i = 0; i < NST; ++i) {
+      tc::mbar_init(full0 + 8 * i, 1);
+      tc::mbar_init(empty0 + 8 * i, 2);  // its last reader on the tensor pipe, and the scan
+    }
+    for (int w = 0; w < 2; ++w) {
+      tc::mbar_init(qf0 + 8 * w, 1);
+      tc::mbar_init(qe0 + 8 * w, 1);
+      tc::mbar_init(s0 + 8 * w, 1);
+      tc::mbar_init(h0 + 8 * w, 128);
+      tc::mbar_init(p0 + 8 * w, 128);
+      tc::mbar_init(o0 + 8 * w, 1);
+    }
+    tc::mbar_init(drain, 1);
+    tc::mbar_init(never, 1);  // nothing arrives on it
+    s_abort = s_zero = 0;
+    for (int i = 0; i < SEEN; ++i) {
+      s_dirty[i] = 0;
+      tc::mbar_init(scan0 + 8 * i, 1);
+    }
+    tc::fence_barrier_init();
+    tc::prefetch_tmap(&P.tmap_q);
+    tc::prefetch_tmap(&P.tmap_k);
+    tc::prefetch_tmap(&P.tmap_v);
+  }
+  if (warp == MMA_WARP) {
+    tc::tmem_alloc(smem_u32(&s_tmem), TMEM_COLS);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = s_tmem;
+  volatile int *abort_flag = &s_abort;
+  const uint64_t wait_ns = P.wait_ns;
+  auto give_up = [&]() {
+    if (*abort_flag == 0) {
+      *abort_flag = 1;
+      flag(p.status, DREAMS_DATA_TIMEOUT);
+    }
+  };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return tc::mbar_wait(bar, parity & 1u, abort_flag, wait_ns); };
+
+  // The items of this CTA; without PAIR it has one, shared by a cluster.
+  const int nsplit = PAIR ? 1 : p.nsplit;
+  const int split = PAIR ? 0 : int(blockIdx.x) % nsplit;
+  int x_next = PAIR ? int(blockIdx.x) : int(blockIdx.x) / nsplit;
+  // the next item with work, and the tiles [j0, j1) of it that are this CTA's
+  auto next_item = [&](Item &it, int &j0, int &j1, bool report) {
+    while (x_next < P.items) {
+      load_item<PAIR>(P, x_next, it, report);
+      x_next += PAIR ? int(gridDim.x) : P.items;
+      const int per = (it.n + nsplit - 1) / nsplit;
+      j0 = ::min(it.n, split * per);
+      j1 = ::min(it.n, j0 + per);
+      if (it.nb > 0 && j0 < j1) return true;
+    }
+    return false;
+  };
+
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
+    // ---------------- softmax warpgroup w: the rows of slot w
+    const int w = warp >> 2;
+    const int row = 32 * (warp & 3) + lane;
+    const uint32_t tl = tmem + (uint32_t(32 * (warp & 3)) << 16) + 256u * w;
+    const bool lead = (warp & 3) == 0 && lane == 0;
+    uint32_t ns_seen = 0, no_seen = 0;  // S tiles and finished items of this slot
+    Pos ring0{0, 0};                    // K of the item's first tile
+    bool ok = true;
+    Item it;
+    int j0, j1, seq = 0;
+    for (; ok && next_item(it, j0, j1, false); ++seq) {
+      const int blk = PAIR ? w : 0;
+      const bool here = !PAIR || w < it.nb;
+      auto next_of = [&](int j) { return PAIR ? it.next(w, j) : ::min(j1, j + 2); };
+      auto place = [&](int j, int kv) {  // of K (0) or V (1) of tile j
+        Pos q = ring0;
+        q.move(2 * int64_t(j - j0) + kv);
+        return q;
+      };
+      // a tile's stages are given back by the slot that reads it last; what copies
+      // must not leave behind is cleaned by the one that reads it first
+      auto last_user = [&](int j) { return !PAIR || !(w == 0 && it.need(1, j)); };
+      auto first_user = [&](int j) { return !PAIR || !(w == 1 && it.need(0, j)); };
+      int j = PAIR ? it.first(w) : ::min(j1, j0 + w);
+      const bool any = j < j1;
+      // this thread's row
+      const int t0 = here ? it.t0(blk) : it.t00, rows_blk = here ? (it.tl(blk) - t0 + 1) * p.G : 0;
+      const bool real = row < rows_blk;
+      const int n_act = ::min(4, (rows_blk + 31) / 32);  // warps with rows
+      const bool live = (warp & 3) < n_act;
+      const int t = real ? t0 + row / p.G : t0;
+      int off = t;
+      bool tree_ok = true;
+      Row r;
+      r.anc = 0ull;
+      if (p.parent != nullptr) {
+        // this warp's copy of the parents, checked before any walk
+        __syncwarp();  // the last item's walks are over
+        int bad = 0;
+        for (int i = lane; i < it.T; i += 32) {
+          const int par = __ldg(p.parent + int64_t(it.b) * p.T_max + i);
+          s_par[warp][i] = int8_t(par);  // (a bad one is not used)
+          bad |= i == 0 ? par != -1 : (par < 0 || par >= i);
+        }
+        tree_ok = !__any_sync(0xffffffffu, bad);
+        if (tree_ok) r.anc = tree_row(p, s_par[warp], it.L, t, off);
+        else if (lead && w == 0 && it.g == 0 && split == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
+      }
+      r.L = it.L;
+      r.plow = ::max(0, it.L + off - p.window + 1);
+      r.phi = p.parent != nullptr ? it.L : it.L + off + 1;
+      r.sink = ::min(p.sinks, r.phi);
+      if (!PAIR && w == 0) {
+        s_row[row].off = tree_ok ? off : -1;
+        s_row[row].t = t;
+        s_row[row].anc = r.anc;
+      }
+      float m_ref = -INFINITY, l = 0.f;
+      int prev = -1;
+      while (j < j1) {
+        if (!__all_sync(0xffffffffu, wait(s0 + 8 * w, ns_seen))) {
+          ok = false;
+          break;
+        }
+        ++ns_seen;
+        tc::fence_after_sync();
+        const int nj = next_of(j);
+        const Pos vpl = place(j, 1);
+        if (lead) {
+          // every MMA up to this S is done: K of this tile, V of the one before
+          if (last_user(j)) tc::mbar_arrive(empty0 + 8 * place(j, 0).s);
+          if (prev >= 0 && (!PAIR || prev == j - 1) && last_user(prev)) tc::mbar_arrive(empty0 + 8 * place(prev, 1).s);
+          if (PAIR && nj >= j1) tc::mbar_arrive(qe0 + 8 * w);  // Q of this slot
+        }
+        const int sl = it.slot0(j), beg = it.beg(j), end = it.end(j), nc = it.ncols(j);
+        uint32_t sv[KT];
+        float corr = 1.f;
+        bool resc = false;
+        uint64_t scale2 = 0, nmu2 = 0, acc2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+        auto p_step = [&](const uint32_t *u, int c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float e0, e1;
+            f32x2_split(ffma2(f32x2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1])), scale2, nmu2), e0, e1);
+            const float a = tc::ex2(e0), b = tc::ex2(e1);
+            acc2[i & 1] = fadd2(acc2[i & 1], f32x2(a, b));
+            pk[i] = pack_bf16x2(a, b);
+          }
+          tc::tmem_st16(tl + 16 * c, pk);
+        };
+        if (live) {
+          float mx;
+          if (nc == KT) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tc::tmem_ld32(tl + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sv[32 * c]));
+            tc::tmem_wait_ld();
+            if (!it.whole(p, blk, j)) {
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const uint32_t m = r.word(sl + 32 * c, beg, end);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (!((m >> e) & 1u)) sv[32 * c + e] = 0xff800000u;
+              }
+            }
+            float mt[43];
+#pragma unroll
+            for (int i = 0; i < 42; ++i)
+              mt[i] = max3f(__uint_as_float(sv[3 * i]), __uint_as_float(sv[3 * i + 1]), __uint_as_float(sv[3 * i + 2]));
+            mt[42] = fmaxf(__uint_as_float(sv[126]), __uint_as_float(sv[127]));
+#pragma unroll
+            for (int i = 0; i < 14; ++i) mt[i] = max3f(mt[3 * i], mt[3 * i + 1], mt[3 * i + 2]);
+            mt[14] = mt[42];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) mt[i] = max3f(mt[3 * i], mt[3 * i + 1], mt[3 * i + 2]);
+            mx = max3f(max3f(mt[0], mt[1], mt[2]), mt[3], mt[4]);
+          } else {
+            // a cut tile: 32 columns at a time, read twice
+            mx = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < nc / 32; ++c) {
+              uint32_t u[32];
+              tc::tmem_ld32(tl + 32 * c, u);
+              tc::tmem_wait_ld();
+              const uint32_t m = r.word(sl + 32 * c, beg, end);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, ((m >> e) & 1u) ? __uint_as_float(u[e]) : -INFINITY);
+            }
+          }
+          mx *= p.scale_log2;  // scale > 0
+          // the reference maximum is raised (and O rescaled) only past 2^RESCALE
+          resc = mx > m_ref + RESCALE;
+          if (resc) {
+            corr = m_ref == -INFINITY ? 0.f : tc::ex2(m_ref - mx);
+            m_ref = mx;
+            l *= corr;
+          }
+          const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
+          scale2 = f32x2(p.scale_log2, p.scale_log2);
+          nmu2 = f32x2(nmu, nmu);
+          if (nc == KT) {
+            p_step(sv, 0);
+            p_step(sv + 32, 1);
+          }
+          // slots outside [beg, end) may hold any bits: their V rows become zeros
+          // once the copy has landed
+          if ((beg > sl || end < sl + nc) && first_user(j)) {
+            if (!__all_sync(0xffffffffu, wait(full0 + 8 * vpl.s, vpl.ph))) {
+              ok = false;
+              break;
+            }
+            const uint32_t st = ring + uint32_t(vpl.s) * C::STAGE;
+            const int head = beg - sl, tail = sl + nc - end;
+            for (int i = row; i < (head + tail) * NR * 8; i += 32 * n_act) {
+              const int z = i / (NR * 8), rc = i % (NR * 8);
+              const int rr = z < head ? z : end - sl + (z - head);
+              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(st + (rc >> 3) * C::KV_REGION + rr * 128 + ((rc & 7) << 4)),
+                           "r"(0u)
+                           : "memory");
+            }
+            tc::fence_proxy_async_smem();
+          }
+          if (prev >= 0 && __any_sync(0xffffffffu, resc)) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t ov[32];
+              tc::tmem_ld32(tl + 128 + c * 32, ov);
+              tc::tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+              tc::tmem_st32(tl + 128 + c * 32, ov);
+            }
+          }
+        }
+        // one thread waits for the copies the MMA thread needs (V of this tile, K
+        // of the slot's next one), so that it waits for P alone
+        bool kv_ok = true;
+        if (lead) kv_ok = wait(full0 + 8 * vpl.s, vpl.ph);
+        if (!__all_sync(0xffffffffu, kv_ok)) {
+          ok = false;
+          break;
+        }
+        tc::tmem_wait_st();
+        tc::fence_before_sync();
+        tc::mbar_arrive(h0 + 8 * w);
+        if (live) {
+          if (nc == KT) {
+            p_step(sv + 64, 2);
+            p_step(sv + 96, 3);
+          } else {
+            // P of 32 columns goes over columns that have been read
+#pragma unroll 1
+            for (int c = 0; c < nc / 32; ++c) {
+              uint32_t u[32];
+              tc::tmem_ld32(tl + 32 * c, u);
+              tc::tmem_wait_ld();
+              const uint32_t m = r.word(sl + 32 * c, beg, end);
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!((m >> e) & 1u)) u[e] = 0xff800000u;
+              p_step(u, c);
+            }
+          }
+          float a0, a1, b0, b1;
+          f32x2_split(acc2[0], a0, a1);
+          f32x2_split(acc2[1], b0, b1);
+          l += (a0 + a1) + (b0 + b1);
+        }
+        if (lead && nj < j1) {
+          const Pos k = place(nj, 0);
+          kv_ok = wait(full0 + 8 * k.s, k.ph);
+        }
+        if (!__all_sync(0xffffffffu, kv_ok)) {
+          ok = false;
+          break;
+        }
+        tc::tmem_wait_st();
+        tc::fence_before_sync();
+        tc::mbar_arrive(p0 + 8 * w);
+        prev = j;
+        j = nj;
+      }
+      if (ok && any) {
+        ok = __all_sync(0xffffffffu, wait(o0 + 8 * w, no_seen));  // all MMAs of the slot are done
+        ++no_seen;
+        tc::fence_after_sync();
+        if (ok && lead && last_user(prev)) tc::mbar_arrive(empty0 + 8 * place(prev, 1).s);
+      }
+      ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
+      if (!ok) break;
+      ring0.move(2 * int64_t(j1 - j0));
+      const bool dirty = *reinterpret_cast<volatile int *>(&s_dirty[seq % SEEN]) != 0;
+
+      if constexpr (PAIR) {
+        if (any && tree_ok && !dirty) {
+          const float inv = 1.f / l;
+          const int64_t orow = (int64_t(it.b) * p.T_max + t) * p.Hq + it.g * p.G + (row - (t - t0) * p.G);
+          if (live) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t ov[32];
+              tc::tmem_ld32(tl + 128 + c * 32, ov);
+              tc::tmem_wait_ld();
+              if (real) {
+                uint4 *dst = reinterpret_cast<uint4 *>(p.out + orow * D + c * 32);
+                auto pk = [&](int e) { return pack_bf16x2(__uint_as_float(ov[e]) * inv, __uint_as_float(ov[e + 1]) * inv); };
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dst[e] = make_uint4(pk(8 * e), pk(8 * e + 2), pk(8 * e + 4), pk(8 * e + 6));
+              }
+            }
+            if (real && p.lse != nullptr) p.lse[orow] = (m_ref + log2f(l)) * LN2;
+          }
+        } else if (any && tree_ok) {
+          for (int i = 0; i < 32; ++i) {
+            const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, off, i);
+            const unsigned long long ai = __shfl_sync(0xffffffffu, r.anc, i);
+            const int ri = 32 * (warp & 3) + i;
+            if (ri < rows_blk) slow_row<D>(p, it.b, it.g, it.L, ti, it.g * p.G + ri - (ti - t0) * p.G, oi, ai);
+          }
+        }
+        tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
+      } else {
+        // the slot's part into shared memory (below)
+        s_ml[w][row] = any && live ? make_float2(m_ref, l) : make_float2(-INFINITY, 0.f);
+      }
+    }
+    if (!ok) give_up();
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+    if (warp == TMA_WARP) {
+      // ---------------- producer: for each item K_0, Q, V_0, K_1, V_1, ...
+      if (lane == 0) {
+        Pos at{0, 0};
+        bool wrapped = false, ok = true;
+        int issued = 0, ktiles = 0;
+        uint32_t nq[2] = {0, 0};
+        Item it;
+        int j0, j1;
+        while (ok && next_item(it, j0, j1, split == 0)) {
+          const int32_t *row = p.table != nullptr ? p.table + int64_t(it.b) * p.P : nullptr;
+          auto fetch = [&](int j, int h) {
+            if (row == nullptr || j >= j1) return 0;
+            const int pi = (it.slot0(j) >> 6) + h;
+            return pi < p.P ? __ldg(row + pi) : -1;
+          };
+          int pg0 = fetch(j0, 0), pg1 = fetch(j0, 1);
+          for (int j = j0; j < j1 && ok; ++j) {
+            const int slot = it.slot0(j), halves = it.ncols(j) > 64 ? 2 : 1;
+            // tensor-map coordinate (dim 3) of a 64-slot half
+            auto coord = [&](int h, int pg) {
+              if (row == nullptr) return it.b;
+              if (pg >= 0 && pg < p.num_pages) return pg;
+              if (::max(it.beg(j), slot + 64 * h) < ::min(it.end(j), slot + 64 * h + 64)) flag(p.status, DREAMS_DATA_BAD_PAGE);
+              return p.num_pages;  // outside the map: the copy fills zeros
+            };
+            const int ca = coord(0, pg0), cb = coord(1, pg1), sa = row != nullptr ? 0 : slot, sb = row != nullptr ? 0 : slot + 64;
+            pg0 = fetch(j + 1, 0);
+            pg1 = fetch(j + 1, 1);
+#pragma unroll 1
+            for (int kv = 0; kv < 2 && ok; ++kv) {
+              if (kv == 0 && P.stall_at >= 0 && ktiles >= P.stall_at) {
+                // test hook: this copy is never issued
+                tc::mbar_wait(never, 0, abort_flag, wait_ns);
+                ok = false;
+                break;
+              }
+              if (wrapped && !wait(empty0 + 8 * at.s, at.ph ^ 1u)) {
+                ok = false;
+                break;
+              }
+              const uint32_t st = ring + uint32_t(at.s) * C::STAGE, bar = full0 + 8 * at.s;
+              tc::mbar_arrive_expect_tx(bar, uint32_t(NR * halves * 8192));
+              const CUtensorMap *map = kv == 0 ? &P.tmap_k : &P.tmap_v;
+#pragma unroll
+              for (int r = 0; r < NR; ++r) {
+                tc::tma_load_4d(st + r * C::KV_REGION, map, bar, r * 64, it.g, sa, ca);
+                if (halves == 2) tc::tma_load_4d(st + r * C::KV_REGION + 8192, map, bar, r * 64, it.g, sb, cb);
+              }
+              ++issued;
+              at = at.plus(1);
+              wrapped |= at.s == 0;
+              if (kv == 1) break;
+              ++ktiles;
+              if (j == j0) {  // the item's Q, once the last item's is done with
+#pragma unroll
+                for (int w = 0; w < C::NQ; ++w) {
+                  if (w >= it.nb || !ok) continue;
+                  if (nq[w] > 0 && !wait(qe0 + 8 * w, nq[w] - 1)) {
+                    ok = false;
+                    continue;
+                  }
+                  ++nq[w];
+                  tc::mbar_arrive_expect_tx(qf0 + 8 * w, uint32_t(NR * p.G * P.TB * 128));
+#pragma unroll
+                  for (int r = 0; r < NR; ++r)
+                    tc::tma_load_5d(q_s(w) + r * C::Q_REGION, &P.tmap_q, qf0 + 8 * w, r * 64, 0, it.g, it.t0(w), it.b);
+                }
+              }
+            }
+          }
+        }
+        if (!ok) give_up();
+        // no copy may still be landing when the CTA ends
+        for (int i = ::max(0, issued - NST); i < issued; ++i) tc::mbar_wait(full0 + 8 * (i % NST), (i / NST) & 1, &s_zero);
+        for (int w = 0; w < C::NQ; ++w)
+          if (nq[w] > 0) tc::mbar_wait(qf0 + 8 * w, (nq[w] - 1) & 1u, &s_zero);
+      }
+    } else if (warp == MMA_WARP) {
+      // ---------------- MMA issuer
+      if (lane == 0) {
+        // low words of the operands' descriptors: address / 16 (of 18 bits: in a
+        // cluster the bits above say which CTA), leading-dimension offset / 16
+        const uint32_t ring16 = (ring & 0x3FFFFu) >> 4;
+        const uint32_t q_lo = ((q_s(0) & 0x3FFFFu) >> 4) | (1u << 16), k_lo = ring16 | (1u << 16), v_lo = ring16 | ((C::KV_REGION >> 4) << 16);
+        constexpr uint32_t IDESC_QK = tc::idesc_bf16_f32(ROWS, 0, false);
+        constexpr uint32_t IDESC_PV = tc::idesc_bf16_f32(ROWS, D, true);
+        // S_w = Q_w K^T over the first nc keys of a stage; announced on bar_s
+        auto qk = [&](int w, int st, int nc) {
+          const uint32_t idesc = IDESC_QK | (uint32_t(nc >> 3) << 17);
+          const uint32_t q = q_lo + (PAIR ? uint32_t(w) * (C::Q_BYTES >> 4) : 0u), k = k_lo + uint32_t(st) * (C::STAGE >> 4);
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const uint32_t off = (i & 3) << 5;
+            mma_ss(tmem + 256u * w, q + (((i >> 2) * C::Q_REGION + off) >> 4), k + (((i >> 2) * C::KV_REGION + off) >> 4), idesc, i > 0 ? 1u : 0u);
+          }
+          tc::mma_commit(s0 + 8 * w);
+        };
+        // O_w (+)= P_w V over the nc keys of a stage, P in two halves of 64 keys
+        auto pv = [&](int w, int st, bool first, uint32_t par, int nc) {
+          const uint32_t v = v_lo + uint32_t(st) * (C::STAGE >> 4);
+          const uint32_t o = tmem + 256u * w + 128u, s = tmem + 256u * w;
+          if (!wait(h0 + 8 * w, par)) return false;
+          if (nc == KT) {
+            tc::fence_after_sync();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_ts(o, s + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+            if (!wait(p0 + 8 * w, par)) return false;
+            tc::fence_after_sync();
+#pragma unroll
+            for (int k = 4; k < 8; ++k) mma_ts(o, s + 8 * k, v + k * 128, IDESC_PV, 1u);
+          } else {
+            if (!wait(p0 + 8 * w, par)) return false;
+            tc::fence_after_sync();
+#pragma unroll 1
+            for (int k = 0; k < nc / 16; ++k) mma_ts(o, s + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+          }
+          return true;
+        };
+        bool ok = true;
+        Item it;
+        int j0, j1;
+        if constexpr (PAIR) {
+          Item nx;
+          Pos kp{0, 0};               // K of the current tile
+          uint32_t np = 0, nq = 0;  // parity of the next P tile and Q block of each slot, as bits
+          bool more = next_item(it, j0, j1, false);
+          for (int w = 0; w < 2 && more && ok && it.need(w, 0); ++w) {
+            ok = wait(qf0 + 8 * w, 0) && wait(full0, 0);
+            if (!ok) break;
+            nq ^= 1u << w;
+            tc::fence_after_sync();
+            qk(w, 0, it.ncols(0));
+          }
+          while (more && ok) {
+            const bool next = next_item(nx, j0, j1, false);
+            for (int j = 1; j <= it.n && ok; ++j) {
+              const Pos vp = kp.plus(1), kn = kp.plus(2);  // V of tile j - 1, K of tile j
+              const int nc = it.ncols(j - 1);
+              const bool one_last = it.need(1, j - 1);
+#pragma unroll 1
+              for (int w = 0; w < 2 && ok; ++w) {
+                const bool had = it.need(w, j - 1), has = j < it.n && it.need(w, j);
+                if (had) {
+                  ok = pv(w, vp.s, it.first(w) == j - 1, np >> w, nc);
+                  np ^= 1u << w;
+                  if (!ok) break;
+                  if (!has) {
+                    if (it.next(w, j - 1) < it.n) {
+                      // its next tile comes after a gap: no S announces that this V is read
+                      if (w == (one_last ? 1 : 0)) tc::mma_commit(empty0 + 8 * vp.s);
+                    } else {
+                      tc::mma_commit(o0 + 8 * w);
+                    }
+                  }
+                }
+                const bool over = j == it.n && next && nx.need(w, 0);  // on to the next item
+                if (has || over) {
+                  if (over || it.first(w) == j) {  // its Q, which the slot has not used yet
+                    ok = wait(qf0 + 8 * w, nq >> w);
+                    if (!ok) break;
+                    nq ^= 1u << w;
+                  }
+                  if (over || !had) {  // no softmax thread has waited for this K
+                    ok = wait(full0 + 8 * kn.s, kn.ph);
+                    if (!ok) break;
+                    tc::fence_after_sync();
+                  }
+                  qk(w, kn.s, over ? nx.ncols(0) : it.ncols(j));
+                }
+              }
+              kp = kn;
+            }
+            it = nx;
+            more = next;
+          }
+        } else {
+          if (next_item(it, j0, j1, false)) {
+            const int m = j1 - j0;
+            auto place = [&](int i, int kv) {
+              Pos q{0, 0};
+              q.move(2 * int64_t(i) + kv);
+              return q;
+            };
+            ok = wait(qf0, 0);
+            for (int i = 0; i < 2 && i < m && ok; ++i) {
+              const Pos k = place(i, 0);
+              ok = wait(full0 + 8 * k.s, k.ph);
+              if (!ok) break;
+              tc::fence_after_sync();
+              qk(i, k.s, it.ncols(j0 + i));
+            }
+            for (int i = 0; i < m && ok; ++i) {
+              const int w = i & 1;
+              ok = pv(w, place(i, 1).s, i < 2, uint32_t(i >> 1), it.ncols(j0 + i));
+              if (!ok) break;
+              if (i + 2 < m) qk(w, place(i + 2, 0).s, it.ncols(j0 + i + 2));
+              else tc::mma_commit(o0 + 8 * w);
+            }
+          }
+        }
+        if (!ok) give_up();
+        tc::mma_commit(drain);
+        tc::mbar_wait(drain, 0, &s_zero);
+      }
+    } else if (warp == SCAN_WARP) {
+      // ---------------- the scan: where rows see a tile in part, an infinity or a
+      // NaN in V would reach the others (0 x inf); such items are done again row by row
+      Pos at{0, 0};
+      bool ok = true;
+      Item it;
+      int j0, j1, seq = 0;
+      while (ok && next_item(it, j0, j1, false)) {
+        if (lane == 0) s_dirty[seq % SEEN] = 0;
+        __syncwarp();
+        for (int j = j0; j < j1 && ok; ++j) {
+          const bool look = (it.need(0, j) && !it.whole(p, 0, j)) || (it.need(1, j) && !it.whole(p, 1, j));
+          for (int kv = 0; kv < 2; ++kv) {
+            ok = __all_sync(0xffffffffu, wait(full0 + 8 * at.s, at.ph));
+            if (!ok) break;
+            if (kv == 1 && look) {
+              const uint32_t st = ring + uint32_t(at.s) * C::STAGE;
+              const int r0 = it.beg(j) - it.slot0(j), rows = it.end(j) - it.beg(j);
+              uint32_t bad = 0;
+#pragma unroll 4
+              for (int i = lane; i < rows * NR * 8; i += 32) {
+                const int rr = r0 + i / (NR * 8), rc = i % (NR * 8);
+                uint32_t u[4];
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                             : "r"(st + (rc >> 3) * C::KV_REGION + rr * 128 + ((rc & 7) << 4)));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  // the exponent of either half all ones: adding one to it carries out of it
+                  const uint32_t y = (u[e] & 0x7f807f80u) + 0x00800080u;
+                  bad |= y & 0x80008000u;
+                }
+              }
+              if (__any_sync(0xffffffffu, bad != 0u) && lane == 0) s_dirty[seq % SEEN] = 1;
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(empty0 + 8 * at.s);
+            at = at.plus(1);
+          }
+        }
+        __syncwarp();
+        if (ok && lane == 0) tc::mbar_arrive(scan0 + 8 * (seq % SEEN));
+        ++seq;
+      }
+      if (!ok) give_up();
+    }
+  }
+
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  if constexpr (!PAIR) {
+    // ---------------- join the slots' and the splits' parts
+    x_next = int(blockIdx.x) / nsplit;
+    Item it;
+    load_item<PAIR>(P, x_next, it, false);
+    const int per = (it.n + nsplit - 1) / nsplit, j0 = ::min(it.n, split * per), m = ::min(it.n, j0 + per) - j0;
+    const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
+    constexpr int CH = D / 4;  // 16-byte columns of a part's row, swizzled by the row
+    float *part = reinterpret_cast<float *>(smem + C::NQ * C::Q_BYTES);
+    if (warp < 8) {
+      const int w = warp >> 2, row = 32 * (warp & 3) + lane;
+      const bool has = w < m && s_abort == 0;
+      if (!has) s_ml[w][row] = make_float2(-INFINITY, 0.f);
+      if (has && 32 * (warp & 3) < rows_blk) {
+        const uint32_t tl = tmem + (uint32_t(32 * (warp & 3)) << 16) + 256u * w;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t ov[32];
+          tc::tmem_ld32(tl + 128 + c * 32, ov);
+          tc::tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint4 *>(part + (w * ROWS + row) * D + (((c * 8 + e) ^ (row & (CH - 1))) << 2)) =
+                make_uint4(ov[4 * e], ov[4 * e + 1], ov[4 * e + 2], ov[4 * e + 3]);
+        }
+      }
+    }
+    tc::fence_before_sync();
+    __syncwarp();
+    if (nsplit > 1) cluster_sync();
+    else __syncthreads();
+    const int parts = 2 * nsplit;
+    const uint32_t ml_a = smem_u32(&s_ml[0][0]), part_a = smem_u32(part), ab_a = smem_u32(&s_abort), dirty_a = smem_u32(&s_dirty[0]);
+    // part i: slot i & 1 of CTA i >> 1
+    int state = 0;  // 1: a CTA gave up, 2: done again row by row
+    if (lane < nsplit) {
+      uint32_t ab, di;
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(ab) : "r"(mapa(ab_a, lane)) : "memory");
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(di) : "r"(mapa(dirty_a, lane)) : "memory");
+      state = (ab ? 1 : 0) | (di ? 2 : 0);
+    }
+    const bool gave_up = __any_sync(0xffffffffu, state & 1), again = __any_sync(0xffffffffu, state & 2);
+    const bool first_has = m > 0;  // (a CTA without tiles has no row descriptions: it joins nothing)
+    const int joiners = it.n > 0 ? ::min(nsplit, (it.n + per - 1) / ::max(1, per)) : 1;
+    if (!gave_up && first_has && warp < 8) {
+      for (int row = split * 8 + warp; row < rows_blk; row += joiners * 8) {
+        const int off = s_row[row].off, t = s_row[row].t;
+        if (off < 0) continue;  // a malformed tree
+        const int h = it.g * p.G + row - (t - it.t00) * p.G;
+        if (again) {
+          slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc);
+          continue;
+        }
+        const float2 ml = lane < parts ? ld_cluster2(mapa(ml_a + ((lane & 1) * ROWS + row) * 8, lane >> 1)) : make_float2(-INFINITY, 0.f);
+        float M = ml.x;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
+        const float c = ml.y == 0.f ? 0.f : tc::ex2(ml.x - M);
+        float Z = ml.y == 0.f ? 0.f : c * ml.y;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) Z += __shfl_xor_sync(0xffffffffu, Z, k);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        const bool some = ml.y != 0.f;
+        for (int i = 0; i < parts; ++i) {
+          if (!__shfl_sync(0xffffffffu, int(some), i)) continue;
+          const float ci = __shfl_sync(0xffffffffu, c, i);
+          if (lane < CH) {
+            const float4 v = ld_cluster4(mapa(part_a + (((i & 1) * ROWS + row) * D + ((lane ^ (row & (CH - 1))) << 2)) * 4, i >> 1));
+            acc.x += ci * v.x;
+            acc.y += ci * v.y;
+            acc.z += ci * v.z;
+            acc.w += ci * v.w;
+          }
+        }
+        const float inv = 1.f / Z;
+        const int64_t orow = (int64_t(it.b) * p.T_max + t) * p.Hq + h;
+        if (lane < CH)
+          *reinterpret_cast<uint2 *>(p.out + orow * D + lane * 4) =
+              make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (lane == 0 && p.lse != nullptr) p.lse[orow] = (M + log2f(Z)) * LN2;
+      }
+    }
+    __syncwarp();
+    if (nsplit > 1) cluster_sync();  // no CTA leaves while another reads its shared memory
+    else __syncthreads();
+    tc::fence_after_sync();
+  }
+  if (warp == MMA_WARP) {
+    __syncwarp();
+    tc::tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+// (64 columns, 1 head, 64 slots, 1) boxes of one layer's K or V, 128-byte swizzle;
+// boxes outside read as zeros. Contiguous: (D, Hkv, capacity, B); paged: (D, Hkv,
+// 64, num_pages).
+bool kv_map(CUtensorMap *m, const void *base, const WinParams &p, int D) {
+  EncodeTiledFn enc = encode_tiled();
+  if (enc == nullptr) return false;
+  const bool paged = p.table != nullptr;
+  const cuuint64_t slots = paged ? 64 : cuuint64_t(p.capacity), outer = paged ? cuuint64_t(p.num_pages) : cuuint64_t(p.B);
+  const cuuint64_t dims[4] = {cuuint64_t(D), cuuint64_t(p.Hkv), slots, outer};
+  const cuuint64_t strides[3] = {cuuint64_t(D) * 2, cuuint64_t(p.Hkv) * D * 2, slots * p.Hkv * D * 2};
+  const cuuint32_t box[4] = {64, 1, 64, 1}, one[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The rows of a block, (token, head) in order: (64 columns, G heads, 1 KV head, TB
+// tokens, 1) boxes of (D, G, Hkv, T_max, B).
+bool q_map(CUtensorMap *m, const WinParams &p, int D, int TB) {
+  EncodeTiledFn enc = encode_tiled();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[5] = {cuuint64_t(D), cuuint64_t(p.G), cuuint64_t(p.Hkv), cuuint64_t(p.T_max), cuuint64_t(p.B)};
+  const cuuint64_t strides[4] = {cuuint64_t(D) * 2, cuuint64_t(p.G) * D * 2, cuuint64_t(p.st) * 2, cuuint64_t(p.sb) * 2};
+  const cuuint32_t box[5] = {64, cuuint32_t(p.G), 1, cuuint32_t(TB), 1}, one[5] = {1, 1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<__nv_bfloat16 *>(p.q), dims, strides, box, one,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool PAIR>
+dreams_status_t launch(TcParams &P, cudaStream_t stream) {
+  const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR>);
+  const dreams_status_t st = ensure_max_dynamic_smem(kernel, int(Cfg<D, PAIR>::SMEM));
+  if (st != DREAMS_OK) return st;
+  // the register shares must add up to no more than the launch's: a build that
+  // used fewer registers would wait for ever
+  static const bool shares_ok = [&] {
+    cudaFuncAttributes a;
+    return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs == LAUNCH_REGS;
+  }();
+  if (!shares_ok) return DREAMS_ERR_UNSUPPORTED;
+  if (!kv_map(&P.tmap_k, P.p.k, P.p, D) || !kv_map(&P.tmap_v, P.p.v, P.p, D) || !q_map(&P.tmap_q, P.p, D, P.TB)) return DREAMS_ERR_UNSUPPORTED;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(PAIR ? unsigned(std::min(P.items, num_sms())) : unsigned(P.items) * unsigned(P.p.nsplit));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = Cfg<D, PAIR>::SMEM;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(P.p.nsplit);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = !PAIR && P.p.nsplit > 1 ? 1 : 0;
+  void *args[] = {&P};
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
+  if (e != cudaSuccess) {
+    set_last_cuda_error(e);
+    return DREAMS_ERR_CUDA;
+  }
+  return check_launch();
+}
+
+}  // namespace
+
+dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaStream_t stream) {
+  TcParams P;
+  memset(&P, 0, sizeof(P));
+  P.p = p;
+  P.TB = std::max(1, ROWS / p.G);
+  const int64_t heads = int64_t(p.B) * p.Hkv;
+  const int64_t blocks = (int64_t(p.T_max) + P.TB - 1) / P.TB, pairs = (blocks + 1) / 2;
+  test_stall(DREAMS_TEST_ATTENTION, &P.stall_at, &P.wait_ns);
+  // Tiles of a block, and the time of either layout in tiles: a pair of tiles
+  // costs about as much as two tiles of one block, and an item's start and end
+  // about five tiles (the pairs' mostly overlap).
+  const int64_t sms = num_sms();
+  const int64_t tiles = std::max<int64_t>(
+      1, (std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB)) + KT - 1) / KT + (p.sinks > 0 ? 1 : 0));
+  auto waves = [&](int64_t n) { return (n + sms - 1) / sms; };
+  const int64_t pair_cost = blocks > 1 ? waves(heads * pairs) * (2 * tiles + 2) + 4 : INT64_MAX;
+  int64_t best = INT64_MAX;
+  int nsplit = 1;
+  for (int ns = 1; ns <= 8; ns *= 2) {
+    if (ns > 1 && tiles < 2 * ns) break;
+    const int64_t cost = waves(heads * blocks * ns) * ((tiles + ns - 1) / ns + 6);
+    if (cost < best) {
+      best = cost;
+      nsplit = ns;
+    }
+  }
+  const bool pair = pair_cost <= best;
+  P.p.nsplit = pair ? 1 : nsplit;
+  P.nblk = int(pair ? pairs : blocks);
+  const int64_t items = heads * P.nblk;
+  if (items * P.p.nsplit > INT_MAX / 2) return DREAMS_ERR_UNSUPPORTED;
+  P.items = int(items);
+  if (kv->D == 128) return pair ? launch<128, true>(P, stream) : launch<128, false>(P, stream);
+  return pair ? launch<64, true>(P, stream) : launch<64, false>(P, stream);
+}
+
+}  // namespace win
+}  // namespace dreams

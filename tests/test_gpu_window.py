@@ -133,6 +133,16 @@ def test_prefill(dreams, Hq, Hkv, D, T, L):
     c.check(c.run(dreams), n=40)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,B,T,L,window,sinks,tree", [
+    (32, 32, 64, 2, 1400, 0, 100, 4, False), (32, 32, 128, 6, 650, 33, 90, 0, False), (32, 8, 128, 40, 64, 200, 150, 3, True),
+    (16, 16, 64, 24, 300, 1000, 1, 1, False), (28, 4, 128, 90, 40, 65, 64, 70, True)])
+def test_more_blocks_than_the_gpu_holds(dreams, Hq, Hkv, D, B, T, L, window, sinks, tree):
+    """Several blocks for every SM, of different lengths, some sequences idle."""
+    q_len = [0 if b % 7 == 3 else T - (b * 37) % T for b in range(B)]
+    c = Case(B + T, Hq, Hkv, D, [(L * (b + 1)) // B for b in range(B)], q_len, window, sinks, tree=tree, paged=tree, T_max=T)
+    c.check(c.run(dreams), n=12)
+
+
 def test_long_split_lists(dreams):
     """Few heads and a long window: the key list is split over a cluster."""
     c = Case(5, 4, 1, 128, [9001], [1], 8000, 16)
