@@ -45,7 +45,7 @@ constexpr int THREADS = 384;
 // gives some to the two softmax warpgroups, which hold 128 scores a thread.
 constexpr int LAUNCH_REGS = 168, SOFTMAX_REGS = 216, OTHER_REGS = 72;
 static_assert(256 * SOFTMAX_REGS + 128 * OTHER_REGS <= THREADS * LAUNCH_REGS, "the shares fit what the block is launched with");
-constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 10;
+constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 11;  // slot w's MMAs: warp MMA_WARP + w
 constexpr int SEEN = 8;  // items whose scan results are kept (more than the ring can be ahead)
 constexpr uint32_t TMEM_COLS = 512;
 constexpr float RESCALE = 8.f;  // log2 headroom of the reference maximum
@@ -79,32 +79,26 @@ struct Item {
   int nb;                  // blocks present (0: nothing to do)
   int lo, lo64, S1, hi;
   int ns, n;
-  int a0, a1, e0, e1;      // window tiles of each block: [a, e)
-  __device__ __forceinline__ int t0(int w) const { return w ? t01 : t00; }
-  __device__ __forceinline__ int tl(int w) const { return w ? tl1 : tl0; }
-  __device__ __forceinline__ int a(int w) const { return w ? a1 : a0; }
-  __device__ __forceinline__ int e(int w) const { return w ? e1 : e0; }
-  __device__ __forceinline__ bool need(int w, int j) const { return w < nb && j < e(w) && (j < ns || j >= a(w)); }
-  // the next tile of block w after j (n: none)
-  __device__ __forceinline__ int next(int w, int j) const {
-    int k = j + 1;
-    if (k >= ns) k = ::max(k, a(w));
-    return k < e(w) ? k : n;
-  }
-  __device__ __forceinline__ int first(int w) const { return w < nb ? next(w, -1) : n; }
+  int e0, a1;              // block 0 reads tiles [0, e0), block 1 [0, ns) and [a1, n)
+  __device__ __forceinline__ bool need0(int j) const { return j < e0; }
+  __device__ __forceinline__ bool need1(int j) const { return nb == 2 && j < n && (j < ns || j >= a1); }
   __device__ __forceinline__ int slot0(int j) const { return j < ns ? j * KT : lo64 + (j - ns) * KT; }
   __device__ __forceinline__ int beg(int j) const { return j < ns ? j * KT : ::max(lo, lo64 + (j - ns) * KT); }
   __device__ __forceinline__ int end(int j) const { return j < ns ? ::min(S1, j * KT + KT) : ::min(hi, lo64 + (j - ns) * KT + KT); }
   __device__ __forceinline__ int ncols(int j) const { return (end(j) - slot0(j) + 31) & ~31; }
-  // does every row of block w see the whole tile?
-  __device__ __forceinline__ bool whole(const WinParams &p, int w, int j) const {
-    const int s = slot0(j);
-    if (beg(j) != s || end(j) != s + KT) return false;
-    if (j < ns) return true;
-    const bool tree = p.parent != nullptr;
-    return s > L + tl(w) - p.window && s + KT <= (tree ? L : L + t0(w) + 1);
-  }
 };
+
+// The tiles that every row of a block sees whole: [0, sink) and [from, to).
+struct Whole {
+  int sink, from, to;
+  __device__ __forceinline__ bool operator()(int j) const { return j < sink || (j >= from && j < to); }
+};
+__device__ __forceinline__ Whole whole_tiles(const WinParams &p, const Item &it, int w) {
+  const int t0 = w ? it.t01 : it.t00, tl = w ? it.tl1 : it.tl0;
+  const int from = ::max(it.lo, it.L + tl - p.window + 1) - it.lo64;                              // >= 0
+  const int to = ::min(it.hi, p.parent != nullptr ? it.L : it.L + t0 + 1) - it.lo64;
+  return Whole{it.S1 / KT, it.ns + (from + KT - 1) / KT, it.ns + (to > 0 ? to / KT : 0)};
+}
 
 template <bool PAIR>
 __device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bool report) {
@@ -141,11 +135,34 @@ __device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bo
   it.n = it.ns + (it.hi - it.lo64 + KT - 1) / KT;
   // with more sinks than slots before the window, the first window tiles hold sinks too
   const int lo1 = ::max(0, it.L + (tree ? 0 : it.t01) - p.window + 1);
-  it.a0 = it.ns;
   it.a1 = p.sinks > it.lo ? it.ns : it.ns + (lo1 - it.lo64) / KT;
   it.e0 = it.ns + (it.L + it.tl0 - it.lo64) / KT + 1;
-  it.e1 = it.n;
 }
+
+// O *= corr, row by row (rare: kept out of the softmax loop's code).
+template <int D>
+__device__ __noinline__ void rescale(uint32_t tl, float corr) {
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t ov[32];
+    tc::tmem_ld32(tl + c * 32, ov);
+    tc::tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+    tc::tmem_st32(tl + c * 32, ov);
+  }
+  tc::tmem_wait_st();
+}
+
+// An arrival by the threads for which `yes` holds, without a branch.
+__device__ __forceinline__ void arrive_if(uint32_t bar, bool yes) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %1, 0;\n @p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar), "r"(int(yes)) : "memory");
+}
+
+// What a softmax warp keeps of an item in shared memory.
+struct Slot {
+  int L, lo, lo64, S1, hi, ns, t0, rows, b, g, first, other, bad;
+};
 
 // A place in the ring of stages: index and phase.
 template <int N>
@@ -160,10 +177,10 @@ struct Place {
     }
     return q;
   }
-  __device__ __forceinline__ void move(int64_t d) {  // any d >= 0
-    const int64_t at = s + d;
-    s = int(at % N);
-    ph ^= uint32_t(at / N) & 1u;
+  __device__ __forceinline__ void move(int d) {  // any d >= 0
+    const uint32_t at = uint32_t(s + d), q = at / N;
+    s = int(at - q * N);
+    ph ^= q & 1u;
   }
 };
 
@@ -217,19 +234,38 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, ui
       "r"(a), "r"(b_lo), "r"(idesc), "r"(acc), "n"(DESC_HI)
       : "memory");
 }
+// tc::mbar_wait with a hint that lets the hardware suspend the warp for longer: a
+// spinning warp takes issue slots from the softmax warps of its scheduler.
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(ok)
+               : "r"(bar), "r"(parity), "r"(20000u)
+               : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int *abort, uint64_t limit_ns) {
+  uint64_t t0 = 0;
+  for (;;) {
+    if (try_wait(bar, parity)) return true;
+    const uint64_t now = tc::global_ns();
+    if (t0 == 0) t0 = now;
+    if (*abort || now - t0 > limit_ns) return false;
+  }
+}
 // The low n bits of a word (n may be any integer).
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// What a query row sees, for the masks.
+// A query row: its position (less L) and, in a tree, the new slots it sees.
 struct Row {
-  int plow, phi;           // window slots [plow, phi) (tree: committed slots)
-  int sink;                // slots below it are seen too: min(sinks, phi)
-  unsigned long long anc;  // tree: the new slots
-  int L;
-  // allowed columns among slots base .. base + 31, inside the tile's [beg, end)
-  __device__ __forceinline__ uint32_t word(int base, int beg, int end) const {
-    uint32_t m = (low_bits(phi - base) & ~low_bits(plow - base)) | low_bits(sink - base);
-    if (anc != 0ull) {
+  int off;
+  unsigned long long anc;
+  // the columns it sees among slots base .. base + 31, inside the tile's [beg, end)
+  __device__ __forceinline__ uint32_t word(const WinParams &p, int L, int base, int beg, int end) const {
+    const int phi = p.parent != nullptr ? L : L + off + 1;  // window slots [plow, phi), sinks below
+    const int plow = ::max(0, L + off - p.window + 1);
+    uint32_t m = (low_bits(phi - base) & ~low_bits(plow - base)) | low_bits(::min(p.sinks, phi) - base);
+    if (p.parent != nullptr) {
       const int sh = base - L;
       m |= (sh >= 64 || sh <= -32) ? 0u : (sh >= 0 ? uint32_t(anc >> sh) : uint32_t(anc << (-sh)));
     }
@@ -300,10 +336,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST];
-  __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain, bar_never;
+  __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
   __shared__ int8_t s_par[8][64];
+  __shared__ Slot s_slot[8];
   __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
   __shared__ struct { int off, t; unsigned long long anc; } s_row[PAIR ? 1 : ROWS];
 
@@ -313,11 +350,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   const uint32_t ring = base + C::NQ * C::Q_BYTES;
   const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty);
   const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
-                 o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain = smem_u32(&bar_drain), never = smem_u32(&bar_never);
+                 o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
   if (tid == TMA_WARP * 32) {
     for (int i = 0; i < NST; ++i) {
       tc::mbar_init(full0 + 8 * i, 1);
-      tc::mbar_init(empty0 + 8 * i, 2);  // its last reader on the tensor pipe, and the scan
+      tc::mbar_init(empty0 + 8 * i, 3);  // both slots, and the scan
     }
     for (int w = 0; w < 2; ++w) {
       tc::mbar_init(qf0 + 8 * w, 1);
@@ -326,8 +363,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       tc::mbar_init(h0 + 8 * w, 128);
       tc::mbar_init(p0 + 8 * w, 128);
       tc::mbar_init(o0 + 8 * w, 1);
+      tc::mbar_init(drain0 + 8 * w, 1);
     }
-    tc::mbar_init(drain, 1);
     tc::mbar_init(never, 1);  // nothing arrives on it
     s_abort = s_zero = 0;
     for (int i = 0; i < SEEN; ++i) {
@@ -355,7 +392,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       flag(p.status, DREAMS_DATA_TIMEOUT);
     }
   };
-  auto wait = [&](uint32_t bar, uint32_t parity) { return tc::mbar_wait(bar, parity & 1u, abort_flag, wait_ns); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return long_wait(bar, parity & 1u, abort_flag, wait_ns); };
 
   // The items of this CTA; without PAIR it has one, shared by a cluster.
   const int nsplit = PAIR ? 1 : p.nsplit;
@@ -377,85 +414,130 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     // ---------------- softmax warpgroup w: the rows of slot w
+    // A thread holds a row's 128 scores, so little else stays in registers: what an
+    // item is lies in shared memory, one copy per warp, and is read where needed.
     const int w = warp >> 2;
     const int row = 32 * (warp & 3) + lane;
     const uint32_t tl = tmem + (uint32_t(32 * (warp & 3)) << 16) + 256u * w;
     const bool lead = (warp & 3) == 0 && lane == 0;
-    uint32_t ns_seen = 0, no_seen = 0;  // S tiles and finished items of this slot
-    Pos ring0{0, 0};                    // K of the item's first tile
+    volatile Slot *sp = &s_slot[warp];
+    uint32_t par = 0;  // bit 0: parity of the next S tile, bit 1: of the next finished O
+    Pos pos{0, 0};     // K of the current tile
     bool ok = true;
-    Item it;
-    int j0, j1, seq = 0;
-    for (; ok && next_item(it, j0, j1, false); ++seq) {
-      const int blk = PAIR ? w : 0;
-      const bool here = !PAIR || w < it.nb;
-      auto next_of = [&](int j) { return PAIR ? it.next(w, j) : ::min(j1, j + 2); };
-      auto place = [&](int j, int kv) {  // of K (0) or V (1) of tile j
-        Pos q = ring0;
-        q.move(2 * int64_t(j - j0) + kv);
-        return q;
-      };
-      // a tile's stages are given back by the slot that reads it last; what copies
-      // must not leave behind is cleaned by the one that reads it first
-      auto last_user = [&](int j) { return !PAIR || !(w == 0 && it.need(1, j)); };
-      auto first_user = [&](int j) { return !PAIR || !(w == 1 && it.need(0, j)); };
-      int j = PAIR ? it.first(w) : ::min(j1, j0 + w);
-      const bool any = j < j1;
-      // this thread's row
-      const int t0 = here ? it.t0(blk) : it.t00, rows_blk = here ? (it.tl(blk) - t0 + 1) * p.G : 0;
-      const bool real = row < rows_blk;
-      const int n_act = ::min(4, (rows_blk + 31) / 32);  // warps with rows
-      const bool live = (warp & 3) < n_act;
-      const int t = real ? t0 + row / p.G : t0;
-      int off = t;
-      bool tree_ok = true;
-      Row r;
-      r.anc = 0ull;
-      if (p.parent != nullptr) {
-        // this warp's copy of the parents, checked before any walk
-        __syncwarp();  // the last item's walks are over
-        int bad = 0;
-        for (int i = lane; i < it.T; i += 32) {
-          const int par = __ldg(p.parent + int64_t(it.b) * p.T_max + i);
-          s_par[warp][i] = int8_t(par);  // (a bad one is not used)
-          bad |= i == 0 ? par != -1 : (par < 0 || par >= i);
+    int seq = 0;
+    while (ok) {
+      int j, jend, gap, to;  // tiles j .. jend-1 but for [gap, to), which only the other slot reads
+      int wfrom, wto;        // tiles that all rows see whole
+      bool live;             // does this warp have rows?
+      int ahead;             // stages between this slot's last tile and the next item
+      {
+        Item it;
+        int j0, j1;
+        if (!next_item(it, j0, j1, false)) break;
+        const int blk = PAIR ? w : 0;
+        const bool here = !PAIR || w < it.nb;
+        const int t0 = blk ? it.t01 : it.t00, rows_blk = here ? ((blk ? it.tl1 : it.tl0) - t0 + 1) * p.G : 0;
+        live = 32 * (warp & 3) < rows_blk;
+        const Whole wh = whole_tiles(p, it, blk);
+        wfrom = wh.from;
+        wto = wh.to;
+        j = j0;
+        jend = j1;
+        gap = to = INT_MAX;
+        if (PAIR) {
+          if (!here) jend = j;
+          else if (w == 0) jend = it.e0;
+          else if (it.a1 > it.ns) {
+            gap = it.ns;
+            to = it.a1;
+          }
+          if (here && j >= gap) j = to;
+        } else {
+          j = ::min(j1, j0 + w);
         }
-        tree_ok = !__any_sync(0xffffffffu, bad);
-        if (tree_ok) r.anc = tree_row(p, s_par[warp], it.L, t, off);
-        else if (lead && w == 0 && it.g == 0 && split == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
+        pos.move(2 * (j - j0));
+        ahead = 2 * (j1 - j0);
+        __syncwarp();  // the last item's readers are done
+        if (lane == 0) {
+          sp->L = it.L;
+          sp->lo = it.lo;
+          sp->lo64 = it.lo64;
+          sp->S1 = it.S1;
+          sp->hi = it.hi;
+          sp->ns = it.ns;
+          sp->t0 = t0;
+          sp->rows = rows_blk;
+          sp->b = it.b;
+          sp->g = it.g;
+          sp->first = j;
+          sp->other = PAIR && w == 1 ? it.e0 : 0;  // tiles below it are block 0's too
+        }
+        int bad = 0;
+        if (p.parent != nullptr) {
+          for (int i = lane; i < it.T; i += 32) {
+            const int q = __ldg(p.parent + int64_t(it.b) * p.T_max + i);
+            s_par[warp][i] = int8_t(q);  // (a bad one is not used)
+            bad |= i == 0 ? q != -1 : (q < 0 || q >= i);
+          }
+          bad = __any_sync(0xffffffffu, bad);
+          if (bad && lead && w == 0 && it.g == 0 && split == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
+        }
+        if (lane == 0) sp->bad = bad;
+        ahead -= 2 * (j - j0);  // from tile j to the next item
+        __syncwarp();
       }
-      r.L = it.L;
-      r.plow = ::max(0, it.L + off - p.window + 1);
-      r.phi = p.parent != nullptr ? it.L : it.L + off + 1;
-      r.sink = ::min(p.sinks, r.phi);
-      if (!PAIR && w == 0) {
-        s_row[row].off = tree_ok ? off : -1;
-        s_row[row].t = t;
-        s_row[row].anc = r.anc;
+      const bool any = j < jend;
+      // this thread's row, and what it sees
+      Row r;
+      int t = 0;
+      {
+        const int t0 = sp->t0;
+        t = row < sp->rows ? t0 + row / p.G : t0;
+        r.off = t;
+        r.anc = 0ull;
+        if (p.parent != nullptr && sp->bad == 0) r.anc = tree_row(p, s_par[warp], sp->L, t, r.off);
       }
       float m_ref = -INFINITY, l = 0.f;
-      int prev = -1;
-      while (j < j1) {
-        if (!__all_sync(0xffffffffu, wait(s0 + 8 * w, ns_seen))) {
+      int v_back = -1;  // V stage to give back at the next wake-up
+      int v_end = -1;   // and the one to give back at the end
+      const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
+      while (j < jend) {
+        ok = wait(s0 + 8 * w, par);
+        if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
           break;
         }
-        ++ns_seen;
+        par ^= 1u;
         tc::fence_after_sync();
-        const int nj = next_of(j);
-        const Pos vpl = place(j, 1);
-        if (lead) {
-          // every MMA up to this S is done: K of this tile, V of the one before
-          if (last_user(j)) tc::mbar_arrive(empty0 + 8 * place(j, 0).s);
-          if (prev >= 0 && (!PAIR || prev == j - 1) && last_user(prev)) tc::mbar_arrive(empty0 + 8 * place(prev, 1).s);
-          if (PAIR && nj >= j1) tc::mbar_arrive(qe0 + 8 * w);  // Q of this slot
-        }
-        const int sl = it.slot0(j), beg = it.beg(j), end = it.end(j), nc = it.ncols(j);
-        uint32_t sv[KT];
-        float corr = 1.f;
-        bool resc = false;
-        uint64_t scale2 = 0, nmu2 = 0, acc2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
-        auto p_step = [&](const uint32_t *u, int c) {
+        // This slot's MMAs up to this S are done: the lead thread gives back K of this
+        // tile, V of the one before, and Q after the last.
+        const Pos vp = pos.plus(1);
+        int nj = j + (PAIR ? 1 : 2);
+        if (PAIR && nj == gap) nj = to;
+        arrive_if(empty0 + 8 * pos.s, lead);
+        arrive_if(empty0 + 8 * v_back, lead && v_back >= 0);
+        if (PAIR) arrive_if(qe0 + 8 * w, lead && nj >= jend);
+        v_end = vp.s;
+        v_back = !PAIR || nj == j + 1 ? v_end : -1;  // (before a gap the issuer's commit does it)
+
+        uint64_t acc2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+        // the reference maximum is raised (and O rescaled) only past 2^RESCALE
+        auto refer = [&](float mx) {
+          const bool resc = mx > m_ref + RESCALE;
+          if (__any_sync(0xffffffffu, resc)) {
+            float corr = 1.f;
+            if (resc) {
+              corr = m_ref == -INFINITY ? 0.f : tc::ex2(m_ref - mx);
+              m_ref = mx;
+              l *= corr;
+            }
+            if (j != sp->first) rescale<D>(tl + 128, corr);
+          }
+          const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
+          return f32x2(nmu, nmu);
+        };
+        // P of 32 columns, over the first half of as many columns of S
+        auto p_step = [&](const uint32_t *u, int c, uint64_t nmu2) {
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -467,153 +549,136 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           }
           tc::tmem_st16(tl + 16 * c, pk);
         };
-        if (live) {
-          float mx;
-          if (nc == KT) {
+        // P goes to the MMA thread in two halves of 64 keys
+        auto hand_over = [&](uint32_t bar) {
+          tc::tmem_wait_st();
+          tc::fence_before_sync();
+          tc::mbar_arrive(bar);
+        };
+        const bool full = j >= wfrom && j < wto;
+        int beg = 0, end = KT, nc = KT;  // the tile's columns
+        uint32_t mask[4] = {~0u, ~0u, ~0u, ~0u};
+        if (__builtin_expect(!full, 0)) {
+          const int ns = sp->ns, sl = j < ns ? j * KT : sp->lo64 + (j - ns) * KT;
+          beg = j < ns ? sl : ::max(sp->lo, sl);
+          end = j < ns ? ::min(sp->S1, sl + KT) : ::min(sp->hi, sl + KT);
+          const int L = sp->L;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tc::tmem_ld32(tl + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sv[32 * c]));
-            tc::tmem_wait_ld();
-            if (!it.whole(p, blk, j)) {
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const uint32_t m = r.word(sl + 32 * c, beg, end);
-#pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if (!((m >> e) & 1u)) sv[32 * c + e] = 0xff800000u;
-              }
-            }
-            float mt[43];
-#pragma unroll
-            for (int i = 0; i < 42; ++i)
-              mt[i] = max3f(__uint_as_float(sv[3 * i]), __uint_as_float(sv[3 * i + 1]), __uint_as_float(sv[3 * i + 2]));
-            mt[42] = fmaxf(__uint_as_float(sv[126]), __uint_as_float(sv[127]));
-#pragma unroll
-            for (int i = 0; i < 14; ++i) mt[i] = max3f(mt[3 * i], mt[3 * i + 1], mt[3 * i + 2]);
-            mt[14] = mt[42];
-#pragma unroll
-            for (int i = 0; i < 5; ++i) mt[i] = max3f(mt[3 * i], mt[3 * i + 1], mt[3 * i + 2]);
-            mx = max3f(max3f(mt[0], mt[1], mt[2]), mt[3], mt[4]);
-          } else {
-            // a cut tile: 32 columns at a time, read twice
-            mx = -INFINITY;
-#pragma unroll 1
-            for (int c = 0; c < nc / 32; ++c) {
-              uint32_t u[32];
-              tc::tmem_ld32(tl + 32 * c, u);
-              tc::tmem_wait_ld();
-              const uint32_t m = r.word(sl + 32 * c, beg, end);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, ((m >> e) & 1u) ? __uint_as_float(u[e]) : -INFINITY);
-            }
-          }
-          mx *= p.scale_log2;  // scale > 0
-          // the reference maximum is raised (and O rescaled) only past 2^RESCALE
-          resc = mx > m_ref + RESCALE;
-          if (resc) {
-            corr = m_ref == -INFINITY ? 0.f : tc::ex2(m_ref - mx);
-            m_ref = mx;
-            l *= corr;
-          }
-          const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
-          scale2 = f32x2(p.scale_log2, p.scale_log2);
-          nmu2 = f32x2(nmu, nmu);
-          if (nc == KT) {
-            p_step(sv, 0);
-            p_step(sv + 32, 1);
-          }
+          for (int c = 0; c < 4; ++c) mask[c] = r.word(p, L, sl + 32 * c, beg, end);
+          beg -= sl;
+          end -= sl;
+          nc = (end + 31) & ~31;
           // slots outside [beg, end) may hold any bits: their V rows become zeros
-          // once the copy has landed
-          if ((beg > sl || end < sl + nc) && first_user(j)) {
-            if (!__all_sync(0xffffffffu, wait(full0 + 8 * vpl.s, vpl.ph))) {
+          // once the copy has landed (by the slot that reads the tile first)
+          if (live && (beg > 0 || end < nc) && !(PAIR && w == 1 && j < sp->other)) {
+            ok = wait(full0 + 8 * vp.s, vp.ph);
+            if (!__all_sync(0xffffffffu, ok)) {
               ok = false;
               break;
             }
-            const uint32_t st = ring + uint32_t(vpl.s) * C::STAGE;
-            const int head = beg - sl, tail = sl + nc - end;
-            for (int i = row; i < (head + tail) * NR * 8; i += 32 * n_act) {
+            const uint32_t st = ring + uint32_t(vp.s) * C::STAGE;
+            const int n_act = ::min(4, (sp->rows + 31) / 32);  // warps with rows
+#pragma unroll 1
+            for (int i = row; i < (beg + nc - end) * NR * 8; i += 32 * n_act) {
               const int z = i / (NR * 8), rc = i % (NR * 8);
-              const int rr = z < head ? z : end - sl + (z - head);
+              const int rr = z < beg ? z : end + (z - beg);
               asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(st + (rc >> 3) * C::KV_REGION + rr * 128 + ((rc & 7) << 4)),
                            "r"(0u)
                            : "memory");
             }
             tc::fence_proxy_async_smem();
           }
-          if (prev >= 0 && __any_sync(0xffffffffu, resc)) {
+        }
+        if (__builtin_expect(nc == KT, 1)) {
+          uint32_t sv[KT];
+          uint64_t nmu2 = 0;
+          if (live) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t ov[32];
-              tc::tmem_ld32(tl + 128 + c * 32, ov);
-              tc::tmem_wait_ld();
+            for (int c = 0; c < 4; ++c) tc::tmem_ld32(tl + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sv[32 * c]));
+            tc::tmem_wait_ld();
+            if (__builtin_expect(!full, 0)) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
-              tc::tmem_st32(tl + 128 + c * 32, ov);
+              for (int c = 0; c < KT; ++c)
+                if (!((mask[c >> 5] >> (c & 31)) & 1u)) sv[c] = 0xff800000u;
             }
+            float mt[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mt[i] = fmaxf(__uint_as_float(sv[32 * i]), __uint_as_float(sv[32 * i + 1]));
+#pragma unroll
+            for (int e = 2; e < 32; e += 2)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) mt[i] = max3f(mt[i], __uint_as_float(sv[32 * i + e]), __uint_as_float(sv[32 * i + e + 1]));
+            nmu2 = refer(fmaxf(max3f(mt[0], mt[1], mt[2]), mt[3]) * p.scale_log2);  // scale > 0
+            p_step(sv, 0, nmu2);
+            p_step(sv + 32, 1, nmu2);
           }
-        }
-        // one thread waits for the copies the MMA thread needs (V of this tile, K
-        // of the slot's next one), so that it waits for P alone
-        bool kv_ok = true;
-        if (lead) kv_ok = wait(full0 + 8 * vpl.s, vpl.ph);
-        if (!__all_sync(0xffffffffu, kv_ok)) {
-          ok = false;
-          break;
-        }
-        tc::tmem_wait_st();
-        tc::fence_before_sync();
-        tc::mbar_arrive(h0 + 8 * w);
-        if (live) {
-          if (nc == KT) {
-            p_step(sv + 64, 2);
-            p_step(sv + 96, 3);
-          } else {
-            // P of 32 columns goes over columns that have been read
+          hand_over(h0 + 8 * w);
+          if (live) {
+            p_step(sv + 64, 2, nmu2);
+            p_step(sv + 96, 3, nmu2);
+          }
+          hand_over(p0 + 8 * w);
+        } else {
+          // a cut tile: 32 columns at a time, read once for the maximum and once for P
+          uint32_t u[32];
+          auto load = [&](int c) {
+            tc::tmem_ld32(tl + 32 * c, u);
+            tc::tmem_wait_ld();
+            const uint32_t m = c == 0 ? mask[0] : c == 1 ? mask[1] : mask[2];
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!((m >> e) & 1u)) u[e] = 0xff800000u;
+          };
+          uint64_t nmu2 = 0;
+          if (live) {
+            float mx = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < nc / 32; ++c) {
-              uint32_t u[32];
-              tc::tmem_ld32(tl + 32 * c, u);
-              tc::tmem_wait_ld();
-              const uint32_t m = r.word(sl + 32 * c, beg, end);
+            for (int c = 0; 32 * c < nc; ++c) {
+              load(c);
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!((m >> e) & 1u)) u[e] = 0xff800000u;
-              p_step(u, c);
+              for (int e = 0; e < 32; e += 2) mx = max3f(mx, __uint_as_float(u[e]), __uint_as_float(u[e + 1]));
             }
+            nmu2 = refer(mx * p.scale_log2);
           }
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            if (live && 32 * c < nc) {
+              load(c);
+              p_step(u, c, nmu2);
+            }
+            if (c & 1) hand_over((c == 1 ? h0 : p0) + 8 * w);
+          }
+        }
+        {
           float a0, a1, b0, b1;
           f32x2_split(acc2[0], a0, a1);
           f32x2_split(acc2[1], b0, b1);
           l += (a0 + a1) + (b0 + b1);
         }
-        if (lead && nj < j1) {
-          const Pos k = place(nj, 0);
-          kv_ok = wait(full0 + 8 * k.s, k.ph);
-        }
-        if (!__all_sync(0xffffffffu, kv_ok)) {
-          ok = false;
-          break;
-        }
-        tc::tmem_wait_st();
-        tc::fence_before_sync();
-        tc::mbar_arrive(p0 + 8 * w);
-        prev = j;
+        pos = pos.plus(2);
+        if (!PAIR) pos = pos.plus(2);
+        else if (nj != j + 1) pos.move(2 * (nj - j - 1));
+        ahead -= 2 * (nj - j);
         j = nj;
       }
       if (ok && any) {
-        ok = __all_sync(0xffffffffu, wait(o0 + 8 * w, no_seen));  // all MMAs of the slot are done
-        ++no_seen;
+        ok = __all_sync(0xffffffffu, wait(o0 + 8 * w, par >> 1));  // all MMAs of the slot are done
+        par ^= 2u;
         tc::fence_after_sync();
-        if (ok && lead && last_user(prev)) tc::mbar_arrive(empty0 + 8 * place(prev, 1).s);
+        if (ok && lead && v_end >= 0) tc::mbar_arrive(empty0 + 8 * v_end);
       }
       ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
       if (!ok) break;
-      ring0.move(2 * int64_t(j1 - j0));
+      if (PAIR) pos.move(ahead);
       const bool dirty = *reinterpret_cast<volatile int *>(&s_dirty[seq % SEEN]) != 0;
+      ++seq;
 
+      const bool real = row < sp->rows, tree_ok = sp->bad == 0;
       if constexpr (PAIR) {
+        const int h = sp->g * p.G + row - (t - sp->t0) * p.G;
         if (any && tree_ok && !dirty) {
           const float inv = 1.f / l;
-          const int64_t orow = (int64_t(it.b) * p.T_max + t) * p.Hq + it.g * p.G + (row - (t - t0) * p.G);
+          const int64_t orow = (int64_t(sp->b) * p.T_max + t) * p.Hq + h;
           if (live) {
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
@@ -631,15 +696,19 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           }
         } else if (any && tree_ok) {
           for (int i = 0; i < 32; ++i) {
-            const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, off, i);
+            const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, r.off, i), hi = __shfl_sync(0xffffffffu, h, i);
             const unsigned long long ai = __shfl_sync(0xffffffffu, r.anc, i);
-            const int ri = 32 * (warp & 3) + i;
-            if (ri < rows_blk) slow_row<D>(p, it.b, it.g, it.L, ti, it.g * p.G + ri - (ti - t0) * p.G, oi, ai);
+            if (__shfl_sync(0xffffffffu, int(real), i)) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai);
           }
         }
         tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
       } else {
-        // the slot's part into shared memory (below)
+        // what the rows are, and the slot's (m, l), for the join below
+        if (w == 0) {
+          s_row[row].off = tree_ok ? r.off : -1;
+          s_row[row].t = t;
+          s_row[row].anc = r.anc;
+        }
         s_ml[w][row] = any && live ? make_float2(m_ref, l) : make_float2(-INFINITY, 0.f);
       }
     }
@@ -712,7 +781,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
                   tc::mbar_arrive_expect_tx(qf0 + 8 * w, uint32_t(NR * p.G * P.TB * 128));
 #pragma unroll
                   for (int r = 0; r < NR; ++r)
-                    tc::tma_load_5d(q_s(w) + r * C::Q_REGION, &P.tmap_q, qf0 + 8 * w, r * 64, 0, it.g, it.t0(w), it.b);
+                    tc::tma_load_5d(q_s(w) + r * C::Q_REGION, &P.tmap_q, qf0 + 8 * w, r * 64, 0, it.g, w ? it.t01 : it.t00, it.b);
                 }
               }
             }
@@ -724,134 +793,122 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         for (int w = 0; w < C::NQ; ++w)
           if (nq[w] > 0) tc::mbar_wait(qf0 + 8 * w, (nq[w] - 1) & 1u, &s_zero);
       }
-    } else if (warp == MMA_WARP) {
-      // ---------------- MMA issuer
+    } else if (warp < SCAN_WARP) {
+      // ---------------- MMA issuers, one for each slot: the tensor pipe takes their
+      // instructions as they come, so one's waits run under the other's MMAs
       if (lane == 0) {
+        const int w = warp - MMA_WARP;
         // low words of the operands' descriptors: address / 16 (of 18 bits: in a
         // cluster the bits above say which CTA), leading-dimension offset / 16
         const uint32_t ring16 = (ring & 0x3FFFFu) >> 4;
-        const uint32_t q_lo = ((q_s(0) & 0x3FFFFu) >> 4) | (1u << 16), k_lo = ring16 | (1u << 16), v_lo = ring16 | ((C::KV_REGION >> 4) << 16);
+        const uint32_t q_lo = ((q_s(w) & 0x3FFFFu) >> 4) | (1u << 16), k_lo = ring16 | (1u << 16), v_lo = ring16 | ((C::KV_REGION >> 4) << 16);
+        const uint32_t s_col = tmem + 256u * w, o_col = s_col + 128u;
         constexpr uint32_t IDESC_QK = tc::idesc_bf16_f32(ROWS, 0, false);
         constexpr uint32_t IDESC_PV = tc::idesc_bf16_f32(ROWS, D, true);
-        // S_w = Q_w K^T over the first nc keys of a stage; announced on bar_s
-        auto qk = [&](int w, int st, int nc) {
+        // S = Q K^T over the first nc keys of a stage
+        auto qk = [&](int st, int nc) {
           const uint32_t idesc = IDESC_QK | (uint32_t(nc >> 3) << 17);
-          const uint32_t q = q_lo + (PAIR ? uint32_t(w) * (C::Q_BYTES >> 4) : 0u), k = k_lo + uint32_t(st) * (C::STAGE >> 4);
+          const uint32_t k = k_lo + uint32_t(st) * (C::STAGE >> 4);
 #pragma unroll
           for (int i = 0; i < D / 16; ++i) {
             const uint32_t off = (i & 3) << 5;
-            mma_ss(tmem + 256u * w, q + (((i >> 2) * C::Q_REGION + off) >> 4), k + (((i >> 2) * C::KV_REGION + off) >> 4), idesc, i > 0 ? 1u : 0u);
+            mma_ss(s_col, q_lo + (((i >> 2) * C::Q_REGION + off) >> 4), k + (((i >> 2) * C::KV_REGION + off) >> 4), idesc, i > 0 ? 1u : 0u);
           }
           tc::mma_commit(s0 + 8 * w);
         };
-        // O_w (+)= P_w V over the nc keys of a stage, P in two halves of 64 keys
-        auto pv = [&](int w, int st, bool first, uint32_t par, int nc) {
-          const uint32_t v = v_lo + uint32_t(st) * (C::STAGE >> 4);
-          const uint32_t o = tmem + 256u * w + 128u, s = tmem + 256u * w;
-          if (!wait(h0 + 8 * w, par)) return false;
-          if (nc == KT) {
-            tc::fence_after_sync();
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mma_ts(o, s + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
-            if (!wait(p0 + 8 * w, par)) return false;
-            tc::fence_after_sync();
-#pragma unroll
-            for (int k = 4; k < 8; ++k) mma_ts(o, s + 8 * k, v + k * 128, IDESC_PV, 1u);
-          } else {
-            if (!wait(p0 + 8 * w, par)) return false;
-            tc::fence_after_sync();
-#pragma unroll 1
-            for (int k = 0; k < nc / 16; ++k) mma_ts(o, s + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
-          }
-          return true;
-        };
         bool ok = true;
+        Pos at{0, 0};                      // K of the item's first tile
+        uint32_t p_par = 0, q_par = 0;     // parities of the next P and Q
         Item it;
         int j0, j1;
-        if constexpr (PAIR) {
-          Item nx;
-          Pos kp{0, 0};               // K of the current tile
-          uint32_t np = 0, nq = 0;  // parity of the next P tile and Q block of each slot, as bits
-          bool more = next_item(it, j0, j1, false);
-          for (int w = 0; w < 2 && more && ok && it.need(w, 0); ++w) {
-            ok = wait(qf0 + 8 * w, 0) && wait(full0, 0);
-            if (!ok) break;
-            nq ^= 1u << w;
-            tc::fence_after_sync();
-            qk(w, 0, it.ncols(0));
-          }
-          while (more && ok) {
-            const bool next = next_item(nx, j0, j1, false);
-            for (int j = 1; j <= it.n && ok; ++j) {
-              const Pos vp = kp.plus(1), kn = kp.plus(2);  // V of tile j - 1, K of tile j
-              const int nc = it.ncols(j - 1);
-              const bool one_last = it.need(1, j - 1);
-#pragma unroll 1
-              for (int w = 0; w < 2 && ok; ++w) {
-                const bool had = it.need(w, j - 1), has = j < it.n && it.need(w, j);
-                if (had) {
-                  ok = pv(w, vp.s, it.first(w) == j - 1, np >> w, nc);
-                  np ^= 1u << w;
-                  if (!ok) break;
-                  if (!has) {
-                    if (it.next(w, j - 1) < it.n) {
-                      // its next tile comes after a gap: no S announces that this V is read
-                      if (w == (one_last ? 1 : 0)) tc::mma_commit(empty0 + 8 * vp.s);
-                    } else {
-                      tc::mma_commit(o0 + 8 * w);
-                    }
-                  }
-                }
-                const bool over = j == it.n && next && nx.need(w, 0);  // on to the next item
-                if (has || over) {
-                  if (over || it.first(w) == j) {  // its Q, which the slot has not used yet
-                    ok = wait(qf0 + 8 * w, nq >> w);
-                    if (!ok) break;
-                    nq ^= 1u << w;
-                  }
-                  if (over || !had) {  // no softmax thread has waited for this K
-                    ok = wait(full0 + 8 * kn.s, kn.ph);
-                    if (!ok) break;
-                    tc::fence_after_sync();
-                  }
-                  qk(w, kn.s, over ? nx.ncols(0) : it.ncols(j));
-                }
-              }
-              kp = kn;
+        while (ok && next_item(it, j0, j1, false)) {
+          auto need = [&](int j) { return PAIR ? (w ? it.need1(j) : it.need0(j)) : ((j - j0) & 1) == w; };
+          bool first = true;      // O is not begun
+          bool have_s = false;    // Q K^T of tile j is under way
+          Pos pos = at;
+          for (int j = j0; j < j1 && ok; ++j) {
+            const Pos vp = pos.plus(1);
+            if (!need(j)) {
+              // the other slot's tile: this one gives it back unread
+              ok = wait(full0 + 8 * pos.s, pos.ph);
+              if (ok) tc::mbar_arrive(empty0 + 8 * pos.s);
+              ok = ok && wait(full0 + 8 * vp.s, vp.ph);
+              if (ok) tc::mbar_arrive(empty0 + 8 * vp.s);
+              pos = pos.plus(2);
+              continue;
             }
-            it = nx;
-            more = next;
-          }
-        } else {
-          if (next_item(it, j0, j1, false)) {
-            const int m = j1 - j0;
-            auto place = [&](int i, int kv) {
-              Pos q{0, 0};
-              q.move(2 * int64_t(i) + kv);
-              return q;
-            };
-            ok = wait(qf0, 0);
-            for (int i = 0; i < 2 && i < m && ok; ++i) {
-              const Pos k = place(i, 0);
-              ok = wait(full0 + 8 * k.s, k.ph);
+            const int nc = it.ncols(j);
+            if (!have_s) {
+              if (first) {
+                ok = wait(qf0 + 8 * (PAIR ? w : 0), q_par);
+                q_par ^= 1u;
+              }
+              ok = ok && wait(full0 + 8 * pos.s, pos.ph);
               if (!ok) break;
               tc::fence_after_sync();
-              qk(i, k.s, it.ncols(j0 + i));
+              qk(pos.s, nc);
             }
-            for (int i = 0; i < m && ok; ++i) {
-              const int w = i & 1;
-              ok = pv(w, place(i, 1).s, i < 2, uint32_t(i >> 1), it.ncols(j0 + i));
+            // the next tile, if its Q K^T can follow at once: K must have landed
+            const int nj = j + (PAIR ? 1 : 2);
+            const bool follow = nj < j1 && need(nj);
+            const Pos np = PAIR ? pos.plus(2) : pos.plus(2).plus(2);
+            const int nnc = follow ? it.ncols(nj) : 0;
+            ok = wait(full0 + 8 * vp.s, vp.ph) && (!follow || !PAIR || wait(full0 + 8 * np.s, np.ph)) && wait(h0 + 8 * w, p_par);
+            if (!ok) break;
+            // O (+)= P V, P in two halves of 64 keys
+            const uint32_t v = v_lo + uint32_t(vp.s) * (C::STAGE >> 4);
+            if (nc == KT) {
+              tc::fence_after_sync();
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+              ok = wait(p0 + 8 * w, p_par);
               if (!ok) break;
-              if (i + 2 < m) qk(w, place(i + 2, 0).s, it.ncols(j0 + i + 2));
+              tc::fence_after_sync();
+#pragma unroll
+              for (int k = 4; k < 8; ++k) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, 1u);
+            } else {
+              ok = wait(p0 + 8 * w, p_par);
+              if (!ok) break;
+              tc::fence_after_sync();
+#pragma unroll 1
+              for (int k = 0; k < nc / 16; ++k) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+            }
+            p_par ^= 1u;
+            first = false;
+            if (follow) {
+              if (!PAIR) {
+                ok = wait(full0 + 8 * np.s, np.ph);
+                if (!ok) break;
+                tc::fence_after_sync();
+              }
+              qk(np.s, nnc);
+              have_s = true;
+            } else {
+              have_s = false;
+              bool later = false;
+              if (PAIR && w == 1) later = j < it.n - 1;  // after a gap: no S announces that this V is read
+              if (later) tc::mma_commit(empty0 + 8 * vp.s);
               else tc::mma_commit(o0 + 8 * w);
             }
+            pos = pos.plus(2);
+            if (!PAIR && j + 1 < j1) {
+              // the tile between is the other slot's
+              const Pos vq = pos.plus(1);
+              ok = wait(full0 + 8 * pos.s, pos.ph);
+              if (ok) tc::mbar_arrive(empty0 + 8 * pos.s);
+              ok = ok && wait(full0 + 8 * vq.s, vq.ph);
+              if (ok) tc::mbar_arrive(empty0 + 8 * vq.s);
+              pos = pos.plus(2);
+              ++j;
+            }
           }
+          at.move(2 * (j1 - j0));
         }
         if (!ok) give_up();
-        tc::mma_commit(drain);
-        tc::mbar_wait(drain, 0, &s_zero);
+        tc::mma_commit(drain0 + 8 * w);
+        tc::mbar_wait(drain0 + 8 * w, 0, &s_zero);
       }
-    } else if (warp == SCAN_WARP) {
+    } else {
       // ---------------- the scan: where rows see a tile in part, an infinity or a
       // NaN in V would reach the others (0 x inf); such items are done again row by row
       Pos at{0, 0};
@@ -859,40 +916,41 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       Item it;
       int j0, j1, seq = 0;
       while (ok && next_item(it, j0, j1, false)) {
-        if (lane == 0) s_dirty[seq % SEEN] = 0;
-        __syncwarp();
+        const Whole w0 = whole_tiles(p, it, 0), w1 = whole_tiles(p, it, 1);
+        uint32_t acc = 0;  // sums of 0 x V: zero, or NaN
         for (int j = j0; j < j1 && ok; ++j) {
-          const bool look = (it.need(0, j) && !it.whole(p, 0, j)) || (it.need(1, j) && !it.whole(p, 1, j));
+          const bool look = (it.need0(j) && !w0(j)) || (it.need1(j) && !w1(j));
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             ok = __all_sync(0xffffffffu, wait(full0 + 8 * at.s, at.ph));
             if (!ok) break;
             if (kv == 1 && look) {
-              const uint32_t st = ring + uint32_t(at.s) * C::STAGE;
-              const int r0 = it.beg(j) - it.slot0(j), rows = it.end(j) - it.beg(j);
-              uint32_t bad = 0;
+              // lanes along a row's 128 bytes, four rows at a time
+              const int s = it.slot0(j), r0 = it.beg(j) - s, r1 = it.end(j) - s;
+              const uint32_t st = ring + uint32_t(at.s) * C::STAGE + ((lane & 7) << 4);
 #pragma unroll 4
-              for (int i = lane; i < rows * NR * 8; i += 32) {
-                const int rr = r0 + i / (NR * 8), rc = i % (NR * 8);
-                uint32_t u[4];
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
-                             : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                             : "r"(st + (rc >> 3) * C::KV_REGION + rr * 128 + ((rc & 7) << 4)));
+              for (int rr = r0 + (lane >> 3); rr < r1; rr += 4) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  // the exponent of either half all ones: adding one to it carries out of it
-                  const uint32_t y = (u[e] & 0x7f807f80u) + 0x00800080u;
-                  bad |= y & 0x80008000u;
+                for (int r = 0; r < NR; ++r) {
+                  uint32_t u[4];
+                  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                               : "r"(st + r * C::KV_REGION + rr * 128));
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(u[e]), "r"(0u));
                 }
               }
-              if (__any_sync(0xffffffffu, bad != 0u) && lane == 0) s_dirty[seq % SEEN] = 1;
             }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(empty0 + 8 * at.s);
             at = at.plus(1);
           }
         }
-        __syncwarp();
-        if (ok && lane == 0) tc::mbar_arrive(scan0 + 8 * (seq % SEEN));
+        const bool bad = __any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0u);
+        if (lane == 0) {
+          s_dirty[seq % SEEN] = bad;
+          if (ok) tc::mbar_arrive(scan0 + 8 * (seq % SEEN));
+        }
         ++seq;
       }
       if (!ok) give_up();
