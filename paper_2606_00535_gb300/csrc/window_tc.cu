@@ -3,14 +3,19 @@
 //
 // A block is 128 / G tokens times the G query heads of a KV head. Its keys come in
 // tiles of 128: the sinks first, then the window of the block's first query up to
-// its last one (from the 64-slot page the window starts in). A tile at either end
-// is cut to the columns it needs (a multiple of 32), so the few sinks cost a
-// quarter of a tile or less.
+// its last one, from the 64-slot page the window starts in. The last tile of either
+// run is cut to the columns it needs (a multiple of 32).
 //
-// One CTA per SM holds two slots of tensor memory (256 columns each: S or P, and
-// O). S = Q K^T and O += P V are one M128 instruction group each; a slot's softmax
-// warpgroup (one row per thread) turns S into P while the tensor pipe works on the
-// other slot, which is what keeps the pipe busy.
+// One CTA per SM holds two slots of tensor memory (256 columns: S, then P, and O).
+// S = Q K^T and O += P V are tcgen05 groups; a slot's softmax warpgroup, one row per
+// thread, turns S into P and hands it over in two halves, so that the first half of
+// P V runs under the second. The slots' chains interleave on the tensor pipe.
+//
+// Softmax without a running maximum: a row's reference m is the maximum of the first
+// tile it sees a key of, and stays; P = 2^(x - m) is as exact at any m, in bf16 and in
+// the f32 sums alike, short of overflow. So the exponentials of a tile start as its
+// scores arrive. A row whose sum ends above 2^100 (a later score exceeds m by some 69
+// nats) is done again from its definition.
 //   PAIR   the slots are two neighbouring blocks of a KV head: every K/V tile is
 //          loaded once for 256 rows. The CTAs are persistent: they walk over the
 //          items with a ring of K/V stages that runs on across them, so the next
@@ -18,12 +23,14 @@
 //   !PAIR  both slots work on one block, alternate tiles; a block's tiles may be
 //          split over a cluster of CTAs, joined through distributed shared memory.
 //          For grids too small to fill the SMs with pairs.
-// The tensor pipe completes in order, so the commit that announces S of a tile
-// also says that everything issued before it is done: the softmax warps give the
-// stages read by it back to the producer, and the issuing thread needs no commits
-// of its own for that. Every mbarrier wait is bounded; a CTA that gives up flags
-// DREAMS_DATA_TIMEOUT, drains its copies and MMAs, frees its tensor memory and
-// leaves unfinished rows untouched.
+// Warps: 0-3 and 4-7 the softmax of slots 0 and 1, 8 the TMA producer, 9 and 10 the
+// MMA issuers of the slots (one thread each, so that one's waits run under the
+// other's MMAs), 11 the scan (below). A slot's MMAs complete in order, so the commit
+// that announces S of a tile also says that the P V before it is done: the softmax
+// warpgroup then gives those stages back, and no further commits are needed.
+// Every mbarrier wait is bounded; a CTA that gives up flags DREAMS_DATA_TIMEOUT,
+// drains its copies and MMAs, frees its tensor memory and leaves unfinished rows
+// untouched.
 #include <cuda.h>
 #include <limits.h>
 #include <math.h>
@@ -41,14 +48,10 @@ namespace {
 constexpr int KT = 128;    // keys of a tile
 constexpr int ROWS = 128;  // query rows of a block
 constexpr int THREADS = 384;
-// Registers a thread: the kernel is launched with 168; the producer's warpgroup
-// gives some to the two softmax warpgroups, which hold 128 scores a thread.
-constexpr int LAUNCH_REGS = 168, SOFTMAX_REGS = 216, OTHER_REGS = 72;
-static_assert(256 * SOFTMAX_REGS + 128 * OTHER_REGS <= THREADS * LAUNCH_REGS, "the shares fit what the block is launched with");
 constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 11;  // slot w's MMAs: warp MMA_WARP + w
-constexpr int SEEN = 8;  // items whose scan results are kept (more than the ring can be ahead)
+constexpr int SEEN = 16;  // items whose scan results are kept (more than the ring can be ahead)
 constexpr uint32_t TMEM_COLS = 512;
-constexpr float RESCALE = 8.f;  // log2 headroom of the reference maximum
+constexpr float MOST_SUM = 1.2676506e30f;  // 2^100: a row's sum above it is done again
 
 template <int D, bool PAIR>
 struct Cfg {
@@ -139,21 +142,6 @@ __device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bo
   it.e0 = it.ns + (it.L + it.tl0 - it.lo64) / KT + 1;
 }
 
-// O *= corr, row by row (rare: kept out of the softmax loop's code).
-template <int D>
-__device__ __noinline__ void rescale(uint32_t tl, float corr) {
-#pragma unroll 1
-  for (int c = 0; c < D / 32; ++c) {
-    uint32_t ov[32];
-    tc::tmem_ld32(tl + c * 32, ov);
-    tc::tmem_wait_ld();
-#pragma unroll
-    for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
-    tc::tmem_st32(tl + c * 32, ov);
-  }
-  tc::tmem_wait_st();
-}
-
 // An arrival by the threads for which `yes` holds, without a branch.
 __device__ __forceinline__ void arrive_if(uint32_t bar, bool yes) {
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %1, 0;\n @p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar), "r"(int(yes)) : "memory");
@@ -161,7 +149,7 @@ __device__ __forceinline__ void arrive_if(uint32_t bar, bool yes) {
 
 // What a softmax warp keeps of an item in shared memory.
 struct Slot {
-  int L, lo, lo64, S1, hi, ns, t0, rows, b, g, first, other, bad;
+  int L, lo, lo64, S1, hi, ns, t0, rows, b, g, first, bad;
 };
 
 // A place in the ring of stages: index and phase.
@@ -184,11 +172,6 @@ struct Place {
   }
 };
 
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
   uint64_t r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
@@ -412,24 +395,23 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   };
 
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     // ---------------- softmax warpgroup w: the rows of slot w
-    // A thread holds a row's 128 scores, so little else stays in registers: what an
-    // item is lies in shared memory, one copy per warp, and is read where needed.
+    // What an item is lies in shared memory, one copy per warp, and is read where
+    // needed.
     const int w = warp >> 2;
     const int row = 32 * (warp & 3) + lane;
     const uint32_t tl = tmem + (uint32_t(32 * (warp & 3)) << 16) + 256u * w;
     const bool lead = (warp & 3) == 0 && lane == 0;
     volatile Slot *sp = &s_slot[warp];
-    uint32_t par = 0;  // bit 0: parity of the next S tile, bit 1: of the next finished O
-    Pos pos{0, 0};     // K of the current tile
+    uint32_t sc = 0, oc = 0;  // S tiles and finished O of this slot so far
+    Pos pos{0, 0};                    // K of the current tile
     bool ok = true;
     int seq = 0;
     while (ok) {
       int j, jend, gap, to;  // tiles j .. jend-1 but for [gap, to), which only the other slot reads
       int wfrom, wto;        // tiles that all rows see whole
       bool live;             // does this warp have rows?
-      int ahead;             // stages between this slot's last tile and the next item
+      int ahead;             // stages from here to the next item
       {
         Item it;
         int j0, j1;
@@ -456,7 +438,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           j = ::min(j1, j0 + w);
         }
         pos.move(2 * (j - j0));
-        ahead = 2 * (j1 - j0);
+        ahead = 2 * (j1 - j);
         __syncwarp();  // the last item's readers are done
         if (lane == 0) {
           sp->L = it.L;
@@ -470,7 +452,6 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           sp->b = it.b;
           sp->g = it.g;
           sp->first = j;
-          sp->other = PAIR && w == 1 ? it.e0 : 0;  // tiles below it are block 0's too
         }
         int bad = 0;
         if (p.parent != nullptr) {
@@ -483,7 +464,6 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           if (bad && lead && w == 0 && it.g == 0 && split == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
         }
         if (lane == 0) sp->bad = bad;
-        ahead -= 2 * (j - j0);  // from tile j to the next item
         __syncwarp();
       }
       const bool any = j < jend;
@@ -498,16 +478,16 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         if (p.parent != nullptr && sp->bad == 0) r.anc = tree_row(p, s_par[warp], sp->L, t, r.off);
       }
       float m_ref = -INFINITY, l = 0.f;
-      int v_back = -1;  // V stage to give back at the next wake-up
-      int v_end = -1;   // and the one to give back at the end
+      bool unset = true;  // does a row of this warp lack its reference?
+      int v1 = -1;        // V stage of the last tile
       const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2);
       while (j < jend) {
-        ok = wait(s0 + 8 * w, par);
+        ok = wait(s0 + 8 * w, sc);
         if (!__all_sync(0xffffffffu, ok)) {
           ok = false;
           break;
         }
-        par ^= 1u;
+        ++sc;
         tc::fence_after_sync();
         // This slot's MMAs up to this S are done: the lead thread gives back K of this
         // tile, V of the one before, and Q after the last.
@@ -515,53 +495,16 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         int nj = j + (PAIR ? 1 : 2);
         if (PAIR && nj == gap) nj = to;
         arrive_if(empty0 + 8 * pos.s, lead);
-        arrive_if(empty0 + 8 * v_back, lead && v_back >= 0);
+        arrive_if(empty0 + 8 * v1, lead && v1 >= 0);
         if (PAIR) arrive_if(qe0 + 8 * w, lead && nj >= jend);
-        v_end = vp.s;
-        v_back = !PAIR || nj == j + 1 ? v_end : -1;  // (before a gap the issuer's commit does it)
+        v1 = vp.s;
 
-        uint64_t acc2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
-        // the reference maximum is raised (and O rescaled) only past 2^RESCALE
-        auto refer = [&](float mx) {
-          const bool resc = mx > m_ref + RESCALE;
-          if (__any_sync(0xffffffffu, resc)) {
-            float corr = 1.f;
-            if (resc) {
-              corr = m_ref == -INFINITY ? 0.f : tc::ex2(m_ref - mx);
-              m_ref = mx;
-              l *= corr;
-            }
-            if (j != sp->first) rescale<D>(tl + 128, corr);
-          }
-          const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
-          return f32x2(nmu, nmu);
-        };
-        // P of 32 columns, over the first half of as many columns of S
-        auto p_step = [&](const uint32_t *u, int c, uint64_t nmu2) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float e0, e1;
-            f32x2_split(ffma2(f32x2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1])), scale2, nmu2), e0, e1);
-            const float a = tc::ex2(e0), b = tc::ex2(e1);
-            acc2[i & 1] = fadd2(acc2[i & 1], f32x2(a, b));
-            pk[i] = pack_bf16x2(a, b);
-          }
-          tc::tmem_st16(tl + 16 * c, pk);
-        };
-        // P goes to the MMA thread in two halves of 64 keys
-        auto hand_over = [&](uint32_t bar) {
-          tc::tmem_wait_st();
-          tc::fence_before_sync();
-          tc::mbar_arrive(bar);
-        };
         const bool full = j >= wfrom && j < wto;
-        int beg = 0, end = KT, nc = KT;  // the tile's columns
+        int nc = KT;
         uint32_t mask[4] = {~0u, ~0u, ~0u, ~0u};
         if (__builtin_expect(!full, 0)) {
           const int ns = sp->ns, sl = j < ns ? j * KT : sp->lo64 + (j - ns) * KT;
-          beg = j < ns ? sl : ::max(sp->lo, sl);
-          end = j < ns ? ::min(sp->S1, sl + KT) : ::min(sp->hi, sl + KT);
+          int beg = j < ns ? sl : ::max(sp->lo, sl), end = j < ns ? ::min(sp->S1, sl + KT) : ::min(sp->hi, sl + KT);
           const int L = sp->L;
 #pragma unroll
           for (int c = 0; c < 4; ++c) mask[c] = r.word(p, L, sl + 32 * c, beg, end);
@@ -569,8 +512,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           end -= sl;
           nc = (end + 31) & ~31;
           // slots outside [beg, end) may hold any bits: their V rows become zeros
-          // once the copy has landed (by the slot that reads the tile first)
-          if (live && (beg > 0 || end < nc) && !(PAIR && w == 1 && j < sp->other)) {
+          // once the copy has landed (both slots see to it: neither waits for the other)
+          if (live && (beg > 0 || end < nc)) {
             ok = wait(full0 + 8 * vp.s, vp.ph);
             if (!__all_sync(0xffffffffu, ok)) {
               ok = false;
@@ -589,65 +532,57 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             tc::fence_proxy_async_smem();
           }
         }
-        if (__builtin_expect(nc == KT, 1)) {
-          uint32_t sv[KT];
-          uint64_t nmu2 = 0;
-          if (live) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tc::tmem_ld32(tl + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sv[32 * c]));
-            tc::tmem_wait_ld();
-            if (__builtin_expect(!full, 0)) {
-#pragma unroll
-              for (int c = 0; c < KT; ++c)
-                if (!((mask[c >> 5] >> (c & 31)) & 1u)) sv[c] = 0xff800000u;
-            }
-            float mt[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mt[i] = fmaxf(__uint_as_float(sv[32 * i]), __uint_as_float(sv[32 * i + 1]));
-#pragma unroll
-            for (int e = 2; e < 32; e += 2)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) mt[i] = max3f(mt[i], __uint_as_float(sv[32 * i + e]), __uint_as_float(sv[32 * i + e + 1]));
-            nmu2 = refer(fmaxf(max3f(mt[0], mt[1], mt[2]), mt[3]) * p.scale_log2);  // scale > 0
-            p_step(sv, 0, nmu2);
-            p_step(sv + 32, 1, nmu2);
-          }
-          hand_over(h0 + 8 * w);
-          if (live) {
-            p_step(sv + 64, 2, nmu2);
-            p_step(sv + 96, 3, nmu2);
-          }
-          hand_over(p0 + 8 * w);
-        } else {
-          // a cut tile: 32 columns at a time, read once for the maximum and once for P
-          uint32_t u[32];
-          auto load = [&](int c) {
-            tc::tmem_ld32(tl + 32 * c, u);
-            tc::tmem_wait_ld();
-            const uint32_t m = c == 0 ? mask[0] : c == 1 ? mask[1] : mask[2];
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!((m >> e) & 1u)) u[e] = 0xff800000u;
-          };
-          uint64_t nmu2 = 0;
+        if (__builtin_expect(!full || unset, 0)) {
+          // the scores again, masked; and references, the maximum of this tile, for
+          // rows that have none
           if (live) {
             float mx = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; 32 * c < nc; ++c) {
-              load(c);
+            for (int c = 0; c < 4; ++c) {
+              uint32_t u[32];
+              tc::tmem_ld32(tl + 32 * c, u);
+              tc::tmem_wait_ld();
+              const uint32_t m = c == 0 ? mask[0] : c == 1 ? mask[1] : c == 2 ? mask[2] : mask[3];
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) mx = max3f(mx, __uint_as_float(u[e]), __uint_as_float(u[e + 1]));
+              for (int e = 0; e < 32; ++e) {
+                if (!((m >> e) & 1u)) u[e] = 0xff800000u;
+                mx = fmaxf(mx, __uint_as_float(u[e]));
+              }
+              if (!full) tc::tmem_st32(tl + 32 * c, u);
             }
-            nmu2 = refer(mx * p.scale_log2);
+            tc::tmem_wait_st();
+            if (m_ref == -INFINITY) m_ref = mx * p.scale_log2;  // scale > 0
           }
-#pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            if (live && 32 * c < nc) {
-              load(c);
-              p_step(u, c, nmu2);
+          unset = __any_sync(0xffffffffu, live && m_ref == -INFINITY);
+        }
+        const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
+        const uint64_t nmu2 = f32x2(nmu, nmu);
+        uint64_t acc2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+        // P of 64 keys at a time, as bf16 over the first half of S
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          if (live && 64 * hh < nc) {
+            uint32_t sv[64];
+            tc::tmem_ld32(tl + 64 * hh, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
+            tc::tmem_ld32(tl + 64 * hh + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float e0, e1;
+                f32x2_split(ffma2(f32x2(__uint_as_float(sv[32 * c + 2 * i]), __uint_as_float(sv[32 * c + 2 * i + 1])), scale2, nmu2), e0, e1);
+                const float a = tc::ex2(e0), b = tc::ex2(e1);
+                acc2[i & 1] = fadd2(acc2[i & 1], f32x2(a, b));
+                pk[i] = pack_bf16x2(a, b);
+              }
+              tc::tmem_st16(tl + 32 * hh + 16 * c, pk);
             }
-            if (c & 1) hand_over((c == 1 ? h0 : p0) + 8 * w);
+            tc::tmem_wait_st();
           }
+          tc::fence_before_sync();
+          tc::mbar_arrive((hh == 0 ? h0 : p0) + 8 * w);
         }
         {
           float a0, a1, b0, b1;
@@ -657,15 +592,18 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         }
         pos = pos.plus(2);
         if (!PAIR) pos = pos.plus(2);
-        else if (nj != j + 1) pos.move(2 * (nj - j - 1));
+        else if (nj != j + 1) {
+          pos.move(2 * (nj - j - 1));
+          v1 = -1;  // (before a gap the issuer's commit gives V back)
+        }
         ahead -= 2 * (nj - j);
         j = nj;
       }
       if (ok && any) {
-        ok = __all_sync(0xffffffffu, wait(o0 + 8 * w, par >> 1));  // all MMAs of the slot are done
-        par ^= 2u;
+        ok = __all_sync(0xffffffffu, wait(o0 + 8 * w, oc));  // all MMAs of the slot are done
+        ++oc;
         tc::fence_after_sync();
-        if (ok && lead && v_end >= 0) tc::mbar_arrive(empty0 + 8 * v_end);
+        if (ok) arrive_if(empty0 + 8 * v1, lead);
       }
       ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
       if (!ok) break;
@@ -676,7 +614,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       const bool real = row < sp->rows, tree_ok = sp->bad == 0;
       if constexpr (PAIR) {
         const int h = sp->g * p.G + row - (t - sp->t0) * p.G;
-        if (any && tree_ok && !dirty) {
+        const uint32_t again = __ballot_sync(0xffffffffu, any && real && (dirty || l > MOST_SUM));
+        if (any && tree_ok) {
           const float inv = 1.f / l;
           const int64_t orow = (int64_t(sp->b) * p.T_max + t) * p.Hq + h;
           if (live) {
@@ -685,20 +624,22 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
               uint32_t ov[32];
               tc::tmem_ld32(tl + 128 + c * 32, ov);
               tc::tmem_wait_ld();
-              if (real) {
+              if (real && !((again >> lane) & 1u)) {
                 uint4 *dst = reinterpret_cast<uint4 *>(p.out + orow * D + c * 32);
                 auto pk = [&](int e) { return pack_bf16x2(__uint_as_float(ov[e]) * inv, __uint_as_float(ov[e + 1]) * inv); };
 #pragma unroll
                 for (int e = 0; e < 4; ++e) dst[e] = make_uint4(pk(8 * e), pk(8 * e + 2), pk(8 * e + 4), pk(8 * e + 6));
               }
             }
-            if (real && p.lse != nullptr) p.lse[orow] = (m_ref + log2f(l)) * LN2;
+            if (real && !((again >> lane) & 1u) && p.lse != nullptr) p.lse[orow] = (m_ref + log2f(l)) * LN2;
           }
-        } else if (any && tree_ok) {
+        }
+        if (__builtin_expect(again != 0u && tree_ok, 0)) {
+          __syncwarp();  // the stores above come first
           for (int i = 0; i < 32; ++i) {
             const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, r.off, i), hi = __shfl_sync(0xffffffffu, h, i);
             const unsigned long long ai = __shfl_sync(0xffffffffu, r.anc, i);
-            if (__shfl_sync(0xffffffffu, int(real), i)) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai);
+            if ((again >> i) & 1u) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai);
           }
         }
         tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
@@ -714,7 +655,6 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     }
     if (!ok) give_up();
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     if (warp == TMA_WARP) {
       // ---------------- producer: for each item K_0, Q, V_0, K_1, V_1, ...
       if (lane == 0) {
@@ -734,12 +674,13 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           int pg0 = fetch(j0, 0), pg1 = fetch(j0, 1);
           for (int j = j0; j < j1 && ok; ++j) {
             const int slot = it.slot0(j), halves = it.ncols(j) > 64 ? 2 : 1;
-            // tensor-map coordinate (dim 3) of a 64-slot half
+            // tensor-map coordinate (dim 3) of a 64-slot half: outside the map (zeros)
+            // where the page is missing
             auto coord = [&](int h, int pg) {
               if (row == nullptr) return it.b;
               if (pg >= 0 && pg < p.num_pages) return pg;
               if (::max(it.beg(j), slot + 64 * h) < ::min(it.end(j), slot + 64 * h + 64)) flag(p.status, DREAMS_DATA_BAD_PAGE);
-              return p.num_pages;  // outside the map: the copy fills zeros
+              return p.num_pages;
             };
             const int ca = coord(0, pg0), cb = coord(1, pg1), sa = row != nullptr ? 0 : slot, sb = row != nullptr ? 0 : slot + 64;
             pg0 = fetch(j + 1, 0);
@@ -818,89 +759,79 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         };
         bool ok = true;
         Pos at{0, 0};                      // K of the item's first tile
-        uint32_t p_par = 0, q_par = 0;     // parities of the next P and Q
+        uint32_t pc = 0, qc = 0;           // P tiles and Q blocks so far
         Item it;
         int j0, j1;
         while (ok && next_item(it, j0, j1, false)) {
-          auto need = [&](int j) { return PAIR ? (w ? it.need1(j) : it.need0(j)) : ((j - j0) & 1) == w; };
-          bool first = true;      // O is not begun
-          bool have_s = false;    // Q K^T of tile j is under way
-          Pos pos = at;
-          for (int j = j0; j < j1 && ok; ++j) {
-            const Pos vp = pos.plus(1);
-            if (!need(j)) {
-              // the other slot's tile: this one gives it back unread
+          const bool here = !PAIR || w < it.nb;
+          auto next_of = [&](int j) {
+            int k = j + (PAIR ? 1 : 2);
+            if (!PAIR) return ::min(j1, k);
+            if (w == 0) return k < it.e0 ? k : j1;
+            return k >= it.ns ? ::max(k, it.a1) : k;
+          };
+          // tiles [a, e) are the other slot's: this one gives them back unread
+          Pos pos = at;  // K of the first tile not dealt with
+          auto skip = [&](int a, int e) {
+#pragma unroll 1
+            for (int x = 2 * a; x < 2 * e && ok; ++x) {
               ok = wait(full0 + 8 * pos.s, pos.ph);
               if (ok) tc::mbar_arrive(empty0 + 8 * pos.s);
-              ok = ok && wait(full0 + 8 * vp.s, vp.ph);
-              if (ok) tc::mbar_arrive(empty0 + 8 * vp.s);
-              pos = pos.plus(2);
-              continue;
+              pos = pos.plus(1);
             }
-            const int nc = it.ncols(j);
-            if (!have_s) {
-              if (first) {
-                ok = wait(qf0 + 8 * (PAIR ? w : 0), q_par);
-                q_par ^= 1u;
-              }
+          };
+          int j = !here ? j1 : PAIR ? next_of(j0 - 1) : ::min(j1, j0 + w);
+          skip(j0, j);
+          Pos kp = pos;
+          if (ok && j < j1) {
+            ok = wait(qf0 + 8 * (PAIR ? w : 0), qc) && wait(full0 + 8 * kp.s, kp.ph);
+            ++qc;
+            if (!ok) break;
+            tc::fence_after_sync();
+            qk(kp.s, it.ncols(j));
+          }
+          bool first = true;
+          while (j < j1 && ok) {
+            const int nj = next_of(j), nc = it.ncols(j), nnc = nj < j1 ? it.ncols(nj) : 0;
+            const Pos vp = kp.plus(1);
+            pos = kp.plus(2);
+            // what the copies bring is waited for ahead of P
+            ok = wait(full0 + 8 * vp.s, vp.ph);
+            if (PAIR && ok && nj < j1) {
+              skip(j + 1, nj);
               ok = ok && wait(full0 + 8 * pos.s, pos.ph);
-              if (!ok) break;
-              tc::fence_after_sync();
-              qk(pos.s, nc);
             }
-            // the next tile, if its Q K^T can follow at once: K must have landed
-            const int nj = j + (PAIR ? 1 : 2);
-            const bool follow = nj < j1 && need(nj);
-            const Pos np = PAIR ? pos.plus(2) : pos.plus(2).plus(2);
-            const int nnc = follow ? it.ncols(nj) : 0;
-            ok = wait(full0 + 8 * vp.s, vp.ph) && (!follow || !PAIR || wait(full0 + 8 * np.s, np.ph)) && wait(h0 + 8 * w, p_par);
+            ok = ok && wait(h0 + 8 * w, pc);
             if (!ok) break;
             // O (+)= P V, P in two halves of 64 keys
             const uint32_t v = v_lo + uint32_t(vp.s) * (C::STAGE >> 4);
-            if (nc == KT) {
-              tc::fence_after_sync();
+            tc::fence_after_sync();
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
-              ok = wait(p0 + 8 * w, p_par);
-              if (!ok) break;
-              tc::fence_after_sync();
+            for (int k = 0; k < 4; ++k)
+              if (16 * k < nc) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+            ok = wait(p0 + 8 * w, pc);
+            if (!ok) break;
+            tc::fence_after_sync();
 #pragma unroll
-              for (int k = 4; k < 8; ++k) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, 1u);
-            } else {
-              ok = wait(p0 + 8 * w, p_par);
-              if (!ok) break;
-              tc::fence_after_sync();
-#pragma unroll 1
-              for (int k = 0; k < nc / 16; ++k) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
-            }
-            p_par ^= 1u;
+            for (int k = 4; k < 8; ++k)
+              if (16 * k < nc) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, 1u);
+            ++pc;
             first = false;
-            if (follow) {
+            if (nj < j1) {
+              if (PAIR && nj != j + 1) tc::mma_commit(empty0 + 8 * vp.s);  // before a gap: no S announces that this V is read
               if (!PAIR) {
-                ok = wait(full0 + 8 * np.s, np.ph);
+                skip(j + 1, nj);
+                ok = ok && wait(full0 + 8 * pos.s, pos.ph);
                 if (!ok) break;
                 tc::fence_after_sync();
               }
-              qk(np.s, nnc);
-              have_s = true;
+              kp = pos;
+              qk(kp.s, nnc);
             } else {
-              have_s = false;
-              bool later = false;
-              if (PAIR && w == 1) later = j < it.n - 1;  // after a gap: no S announces that this V is read
-              if (later) tc::mma_commit(empty0 + 8 * vp.s);
-              else tc::mma_commit(o0 + 8 * w);
+              tc::mma_commit(o0 + 8 * w);
+              skip(j + 1, j1);
             }
-            pos = pos.plus(2);
-            if (!PAIR && j + 1 < j1) {
-              // the tile between is the other slot's
-              const Pos vq = pos.plus(1);
-              ok = wait(full0 + 8 * pos.s, pos.ph);
-              if (ok) tc::mbar_arrive(empty0 + 8 * pos.s);
-              ok = ok && wait(full0 + 8 * vq.s, vq.ph);
-              if (ok) tc::mbar_arrive(empty0 + 8 * vq.s);
-              pos = pos.plus(2);
-              ++j;
-            }
+            j = nj;
           }
           at.move(2 * (j1 - j0));
         }
@@ -1009,11 +940,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         const int off = s_row[row].off, t = s_row[row].t;
         if (off < 0) continue;  // a malformed tree
         const int h = it.g * p.G + row - (t - it.t00) * p.G;
-        if (again) {
+        const float2 ml = lane < parts ? ld_cluster2(mapa(ml_a + ((lane & 1) * ROWS + row) * 8, lane >> 1)) : make_float2(-INFINITY, 0.f);
+        if (again || __any_sync(0xffffffffu, ml.y > MOST_SUM)) {
           slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc);
           continue;
         }
-        const float2 ml = lane < parts ? ld_cluster2(mapa(ml_a + ((lane & 1) * ROWS + row) * 8, lane >> 1)) : make_float2(-INFINITY, 0.f);
         float M = ml.x;
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
@@ -1087,13 +1018,6 @@ dreams_status_t launch(TcParams &P, cudaStream_t stream) {
   const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR>);
   const dreams_status_t st = ensure_max_dynamic_smem(kernel, int(Cfg<D, PAIR>::SMEM));
   if (st != DREAMS_OK) return st;
-  // the register shares must add up to no more than the launch's: a build that
-  // used fewer registers would wait for ever
-  static const bool shares_ok = [&] {
-    cudaFuncAttributes a;
-    return cudaFuncGetAttributes(&a, kernel) == cudaSuccess && a.numRegs == LAUNCH_REGS;
-  }();
-  if (!shares_ok) return DREAMS_ERR_UNSUPPORTED;
   if (!kv_map(&P.tmap_k, P.p.k, P.p, D) || !kv_map(&P.tmap_v, P.p.v, P.p, D) || !q_map(&P.tmap_q, P.p, D, P.TB)) return DREAMS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(PAIR ? unsigned(std::min(P.items, num_sms())) : unsigned(P.items) * unsigned(P.p.nsplit));
@@ -1127,7 +1051,7 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   test_stall(DREAMS_TEST_ATTENTION, &P.stall_at, &P.wait_ns);
   // Tiles of a block, and the time of either layout in tiles: a pair of tiles
   // costs about as much as two tiles of one block, and an item's start and end
-  // about five tiles (the pairs' mostly overlap).
+  // about six tiles (the pairs' mostly overlap).
   const int64_t sms = num_sms();
   const int64_t tiles = std::max<int64_t>(
       1, (std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB)) + KT - 1) / KT + (p.sinks > 0 ? 1 : 0));
