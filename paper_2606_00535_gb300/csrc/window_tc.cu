@@ -9,7 +9,8 @@
 // One CTA per SM holds two slots of tensor memory (256 columns: S, then P, and O).
 // S = Q K^T and O += P V are tcgen05 groups; a slot's softmax warpgroup, one row per
 // thread, turns S into P and hands it over in two halves, so that the first half of
-// P V runs under the second. The slots' chains interleave on the tensor pipe.
+// P V runs under the second. The slots' chains interleave on the tensor pipe. With
+// head dim 64 P lies beside S, and the next Q K^T starts when S has been read.
 //
 // Softmax without a running maximum: a row's reference m is the maximum of the first
 // tile it sees a key of, and stays; P = 2^(x - m) is as exact at any m, in bf16 and in
@@ -60,6 +61,10 @@ struct Cfg {
   static constexpr uint32_t Q_BYTES = NR * Q_REGION;
   static constexpr uint32_t STAGE = NR * KV_REGION;
   static constexpr int NQ = PAIR ? 2 : 1;
+  // A slot's columns: S at 0; with head dim 64 there is room for P beside it, and the
+  // next Q K^T can start once the scores are in registers; with 128 P goes over S.
+  static constexpr bool BESIDE = D == 64;
+  static constexpr uint32_t P_COL = BESIDE ? 128 : 0, O_COL = BESIDE ? 192 : 128;
   static constexpr int NST = D == 64 ? 8 : 5;
   static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + 1024, 120 * 1024);
 };
@@ -319,7 +324,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST];
-  __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
+  __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_r[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
   __shared__ int8_t s_par[8][64];
@@ -332,7 +337,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   auto q_s = [&](int w) { return base + uint32_t(PAIR ? w : 0) * C::Q_BYTES; };
   const uint32_t ring = base + C::NQ * C::Q_BYTES;
   const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty);
-  const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
+  const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), r0 = smem_u32(bar_r), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
                  o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
   if (tid == TMA_WARP * 32) {
     for (int i = 0; i < NST; ++i) {
@@ -343,6 +348,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       tc::mbar_init(qf0 + 8 * w, 1);
       tc::mbar_init(qe0 + 8 * w, 1);
       tc::mbar_init(s0 + 8 * w, 1);
+      tc::mbar_init(r0 + 8 * w, 128);
       tc::mbar_init(h0 + 8 * w, 128);
       tc::mbar_init(p0 + 8 * w, 128);
       tc::mbar_init(o0 + 8 * w, 1);
@@ -490,13 +496,14 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         ++sc;
         tc::fence_after_sync();
         // This slot's MMAs up to this S are done: the lead thread gives back K of this
-        // tile, V of the one before, and Q after the last.
+        // tile, V of the one before (P over S: its P V is), and Q after the last.
         const Pos vp = pos.plus(1);
         int nj = j + (PAIR ? 1 : 2);
         if (PAIR && nj == gap) nj = to;
         arrive_if(empty0 + 8 * pos.s, lead);
-        arrive_if(empty0 + 8 * v1, lead && v1 >= 0);
+        if (!C::BESIDE) arrive_if(empty0 + 8 * v1, lead && v1 >= 0);
         if (PAIR) arrive_if(qe0 + 8 * w, lead && nj >= jend);
+        const int v0 = v1;  // V stage of the tile before
         v1 = vp.s;
 
         const bool full = j >= wfrom && j < wto;
@@ -532,25 +539,20 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             tc::fence_proxy_async_smem();
           }
         }
-        if (__builtin_expect(!full || unset, 0)) {
-          // the scores again, masked; and references, the maximum of this tile, for
-          // rows that have none
+        if (__builtin_expect(unset, 0)) {
+          // references: the maximum of this tile, for rows that have none
           if (live) {
             float mx = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; 32 * c < nc; ++c) {
+              const uint32_t m = c == 0 ? mask[0] : c == 1 ? mask[1] : c == 2 ? mask[2] : mask[3];
+              if (!__any_sync(0xffffffffu, m != 0u)) continue;
               uint32_t u[32];
               tc::tmem_ld32(tl + 32 * c, u);
               tc::tmem_wait_ld();
-              const uint32_t m = c == 0 ? mask[0] : c == 1 ? mask[1] : c == 2 ? mask[2] : mask[3];
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                if (!((m >> e) & 1u)) u[e] = 0xff800000u;
-                mx = fmaxf(mx, __uint_as_float(u[e]));
-              }
-              if (!full) tc::tmem_st32(tl + 32 * c, u);
+              for (int e = 0; e < 32; ++e) mx = fmaxf(mx, ((m >> e) & 1u) ? __uint_as_float(u[e]) : -INFINITY);
             }
-            tc::tmem_wait_st();
             if (m_ref == -INFINITY) m_ref = mx * p.scale_log2;  // scale > 0
           }
           unset = __any_sync(0xffffffffu, live && m_ref == -INFINITY);
@@ -558,32 +560,58 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
         const uint64_t nmu2 = f32x2(nmu, nmu);
         uint64_t acc2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
-        // P of 64 keys at a time, as bf16 over the first half of S
-#pragma unroll
+        // P of 64 keys at a time, as bf16 over the first half of S, or beside it
+#pragma unroll 1
         for (int hh = 0; hh < 2; ++hh) {
+          uint32_t u[64];
           if (live && 64 * hh < nc) {
-            uint32_t sv[64];
-            tc::tmem_ld32(tl + 64 * hh, *reinterpret_cast<uint32_t(*)[32]>(&sv[0]));
-            tc::tmem_ld32(tl + 64 * hh + 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[32]));
+            tc::tmem_ld32(tl + 64 * hh, *reinterpret_cast<uint32_t(*)[32]>(&u[0]));
+            tc::tmem_ld32(tl + 64 * hh + 32, *reinterpret_cast<uint32_t(*)[32]>(&u[32]));
             tc::tmem_wait_ld();
+            if (__builtin_expect(!full, 0)) {
+              const uint32_t m0 = hh ? mask[2] : mask[0], m1 = hh ? mask[3] : mask[1];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                if (!((m0 >> e) & 1u)) u[e] = 0xff800000u;
+                if (!((m1 >> e) & 1u)) u[32 + e] = 0xff800000u;
+              }
+            }
+          }
+          if (C::BESIDE && hh == 1) {
+            tc::fence_before_sync();
+            tc::mbar_arrive(r0 + 8 * w);  // S may be overwritten
+          }
+          if (C::BESIDE && hh == 0 && v0 >= 0) {
+            // P may be overwritten once the P V before is done; and its V goes back
+            ok = wait(o0 + 8 * w, oc);
+            if (!__all_sync(0xffffffffu, ok)) {
+              ok = false;
+              break;
+            }
+            ++oc;
+            tc::fence_after_sync();
+            arrive_if(empty0 + 8 * v0, lead);
+          }
+          if (live && 64 * hh < nc) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               uint32_t pk[16];
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 float e0, e1;
-                f32x2_split(ffma2(f32x2(__uint_as_float(sv[32 * c + 2 * i]), __uint_as_float(sv[32 * c + 2 * i + 1])), scale2, nmu2), e0, e1);
+                f32x2_split(ffma2(f32x2(__uint_as_float(u[32 * c + 2 * i]), __uint_as_float(u[32 * c + 2 * i + 1])), scale2, nmu2), e0, e1);
                 const float a = tc::ex2(e0), b = tc::ex2(e1);
                 acc2[i & 1] = fadd2(acc2[i & 1], f32x2(a, b));
                 pk[i] = pack_bf16x2(a, b);
               }
-              tc::tmem_st16(tl + 32 * hh + 16 * c, pk);
+              tc::tmem_st16(tl + C::P_COL + 32 * hh + 16 * c, pk);
             }
             tc::tmem_wait_st();
           }
           tc::fence_before_sync();
           tc::mbar_arrive((hh == 0 ? h0 : p0) + 8 * w);
         }
+        if (!ok) break;
         {
           float a0, a1, b0, b1;
           f32x2_split(acc2[0], a0, a1);
@@ -594,7 +622,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         if (!PAIR) pos = pos.plus(2);
         else if (nj != j + 1) {
           pos.move(2 * (nj - j - 1));
-          v1 = -1;  // (before a gap the issuer's commit gives V back)
+          if (!C::BESIDE) v1 = -1;  // (before a gap the issuer's commit gives V back)
         }
         ahead -= 2 * (nj - j);
         j = nj;
@@ -622,7 +650,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
               uint32_t ov[32];
-              tc::tmem_ld32(tl + 128 + c * 32, ov);
+              tc::tmem_ld32(tl + C::O_COL + c * 32, ov);
               tc::tmem_wait_ld();
               if (real && !((again >> lane) & 1u)) {
                 uint4 *dst = reinterpret_cast<uint4 *>(p.out + orow * D + c * 32);
@@ -743,7 +771,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         // cluster the bits above say which CTA), leading-dimension offset / 16
         const uint32_t ring16 = (ring & 0x3FFFFu) >> 4;
         const uint32_t q_lo = ((q_s(w) & 0x3FFFFu) >> 4) | (1u << 16), k_lo = ring16 | (1u << 16), v_lo = ring16 | ((C::KV_REGION >> 4) << 16);
-        const uint32_t s_col = tmem + 256u * w, o_col = s_col + 128u;
+        const uint32_t s_col = tmem + 256u * w, p_col = s_col + C::P_COL, o_col = s_col + C::O_COL;
         constexpr uint32_t IDESC_QK = tc::idesc_bf16_f32(ROWS, 0, false);
         constexpr uint32_t IDESC_PV = tc::idesc_bf16_f32(ROWS, D, true);
         // S = Q K^T over the first nc keys of a stage
@@ -797,7 +825,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             pos = kp.plus(2);
             // what the copies bring is waited for ahead of P
             ok = wait(full0 + 8 * vp.s, vp.ph);
-            if (PAIR && ok && nj < j1) {
+            if ((C::BESIDE || PAIR) && ok && nj < j1) {
               skip(j + 1, nj);
               ok = ok && wait(full0 + 8 * pos.s, pos.ph);
             }
@@ -808,16 +836,24 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             tc::fence_after_sync();
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              if (16 * k < nc) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+              if (16 * k < nc) mma_ts(o_col, p_col + 8 * k, v + k * 128, IDESC_PV, (k > 0 || !first) ? 1u : 0u);
+            if (C::BESIDE) {
+              // S has been read: the next one
+              ok = wait(r0 + 8 * w, pc);
+              if (!ok) break;
+              tc::fence_after_sync();
+              if (nj < j1) qk(pos.s, nnc);
+            }
             ok = wait(p0 + 8 * w, pc);
             if (!ok) break;
             tc::fence_after_sync();
 #pragma unroll
             for (int k = 4; k < 8; ++k)
-              if (16 * k < nc) mma_ts(o_col, s_col + 8 * k, v + k * 128, IDESC_PV, 1u);
+              if (16 * k < nc) mma_ts(o_col, p_col + 8 * k, v + k * 128, IDESC_PV, 1u);
             ++pc;
             first = false;
-            if (nj < j1) {
+            if (C::BESIDE || nj >= j1) tc::mma_commit(o0 + 8 * w);
+            if (!C::BESIDE && nj < j1) {
               if (PAIR && nj != j + 1) tc::mma_commit(empty0 + 8 * vp.s);  // before a gap: no S announces that this V is read
               if (!PAIR) {
                 skip(j + 1, nj);
@@ -825,12 +861,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
                 if (!ok) break;
                 tc::fence_after_sync();
               }
-              kp = pos;
-              qk(kp.s, nnc);
-            } else {
-              tc::mma_commit(o0 + 8 * w);
-              skip(j + 1, j1);
+              qk(pos.s, nnc);
             }
+            if (nj >= j1) skip(j + 1, j1);
+            kp = pos;
             j = nj;
           }
           at.move(2 * (j1 - j0));
@@ -909,7 +943,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t ov[32];
-          tc::tmem_ld32(tl + 128 + c * 32, ov);
+          tc::tmem_ld32(tl + C::O_COL + c * 32, ov);
           tc::tmem_wait_ld();
 #pragma unroll
           for (int e = 0; e < 8; ++e)
