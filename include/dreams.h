@@ -424,7 +424,9 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
  * visible slot and whose entry is out of range is flagged DREAMS_DATA_BAD_PAGE,
  * and its slots read as zeros. What a slot holds does not reach a query that does
  * not see it, infinities and NaN included. Accumulation is fp32; probabilities
- * enter the PV product as bf16, and the output is rounded to bf16 once.
+ * enter the PV product as bf16, and the output is rounded to bf16 once. One
+ * launch. The workspace (0 bytes for many shapes) holds counters that reset
+ * themselves: zero-fill it once when it is allocated.
  */
 size_t dreams_window_attention_workspace_size(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max, int32_t Hq,
                                               int32_t window, int32_t sinks, int32_t tree);

@@ -197,8 +197,11 @@ struct ForkState {
 };
 constexpr int FORK_HEAD = 2 + FORK_CTAS;
 
+// (Not the .aligned forms: warps come here from loops that their lanes left at
+// different turns.)
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // The new table, counts and lengths, and the list of pages to copy: one

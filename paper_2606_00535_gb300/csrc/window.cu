@@ -7,14 +7,19 @@
 // its first query up to its last one; the kernel numbers them 0 .. n-1 as one list,
 // so sinks and window share tiles and nothing between them is read.
 //
-// window_rows_kernel: a CTA takes 16 query rows (token, head of the GQA group) of
-// one KV head and a contiguous part of their key list; its four warps take 16-key
-// tiles in turn, each with its own ring of cp.async stages, so no barrier stands
-// in the stream. Scores and P V run on m16n8k16 tensor instructions with the
-// running maximum and sum of each row in f32 registers. The warps' partial sums
-// join in shared memory, and the parts of a split key list in distributed shared
-// memory (the parts are one cluster), in a fixed order. For few rows the kernel is
-// bound by reading K and V once.
+// Few rows (at most 16 of a KV head: single tokens, short drafts), bound by reading K
+// and V once. A CTA takes part of the key list of a sequence and KV head; its four
+// warps take 16-key tiles in turn, each with its own ring of cp.async stages, so no
+// barrier stands in the stream. Scores and P V run on m16n8k16 tensor instructions
+// (16 rows are all there are: the fifth-generation ones would work on 128), with the
+// running maximum and sum of each row in f32 registers. How the lists are cut:
+//   window_rows_kernel    one list to a CTA or, split, to a cluster, whose CTAs push
+//                         their parts into each other's shared memory: least latency
+//   window_stream_kernel  all lists end to end, cut evenly over two CTAs per SM, so
+//                         that every SM reads to the end; parts of a cut list join in
+//                         the workspace, by the CTA that comes last
+// Either way parts are joined in list order, so results repeat bit for bit. More rows
+// go to window_tc.cu.
 #include <limits.h>
 #include <math.h>
 
@@ -53,11 +58,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-  return v;
-}
 // Does a pair of bf16 values hold an infinity or a NaN?
 __device__ __forceinline__ bool nonfinite2(uint32_t x) {
   return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
@@ -73,8 +73,9 @@ struct RowsCfg {
   static constexpr int ROW = D * 2;                // bytes of a key
   static constexpr int TILE = KT * ROW;            // K or V of a tile
   static constexpr int WARP_BYTES = STAGES * 2 * TILE;
-  static constexpr int SMEM = WARPS * WARP_BYTES;  // at the end: WARPS partial outputs [16][D] f32 and the CTA's
-  static_assert(SMEM >= (WARPS + 1) * RB * D * 4, "partials fit");
+  static constexpr int RING = WARPS * WARP_BYTES;  // afterwards the warps' outputs [WARPS][16][D] f32
+  static constexpr int SMEM = RING + RB * D * 4;   // and what the CTAs of a cluster push here
+  static_assert(RING >= WARPS * RB * D * 4, "partials fit");
 };
 
 // What a row of the block is: its position, and for a tree its visible new slots.
@@ -83,85 +84,53 @@ struct RowInfo {
   unsigned long long anc;  // tree: bit a = sees slot L + a
 };
 
-template <int D>
-__global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams p) {
-  using C = RowsCfg<D>;
-  constexpr int CH = D / 8;  // 16-byte columns of a key
-  extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ int s_par[64];
-  __shared__ RowInfo s_row[RB];
-  __shared__ float2 s_ml[WARPS + 1][RB];
+struct RowsShared {
+  int par[64];
+  RowInfo row[RB];
+  float2 ml[WARPS][RB];    // the warps' maxima and sums
+  float2 part[8][RB];      // those of a list's parts
+};
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  int x = blockIdx.x;
-  const int split = x % p.nsplit;
-  x /= p.nsplit;
-  const int rb = x % p.nrb;
-  x /= p.nrb;
-  const int g = x % p.Hkv, b = x / p.Hkv;
-  const bool reporter = rb == 0 && split == 0 && g == 0 && tid == 0;
-
-  const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
-  if (T < 0 || T > p.T_max) {
-    if (reporter) flag(p.status, DREAMS_DATA_BAD_TREE_LEN);
-    return;
-  }
-  if (L < 0 || int64_t(L) + T > p.capacity) {
-    if (reporter) flag(p.status, DREAMS_DATA_BAD_KV_LEN);
-    return;
-  }
-  const int t_first = rb * RB / p.G;
-  if (t_first >= T) return;  // (as do all CTAs of the cluster)
-  const int t_last = ::min(T - 1, (rb * RB + RB - 1) / p.G);
-
-  // ---- rows
+// The queries of a sequence and KV head; false (flagged by `report`): a bad tree.
+__device__ __forceinline__ bool load_rows(const WinParams &p, RowsShared &sh, int b, int L, int T, bool report) {
+  const int tid = threadIdx.x;
+  __syncthreads();  // the last part's readers are done
   if (p.parent != nullptr) {
     int bad = 0;
     for (int i = tid; i < T; i += 32 * WARPS) {
       const int par = __ldg(p.parent + int64_t(b) * p.T_max + i);
-      s_par[i] = par;
+      sh.par[i] = par;
       bad |= i == 0 ? par != -1 : (par < 0 || par >= i);
     }
     if (__syncthreads_or(bad)) {
-      if (reporter) flag(p.status, DREAMS_DATA_BAD_PARENT);
-      return;
+      if (report && tid == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
+      return false;
     }
   }
   if (tid < RB) {
-    const int t = (rb * RB + tid) / p.G;
+    const int t = tid / p.G;
     RowInfo r{-1, 0ull};
     if (t < T) {
       r.off = t;
-      if (p.parent != nullptr) r.anc = tree_row(p, s_par, L, t, r.off);
+      if (p.parent != nullptr) r.anc = tree_row(p, sh.par, L, t, r.off);
     }
-    s_row[tid] = r;
+    sh.row[tid] = r;
   }
   __syncthreads();
+  return true;
+}
 
-  const KeyList kl = key_list(p, L, t_first, t_last);
-  const int64_t per = ((int64_t(kl.n) + p.nsplit - 1) / p.nsplit + KT - 1) / KT * KT;
-  const int i0 = int(::min(int64_t(kl.n), split * per)), i1 = int(::min(int64_t(kl.n), i0 + per));
+// Attention of the rows over keys [i0, i1) of the list. Afterwards sh.ml holds each
+// warp's (m, l) per row, and `ring` its unnormalised outputs [warp][row][D] in f32.
+template <int D>
+__device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, uint8_t *smem, const KeyList &kl, int b, int g, int L, int T,
+                                            int i0, int i1) {
+  using C = RowsCfg<D>;
+  constexpr int CH = D / 8;  // 16-byte columns of a key
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int ntiles = (i1 - i0 + KT - 1) / KT;
 
-  // ---- this thread's part of Q: rows lane / 4 and lane / 4 + 8
-  const int r0 = lane >> 2, c0 = (lane & 3) * 2;
-  uint32_t qf[D / 16][4];
-  int off[2];
-  unsigned long long anc[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = r0 + 8 * h, flat = rb * RB + r, t = flat / p.G;
-    off[h] = s_row[r].off;
-    anc[h] = s_row[r].anc;
-    const __nv_bfloat16 *src = p.q + b * p.sb + t * p.st + int64_t(g * p.G + flat - t * p.G) * D + c0;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      qf[kk][h] = t < T ? *reinterpret_cast<const uint32_t *>(src + kk * 16) : 0u;
-      qf[kk][h + 2] = t < T ? *reinterpret_cast<const uint32_t *>(src + kk * 16 + 8) : 0u;
-    }
-  }
-
-  // ---- the stream of this warp: tiles warp, warp + WARPS, ...
+  // this warp's tiles: warp, warp + WARPS, ...
   const uint32_t ring = smem_u32(smem) + warp * C::WARP_BYTES;
   const int my = ntiles > warp ? (ntiles - warp + WARPS - 1) / WARPS : 0;
   // lane k (mod 16) looks after key k of a tile: its slot and page entry one
@@ -203,12 +172,29 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
 #pragma unroll
   for (int j = 0; j < C::STAGES - 1; ++j) issue(j);
 
+  // this thread's part of Q: rows lane / 4 and lane / 4 + 8
+  const int r0 = lane >> 2, c0 = (lane & 3) * 2;
+  uint32_t qf[D / 16][4];
+  int off[2];
+  unsigned long long anc[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = r0 + 8 * h, t = r / p.G;
+    off[h] = sh.row[r].off;
+    anc[h] = sh.row[r].anc;
+    const __nv_bfloat16 *src = p.q + b * p.sb + t * p.st + int64_t(g * p.G + r - t * p.G) * D + c0;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      qf[kk][h] = t < T ? *reinterpret_cast<const uint32_t *>(src + kk * 16) : 0u;
+      qf[kk][h + 2] = t < T ? *reinterpret_cast<const uint32_t *>(src + kk * 16 + 8) : 0u;
+    }
+  }
   float o[D / 8][4];
 #pragma unroll
   for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
-  const int off_min = p.parent != nullptr ? 0 : t_first, off_max = t_last;
+  const int off_max = T - 1;
   for (int j = 0; j < my; ++j) {
     cp_wait<C::STAGES - 2>();
     __syncwarp();
@@ -233,7 +219,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
     const bool all = ib + KT <= i1 &&
                      (ib + KT <= kl.S1 ||
                       (ib >= kl.S1 && int64_t(L) + off_max - kl.slot(ib) < p.window &&
-                       (p.parent != nullptr ? sl < L : sl <= L + off_min)));
+                       (p.parent != nullptr ? sl < L : sl <= L)));
     if (!all) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
@@ -282,7 +268,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
         if (!all && __any_sync(0xffffffffu, nonfinite2(vb[0]) || nonfinite2(vb[1]) || nonfinite2(vb[2]) || nonfinite2(vb[3]))) {
 #pragma unroll 1
           for (int r = 0; r < RB; ++r) {
-            const RowInfo ri = s_row[r];
+            const RowInfo ri = sh.row[r];
             uint32_t keep[2];
 #pragma unroll
             for (int hh = 0; hh < 2; ++hh) {
@@ -315,97 +301,286 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
   cp_wait<0>();
   __syncthreads();  // the stages are free
 
-  // ---- the warps' parts, then the CTA's: [warp][row][D] and (m, l)
   float *so = reinterpret_cast<float *>(smem);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
     const int r = r0 + 8 * h;
-    if ((lane & 3) == 0) s_ml[warp][r] = make_float2(m[h], l[h]);
+    if ((lane & 3) == 0) sh.ml[warp][r] = make_float2(m[h], l[h]);
+    if (off[h] >= 0) {
 #pragma unroll
-    for (int n = 0; n < D / 8; ++n)
-      *reinterpret_cast<float2 *>(so + (warp * RB + r) * D + n * 8 + c0) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+      for (int n = 0; n < D / 8; ++n)
+        *reinterpret_cast<float2 *>(so + (warp * RB + r) * D + n * 8 + c0) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+    }
   }
   __syncthreads();
-  const bool whole = p.nsplit == 1;
-  auto emit = [&](int r, int d, float2 v, float M, float Z) {
-    const int flat = rb * RB + r, t = flat / p.G;
-    if (t >= T) return;
-    const int64_t row = (int64_t(b) * p.T_max + t) * p.Hq + g * p.G + (flat - t * p.G);
-    const float inv = 1.f / Z;
-    *reinterpret_cast<uint32_t *>(p.out + row * D + d) = pack_bf16x2(v.x * inv, v.y * inv);
-    if (d == 0 && p.lse != nullptr) p.lse[row] = (M + log2f(Z)) * LN2;
-  };
-  float *sc = so + WARPS * RB * D;  // the CTA's part
-#pragma unroll 1
-  for (int u = tid; u < RB * D / 2; u += 32 * WARPS) {
-    const int r = u / (D / 2), d = (u - r * (D / 2)) * 2;
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) M = fmaxf(M, s_ml[w][r].x);
-    float Z = 0.f;
-    float2 acc = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      const float2 ml = s_ml[w][r];
-      if (ml.y == 0.f) continue;  // no key (a NaN sum goes through)
-      const float c = tc::ex2(ml.x - M);
-      const float2 ov = *reinterpret_cast<const float2 *>(so + (w * RB + r) * D + d);
-      Z += c * ml.y;
-      acc.x += c * ov.x;
-      acc.y += c * ov.y;
-    }
-    if (whole) {
-      emit(r, d, acc, M, Z);
-    } else {
-      *reinterpret_cast<float2 *>(sc + r * D + d) = acc;
-      if (d == 0) s_ml[WARPS][r] = make_float2(M, Z);
-    }
-  }
-  if (whole) return;
+}
 
-  // ---- the parts of a split list: each CTA of the cluster joins its share of
-  // the outputs from all of them
-  cluster_sync();
-  const uint32_t ml_a = smem_u32(&s_ml[WARPS][0]), sc_a = smem_u32(sc);
-  for (int u = split * 32 * WARPS + tid; u < RB * D / 2; u += p.nsplit * 32 * WARPS) {
-    const int r = u / (D / 2), d = (u - r * (D / 2)) * 2;
-    float M = -INFINITY;
-    for (int c = 0; c < p.nsplit; ++c) M = fmaxf(M, ld_cluster2(mapa(ml_a + r * 8, c)).x);
-    float Z = 0.f;
-    float2 acc = make_float2(0.f, 0.f);
-    for (int c = 0; c < p.nsplit; ++c) {
-      const float2 ml = ld_cluster2(mapa(ml_a + r * 8, c));
-      if (ml.y == 0.f) continue;
-      const float w = tc::ex2(ml.x - M);
-      const float2 ov = ld_cluster2(mapa(sc_a + (r * D + d) * 4, c));
-      Z += w * ml.y;
-      acc.x += w * ov.x;
-      acc.y += w * ov.y;
-    }
-    emit(r, d, acc, M, Z);
+// Parts joined by log-sum-exp: sum of 2^(m_i - M) (l_i, o_i) over n parts.
+template <int N, typename ML, typename O>
+__device__ __forceinline__ float4 join(int n, ML ml_of, O o_of, float &M, float &Z) {
+  float2 ml[N];
+  float4 o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {  // all loads first
+    ml[i] = i < n ? ml_of(i) : make_float2(-INFINITY, 0.f);
+    o[i] = i < n ? o_of(i) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  cluster_sync();  // no CTA leaves while another reads its shared memory
+  M = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) M = fmaxf(M, ml[i].x);
+  Z = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (ml[i].y == 0.f) continue;  // no key (a NaN sum goes through)
+    const float c = tc::ex2(ml[i].x - M);
+    Z += c * ml[i].y;
+    acc.x += c * o[i].x;
+    acc.y += c * o[i].y;
+    acc.z += c * o[i].z;
+    acc.w += c * o[i].w;
+  }
+  return acc;
+}
+
+// Unit u of the rows: row u / (D / 4), four columns.
+template <int D>
+__device__ __forceinline__ float4 join_warps(const RowsShared &sh, const uint8_t *smem, int u, float &M, float &Z) {
+  const float *so = reinterpret_cast<const float *>(smem);
+  const int r = u / (D / 4), d = (u % (D / 4)) * 4;
+  return join<WARPS>(
+      WARPS, [&](int w) { return sh.ml[w][r]; },
+      [&](int w) { return *reinterpret_cast<const float4 *>(so + (w * RB + r) * D + d); }, M, Z);
+}
+
+template <int D>
+__device__ __forceinline__ void emit(const WinParams &p, int b, int g, int u, float4 v, float M, float Z) {
+  const int r = u / (D / 4), d = (u % (D / 4)) * 4, t = r / p.G;
+  const int64_t row = (int64_t(b) * p.T_max + t) * p.Hq + g * p.G + (r - t * p.G);
+  const float inv = 1.f / Z;
+  *reinterpret_cast<uint2 *>(p.out + row * D + d) = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+  if (d == 0 && p.lse != nullptr) p.lse[row] = (M + log2f(Z)) * LN2;
+}
+
+template <int D>
+__global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams p) {
+  using C = RowsCfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ RowsShared sh;
+  const int tid = threadIdx.x;
+  int x = blockIdx.x;
+  const int split = x % p.nsplit;
+  x /= p.nsplit;
+  const int g = x % p.Hkv, b = x / p.Hkv;
+  if (p.nsplit > 1) cluster_arrive();  // this CTA runs: it may be written to
+  const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
+  const bool report = split == 0 && g == 0;
+  int bad = 0;
+  if (T < 0 || T > p.T_max) bad = DREAMS_DATA_BAD_TREE_LEN;
+  else if (L < 0 || int64_t(L) + T > p.capacity) bad = DREAMS_DATA_BAD_KV_LEN;
+  if (bad && report && tid == 0) flag(p.status, bad);
+  // (all CTAs of a cluster come to the same answer; none leaves while it may be written to)
+  if (bad || T == 0 || !load_rows(p, sh, b, L, T, report)) {
+    if (p.nsplit > 1) cluster_wait();
+    return;
+  }
+  const KeyList kl = key_list(p, L, 0, T - 1);
+  const int64_t per = ((int64_t(kl.n) + p.nsplit - 1) / p.nsplit + KT - 1) / KT * KT;
+  const int i0 = int(::min(int64_t(kl.n), split * per)), i1 = int(::min(int64_t(kl.n), i0 + per));
+  stream_keys<D>(p, sh, smem, kl, b, g, L, T, i0, i1);
+  const int units = T * p.G * (D / 4);
+  if (p.nsplit == 1) {
+    for (int u = tid; u < units; u += 32 * WARPS) {
+      float M, Z;
+      const float4 v = join_warps<D>(sh, smem, u, M, Z);
+      emit<D>(p, b, g, u, v, M, Z);
+    }
+    return;
+  }
+  // Unit u goes to CTA u % nsplit, place u / nsplit of this CTA's row there.
+  cluster_wait();
+  const uint32_t box = smem_u32(smem) + C::RING, part = smem_u32(&sh.part[0][0]);
+  const int room = RB * (D / 4) / p.nsplit;  // units of a CTA
+  for (int u = tid; u < units; u += 32 * WARPS) {
+    float M, Z;
+    const float4 v = join_warps<D>(sh, smem, u, M, Z);
+    const int to = u % p.nsplit;
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(mapa(box + (split * room + u / p.nsplit) * 16, to)), "f"(v.x),
+                 "f"(v.y), "f"(v.z), "f"(v.w)
+                 : "memory");
+    if (u % (D / 4) < p.nsplit)  // the row's (M, Z) to every CTA, one thread each
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(mapa(part + (split * RB + u / (D / 4)) * 8, u % (D / 4))), "f"(M), "f"(Z)
+                   : "memory");
+  }
+  cluster_sync();
+  const float4 *in = reinterpret_cast<const float4 *>(smem + C::RING);
+  for (int u = split + p.nsplit * tid; u < units; u += p.nsplit * 32 * WARPS) {
+    float M, Z;
+    const float4 v = join<8>(
+        p.nsplit, [&](int c) { return sh.part[c][u / (D / 4)]; }, [&](int c) { return in[c * room + u / p.nsplit]; }, M, Z);
+    emit<D>(p, b, g, u, v, M, Z);
+  }
+}
+
+// ------------------------------------------------------------------ even cut
+constexpr int UNIT = 64;        // keys: what the lists are cut into
+constexpr int MAX_SEQS = 2048;  // sequences whose prefix sums fit in shared memory
+
+// Two parts a CTA at most lie in cut lists: the end of one, and the start of another.
+struct StreamSpace {
+  int32_t *count;  // [B * Hkv] parts of a list that are done (zero between calls)
+  float *o;        // [2 * CTAs][16][D]
+  float2 *ml;      // [2 * CTAs][16]
+};
+
+template <int D>
+__global__ void __launch_bounds__(32 * WARPS) window_stream_kernel(const WinParams p, const StreamSpace ws) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ RowsShared sh;
+  __shared__ int s_first[MAX_SEQS + 1];  // units before sequence b, for one KV head
+  __shared__ int s_warp[WARPS], s_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // units of every sequence, as prefix sums
+  int base = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 32 * WARPS) {
+    const int b = b0 + tid;
+    int n = 0;
+    if (b < p.B) {
+      const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
+      int bad = 0;
+      if (T < 0 || T > p.T_max) bad = DREAMS_DATA_BAD_TREE_LEN;
+      else if (L < 0 || int64_t(L) + T > p.capacity) bad = DREAMS_DATA_BAD_KV_LEN;
+      if (bad && blockIdx.x == 0) flag(p.status, bad);
+      if (!bad && T > 0) n = (key_list(p, L, 0, T - 1).n + UNIT - 1) / UNIT;
+    }
+    int y = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int z = __shfl_up_sync(0xffffffffu, y, o);
+      if (lane >= o) y += z;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = y;
+    __syncthreads();
+    int before = base;
+    for (int w = 0; w < warp; ++w) before += s_warp[w];
+    if (b < p.B) s_first[b] = before + y - n;
+    for (int w = 0; w < WARPS; ++w) base += s_warp[w];
+  }
+  if (tid == 0) s_first[p.B] = base;
+  __syncthreads();
+  const int64_t all = int64_t(base) * p.Hkv;
+  const int64_t per = ::max(int64_t(4), (all + gridDim.x - 1) / gridDim.x);
+  int64_t u0 = blockIdx.x * per;
+  const int64_t u1 = ::min(all, u0 + per);
+  const int64_t begin = u0;
+  if (u0 >= u1) return;
+  int b = 0;  // the sequence of unit u0
+  for (int step = 1024; step > 0; step >>= 1)
+    if (b + step < p.B && int64_t(s_first[b + step]) * p.Hkv <= u0) b += step;
+  // (step 1024 reaches 2047; sequences without units share their successor's start)
+  while (u0 < u1) {
+    while (int64_t(s_first[b + 1]) * p.Hkv <= u0) ++b;
+    const int n = s_first[b + 1] - s_first[b];
+    const int64_t seq0 = int64_t(s_first[b]) * p.Hkv;
+    const int g = int((u0 - seq0) / n);
+    const int64_t list0 = seq0 + int64_t(g) * n, list1 = list0 + n;  // the list's units
+    const int64_t e = ::min(u1, list1);
+    const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
+    const KeyList kl = key_list(p, L, 0, T - 1);
+    if (load_rows(p, sh, b, L, T, g == 0 && u0 == list0)) {
+      stream_keys<D>(p, sh, smem, kl, b, g, L, T, int(u0 - list0) * UNIT, int(::min(int64_t(kl.n), (e - list0) * UNIT)));
+      const int units = T * p.G * (D / 4);
+      if (u0 == list0 && e == list1) {
+        for (int u = tid; u < units; u += 32 * WARPS) {
+          float M, Z;
+          const float4 v = join_warps<D>(sh, smem, u, M, Z);
+          emit<D>(p, b, g, u, v, M, Z);
+        }
+      } else {
+        // this part into the workspace; the CTA that completes the list joins them
+        const int64_t slot = 2 * int64_t(blockIdx.x) + (begin < list0 ? 1 : 0);
+        for (int u = tid; u < units; u += 32 * WARPS) {
+          float M, Z;
+          const float4 v = join_warps<D>(sh, smem, u, M, Z);
+          reinterpret_cast<float4 *>(ws.o)[slot * (RB * D / 4) + u] = v;
+          if (u % (D / 4) == 0) ws.ml[slot * RB + u / (D / 4)] = make_float2(M, Z);
+        }
+        __threadfence();
+        __syncthreads();
+        const int c0 = int(list0 / per), c1 = int((list1 - 1) / per);  // the CTAs of the list
+        if (tid == 0) s_last = atomicAdd(ws.count + int64_t(b) * p.Hkv + g, 1) == c1 - c0;
+        __syncthreads();
+        if (s_last) {
+          __threadfence();
+          for (int u = tid; u < units; u += 32 * WARPS) {
+            float M = -INFINITY, Z = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = c0; c <= c1; c += 8) {
+              float Mi, Zi;
+              auto slot_of = [&](int i) { return 2 * int64_t(c + i) + ((c + i) * per < list0 ? 1 : 0); };
+              const float4 v = join<8>(
+                  ::min(8, c1 - c + 1), [&](int i) { return __ldcg(ws.ml + slot_of(i) * RB + u / (D / 4)); },
+                  [&](int i) { return __ldcg(reinterpret_cast<const float4 *>(ws.o) + slot_of(i) * (RB * D / 4) + u); }, Mi, Zi);
+              if (Zi == 0.f) continue;
+              const float Mn = fmaxf(M, Mi), a = Z == 0.f ? 0.f : tc::ex2(M - Mn), w = tc::ex2(Mi - Mn);
+              Z = a * Z + w * Zi;
+              acc = make_float4(a * acc.x + w * v.x, a * acc.y + w * v.y, a * acc.z + w * v.z, a * acc.w + w * v.w);
+              M = Mn;
+            }
+            emit<D>(p, b, g, u, acc, M, Z);
+          }
+          if (tid == 0) ws.count[int64_t(b) * p.Hkv + g] = 0;
+        }
+      }
+    }
+    u0 = e;
+  }
 }
 
 // ------------------------------------------------------------------ host side
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+// The even cut pays where every CTA (two per SM) gets about four units or more: it
+// ends all SMs together, where whole lists leave a last partial wave; below that, the
+// cluster's join is quicker than the one through memory. Measured for 32 query / 8 KV
+// heads and a window of 4096: 64 sequences EVEN64, one sequence EVEN1.
+int stream_ctas() { return 2 * num_sms(); }
+bool use_stream(const dreams_kv_cache_t *kv, int B, int T_max, int window, int sinks) {
+  const int64_t keys = std::min<int64_t>(kv->capacity, int64_t(window) - 1 + T_max + sinks);
+  return B <= MAX_SEQS && int64_t(B) * kv->Hkv * ((keys + UNIT - 1) / UNIT) >= 4 * int64_t(stream_ctas());
+}
+size_t stream_space(int B, int Hkv, uint8_t *ws, StreamSpace *s) {
+  // the counters last, behind the most that parts of any call take: what one call
+  // leaves in the parts must not be another's counters
+  const size_t slots = 2 * size_t(stream_ctas()), o = slots * RB * 128 * 4, ml = slots * RB * 8;
+  if (s != nullptr) *s = {reinterpret_cast<int32_t *>(ws + o + ml), reinterpret_cast<float *>(ws), reinterpret_cast<float2 *>(ws + o)};
+  return o + ml + align_up(size_t(B) * Hkv * 4, 256);
+}
+
 template <int D>
-dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
-  const void *kernel = reinterpret_cast<const void *>(window_rows_kernel<D>);
-  const dreams_status_t st = ensure_max_dynamic_smem(kernel, RowsCfg<D>::SMEM);
+dreams_status_t launch_rows(WinParams p, const dreams_kv_cache_t *kv, uint8_t *ws, cudaStream_t stream) {
+  const bool even = use_stream(kv, p.B, p.T_max, p.window, p.sinks);
+  const void *kernel = even ? reinterpret_cast<const void *>(window_stream_kernel<D>) : reinterpret_cast<const void *>(window_rows_kernel<D>);
+  const int smem = even ? RowsCfg<D>::RING : RowsCfg<D>::SMEM;
+  const dreams_status_t st = ensure_max_dynamic_smem(kernel, smem);
   if (st != DREAMS_OK) return st;
-  p.nrb = int((int64_t(p.T_max) * p.G + RB - 1) / RB);
-  const int64_t items = int64_t(p.B) * p.Hkv * p.nrb;
-  // keys a block can see at most
-  const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + p.sinks + std::min<int64_t>(p.T_max, RB));
+  StreamSpace space{};
+  const int64_t items = int64_t(p.B) * p.Hkv;
   p.nsplit = 1;
-  while (p.nsplit < 8 && items * p.nsplit < 4 * int64_t(num_sms()) && keys / p.nsplit > 2 * WARPS * KT) p.nsplit *= 2;
+  if (even) {
+    stream_space(p.B, p.Hkv, ws, &space);
+  } else {
+    const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) - 1 + p.T_max + p.sinks);
+    while (p.nsplit < 8 && items * p.nsplit < 2 * int64_t(num_sms()) && keys / p.nsplit > WARPS * KT) p.nsplit *= 2;
+  }
   if (items * p.nsplit > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(items * p.nsplit));
+  cfg.gridDim = dim3(even ? unsigned(stream_ctas()) : unsigned(items * p.nsplit));
   cfg.blockDim = dim3(32 * WARPS);
-  cfg.dynamicSmemBytes = RowsCfg<D>::SMEM;
+  cfg.dynamicSmemBytes = size_t(smem);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -413,7 +588,7 @@ dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.nsplit > 1 ? 1 : 0;
-  void *args[] = {&p};
+  void *args[] = {&p, &space};
   const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
   if (e != cudaSuccess) {
     set_last_cuda_error(e);
@@ -436,8 +611,9 @@ using namespace dreams;
 
 extern "C" size_t dreams_window_attention_workspace_size(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max,
                                                          int32_t Hq, int32_t window, int32_t sinks, int32_t tree) {
-  if (!shapes_ok(kv, B, T_max, Hq, window, sinks, tree != 0)) return 0;
-  return 0;
+  if (!shapes_ok(kv, B, T_max, Hq, window, sinks, tree != 0) || (kv->D != 64 && kv->D != 128)) return 0;
+  if (int64_t(T_max) * (Hq / kv->Hkv) > RB || !use_stream(kv, B, T_max, window, sinks)) return 0;
+  return stream_space(B, kv->Hkv, nullptr, nullptr);
 }
 
 extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
@@ -490,7 +666,10 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
   p.sinks = sinks;
   p.scale_log2 = scale * LOG2E;
   p.status = status_word;
+  const size_t need = dreams_window_attention_workspace_size(kv, B, T_max, Hq, window, sinks, parent != nullptr);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return DREAMS_ERR_WORKSPACE;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
   if (int64_t(T_max) * p.G > RB) return launch_tc(p, kv, s);
-  return kv->D == 128 ? launch_rows<128>(p, s) : launch_rows<64>(p, s);
+  return kv->D == 128 ? launch_rows<128>(p, kv, ws, s) : launch_rows<64>(p, kv, ws, s);
 }

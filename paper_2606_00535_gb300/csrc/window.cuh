@@ -23,7 +23,7 @@ struct WinParams {
   int32_t B, T_max, Hq, Hkv, G;
   int32_t window, sinks;
   float scale_log2;
-  int32_t nrb, nsplit;
+  int32_t nsplit;
   int32_t *status;
 };
 
@@ -42,8 +42,8 @@ __device__ __forceinline__ KeyList key_list(const WinParams &p, int L, int t_fir
   return kl;
 }
 
-// The new slots a tree node sees, as a bit per node, and its depth: the walk from
-// the node to the root over a checked parent array.
+// The new slots a tree node (t < q_len) sees, as a bit per node, and its depth: the
+// walk from the node to the root over a checked parent array.
 template <typename I>
 __device__ __forceinline__ unsigned long long tree_row(const WinParams &p, const I *par, int L, int t, int &depth) {
   depth = 0;
@@ -61,8 +61,14 @@ __device__ __forceinline__ bool sees(const WinParams &p, int L, int off, unsigne
   return slot < L ? near : ((anc >> (slot - L)) & 1ull) != 0;
 }
 
+// Barriers of a cluster. Not the .aligned forms: a warp may come here from a loop that
+// its lanes left at different turns.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
 }
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t cta) {
   uint32_t r;

@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         t = row < sp->rows ? t0 + row / p.G : t0;
         r.off = t;
         r.anc = 0ull;
-        if (p.parent != nullptr && sp->bad == 0) r.anc = tree_row(p, s_par[warp], sp->L, t, r.off);
+        if (p.parent != nullptr && row < sp->rows && sp->bad == 0) r.anc = tree_row(p, s_par[warp], sp->L, t, r.off);
       }
       float m_ref = -INFINITY, l = 0.f;
       bool unset = true;  // does a row of this warp lack its reference?
