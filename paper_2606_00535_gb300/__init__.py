@@ -272,6 +272,7 @@ class KVCache:
                            self.D, self.capacity,
                            None if self.page_table is None else self.page_table.data_ptr(),
                            self.page_size, self.pages_per_seq, self.num_pages)
+        self._window_bytes: Dict[tuple, int] = {}  # window_attention's workspace by shape
 
 
 @dataclass
@@ -340,9 +341,10 @@ def _q_strides(q: torch.Tensor, name: str = "q", heads: str = "Hq") -> Tuple[int
     qualifies)."""
     if not isinstance(q, torch.Tensor) or q.dtype != torch.bfloat16 or q.dim() != 4:
         raise TypeError(f"{name} must be a 4-D bfloat16 tensor [B, T, {heads}, D]")
-    if q.stride(3) != 1 or q.stride(2) != q.shape[3]:
+    sb, st, sh, sd = q.stride()
+    if sd != 1 or sh != q.shape[3]:
         raise ValueError(f"{name}'s head rows must be dense (strides [.., .., D, 1])")
-    return int(q.stride(0)), int(q.stride(1))
+    return sb, st
 
 
 def tree_verify_attn(q: torch.Tensor, kv: KVCache, tree: Tree, scale: float, layer: int = 0,
@@ -699,7 +701,10 @@ def _scratch(kind: str, need: int, workspace: Optional[torch.Tensor], dev: torch
         return ws, n
     if need == 0 or dev.type != "cuda":  # off the GPU the launch refuses
         return None, 0
-    ws = _workspace(kind, need, dev, stream)
+    s = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+    ws = _WS.get((kind, dev.index, s))
+    if ws is None or ws.numel() < need:
+        ws = _workspace(kind, need, dev, stream)
     return ws.data_ptr(), ws.numel()
 
 
@@ -781,7 +786,12 @@ def window_attention(q: torch.Tensor, kv: KVCache, q_len: torch.Tensor, kv_len: 
         _need(lse, "lse", torch.float32, dev)
         if lse.shape != q.shape[:3]:
             raise ValueError("lse must be [B, T_max, Hq]")
-    need = window_attention_workspace_size(kv, B, T_max, Hq, window, sinks, parent is not None)
+    key = (B, T_max, Hq, window, sinks, parent is None)
+    need = kv._window_bytes.get(key)
+    if need is None:
+        if len(kv._window_bytes) > 256:
+            kv._window_bytes.clear()
+        need = kv._window_bytes[key] = window_attention_workspace_size(kv, B, T_max, Hq, window, sinks, parent is not None)
     ws, ws_bytes = _scratch("window", need, workspace, dev, stream)
     _launch("dreams_window_attention", dev, stream, q.data_ptr(), sb, stt, ctypes.byref(kv._c), layer, par, ql, kl, B,
             T_max, Hq, float(scale), window, sinks, out.data_ptr(), None if lse is None else lse.data_ptr(), ws, ws_bytes,

@@ -58,11 +58,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Does a pair of bf16 values hold an infinity or a NaN?
-__device__ __forceinline__ bool nonfinite2(uint32_t x) {
-  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-}
-
 constexpr int RB = 16;    // query rows of a CTA
 constexpr int KT = 16;    // keys of a warp's tile
 constexpr int WARPS = 4;
@@ -141,7 +136,7 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
     nslot = j < my && i < i1 ? kl.slot(i) : -1;
     if (p.table != nullptr && nslot >= 0) npage = __ldg(p.table + int64_t(b) * p.P + (nslot >> 6));
   };
-  auto issue = [&](int j) {
+  auto issue = [&](int j, uint32_t st) {
     if (j < my) {
       int64_t at = -1;
       if (nslot >= 0) {
@@ -154,7 +149,6 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
         }
       }
       look(j + 1);
-      const uint32_t st = ring + (j % C::STAGES) * 2 * C::TILE;
 #pragma unroll
       for (int it = 0; it < KT * CH / 32; ++it) {
         const int u = it * 32 + lane, key = u / CH, ch = u % CH;
@@ -169,8 +163,6 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
     cp_commit();
   };
   look(0);
-#pragma unroll
-  for (int j = 0; j < C::STAGES - 1; ++j) issue(j);
 
   // this thread's part of Q: rows lane / 4 and lane / 4 + 8
   const int r0 = lane >> 2, c0 = (lane & 3) * 2;
@@ -180,8 +172,12 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int r = r0 + 8 * h, t = r / p.G;
-    off[h] = sh.row[r].off;
-    anc[h] = sh.row[r].anc;
+    off[h] = t < T ? t : -1;
+    anc[h] = 0ull;
+    if (p.parent != nullptr) {
+      off[h] = sh.row[r].off;
+      anc[h] = sh.row[r].anc;
+    }
     const __nv_bfloat16 *src = p.q + b * p.sb + t * p.st + int64_t(g * p.G + r - t * p.G) * D + c0;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
@@ -195,11 +191,17 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
   const int off_max = T - 1;
-  for (int j = 0; j < my; ++j) {
-    cp_wait<C::STAGES - 2>();
-    __syncwarp();
-    issue(j + C::STAGES - 1);
-    const uint32_t st = ring + (j % C::STAGES) * 2 * C::TILE;
+  uint32_t st_in = ring, st = ring;  // the stages of the copy and of the tile
+  // (one copy of the code for the ramp and the stream: a short call runs it cold)
+#pragma unroll 1
+  for (int j = 1 - C::STAGES; j < my; ++j) {
+    if (j >= 0) {
+      cp_wait<C::STAGES - 2>();
+      __syncwarp();
+    }
+    issue(j + C::STAGES - 1, st_in);
+    st_in = st_in + 2 * C::TILE == ring + C::WARP_BYTES ? ring : st_in + 2 * C::TILE;
+    if (j < 0) continue;
     const int ib = i0 + (warp + j * WARPS) * KT;
 
     // scores: two 8-key column blocks
@@ -257,46 +259,65 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
       }
     }
     // O += P V
-    {
-      const int key = (((lane >> 3) & 1) << 3) + (lane & 7), half = lane >> 4;
+    const int vkey = (((lane >> 3) & 1) << 3) + (lane & 7), vhalf = lane >> 4;
+    const uint32_t vrow = st + C::TILE + vkey * C::ROW;
+    // 0 x inf and 0 x NaN are NaN: where a key that not every row sees holds one, each
+    // row takes its product from its own keys alone
+    bool odd = false;
+    if (!all) {
+      uint32_t acc = 0;  // sums of 0 x V: zero, or NaN
+#pragma unroll 2
+      for (int c = 0; c < C::TILE / 512; ++c) {
+        uint32_t u[4];
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                     : "r"(st + C::TILE + c * 512 + lane * 16));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(u[e]), "r"(0u));
+      }
+      odd = __any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0u);
+    }
+    if (__builtin_expect(!odd, 1)) {
 #pragma unroll
       for (int n = 0; n < D / 8; n += 2) {
         uint32_t vb[4];
-        ldsm4t(st + C::TILE + key * C::ROW + (((n + half) ^ (key & 7)) << 4), vb);
-        // 0 x inf and 0 x NaN are NaN: where a key that not every row sees holds
-        // one, each row takes its product from its own keys alone
-        if (!all && __any_sync(0xffffffffu, nonfinite2(vb[0]) || nonfinite2(vb[1]) || nonfinite2(vb[2]) || nonfinite2(vb[3]))) {
+        ldsm4t(vrow + (((n + vhalf) ^ (vkey & 7)) << 4), vb);
+        mma16816(o[n], pf, vb[0], vb[1]);
+        mma16816(o[n + 1], pf, vb[2], vb[3]);
+      }
+    } else {
 #pragma unroll 1
-          for (int r = 0; r < RB; ++r) {
-            const RowInfo ri = sh.row[r];
-            uint32_t keep[2];
+      for (int r = 0; r < RB; ++r) {
+        const RowInfo ri = sh.row[r];
+        uint32_t keep[2];
 #pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-              keep[hh] = 0u;
+        for (int hh = 0; hh < 2; ++hh) {
+          keep[hh] = 0u;
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int i = ib + hh * 8 + c0 + e;
-                if (i < i1 && ri.off >= 0 && sees(p, L, ri.off, ri.anc, kl.slot(i))) keep[hh] |= 0xffffu << (16 * e);
-              }
-            }
-            float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816(a0, pf, vb[0] & keep[0], vb[1] & keep[1]);
-            mma16816(a1, pf, vb[2] & keep[0], vb[3] & keep[1]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (r0 + 8 * h == r) {
-                o[n][2 * h] += a0[2 * h];
-                o[n][2 * h + 1] += a0[2 * h + 1];
-                o[n + 1][2 * h] += a1[2 * h];
-                o[n + 1][2 * h + 1] += a1[2 * h + 1];
-              }
+          for (int e = 0; e < 2; ++e) {
+            const int i = ib + hh * 8 + c0 + e;
+            if (i < i1 && ri.off >= 0 && sees(p, L, ri.off, ri.anc, kl.slot(i))) keep[hh] |= 0xffffu << (16 * e);
           }
-        } else {
-          mma16816(o[n], pf, vb[0], vb[1]);
-          mma16816(o[n + 1], pf, vb[2], vb[3]);
+        }
+#pragma unroll
+        for (int n = 0; n < D / 8; n += 2) {
+          uint32_t vb[4];
+          ldsm4t(vrow + (((n + vhalf) ^ (vkey & 7)) << 4), vb);
+          float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+          mma16816(a0, pf, vb[0] & keep[0], vb[1] & keep[1]);
+          mma16816(a1, pf, vb[2] & keep[0], vb[3] & keep[1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (r0 + 8 * h == r) {
+              o[n][2 * h] += a0[2 * h];
+              o[n][2 * h + 1] += a0[2 * h + 1];
+              o[n + 1][2 * h] += a1[2 * h];
+              o[n + 1][2 * h + 1] += a1[2 * h + 1];
+            }
         }
       }
     }
+    st = st + 2 * C::TILE == ring + C::WARP_BYTES ? ring : st + 2 * C::TILE;
   }
   cp_wait<0>();
   __syncthreads();  // the stages are free
