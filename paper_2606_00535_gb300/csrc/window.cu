@@ -136,14 +136,20 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
     nslot = j < my && i < i1 ? kl.slot(i) : -1;
     if (p.table != nullptr && nslot >= 0) npage = __ldg(p.table + int64_t(b) * p.P + (nslot >> 6));
   };
+  // Copies of 16 bytes: lanes CH to a key, 32 / CH keys at a time. A key is known by
+  // its row (slot and page, without the head): below 2^32 in any memory.
+  constexpr uint32_t NO_ROW = 0xffffffffu;
+  const int ch = lane % CH;
+  const int64_t pitch = int64_t(p.Hkv) * D;
+  const __nv_bfloat16 *kp = p.k + int64_t(g) * D + ch * 8, *vp = p.v + int64_t(g) * D + ch * 8;
   auto issue = [&](int j, uint32_t st) {
     if (j < my) {
-      int64_t at = -1;
+      uint32_t at = NO_ROW;
       if (nslot >= 0) {
         if (p.table == nullptr) {
-          at = (int64_t(b) * p.capacity + nslot) * p.Hkv + g;
+          at = uint32_t(b) * uint32_t(p.capacity) + uint32_t(nslot);
         } else if (npage >= 0 && npage < p.num_pages) {
-          at = (int64_t(npage) * 64 + (nslot & 63)) * p.Hkv + g;
+          at = uint32_t(npage) * 64u + uint32_t(nslot & 63);
         } else if (lane < 16) {
           flag(p.status, DREAMS_DATA_BAD_PAGE);
         }
@@ -151,13 +157,13 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
       look(j + 1);
 #pragma unroll
       for (int it = 0; it < KT * CH / 32; ++it) {
-        const int u = it * 32 + lane, key = u / CH, ch = u % CH;
-        const int64_t o = __shfl_sync(0xffffffffu, at, key);
+        const int key = it * (32 / CH) + lane / CH;
+        const uint32_t row = __shfl_sync(0xffffffffu, at, key);
         const uint32_t dst = st + key * C::ROW + ((ch ^ (key & 7)) << 4);
-        const int64_t e = o < 0 ? 0 : o * D + ch * 8;
-        const int bytes = o < 0 ? 0 : 16;
-        cp_async16(dst, p.k + e, bytes);
-        cp_async16(dst + C::TILE, p.v + e, bytes);
+        const int64_t e = row == NO_ROW ? 0 : row * pitch;
+        const int bytes = row == NO_ROW ? 0 : 16;
+        cp_async16(dst, kp + e, bytes);
+        cp_async16(dst + C::TILE, vp + e, bytes);
       }
     }
     cp_commit();
@@ -232,24 +238,31 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
         }
     }
     uint32_t pf[4];
+    float mx[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float mx = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      mx *= p.scale_log2;
-      const float mn = fmaxf(m[h], mx);
-      if (mn > m[h]) {  // the same in the four threads of a row
-        const float corr = tc::ex2(m[h] - mn);
+    for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], o));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) mx[h] = fmaxf(m[h], mx[h] * p.scale_log2);
+    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float corr = mx[h] == m[h] ? 1.f : tc::ex2(m[h] - mx[h]);  // (also where both are -inf)
+        m[h] = mx[h];
         l[h] *= corr;
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) {
           o[n][2 * h] *= corr;
           o[n][2 * h + 1] *= corr;
         }
-        m[h] = mn;
       }
-      const float nm = mn == -INFINITY ? 0.f : -mn;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float nm = m[h] == -INFINITY ? 0.f : -m[h];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const float p0 = tc::ex2(fmaf(s[n][2 * h], p.scale_log2, nm));
@@ -338,30 +351,25 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
   __syncthreads();
 }
 
-// Parts joined by log-sum-exp: sum of 2^(m_i - M) (l_i, o_i) over n parts.
-template <int N, typename ML, typename O>
+// Parts joined by log-sum-exp: sum of 2^(m_i - M) (l_i, o_i) over n parts, in order.
+template <int UNROLL, typename ML, typename O>
 __device__ __forceinline__ float4 join(int n, ML ml_of, O o_of, float &M, float &Z) {
-  float2 ml[N];
-  float4 o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {  // all loads first
-    ml[i] = i < n ? ml_of(i) : make_float2(-INFINITY, 0.f);
-    o[i] = i < n ? o_of(i) : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
   M = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < N; ++i) M = fmaxf(M, ml[i].x);
+#pragma unroll UNROLL
+  for (int i = 0; i < n; ++i) M = fmaxf(M, ml_of(i).x);
   Z = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (ml[i].y == 0.f) continue;  // no key (a NaN sum goes through)
-    const float c = tc::ex2(ml[i].x - M);
-    Z += c * ml[i].y;
-    acc.x += c * o[i].x;
-    acc.y += c * o[i].y;
-    acc.z += c * o[i].z;
-    acc.w += c * o[i].w;
+#pragma unroll UNROLL
+  for (int i = 0; i < n; ++i) {
+    const float2 ml = ml_of(i);
+    const float4 o = o_of(i);
+    const bool some = ml.y != 0.f;  // (a NaN sum goes through; without keys o may hold anything)
+    const float c = some ? tc::ex2(ml.x - M) : 0.f;
+    Z += some ? c * ml.y : 0.f;
+    acc.x += some ? c * o.x : 0.f;
+    acc.y += some ? c * o.y : 0.f;
+    acc.z += some ? c * o.z : 0.f;
+    acc.w += some ? c * o.w : 0.f;
   }
   return acc;
 }
@@ -380,7 +388,7 @@ template <int D>
 __device__ __forceinline__ void emit(const WinParams &p, int b, int g, int u, float4 v, float M, float Z) {
   const int r = u / (D / 4), d = (u % (D / 4)) * 4, t = r / p.G;
   const int64_t row = (int64_t(b) * p.T_max + t) * p.Hq + g * p.G + (r - t * p.G);
-  const float inv = 1.f / Z;
+  const float inv = __frcp_rn(Z);
   *reinterpret_cast<uint2 *>(p.out + row * D + d) = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
   if (d == 0 && p.lse != nullptr) p.lse[row] = (M + log2f(Z)) * LN2;
 }
@@ -439,7 +447,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
   const float4 *in = reinterpret_cast<const float4 *>(smem + C::RING);
   for (int u = split + p.nsplit * tid; u < units; u += p.nsplit * 32 * WARPS) {
     float M, Z;
-    const float4 v = join<8>(
+    const float4 v = join<4>(
         p.nsplit, [&](int c) { return sh.part[c][u / (D / 4)]; }, [&](int c) { return in[c * room + u / p.nsplit]; }, M, Z);
     emit<D>(p, b, g, u, v, M, Z);
   }
