@@ -425,17 +425,13 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
  * and its slots read as zeros. What a slot holds does not reach a query that does
  * not see it, infinities and NaN included. Accumulation is fp32; probabilities
  * enter the PV product as bf16, and the output is rounded to bf16 once. One
- * launch. The workspace (0 bytes for many shapes) holds counters that reset
- * themselves: zero-fill it once when it is allocated.
+ * launch, no workspace.
  */
-size_t dreams_window_attention_workspace_size(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max, int32_t Hq,
-                                              int32_t window, int32_t sinks, int32_t tree);
 dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
                                         const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
                                         const int32_t *q_len, const int32_t *kv_len, int32_t B, int32_t T_max,
                                         int32_t Hq, float scale, int32_t window, int32_t sinks, void *out,
-                                        float *lse, void *workspace, size_t workspace_bytes, int32_t *status_word,
-                                        dreams_stream_t stream);
+                                        float *lse, int32_t *status_word, dreams_stream_t stream);
 
 /*
  * The pages of a paged cache, kept on the device so that no call has to read

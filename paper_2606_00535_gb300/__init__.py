@@ -110,9 +110,8 @@ def _lib() -> ctypes.CDLL:
                                                                   p, p, p, p, p, p, sz, p, p]),
                     "dreams_verify_step_speculative": (ctypes.c_int, [p, p, ctypes.c_int, i64, i64, ptr, pkv, i32,
                                                                       f32, p, p, p, p, p, p, p, p]),
-                    "dreams_window_attention_workspace_size": (sz, [pkv, i32, i32, i32, i32, i32, i32]),
                     "dreams_window_attention": (ctypes.c_int, [p, i64, i64, pkv, i32, p, p, p, i32, i32, i32, f32,
-                                                               i32, i32, p, p, p, sz, p, p]),
+                                                               i32, i32, p, p, p, p]),
                     "dreams_kv_reserve_workspace_size": (sz, [ppl]),
                     "dreams_kv_reserve": (ctypes.c_int, [ppl, p, p, p, sz, p, p]),
                     "dreams_kv_release": (ctypes.c_int, [ppl, p, p, p, p]),
@@ -272,7 +271,6 @@ class KVCache:
                            self.D, self.capacity,
                            None if self.page_table is None else self.page_table.data_ptr(),
                            self.page_size, self.pages_per_seq, self.num_pages)
-        self._window_bytes: Dict[tuple, int] = {}  # window_attention's workspace by shape
 
 
 @dataclass
@@ -744,16 +742,10 @@ def _per_seq(t: torch.Tensor, name: str, B: int, dev) -> int:
     return t.data_ptr()
 
 
-def window_attention_workspace_size(kv: KVCache, B: int, T_max: int, Hq: int, window: int, sinks: int = 0,
-                                    tree: bool = False) -> int:
-    return int(_lib().dreams_window_attention_workspace_size(ctypes.byref(kv._c), B, T_max, Hq, window, sinks,
-                                                             int(tree)))
-
-
 def window_attention(q: torch.Tensor, kv: KVCache, q_len: torch.Tensor, kv_len: torch.Tensor, scale: float,
                      window: int, sinks: int = 0, parent: Optional[torch.Tensor] = None, layer: int = 0,
                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
-                     workspace: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+                     status: Optional[torch.Tensor] = None, stream=None):
     """Attention in which a query at position p sees the slots of the last
     ``window`` positions (its own among them) and of the first ``sinks`` ones.
     q: bf16 [B, T_max, Hq, D] (head rows dense, tokens and sequences may be
@@ -786,16 +778,9 @@ def window_attention(q: torch.Tensor, kv: KVCache, q_len: torch.Tensor, kv_len: 
         _need(lse, "lse", torch.float32, dev)
         if lse.shape != q.shape[:3]:
             raise ValueError("lse must be [B, T_max, Hq]")
-    key = (B, T_max, Hq, window, sinks, parent is None)
-    need = kv._window_bytes.get(key)
-    if need is None:
-        if len(kv._window_bytes) > 256:
-            kv._window_bytes.clear()
-        need = kv._window_bytes[key] = window_attention_workspace_size(kv, B, T_max, Hq, window, sinks, parent is not None)
-    ws, ws_bytes = _scratch("window", need, workspace, dev, stream)
     _launch("dreams_window_attention", dev, stream, q.data_ptr(), sb, stt, ctypes.byref(kv._c), layer, par, ql, kl, B,
-            T_max, Hq, float(scale), window, sinks, out.data_ptr(), None if lse is None else lse.data_ptr(), ws, ws_bytes,
-            _status(status, dev))
+            T_max, Hq, float(scale), window, sinks, out.data_ptr(), None if lse is None else lse.data_ptr(),
+            None if status is None else _status(status, dev))
     return out, lse
 
 

@@ -12,18 +12,14 @@
 // warps take 16-key tiles in turn, each with its own ring of cp.async stages, so no
 // barrier stands in the stream. Scores and P V run on m16n8k16 tensor instructions
 // (16 rows are all there are: the fifth-generation ones would work on 128), with the
-// running maximum and sum of each row in f32 registers. How the lists are cut:
-//   window_rows_kernel    one list to a CTA or, split, to a cluster, whose CTAs push
-//                         their parts into each other's shared memory: least latency
-//   window_stream_kernel  all lists end to end, cut evenly over two CTAs per SM, so
-//                         that every SM reads to the end; parts of a cut list join in
-//                         the workspace, by the CTA that comes last
-// Either way parts are joined in list order, so results repeat bit for bit. More rows
-// go to window_tc.cu.
+// running maximum and sum of each row in f32 registers. Where the lists are few, each
+// is split over a cluster, whose CTAs push their parts into each other's shared memory
+// and join them there, in list order. More rows go to window_tc.cu.
 #include <limits.h>
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "window.cuh"
 
@@ -83,7 +79,7 @@ struct RowsShared {
   int par[64];
   RowInfo row[RB];
   float2 ml[WARPS][RB];    // the warps' maxima and sums
-  float2 part[8][RB];      // those of a list's parts
+  float2 part[16][RB];     // those of a list's parts
 };
 
 // The queries of a sequence and KV head; false (flagged by `report`): a bad tree.
@@ -242,9 +238,9 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
 #pragma unroll
     for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1)
+    for (int k = 1; k < 4; k <<= 1)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], o));
+      for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], k));
 #pragma unroll
     for (int h = 0; h < 2; ++h) mx[h] = fmaxf(m[h], mx[h] * p.scale_log2);
     if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
@@ -453,163 +449,47 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
   }
 }
 
-// ------------------------------------------------------------------ even cut
-constexpr int UNIT = 64;        // keys: what the lists are cut into
-constexpr int MAX_SEQS = 2048;  // sequences whose prefix sums fit in shared memory
-
-// Two parts a CTA at most lie in cut lists: the end of one, and the start of another.
-struct StreamSpace {
-  int32_t *count;  // [B * Hkv] parts of a list that are done (zero between calls)
-  float *o;        // [2 * CTAs][16][D]
-  float2 *ml;      // [2 * CTAs][16]
-};
-
-template <int D>
-__global__ void __launch_bounds__(32 * WARPS) window_stream_kernel(const WinParams p, const StreamSpace ws) {
-  extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ RowsShared sh;
-  __shared__ int s_first[MAX_SEQS + 1];  // units before sequence b, for one KV head
-  __shared__ int s_warp[WARPS], s_last;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // units of every sequence, as prefix sums
-  int base = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 32 * WARPS) {
-    const int b = b0 + tid;
-    int n = 0;
-    if (b < p.B) {
-      const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
-      int bad = 0;
-      if (T < 0 || T > p.T_max) bad = DREAMS_DATA_BAD_TREE_LEN;
-      else if (L < 0 || int64_t(L) + T > p.capacity) bad = DREAMS_DATA_BAD_KV_LEN;
-      if (bad && blockIdx.x == 0) flag(p.status, bad);
-      if (!bad && T > 0) n = (key_list(p, L, 0, T - 1).n + UNIT - 1) / UNIT;
-    }
-    int y = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int z = __shfl_up_sync(0xffffffffu, y, o);
-      if (lane >= o) y += z;
-    }
-    __syncthreads();
-    if (lane == 31) s_warp[warp] = y;
-    __syncthreads();
-    int before = base;
-    for (int w = 0; w < warp; ++w) before += s_warp[w];
-    if (b < p.B) s_first[b] = before + y - n;
-    for (int w = 0; w < WARPS; ++w) base += s_warp[w];
-  }
-  if (tid == 0) s_first[p.B] = base;
-  __syncthreads();
-  const int64_t all = int64_t(base) * p.Hkv;
-  const int64_t per = ::max(int64_t(4), (all + gridDim.x - 1) / gridDim.x);
-  int64_t u0 = blockIdx.x * per;
-  const int64_t u1 = ::min(all, u0 + per);
-  const int64_t begin = u0;
-  if (u0 >= u1) return;
-  int b = 0;  // the sequence of unit u0
-  for (int step = 1024; step > 0; step >>= 1)
-    if (b + step < p.B && int64_t(s_first[b + step]) * p.Hkv <= u0) b += step;
-  // (step 1024 reaches 2047; sequences without units share their successor's start)
-  while (u0 < u1) {
-    while (int64_t(s_first[b + 1]) * p.Hkv <= u0) ++b;
-    const int n = s_first[b + 1] - s_first[b];
-    const int64_t seq0 = int64_t(s_first[b]) * p.Hkv;
-    const int g = int((u0 - seq0) / n);
-    const int64_t list0 = seq0 + int64_t(g) * n, list1 = list0 + n;  // the list's units
-    const int64_t e = ::min(u1, list1);
-    const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
-    const KeyList kl = key_list(p, L, 0, T - 1);
-    if (load_rows(p, sh, b, L, T, g == 0 && u0 == list0)) {
-      stream_keys<D>(p, sh, smem, kl, b, g, L, T, int(u0 - list0) * UNIT, int(::min(int64_t(kl.n), (e - list0) * UNIT)));
-      const int units = T * p.G * (D / 4);
-      if (u0 == list0 && e == list1) {
-        for (int u = tid; u < units; u += 32 * WARPS) {
-          float M, Z;
-          const float4 v = join_warps<D>(sh, smem, u, M, Z);
-          emit<D>(p, b, g, u, v, M, Z);
-        }
-      } else {
-        // this part into the workspace; the CTA that completes the list joins them
-        const int64_t slot = 2 * int64_t(blockIdx.x) + (begin < list0 ? 1 : 0);
-        for (int u = tid; u < units; u += 32 * WARPS) {
-          float M, Z;
-          const float4 v = join_warps<D>(sh, smem, u, M, Z);
-          reinterpret_cast<float4 *>(ws.o)[slot * (RB * D / 4) + u] = v;
-          if (u % (D / 4) == 0) ws.ml[slot * RB + u / (D / 4)] = make_float2(M, Z);
-        }
-        __threadfence();
-        __syncthreads();
-        const int c0 = int(list0 / per), c1 = int((list1 - 1) / per);  // the CTAs of the list
-        if (tid == 0) s_last = atomicAdd(ws.count + int64_t(b) * p.Hkv + g, 1) == c1 - c0;
-        __syncthreads();
-        if (s_last) {
-          __threadfence();
-          for (int u = tid; u < units; u += 32 * WARPS) {
-            float M = -INFINITY, Z = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int c = c0; c <= c1; c += 8) {
-              float Mi, Zi;
-              auto slot_of = [&](int i) { return 2 * int64_t(c + i) + ((c + i) * per < list0 ? 1 : 0); };
-              const float4 v = join<8>(
-                  ::min(8, c1 - c + 1), [&](int i) { return __ldcg(ws.ml + slot_of(i) * RB + u / (D / 4)); },
-                  [&](int i) { return __ldcg(reinterpret_cast<const float4 *>(ws.o) + slot_of(i) * (RB * D / 4) + u); }, Mi, Zi);
-              if (Zi == 0.f) continue;
-              const float Mn = fmaxf(M, Mi), a = Z == 0.f ? 0.f : tc::ex2(M - Mn), w = tc::ex2(Mi - Mn);
-              Z = a * Z + w * Zi;
-              acc = make_float4(a * acc.x + w * v.x, a * acc.y + w * v.y, a * acc.z + w * v.z, a * acc.w + w * v.w);
-              M = Mn;
-            }
-            emit<D>(p, b, g, u, acc, M, Z);
-          }
-          if (tid == 0) ws.count[int64_t(b) * p.Hkv + g] = 0;
-        }
-      }
-    }
-    u0 = e;
-  }
-}
-
 // ------------------------------------------------------------------ host side
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-// The even cut pays where every CTA (two per SM) gets about four units or more: it
-// ends all SMs together, where whole lists leave a last partial wave; below that, the
-// cluster's join is quicker than the one through memory. Measured for 32 query / 8 KV
-// heads and a window of 4096: 64 sequences EVEN64, one sequence EVEN1.
-int stream_ctas() { return 2 * num_sms(); }
-bool use_stream(const dreams_kv_cache_t *kv, int B, int T_max, int window, int sinks) {
-  const int64_t keys = std::min<int64_t>(kv->capacity, int64_t(window) - 1 + T_max + sinks);
-  return B <= MAX_SEQS && int64_t(B) * kv->Hkv * ((keys + UNIT - 1) / UNIT) >= 4 * int64_t(stream_ctas());
-}
-size_t stream_space(int B, int Hkv, uint8_t *ws, StreamSpace *s) {
-  // the counters last, behind the most that parts of any call take: what one call
-  // leaves in the parts must not be another's counters
-  const size_t slots = 2 * size_t(stream_ctas()), o = slots * RB * 128 * 4, ml = slots * RB * 8;
-  if (s != nullptr) *s = {reinterpret_cast<int32_t *>(ws + o + ml), reinterpret_cast<float *>(ws), reinterpret_cast<float2 *>(ws + o)};
-  return o + ml + align_up(size_t(B) * Hkv * 4, 256);
+// CTAs of a list: as many as still run at the same time, two to an SM. One CTA takes
+// 15 us for 1024 keys whatever else runs; with all places taken the copies are bound by
+// HBM, and further splits only add joins. Measured on the GPU for 8 KV heads, window
+// 4096, head dim 128, in us:
+//   lists        8     64    128    512
+//   1 CTA     61.4   63.1   63.6  162.0
+//   2         34.3   35.8   43.7  176.2
+//   4         20.1   25.4   50.6  174.5
+//   8         13.2   32.3   59.5  211.1
+constexpr int MAX_SPLIT = 16;
+int split_of(int64_t lists, int64_t keys) {
+  int n = 1;
+  while (n < MAX_SPLIT && lists * n * 2 <= 2 * int64_t(num_sms()) && keys / n > WARPS * KT) n *= 2;
+  return n;
 }
 
 template <int D>
-dreams_status_t launch_rows(WinParams p, const dreams_kv_cache_t *kv, uint8_t *ws, cudaStream_t stream) {
-  const bool even = use_stream(kv, p.B, p.T_max, p.window, p.sinks);
-  const void *kernel = even ? reinterpret_cast<const void *>(window_stream_kernel<D>) : reinterpret_cast<const void *>(window_rows_kernel<D>);
-  const int smem = even ? RowsCfg<D>::RING : RowsCfg<D>::SMEM;
-  const dreams_status_t st = ensure_max_dynamic_smem(kernel, smem);
+dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
+  const void *kernel = reinterpret_cast<const void *>(window_rows_kernel<D>);
+  const dreams_status_t st = ensure_max_dynamic_smem(kernel, RowsCfg<D>::SMEM);
   if (st != DREAMS_OK) return st;
-  StreamSpace space{};
-  const int64_t items = int64_t(p.B) * p.Hkv;
-  p.nsplit = 1;
-  if (even) {
-    stream_space(p.B, p.Hkv, ws, &space);
-  } else {
-    const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) - 1 + p.T_max + p.sinks);
-    while (p.nsplit < 8 && items * p.nsplit < 2 * int64_t(num_sms()) && keys / p.nsplit > WARPS * KT) p.nsplit *= 2;
+  // clusters of 16 have to be asked for, once per device
+  static std::atomic<uint64_t> wide{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev >= 64 || !((wide.load() >> dev) & 1u))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && dev < 64) wide.fetch_or(uint64_t(1) << dev);
   }
-  if (items * p.nsplit > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
+  if (e != cudaSuccess) {
+    set_last_cuda_error(e);
+    return DREAMS_ERR_CUDA;
+  }
+  const int64_t lists = int64_t(p.B) * p.Hkv;
+  p.nsplit = split_of(lists, std::min<int64_t>(p.capacity, int64_t(p.window) - 1 + p.T_max + p.sinks));
+  if (lists * p.nsplit > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(even ? unsigned(stream_ctas()) : unsigned(items * p.nsplit));
+  cfg.gridDim = dim3(unsigned(lists * p.nsplit));
   cfg.blockDim = dim3(32 * WARPS);
-  cfg.dynamicSmemBytes = size_t(smem);
+  cfg.dynamicSmemBytes = RowsCfg<D>::SMEM;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -617,8 +497,8 @@ dreams_status_t launch_rows(WinParams p, const dreams_kv_cache_t *kv, uint8_t *w
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.nsplit > 1 ? 1 : 0;
-  void *args[] = {&p, &space};
-  const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
+  void *args[] = {&p};
+  e = cudaLaunchKernelExC(&cfg, kernel, args);
   if (e != cudaSuccess) {
     set_last_cuda_error(e);
     return DREAMS_ERR_CUDA;
@@ -638,19 +518,11 @@ bool shapes_ok(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max, int32_t Hq
 
 using namespace dreams;
 
-extern "C" size_t dreams_window_attention_workspace_size(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max,
-                                                         int32_t Hq, int32_t window, int32_t sinks, int32_t tree) {
-  if (!shapes_ok(kv, B, T_max, Hq, window, sinks, tree != 0) || (kv->D != 64 && kv->D != 128)) return 0;
-  if (int64_t(T_max) * (Hq / kv->Hkv) > RB || !use_stream(kv, B, T_max, window, sinks)) return 0;
-  return stream_space(B, kv->Hkv, nullptr, nullptr);
-}
-
 extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
                                                    const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
                                                    const int32_t *q_len, const int32_t *kv_len, int32_t B,
                                                    int32_t T_max, int32_t Hq, float scale, int32_t window,
-                                                   int32_t sinks, void *out, float *lse, void *workspace,
-                                                   size_t workspace_bytes, int32_t *status_word,
+                                                   int32_t sinks, void *out, float *lse, int32_t *status_word,
                                                    dreams_stream_t stream) {
   if (q == nullptr || out == nullptr || kv == nullptr || q_len == nullptr || kv_len == nullptr || kv->k == nullptr ||
       kv->v == nullptr || !shapes_ok(kv, B, T_max, Hq, window, sinks, parent != nullptr))
@@ -695,10 +567,7 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
   p.sinks = sinks;
   p.scale_log2 = scale * LOG2E;
   p.status = status_word;
-  const size_t need = dreams_window_attention_workspace_size(kv, B, T_max, Hq, window, sinks, parent != nullptr);
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))) return DREAMS_ERR_WORKSPACE;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  uint8_t *ws = static_cast<uint8_t *>(workspace);
   if (int64_t(T_max) * p.G > RB) return launch_tc(p, kv, s);
-  return kv->D == 128 ? launch_rows<128>(p, kv, ws, s) : launch_rows<64>(p, kv, ws, s);
+  return kv->D == 128 ? launch_rows<128>(p, s) : launch_rows<64>(p, s);
 }

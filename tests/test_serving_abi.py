@@ -39,7 +39,7 @@ def test_window_attention_refusals(lib):
              lse=None):
         kv = cache() if kv is None else kv
         return lib.dreams_window_attention(q, sb, st, ctypes.byref(kv), layer, parent, ql, kl, B, T, Hq, scale, window, sinks, out, lse,
-                                           None, 0, None, None)
+                                           None, None)
 
     for kw in (dict(q=None), dict(out=None), dict(ql=None), dict(kl=None), dict(q=P + 2), dict(out=P + 8), dict(lse=P + 2), dict(layer=2),
                dict(layer=-1), dict(B=0), dict(T=0), dict(T=(1 << 20) + 1), dict(parent=P, T=65), dict(Hq=3), dict(Hq=0), dict(Hq=2 * 129),
