@@ -101,64 +101,94 @@ __device__ int list_free(const int32_t *ref, int lo, int hi, int most, int32_t *
 }
 
 // ------------------------------------------------------------------ reserve
-// One block: rows in chunks of its threads, each thread counting what its row
-// lacks; a prefix sum gives every row its place in the list of free pages. A
-// call is a few microseconds of dependent loads, whatever the pool's size up
-// to about 10^5 pages.
+// One block. `g` lanes of a warp share a row and walk its entries side by side
+// (32 of them while rows are few, so that a chunk of 2048 tokens is two turns
+// and not 33), counting what the row lacks; a prefix sum gives every row its
+// place in the list of free pages, and a second walk fills the entries in. The
+// call is a chain of about six dependent loads, whatever the pool's size up to
+// some 10^4 pages: 2.4 us for one row of one entry, 2.9 us for 16 rows of up to
+// 33 (12.9 with a thread per row).
+struct RowSpan {
+  int e0, e1, bad;  // the entries that the new tokens touch
+};
+__device__ __forceinline__ RowSpan row_span(const Pool &p, const int32_t *kv_len, const int32_t *n_new, int b) {
+  const int64_t L = __ldg(kv_len + b), n = __ldg(n_new + b);
+  if (L < 0 || n < 0 || L + n > int64_t(p.P) * PAGE) return {0, 0, DREAMS_DATA_BAD_KV_LEN};
+  return {int(L / PAGE), n > 0 ? int((L + n + PAGE - 1) / PAGE) : int(L / PAGE), 0};
+}
+
+constexpr int LIST_SHARED = 4096;
 __global__ void __launch_bounds__(BOOK_THREADS) kv_reserve_kernel(const Pool p, const int32_t *kv_len,
                                                                   const int32_t *n_new, int32_t *start,
-                                                                  int32_t *list, int32_t *status) {
-  __shared__ int s_warp[32];
-  const int64_t cap = int64_t(p.P) * PAGE;
+                                                                  int32_t *list_ws, int32_t *status, int g) {
+  __shared__ int s_warp[32], s_list[LIST_SHARED];
+  const int lane = threadIdx.x & (g - 1);
+  const int row0 = int(threadIdx.x) / g, rows = BOOK_THREADS / g;
+  const unsigned shift = (threadIdx.x & 31) & ~(g - 1);  // the row's lanes within the warp
+  const unsigned mask = g == 32 ? 0xffffffffu : (1u << g) - 1;
   int base = 0;
-  for (int b0 = 0; b0 < p.B; b0 += BOOK_THREADS) {
-    const int b = b0 + int(threadIdx.x);
-    int need = 0;
+  for (int b0 = 0; b0 < p.B; b0 += rows) {
+    const int b = b0 + row0;
+    int need = 0, bad = 0;
     if (b < p.B) {
-      const int64_t L = __ldg(kv_len + b), n = __ldg(n_new + b);
-      if (L < 0 || n < 0 || L + n > cap) {
-        flag(status, DREAMS_DATA_BAD_KV_LEN);
-      } else if (n > 0) {
-        const int e1 = int((L + n + PAGE - 1) / PAGE);
-        int bad = 0;
-        for (int e = int(L / PAGE); e < e1; ++e) {
-          const int pg = p.table[int64_t(b) * p.P + e];
-          if (pg == -1) ++need;
-          else if (pg < 0 || pg >= p.num_pages) bad |= DREAMS_DATA_BAD_PAGE;
-          else if (__ldcg(p.ref + pg) != 1) bad |= DREAMS_DATA_SHARED_PAGE;
-        }
-        if (bad) {
-          flag(status, bad);
-          need = 0;
-        }
+      const RowSpan s = row_span(p, kv_len, n_new, b);
+      bad = s.bad;
+      for (int e = s.e0 + lane; e < s.e1; e += g) {
+        const int pg = p.table[int64_t(b) * p.P + e];
+        if (pg == -1) ++need;
+        else if (pg < 0 || pg >= p.num_pages) bad |= DREAMS_DATA_BAD_PAGE;
+        else if (__ldcg(p.ref + pg) != 1) bad |= DREAMS_DATA_SHARED_PAGE;
       }
     }
+    __syncwarp();
+    for (int o = 1; o < g; o <<= 1) {
+      need += __shfl_xor_sync(0xffffffffu, need, o);
+      bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+    }
+    if (bad) {
+      if (lane == 0) flag(status, bad);
+      need = 0;
+    }
     int total;
-    const int r = base + block_scan(need, s_warp, total);
-    if (b < p.B) start[b] = need > 0 ? r : -1;
+    const int r = base + block_scan(lane == 0 ? need : 0, s_warp, total);
+    if (b < p.B && lane == 0) start[b] = need > 0 ? r : -1;
     base += total;
   }
   if (base == 0) return;
-  const int have = list_free(p.ref, 0, p.num_pages, ::min(base, p.num_pages), list, s_warp);
+  const int want = ::min(base, p.num_pages);
+  int32_t *list = want <= LIST_SHARED ? s_list : list_ws;
+  const int have = list_free(p.ref, 0, p.num_pages, want, list, s_warp);
   __syncthreads();  // start[] and list[] are written
-  for (int b = int(threadIdx.x); b < p.B; b += BOOK_THREADS) {
-    int r = start[b];
-    if (r < 0) continue;
-    const int L = __ldg(kv_len + b);
-    const int e0 = L / PAGE, e1 = int((int64_t(L) + __ldg(n_new + b) + PAGE - 1) / PAGE);
-    int32_t *row = p.table + int64_t(b) * p.P;
-    int need = 0;
-    for (int e = e0; e < e1; ++e) need += row[e] == -1;
-    if (r + need > have) {
-      flag(status, DREAMS_DATA_NO_PAGES);
-      continue;
+  for (int b0 = 0; b0 < p.B; b0 += rows) {
+    const int b = b0 + row0;
+    const int r = b < p.B ? start[b] : -1;
+    int e0 = 0, e1 = 0;
+    if (r >= 0) {
+      const RowSpan s = row_span(p, kv_len, n_new, b);
+      e0 = s.e0;
+      e1 = s.e1;
     }
-    for (int e = e0; e < e1; ++e)
-      if (row[e] == -1) {
-        const int pg = list[r++];
-        row[e] = pg;
+    int32_t *row = p.table + int64_t(b) * p.P;
+    // a row gets all that it lacks or nothing
+    int need = 0;
+    for (int e = e0 + lane; e < e1; e += g) need += row[e] == -1;
+    __syncwarp();
+    for (int o = 1; o < g; o <<= 1) need += __shfl_xor_sync(0xffffffffu, need, o);
+    if (r >= 0 && r + need > have) {
+      if (lane == 0) flag(status, DREAMS_DATA_NO_PAGES);
+      e1 = e0;
+    }
+    int at = r;
+    for (int e = e0; __any_sync(0xffffffffu, e < e1); e += g) {
+      const bool lacks = e + lane < e1 && row[e + lane] == -1;
+      const unsigned who = (__ballot_sync(0xffffffffu, lacks) >> shift) & mask;
+      if (lacks) {
+        const int pg = list[at + __popc(who & ((1u << lane) - 1))];
+        row[e + lane] = pg;
         p.ref[pg] = 1;
       }
+      at += __popc(who);
+    }
   }
 }
 
@@ -186,180 +216,243 @@ __global__ void __launch_bounds__(256) kv_release_kernel(const Pool p, const int
 }
 
 // ------------------------------------------------------------------ fork
-// What the two launches share, in the workspace.
+// The workspace.
 struct ForkState {
-  int32_t *head;   // [0] data flags, [1] copies, [2 + c] free pages found by CTA c
-  int32_t *first;  // [B] the lowest row of each parent (B: none)
-  int32_t *len;    // [B] new lengths
+  int32_t *head;   // [0] copies, then a word per CTA with its data flags, then one with the free pages it found
   int32_t *src, *dst, *rows;  // [B] copies: page, new page, rows of it
   int32_t *list;   // [FORK_CTAS][B] free pages by CTA
+  int32_t *by_row;  // [FORK_CTAS][4][B] where the rows do not fit into shared memory
   int32_t *table;  // [B, P] the new table
 };
-constexpr int FORK_HEAD = 2 + FORK_CTAS;
+constexpr int HEAD_FLAGS = 1, HEAD_FOUND = HEAD_FLAGS + FORK_CTAS, FORK_HEAD = HEAD_FOUND + FORK_CTAS;
+constexpr int FORK_SHARED_ROWS = 2048, FORK_UNROLL = 4;
+// One CTA for tables of up to so many entries: its barriers are cheaper; eight
+// keep more loads in flight. (Whole call with copies of next to nothing: 448
+// entries 7.5 us against 9.4, 544 8.5 against 10.6; 12288 14.7 against 11.6.)
+constexpr int FORK_ONE_CELLS = 4096;
 
-// (Not the .aligned forms: warps come here from loops that their lanes left at
-// different turns.)
-__device__ __forceinline__ void cluster_sync() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+template <int CTAS>
+__device__ __forceinline__ void fork_sync() {
+  if (CTAS == 1) {
+    __syncthreads();
+  } else {
+    // (Not the .aligned forms: warps come here from loops that their lanes left
+    // at different turns.)
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
+  }
 }
 
-// The new table, counts and lengths, and the list of pages to copy: one
-// cluster, whose barrier separates the phases (new entries from the old table;
-// counts; free pages; the table).
-__global__ void __cluster_dims__(FORK_CTAS, 1, 1) __launch_bounds__(BOOK_THREADS)
+// The new table, counts and lengths, and the list of pages to copy. A chain of
+// dependent loads and barriers: what concerns rows is worked out by every CTA
+// for itself, so that the CTAs meet only twice, after the counts have changed
+// and after the free pages have been listed. An error found there puts the
+// counts back.
+template <int CTAS>
+__global__ void __launch_bounds__(BOOK_THREADS)
     kv_fork_table_kernel(const Pool p, const int32_t *parent, const int32_t *kv_len, int32_t *new_kv_len,
                          const ForkState f, int32_t *status) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  __shared__ int s_warp[32];
-  const int rank = blockIdx.x;
-  const int t0 = rank * BOOK_THREADS + int(threadIdx.x), nt = FORK_CTAS * BOOK_THREADS;
-  const int64_t cells = int64_t(p.B) * p.P;
-  const int64_t cap = int64_t(p.P) * PAGE;
+  __shared__ int s_warp[32], s_bad;
+  __shared__ int32_t s_rows[4 * FORK_SHARED_ROWS];
+  const int rank = CTAS == 1 ? 0 : int(blockIdx.x);
+  const int t0 = rank * BOOK_THREADS + int(threadIdx.x);
+  constexpr int nt = CTAS * BOOK_THREADS;
+  const unsigned cells = unsigned(p.B) * unsigned(p.P);
+  const bool near = p.B <= FORK_SHARED_ROWS;
+  const int pitch = near ? FORK_SHARED_ROWS : p.B;
+  int32_t *first = near ? s_rows : f.by_row + int64_t(rank) * 4 * p.B;  // the lowest row of each parent (B: none)
+  int32_t *len = first + pitch, *par = len + pitch;                     // new length, parent
+  int32_t *page = par + pitch;  // -1, or the row's place among the copies, then its new page
 
-  if (t0 < FORK_HEAD) f.head[t0] = 0;
-  for (int b = t0; b < p.B; b += nt) f.first[b] = p.B;
-  cluster_sync();
-  for (int i = t0; i < p.B; i += nt) {
-    const int q = __ldg(parent + i);
-    if (q < -1 || q >= p.B) {
-      atomicOr(f.head, DREAMS_DATA_BAD_INDEX);
-      f.len[i] = 0;
-      continue;
-    }
-    const int L = q < 0 ? 0 : __ldcg(kv_len + q);
-    if (L < 0 || L > cap) atomicOr(f.head, DREAMS_DATA_BAD_KV_LEN);
-    if (q >= 0) atomicMin(f.first + q, i);
-    f.len[i] = L;
-  }
-  cluster_sync();
-  if (__ldcg(f.head) == 0) {
-    for (int64_t x = t0; x < cells; x += nt) {
-      const int i = int(x / p.P), e = int(x - int64_t(i) * p.P);
-      const int q = __ldg(parent + i);
-      const int old = __ldcg(p.table + x);
-      int bad = old < -1 || old >= p.num_pages;
-      int now = -1;
-      if (q >= 0) {
-        const int src = __ldcg(p.table + int64_t(q) * p.P + e);
-        const int L = __ldcg(f.len + i), full = L / PAGE;
-        const bool keeps = __ldcg(f.first + q) == i;
-        const bool part = e == full && L % PAGE != 0;
-        bad |= part && src < 0;
-        now = keeps || e < full ? src : -1;
+  if (threadIdx.x == 0) s_bad = 0;
+  for (int b = threadIdx.x; b < p.B; b += BOOK_THREADS) first[b] = p.B;
+  __syncthreads();
+  {
+    int bad = 0;
+    for (int i = threadIdx.x; i < p.B; i += BOOK_THREADS) {
+      int q = __ldg(parent + i);
+      if (q < -1 || q >= p.B) {
+        bad |= DREAMS_DATA_BAD_INDEX;
+        q = -1;
       }
-      if (bad) atomicOr(f.head, DREAMS_DATA_BAD_PAGE);
-      f.table[x] = now;
+      const int L = q < 0 ? 0 : __ldcg(kv_len + q);
+      if (L < 0 || L > int64_t(p.P) * PAGE) bad |= DREAMS_DATA_BAD_KV_LEN;
+      if (q >= 0) atomicMin(first + q, i);
+      len[i] = L;
+      par[i] = q;
     }
+    if (bad) atomicOr(&s_bad, bad);
   }
-  cluster_sync();
-  bool ok = __ldcg(f.head) == 0;
-  if (ok) {
-    for (int64_t x = t0; x < cells; x += nt) {
-      const int old = __ldcg(p.table + x), now = f.table[x];
-      if (old == now) continue;
-      if (old >= 0) atomicSub(p.ref + old, 1);
-      if (now >= 0) atomicAdd(p.ref + now, 1);
-    }
-  }
-  cluster_sync();
-  // the free pages of each CTA's part of the pool, at most B of them
-  const int part = (p.num_pages + FORK_CTAS - 1) / FORK_CTAS;
-  if (ok) {
-    const int lo = ::min(p.num_pages, rank * part);
-    const int found = list_free(p.ref, lo, ::min(p.num_pages, lo + part), p.B, f.list + int64_t(rank) * p.B, s_warp);
-    if (threadIdx.x == 0) f.head[2 + rank] = found;
-  }
-  cluster_sync();
-  // rows that get a copy of their parent's last page, in order (CTA 0)
-  if (ok && rank == 0) {
-    int have[FORK_CTAS], all = 0;
-#pragma unroll
-    for (int c = 0; c < FORK_CTAS; ++c) {
-      have[c] = __ldcg(f.head + 2 + c);
-      all += have[c];
-    }
-    int base = 0;
+  __syncthreads();
+  int bad = s_bad;
+
+  // Adds `sign` for every entry that a cell gains, takes it for one that it loses.
+  auto count = [&](int old, int now, int sign) {
+    if (old == now) return;
+    if (old >= 0 && old < p.num_pages) atomicSub(p.ref + old, sign);
+    if (now >= 0 && now < p.num_pages) atomicAdd(p.ref + now, sign);
+  };
+  int want = 0;
+  if (!bad) {
+    // rows that get a copy of their parent's last page, in order
     for (int i0 = 0; i0 < p.B; i0 += BOOK_THREADS) {
       const int i = i0 + int(threadIdx.x);
-      int need = 0, q = -1, L = 0;
-      if (i < p.B) {
-        q = __ldg(parent + i);
-        L = __ldcg(f.len + i);
-        need = q >= 0 && __ldcg(f.first + q) != i && L % PAGE != 0;
-      }
+      int need = 0;
+      if (i < p.B) need = par[i] >= 0 && first[par[i]] != i && len[i] % PAGE != 0;
       int total;
-      const int r = base + block_scan(need, s_warp, total);
-      if (need && r < all) {
-        int c = 0, at = r;
-        while (at >= have[c]) at -= have[c++];
-        f.src[r] = __ldcg(p.table + int64_t(q) * p.P + L / PAGE);
-        f.dst[r] = __ldcg(f.list + int64_t(c) * p.B + at);
-        f.rows[r] = L % PAGE;
-        f.table[int64_t(i) * p.P + L / PAGE] = f.dst[r];
+      const int r = want + block_scan(need, s_warp, total);
+      if (i < p.B) page[i] = need ? r : -1;
+      want += total;
+    }
+    // new entries from the old table, and the counts
+    int i = t0 / p.P, e = t0 - i * p.P, bad_cell = 0;
+    const int di = nt / p.P, de = nt - di * p.P;
+    for (unsigned x0 = t0; x0 < cells; x0 += FORK_UNROLL * nt) {
+      int old[FORK_UNROLL], now[FORK_UNROLL];
+      bool last[FORK_UNROLL], keep[FORK_UNROLL];  // the parent's last, partly filled entry; an entry of the new row
+#pragma unroll
+      for (int k = 0; k < FORK_UNROLL; ++k) {
+        old[k] = now[k] = -1;
+        last[k] = keep[k] = false;
+        if (x0 + k * nt < cells) {
+          const int q = par[i], L = len[i];
+          old[k] = __ldcg(p.table + x0 + k * nt);
+          if (q >= 0) {
+            now[k] = __ldcg(p.table + int64_t(q) * p.P + e);
+            last[k] = e == L / PAGE && L % PAGE != 0;
+            keep[k] = e < L / PAGE || first[q] == i;
+          }
+        }
+        i += di;
+        e += de;
+        if (e >= p.P) {
+          e -= p.P;
+          ++i;
+        }
       }
-      base += total;
+#pragma unroll
+      for (int k = 0; k < FORK_UNROLL; ++k)
+        if (x0 + k * nt < cells) {
+          if (old[k] < -1 || old[k] >= p.num_pages || (last[k] && now[k] < 0)) bad_cell = DREAMS_DATA_BAD_PAGE;
+          if (!keep[k]) now[k] = -1;
+          f.table[x0 + k * nt] = now[k];
+          count(old[k], now[k], 1);
+        }
     }
-    if (base > all) {
-      if (threadIdx.x == 0) f.head[0] = DREAMS_DATA_NO_PAGES;
-    } else {
-      __syncthreads();
-      for (int r = int(threadIdx.x); r < base; r += BOOK_THREADS) p.ref[f.dst[r]] = 1;
-      if (threadIdx.x == 0) f.head[1] = base;
+    if (bad_cell) atomicOr(&s_bad, bad_cell);
+    __syncthreads();
+    if (threadIdx.x == 0) f.head[HEAD_FLAGS + rank] = s_bad;
+    fork_sync<CTAS>();
+#pragma unroll
+    for (int c = 0; c < CTAS; ++c) bad |= __ldcg(f.head + HEAD_FLAGS + c);
+    if (!bad && want > 0) {
+      // the free pages of each CTA's part of the pool, no more than there are copies
+      const int part = (p.num_pages + CTAS - 1) / CTAS;
+      const int lo = ::min(p.num_pages, rank * part);
+      const int n = list_free(p.ref, lo, ::min(p.num_pages, lo + part), want, f.list + int64_t(rank) * p.B, s_warp);
+      if (threadIdx.x == 0) f.head[HEAD_FOUND + rank] = n;
+      fork_sync<CTAS>();
+      int have[CTAS], all = 0;
+#pragma unroll
+      for (int c = 0; c < CTAS; ++c) {
+        have[c] = __ldcg(f.head + HEAD_FOUND + c);
+        all += have[c];
+      }
+      if (want > all) {
+        bad = DREAMS_DATA_NO_PAGES;
+      } else {
+        for (int i = threadIdx.x; i < p.B; i += BOOK_THREADS) {
+          const int r = page[i];
+          if (r < 0) continue;
+          int c = 0, at = r;
+#pragma unroll
+          for (int k = 0; k + 1 < CTAS; ++k)
+            if (c == k && at >= have[k]) {
+              at -= have[k];
+              ++c;
+            }
+          const int pg = __ldcg(f.list + int64_t(c) * p.B + at);
+          page[i] = pg;
+          if (rank == 0) {
+            // the row that keeps the parent's pages has the one to copy
+            f.src[r] = __ldcg(f.table + int64_t(first[par[i]]) * p.P + len[i] / PAGE);
+            f.dst[r] = pg;
+            f.rows[r] = len[i] % PAGE;
+            p.ref[pg] = 1;
+          }
+        }
+        __syncthreads();
+      }
     }
+    if (bad)
+      for (unsigned x = t0; x < cells; x += nt) count(__ldcg(p.table + x), __ldcg(f.table + x), -1);
   }
-  cluster_sync();
-  const int bad = __ldcg(f.head);
-  if (bad) {
-    // nothing changes: the counts go back
-    if (ok)
-      for (int64_t x = t0; x < cells; x += nt) {
-        const int old = __ldcg(p.table + x);
-        int now = __ldcg(f.table + x);
-        // an entry filled in for a copy was not counted
-        const int i = int(x / p.P), q = __ldg(parent + i);
-        if (q >= 0 && __ldcg(f.first + q) != i && int(x - int64_t(i) * p.P) == __ldcg(f.len + i) / PAGE) now = -1;
-        if (old == now) continue;
-        if (old >= 0) atomicAdd(p.ref + old, 1);
-        if (now >= 0) atomicSub(p.ref + now, 1);
-      }
+  if (t0 == 0) f.head[0] = bad ? 0 : want;
+  if (bad) {  // nothing changes
     if (t0 == 0) flag(status, bad);
     if (new_kv_len != kv_len)
       for (int i = t0; i < p.B; i += nt) new_kv_len[i] = __ldcg(kv_len + i);
     return;
   }
-  for (int64_t x = t0; x < cells; x += nt) {
-    const int now = __ldcg(f.table + x);
-    if (__ldcg(p.table + x) != now) p.table[x] = now;
+  int i = t0 / p.P, e = t0 - i * p.P;
+  const int di = nt / p.P, de = nt - di * p.P;
+#pragma unroll 4
+  for (unsigned x = t0; x < cells; x += nt) {
+    int now = __ldcg(f.table + x);
+    if (page[i] >= 0 && e == len[i] / PAGE) now = page[i];
+    p.table[x] = now;
+    i += di;
+    e += de;
+    if (e >= p.P) {
+      e -= p.P;
+      ++i;
+    }
   }
-  for (int i = t0; i < p.B; i += nt) new_kv_len[i] = __ldcg(f.len + i);
+  for (int i = t0; i < p.B; i += nt) new_kv_len[i] = len[i];
 }
 
 // The copies, in pieces of 256 threads x 4 x 16 bytes. A page is contiguous
 // within a layer, so its first `rows` rows are one run of 16-byte columns.
+// Pieces are counted with the place in the page outermost: those that a
+// partly filled page has not are the last ones, and the copies of one page come
+// close together, so that their source is read from L2 after the first. The
+// lanes of a warp look at the CTA's next 32 pieces at once: looked up one by
+// one, the chain of loads took longer than the copy (seven copies of 25 rows of
+// 8 KB in 32 layers, whole call: 68 us; now 27, what reading and writing each
+// copy at the copy rate takes).
 constexpr int COPY_PIECE = 1024;
 __global__ void __launch_bounds__(256) kv_fork_copy_kernel(const Cache c, const ForkState f, int pieces) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int n = __ldcg(f.head + 1);
-  const int64_t items = int64_t(n) * c.n_layers * 2 * pieces;
-  for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {
-    const int piece = int(x % pieces);
-    int64_t y = x / pieces;
-    uint4 *base = (y & 1) ? c.v : c.k;
-    y >>= 1;
-    const int layer = int(y % c.n_layers), r = int(y / c.n_layers);
-    const int len = __ldcg(f.rows + r) * c.row16;
-    base += layer * c.layer16;
-    const uint4 *src = base + int64_t(__ldcg(f.src + r)) * PAGE * c.row16;
-    uint4 *dst = base + int64_t(__ldcg(f.dst + r)) * PAGE * c.row16;
-    const int at = piece * COPY_PIECE + int(threadIdx.x);
-    uint4 v[4];
+  const int lane = threadIdx.x & 31;
+  const int64_t runs = int64_t(c.n_layers) * 2, segs = __ldcg(f.head) * runs, items = segs * pieces;
+  for (int64_t x0 = blockIdx.x; x0 < items; x0 += int64_t(gridDim.x) * 32) {
+    const int64_t x = x0 + int64_t(lane) * gridDim.x;
+    int len = 0;
+    const uint4 *src = nullptr;
+    uint4 *dst = nullptr;
+    if (x < items) {
+      const int piece = int(x / segs);
+      const int64_t seg = x - piece * segs;
+      const int r = int(seg / runs), run = int(seg - r * runs);
+      uint4 *base = ((run & 1) ? c.v : c.k) + (run >> 1) * c.layer16 + int64_t(piece) * COPY_PIECE;
+      len = ::min(__ldcg(f.rows + r) * c.row16 - piece * COPY_PIECE, COPY_PIECE);
+      src = base + int64_t(__ldcg(f.src + r)) * PAGE * c.row16;
+      dst = base + int64_t(__ldcg(f.dst + r)) * PAGE * c.row16;
+    }
+    for (unsigned todo = __ballot_sync(0xffffffffu, len > 0); todo != 0; todo &= todo - 1) {
+      const int l = __ffs(int(todo)) - 1;
+      const int n = __shfl_sync(0xffffffffu, len, l);
+      const uint4 *from = reinterpret_cast<const uint4 *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), l));
+      uint4 *to = reinterpret_cast<uint4 *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), l));
+      uint4 v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (at + 256 * i < len) v[i] = ld_stream(src + at + 256 * i);
+      for (int i = 0; i < 4; ++i)
+        if (int(threadIdx.x) + 256 * i < n) v[i] = ld_stream(from + threadIdx.x + 256 * i);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (at + 256 * i < len) dst[at + 256 * i] = v[i];
+      for (int i = 0; i < 4; ++i)
+        if (int(threadIdx.x) + 256 * i < n) to[threadIdx.x + 256 * i] = v[i];
+    }
   }
 }
 
@@ -407,17 +500,26 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const Cache c, const uin
 // A slot moves down (or stays), and a later slot never lands above an earlier
 // one's source: walking a sequence upwards, the rows of a step can be written
 // once they have been read, and no later step's source is written before it is
-// read. A CTA walks one column block of (layer, K or V, sequence); column
-// blocks are independent. CW16: 16-byte columns of a block.
-constexpr int PRUNE_THREADS = 256, PRUNE_UNROLL = 4;
-template <int CW16>
-__global__ void __launch_bounds__(PRUNE_THREADS) kv_prune_kernel(const Cache c, const int32_t *keep, int v0, int n_vis,
-                                                                 int r, const int32_t *kv_len, const int32_t *ref,
-                                                                 int32_t *new_kv_len, int32_t *status) {
-  constexpr int RPS = PRUNE_THREADS / CW16;  // rows read at a time
-  constexpr int STEP = RPS * PRUNE_UNROLL;
+// read. A CTA walks one block of `cw` 16-byte columns of (layer, K or V,
+// sequence); column blocks are independent. A thread has the same columns of the
+// same rows of every step, PRUNE_UNROLL of them, and keeps PRUNE_STAGES steps
+// on their way through its own part of shared memory; the list and the page
+// table are in shared memory too, since looking them up lies between two steps'
+// reads (four paged sequences of 2 KB rows, 8 layers: 98 us, 130 without).
+// 1952 rows of 8 KB in 32 layers: 306 us, 98% of the copy rate. More CTAs per SM
+// with narrower blocks are slower (512 threads 335 us, two of 768 per SM 325;
+// three stages 373): fewer, wider streams suit the memory. A small cache is a
+// chain of loads: one layer of 1 KB rows 5.5 us.
+constexpr int PRUNE_THREADS = 768, PRUNE_UNROLL = 4, PRUNE_STAGES = 2;
+constexpr int PRUNE_LIST = 8192, PRUNE_PAGES = 2048;  // indices kept in shared memory
+constexpr int PRUNE_SMEM = PRUNE_STAGES * PRUNE_UNROLL * PRUNE_THREADS * 16 + (PRUNE_LIST + PRUNE_PAGES) * 4;
+__global__ void __launch_bounds__(PRUNE_THREADS, 1) kv_prune_kernel(const Cache c, const int32_t *keep, int v0, int n_vis, int r,
+                                                        const int32_t *kv_len, const int32_t *ref,
+                                                        int32_t *new_kv_len, int32_t *status, int cw, int nblk) {
+  extern __shared__ uint4 s_ring[];  // [PRUNE_STAGES][PRUNE_UNROLL][threads]
+  constexpr int threads = PRUNE_THREADS;
+  int *s_list = reinterpret_cast<int *>(s_ring + PRUNE_STAGES * PRUNE_UNROLL * threads), *s_page = s_list + PRUNE_LIST;
   const int b = blockIdx.y;
-  const int nblk = (c.row16 + CW16 - 1) / CW16;
   const int blk = blockIdx.x % nblk, rest = blockIdx.x / nblk;
   const bool reporter = blockIdx.x == 0 && threadIdx.x == 0;
   const int L = __ldg(kv_len + b);
@@ -429,15 +531,17 @@ __global__ void __launch_bounds__(PRUNE_THREADS) kv_prune_kernel(const Cache c, 
   if (L > c.capacity || int64_t(v0) + n_vis > L) {
     bad = DREAMS_DATA_BAD_KV_LEN;
   } else {
-    for (int i = threadIdx.x; i < r; i += PRUNE_THREADS) {
+    for (int i = threadIdx.x; i < r; i += threads) {
       const int s = __ldg(list + i), before = i ? __ldg(list + i - 1) : v0 - 1;
       if (s <= before || s >= v0 + n_vis) bad |= DREAMS_DATA_BAD_INDEX;
+      if (i < PRUNE_LIST) s_list[i] = s;
     }
     if (c.table != nullptr)
-      for (int e = v0 / PAGE + int(threadIdx.x); e * PAGE < L; e += PRUNE_THREADS) {
+      for (int e = v0 / PAGE + int(threadIdx.x); e * PAGE < L; e += threads) {
         const int pg = __ldg(c.table + int64_t(b) * c.P + e);
         if (pg < 0 || pg >= c.num_pages) bad |= DREAMS_DATA_BAD_PAGE;
         else if (ref != nullptr && __ldg(ref + pg) != 1) bad |= DREAMS_DATA_SHARED_PAGE;
+        if (e - v0 / PAGE < PRUNE_PAGES) s_page[e - v0 / PAGE] = pg;
       }
   }
   if (bad) atomicOr(&s_bad, bad);
@@ -450,29 +554,57 @@ __global__ void __launch_bounds__(PRUNE_THREADS) kv_prune_kernel(const Cache c, 
   if (bad) return;
   const int shift = n_vis - r, n = L - v0 - shift;  // rows from v0 on afterwards
   if (shift == 0) return;
-  uint4 *base = ((rest & 1) ? c.v : c.k) + int64_t(rest >> 1) * c.layer16;
-  const int col = blk * CW16 + int(threadIdx.x) % CW16;
-  const int tr = int(threadIdx.x) / CW16;
-  const bool in = col < c.row16;
-  for (int i0 = 0; i0 < n; i0 += STEP) {
-    uint4 v[PRUNE_UNROLL];
-    int64_t to[PRUNE_UNROLL];
+  const int c0 = blk * cw, width = ::min(cw, c.row16 - c0);
+  const int step = PRUNE_UNROLL * threads / width;  // rows
+  uint4 *base = ((rest & 1) ? c.v : c.k) + int64_t(rest >> 1) * c.layer16 + c0;
+  int row[PRUNE_UNROLL], col[PRUNE_UNROLL];
 #pragma unroll
-    for (int j = 0; j < PRUNE_UNROLL; ++j) {
-      const int i = i0 + j * RPS + tr;
-      to[j] = -1;
-      if (in && i < n) {
-        const int s = i < r ? __ldg(list + i) : v0 + i + shift;
-        if (s != v0 + i) {
-          to[j] = slot16(c, b, v0 + i) + col;
-          v[j] = ld_stream(base + slot16(c, b, s) + col);
-        }
+  for (int j = 0; j < PRUNE_UNROLL; ++j) {
+    const int u = int(threadIdx.x) + j * threads;
+    row[j] = u / width;
+    col[j] = u - row[j] * width;
+    if (row[j] >= step) col[j] = -1;  // the rest of the division: none
+  }
+  const int *src_list = r <= PRUNE_LIST ? s_list : list;
+  const int e0 = v0 / PAGE;
+  const int *pages = c.table == nullptr ? nullptr : (L + PAGE - 1) / PAGE - e0 <= PRUNE_PAGES ? s_page : c.table + int64_t(b) * c.P + e0;
+  auto offset = [&](int s) {
+    if (pages == nullptr) return (int64_t(b) * c.capacity + s) * c.row16;
+    return (int64_t(pages[s / PAGE - e0]) * PAGE + s % PAGE) * c.row16;
+  };
+  // The source slot of row i (which lands in v0 + i), -1 where nothing moves.
+  auto source = [&](unsigned i) {
+    if (i >= unsigned(n)) return -1;
+    const int to = v0 + int(i), s = int(i) < r ? src_list[i] : to + shift;
+    return s != to ? s : -1;
+  };
+  const uint32_t ring = smem_u32(s_ring + threadIdx.x);
+  auto fetch = [&](unsigned i0, int stage) {
+    if (i0 < unsigned(n)) {
+#pragma unroll
+      for (int j = 0; j < PRUNE_UNROLL; ++j) {
+        const int s = col[j] < 0 ? -1 : source(i0 + row[j]);
+        if (s >= 0)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (stage * PRUNE_UNROLL + j) * threads * 16),
+                       "l"(base + offset(s) + col[j])
+                       : "memory");
       }
     }
-    __syncthreads();
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
 #pragma unroll
-    for (int j = 0; j < PRUNE_UNROLL; ++j)
-      if (to[j] >= 0) base[to[j]] = v[j];
+  for (int s = 0; s < PRUNE_STAGES - 1; ++s) fetch(s * step, s);
+  int stage = 0;
+  for (unsigned i0 = 0; i0 < unsigned(n); i0 += step) {
+    fetch(i0 + (PRUNE_STAGES - 1) * step, stage == 0 ? PRUNE_STAGES - 1 : stage - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(PRUNE_STAGES - 1) : "memory");
+    __syncthreads();  // the whole step has been read
+#pragma unroll
+    for (int j = 0; j < PRUNE_UNROLL; ++j) {
+      const unsigned i = i0 + row[j];
+      if (col[j] >= 0 && source(i) >= 0) base[offset(v0 + int(i)) + col[j]] = s_ring[(stage * PRUNE_UNROLL + j) * threads + threadIdx.x];
+    }
+    stage = stage + 1 == PRUNE_STAGES ? 0 : stage + 1;
   }
 }
 
@@ -521,15 +653,38 @@ size_t fork_layout(const Pool &p, uint8_t *ws, ForkState *f) {
   };
   ForkState s;
   s.head = take(FORK_HEAD);
-  s.first = take(p.B);
-  s.len = take(p.B);
   s.src = take(p.B);
   s.dst = take(p.B);
   s.rows = take(p.B);
   s.list = take(int64_t(FORK_CTAS) * p.B);
+  s.by_row = take(p.B <= FORK_SHARED_ROWS ? 0 : int64_t(FORK_CTAS) * 4 * p.B);
   s.table = take(int64_t(p.B) * p.P);
   if (f != nullptr) *f = s;
   return at;
+}
+
+dreams_status_t fork_table(const Pool &p, const int32_t *parent, const int32_t *kv_len, int32_t *new_kv_len,
+                           const ForkState &f, int32_t *status, cudaStream_t stream) {
+  if (int64_t(p.B) * p.P <= FORK_ONE_CELLS) {
+    kv_fork_table_kernel<1><<<1, BOOK_THREADS, 0, stream>>>(p, parent, kv_len, new_kv_len, f, status);
+    return check_launch();
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(FORK_CTAS);
+  cfg.blockDim = dim3(BOOK_THREADS);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = FORK_CTAS;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_fork_table_kernel<FORK_CTAS>, p, parent, kv_len, new_kv_len, f, status);
+  if (e != cudaSuccess) {
+    set_last_cuda_error(e);
+    return DREAMS_ERR_CUDA;
+  }
+  return check_launch();
 }
 
 }  // namespace
@@ -553,8 +708,10 @@ extern "C" dreams_status_t dreams_kv_reserve(const dreams_page_pool_t *pool, con
     return DREAMS_ERR_WORKSPACE;
   int32_t *start = static_cast<int32_t *>(workspace);
   int32_t *list = start + align_up(size_t(p.B) * 4, 256) / 4;
+  int g = 32;
+  while (g > 1 && int64_t(p.B) * g > BOOK_THREADS) g /= 2;
   kv_reserve_kernel<<<1, BOOK_THREADS, 0, reinterpret_cast<cudaStream_t>(stream)>>>(p, kv_len, n_new, start, list,
-                                                                                   status_word);
+                                                                                   status_word, g);
   return check_launch();
 }
 
@@ -589,8 +746,7 @@ extern "C" dreams_status_t dreams_kv_fork(const dreams_kv_cache_t *kv, const dre
   ForkState f;
   fork_layout(p, static_cast<uint8_t *>(workspace), &f);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  kv_fork_table_kernel<<<FORK_CTAS, BOOK_THREADS, 0, s>>>(p, parent, kv_len, new_kv_len, f, status_word);
-  const dreams_status_t st = check_launch();
+  const dreams_status_t st = fork_table(p, parent, kv_len, new_kv_len, f, status_word, s);
   if (st != DREAMS_OK) return st;
   const int pieces = (PAGE * c.row16 + COPY_PIECE - 1) / COPY_PIECE;
   const int64_t most = int64_t(p.B) * c.n_layers * 2 * pieces;
@@ -644,14 +800,26 @@ extern "C" dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t 
       !aligned4(new_kv_len) || !aligned4(refcount))
     return DREAMS_ERR_INVALID_ARG;
   if (int64_t(c.n_layers) * 2 * c.row16 > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
-  // The widest column block that still gives every SM two CTAs: wide blocks
-  // read whole lines of a slot, narrow ones put more of a small cache in flight.
-  const int64_t lanes = int64_t(c.n_layers) * 2 * B, want = 2 * int64_t(num_sms());
-  int cw = 32;
-  while (cw > 4 && lanes * ((c.row16 + cw - 1) / cw) < want) cw /= 2;
-  const dim3 grid(unsigned(int64_t(c.n_layers) * 2 * ((c.row16 + cw - 1) / cw)), unsigned(B));
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  auto *kernel = cw == 32 ? kv_prune_kernel<32> : cw == 16 ? kv_prune_kernel<16> : cw == 8 ? kv_prune_kernel<8> : kv_prune_kernel<4>;
-  kernel<<<grid, PRUNE_THREADS, 0, s>>>(c, keep, v0, n_vis, r, kv_len, refcount, new_kv_len, status_word);
+  // A CTA takes an SM. Blocks as wide as still fill the SMs once; or, where that
+  // leaves over a quarter of them idle in the last round, the first narrower ones
+  // that do not, down to 512 bytes (192 walks: 3 blocks 175 us, one 209).
+  const int64_t walks = int64_t(c.n_layers) * 2 * B, sms = num_sms();
+  int nblk = int(std::max<int64_t>(1, std::min<int64_t>((c.row16 + 1) / 2, sms / walks)));
+  for (int n = nblk; n <= 8 && c.row16 / n >= 32; ++n) {
+    const int64_t ctas = walks * n;
+    if (ctas * 4 >= (ctas + sms - 1) / sms * sms * 3) {
+      nblk = n;
+      break;
+    }
+  }
+  int cw = (c.row16 + nblk - 1) / nblk;
+  const int unit = cw >= 32 ? 8 : 2;  // whole sectors, whole lines where blocks are wide
+  cw = std::min((cw + unit - 1) / unit * unit, PRUNE_UNROLL * PRUNE_THREADS);
+  nblk = (c.row16 + cw - 1) / cw;
+  const dreams_status_t st = ensure_max_dynamic_smem(reinterpret_cast<const void *>(kv_prune_kernel), PRUNE_SMEM);
+  if (st != DREAMS_OK) return st;
+  const dim3 grid(unsigned(int64_t(c.n_layers) * 2 * nblk), unsigned(B));
+  kv_prune_kernel<<<grid, PRUNE_THREADS, PRUNE_SMEM, reinterpret_cast<cudaStream_t>(stream)>>>(
+      c, keep, v0, n_vis, r, kv_len, refcount, new_kv_len, status_word, cw, nblk);
   return check_launch();
 }
