@@ -566,8 +566,9 @@ dreams_status_t dreams_vocab_argmax_noalloc(const void *logits, dreams_dtype_t d
  * on its own copy or MMA pipeline gives up after a limit instead of hanging
  * the GPU, and this hook lets a test make such a wait run out without any
  * fault. While stall_at >= 0, every later launch of the kernels selected by
- * `kernels` (DREAMS_TEST_ATTENTION: dreams_tree_verify_attn and
- * dreams_attention; DREAMS_TEST_LM_HEAD: dreams_lm_head_argmax) withholds the
+ * `kernels` (DREAMS_TEST_ATTENTION: dreams_tree_verify_attn,
+ * dreams_attention and, for more than 16 rows per KV head,
+ * dreams_window_attention; DREAMS_TEST_LM_HEAD: dreams_lm_head_argmax) withholds the
  * TMA copies of each CTA from its stall_at-th K tile (attention) or k-block
  * (LM head, counted over the CTA's tiles) on, waiting instead on a barrier
  * that nothing arrives on, and every pipeline wait gives up after
