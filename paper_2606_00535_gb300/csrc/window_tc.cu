@@ -1,10 +1,11 @@
 // window_tc.cu -- windowed attention for blocks of 128 query rows on tcgen05
 // tensor cores (prefill, chunks, draft trees).
 //
-// A block is 128 / G tokens times the G query heads of a KV head. Its keys come in
-// tiles of 128: the sinks first, then the window of the block's first query up to
-// its last one, from the 64-slot page the window starts in. The last tile of either
-// run is cut to the columns it needs (a multiple of 32).
+// A block is 128 / G tokens times the G query heads of a KV head. Its keys are a row of
+// 64-slot pages: those of the sinks first, then the window of the block's first query
+// up to its last one. Two pages make a tile; the last one is cut to the columns it
+// needs (a multiple of 32). A few sinks so cost half a tile (as a tile of their own
+// they cost more than a full one: 2500 tokens with window 700 55 us, now 48).
 //
 // One CTA per SM holds two slots of tensor memory (256 columns: S, then P, and O).
 // S = Q K^T and O += P V are tcgen05 groups; a slot's softmax warpgroup, one row per
@@ -26,7 +27,7 @@
 //          For grids too small to fill the SMs with pairs.
 // Warps: 0-3 and 4-7 the softmax of slots 0 and 1, 8 the TMA producer, 9 and 10 the
 // MMA issuers of the slots (one thread each, so that one's waits run under the
-// other's MMAs), 11 the scan (below). A slot's MMAs complete in order, so the commit
+// other's MMAs), 11 the scan (below), which also zeroes the V rows that nobody sees. A slot's MMAs complete in order, so the commit
 // that announces S of a tile also says that the P V before it is done: the softmax
 // warpgroup then gives those stages back, and no further commits are needed.
 // Every mbarrier wait is bounded; a CTA that gives up flags DREAMS_DATA_TIMEOUT,
@@ -38,6 +39,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "tmap.cuh"
 #include "window.cuh"
@@ -79,21 +81,28 @@ struct TcParams {
   uint64_t wait_ns;
 };
 
-// An item: a pair of blocks, or one block, of a sequence and KV head. Tiles are
-// numbered 0 .. n-1, the ns sink tiles first.
+// An item: a pair of blocks, or one block, of a sequence and KV head. Its keys are
+// np half tiles of up to 64 slots, the nsp sink ones first; tile j is the halves
+// 2j and 2j + 1. A key's column is its place in that row of halves.
 struct Item {
   int b, g, L, T;
   int t00, t01, tl0, tl1;  // first and last token of each block
   int nb;                  // blocks present (0: nothing to do)
   int lo, lo64, S1, hi;
-  int ns, n;
+  int nsp, np, ns, n;      // ns: tiles with sinks
   int e0, a1;              // block 0 reads tiles [0, e0), block 1 [0, ns) and [a1, n)
   __device__ __forceinline__ bool need0(int j) const { return j < e0; }
   __device__ __forceinline__ bool need1(int j) const { return nb == 2 && j < n && (j < ns || j >= a1); }
-  __device__ __forceinline__ int slot0(int j) const { return j < ns ? j * KT : lo64 + (j - ns) * KT; }
-  __device__ __forceinline__ int beg(int j) const { return j < ns ? j * KT : ::max(lo, lo64 + (j - ns) * KT); }
-  __device__ __forceinline__ int end(int j) const { return j < ns ? ::min(S1, j * KT + KT) : ::min(hi, lo64 + (j - ns) * KT + KT); }
-  __device__ __forceinline__ int ncols(int j) const { return (end(j) - slot0(j) + 31) & ~31; }
+  __device__ __forceinline__ int slot0(int q) const { return q < nsp ? q * 64 : lo64 + (q - nsp) * 64; }
+  // the slots of half q that a row may see, from its first one on
+  __device__ __forceinline__ int beg(int q) const { return q < nsp ? 0 : ::max(0, lo - slot0(q)); }
+  __device__ __forceinline__ int end(int q) const { return ::min(64, (q < nsp ? S1 : hi) - slot0(q)); }
+  // the first tile of a split, all as long as the last or one longer
+  __device__ __forceinline__ int first_of(int split, int of) const { return split * (n / of) + ::min(split, n % of); }
+  __device__ __forceinline__ bool part(int q) const { return beg(q) > 0 || end(q) < 64; }
+  __device__ __forceinline__ bool cut(int j) const { return part(2 * j) || (2 * j + 1 < np && part(2 * j + 1)); }
+  __device__ __forceinline__ int column(int slot) const { return nsp * 64 + slot - lo64; }  // of the window's run
+  __device__ __forceinline__ int ncols(int j) const { return ::min(KT, (column(hi) - j * KT + 31) & ~31); }
 };
 
 // The tiles that every row of a block sees whole: [0, sink) and [from, to).
@@ -105,7 +114,7 @@ __device__ __forceinline__ Whole whole_tiles(const WinParams &p, const Item &it,
   const int t0 = w ? it.t01 : it.t00, tl = w ? it.tl1 : it.tl0;
   const int from = ::max(it.lo, it.L + tl - p.window + 1) - it.lo64;                              // >= 0
   const int to = ::min(it.hi, p.parent != nullptr ? it.L : it.L + t0 + 1) - it.lo64;
-  return Whole{it.S1 / KT, it.ns + (from + KT - 1) / KT, it.ns + (to > 0 ? to / KT : 0)};
+  return Whole{it.S1 / KT, (it.nsp + (from + 63) / 64 + 1) / 2, (it.nsp + (to > 0 ? to / 64 : 0)) / 2};
 }
 
 template <bool PAIR>
@@ -136,15 +145,19 @@ __device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bo
   it.tl1 = it.nb == 2 ? ::min(it.T, it.t01 + P.TB) - 1 : it.tl0;
   const bool tree = p.parent != nullptr;
   it.lo = ::max(0, it.L + (tree ? 0 : it.t00) - p.window + 1);
+  // with more sinks than slots before the window, all slots are one run
+  const bool one_run = p.sinks > it.lo;
+  if (one_run) it.lo = 0;
+  it.S1 = one_run ? 0 : p.sinks;
   it.lo64 = it.lo & ~63;
-  it.S1 = ::min(p.sinks, it.lo);
-  it.ns = (it.S1 + KT - 1) / KT;
+  it.nsp = (it.S1 + 63) / 64;
+  it.ns = (it.nsp + 1) / 2;
   it.hi = it.L + it.tl1 + 1;
-  it.n = it.ns + (it.hi - it.lo64 + KT - 1) / KT;
-  // with more sinks than slots before the window, the first window tiles hold sinks too
+  it.np = it.nsp + (it.hi - it.lo64 + 63) / 64;
+  it.n = (it.np + 1) / 2;
   const int lo1 = ::max(0, it.L + (tree ? 0 : it.t01) - p.window + 1);
-  it.a1 = p.sinks > it.lo ? it.ns : it.ns + (lo1 - it.lo64) / KT;
-  it.e0 = it.ns + (it.L + it.tl0 - it.lo64) / KT + 1;
+  it.a1 = one_run ? 0 : ::max(it.ns, (it.nsp + (lo1 - it.lo64) / 64) / 2);
+  it.e0 = (it.nsp + (it.L + it.tl0 - it.lo64) / 64) / 2 + 1;
 }
 
 // An arrival by the threads for which `yes` holds, without a branch.
@@ -152,9 +165,17 @@ __device__ __forceinline__ void arrive_if(uint32_t bar, bool yes) {
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %1, 0;\n @p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar), "r"(int(yes)) : "memory");
 }
 
+// What the rows of an item see: columns [0, sinks) and from their window's first one
+// on, in a tree up to those of the new slots, of which a row sees its ancestors.
+struct View {
+  int first, lowest;  // first column of the window at offset 0; no row's is lower
+  int fresh, sinks;   // column of slot L; sinks
+};
+
 // What a softmax warp keeps of an item in shared memory.
-struct Slot {
-  int L, lo, lo64, S1, hi, ns, t0, rows, b, g, first, bad;
+struct __align__(16) Slot {
+  View view;
+  int L, cols, t0, rows, b, g, bad;
 };
 
 // A place in the ring of stages: index and phase.
@@ -232,7 +253,16 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
                : "memory");
   return ok != 0;
 }
+// Waiting for what has happened takes half as long without the hint (135 clocks
+// against 270), and an MMA
+// issuer does it four times a tile.
+__device__ __forceinline__ bool quick(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int *abort, uint64_t limit_ns) {
+  if (quick(bar, parity)) return true;
   uint64_t t0 = 0;
   for (;;) {
     if (try_wait(bar, parity)) return true;
@@ -241,24 +271,21 @@ __device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatil
     if (*abort || now - t0 > limit_ns) return false;
   }
 }
+__device__ __forceinline__ void st_global_v8(void *p, const uint32_t *v) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
 // The low n bits of a word (n may be any integer).
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  uint32_t r;
+  asm("shl.b32 %0, %1, %2;" : "=r"(r) : "r"(0xffffffffu), "r"(::max(n, 0)));  // (a shift by 32 or more leaves nothing)
+  return ~r;
+}
 
 // A query row: its position (less L) and, in a tree, the new slots it sees.
 struct Row {
   int off;
   unsigned long long anc;
-  // the columns it sees among slots base .. base + 31, inside the tile's [beg, end)
-  __device__ __forceinline__ uint32_t word(const WinParams &p, int L, int base, int beg, int end) const {
-    const int phi = p.parent != nullptr ? L : L + off + 1;  // window slots [plow, phi), sinks below
-    const int plow = ::max(0, L + off - p.window + 1);
-    uint32_t m = (low_bits(phi - base) & ~low_bits(plow - base)) | low_bits(::min(p.sinks, phi) - base);
-    if (p.parent != nullptr) {
-      const int sh = base - L;
-      m |= (sh >= 64 || sh <= -32) ? 0u : (sh >= 0 ? uint32_t(anc >> sh) : uint32_t(anc << (-sh)));
-    }
-    return m & low_bits(end - base) & ~low_bits(beg - base);
-  }
 };
 
 // One row by a whole warp, straight from the definition: used when a tile with
@@ -323,7 +350,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   constexpr int NST = C::NST, NR = C::NR;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST];
+  __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST], bar_ready[NST];
   __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_r[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
@@ -336,12 +363,13 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   const uint32_t base = smem_u32(smem);
   auto q_s = [&](int w) { return base + uint32_t(PAIR ? w : 0) * C::Q_BYTES; };
   const uint32_t ring = base + C::NQ * C::Q_BYTES;
-  const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty);
+  const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty), ready0 = smem_u32(bar_ready);
   const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), r0 = smem_u32(bar_r), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
                  o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
   if (tid == TMA_WARP * 32) {
     for (int i = 0; i < NST; ++i) {
       tc::mbar_init(full0 + 8 * i, 1);
+      tc::mbar_init(ready0 + 8 * i, 1);  // the scan
       tc::mbar_init(empty0 + 8 * i, 3);  // both slots, and the scan
     }
     for (int w = 0; w < 2; ++w) {
@@ -392,9 +420,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     while (x_next < P.items) {
       load_item<PAIR>(P, x_next, it, report);
       x_next += PAIR ? int(gridDim.x) : P.items;
-      const int per = (it.n + nsplit - 1) / nsplit;
-      j0 = ::min(it.n, split * per);
-      j1 = ::min(it.n, j0 + per);
+      j0 = it.first_of(split, nsplit);
+      j1 = it.first_of(split + 1, nsplit);
       if (it.nb > 0 && j0 < j1) return true;
     }
     return false;
@@ -448,16 +475,15 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         __syncwarp();  // the last item's readers are done
         if (lane == 0) {
           sp->L = it.L;
-          sp->lo = it.lo;
-          sp->lo64 = it.lo64;
-          sp->S1 = it.S1;
-          sp->hi = it.hi;
-          sp->ns = it.ns;
+          sp->view.first = it.column(it.L - p.window + 1);
+          sp->view.lowest = it.column(it.lo);
+          sp->view.fresh = it.column(it.L);
+          sp->view.sinks = it.nsp > 0 ? it.S1 : p.sinks;
+          sp->cols = it.column(it.hi);
           sp->t0 = t0;
           sp->rows = rows_blk;
           sp->b = it.b;
           sp->g = it.g;
-          sp->first = j;
         }
         int bad = 0;
         if (p.parent != nullptr) {
@@ -509,53 +535,46 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         const bool full = j >= wfrom && j < wto;
         int nc = KT;
         uint32_t mask[4] = {~0u, ~0u, ~0u, ~0u};
+        uint32_t none = 0, part = 0;  // groups of 32 columns that no row of the warp sees; that some see in part
         if (__builtin_expect(!full, 0)) {
-          const int ns = sp->ns, sl = j < ns ? j * KT : sp->lo64 + (j - ns) * KT;
-          int beg = j < ns ? sl : ::max(sp->lo, sl), end = j < ns ? ::min(sp->S1, sl + KT) : ::min(sp->hi, sl + KT);
-          const int L = sp->L;
+          View v;
+          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.first), "=r"(v.lowest), "=r"(v.fresh), "=r"(v.sinks) : "r"(smem_u32(&s_slot[warp].view)));
+          nc = ::min(KT, (sp->cols - j * KT + 31) & ~31);
+          const bool tree = p.parent != nullptr;
+          const int from = ::max(r.off + v.first, v.lowest), to = tree ? v.fresh : v.fresh + r.off + 1, sinks = ::min(v.sinks, to);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) mask[c] = r.word(p, L, sl + 32 * c, beg, end);
-          beg -= sl;
-          end -= sl;
-          nc = (end + 31) & ~31;
-          // slots outside [beg, end) may hold any bits: their V rows become zeros
-          // once the copy has landed (both slots see to it: neither waits for the other)
-          if (live && (beg > 0 || end < nc)) {
-            ok = wait(full0 + 8 * vp.s, vp.ph);
-            if (!__all_sync(0xffffffffu, ok)) {
-              ok = false;
-              break;
+          for (int c = 0; c < 4; ++c) {
+            const int col = j * KT + 32 * c;
+            uint32_t m = low_bits(sinks - col) | (low_bits(to - col) & ~low_bits(from - col));
+            if (tree) {
+              const int sh = col - v.fresh;
+              m |= (sh >= 64 || sh <= -32) ? 0u : (sh >= 0 ? uint32_t(r.anc >> sh) : uint32_t(r.anc << (-sh)));
             }
-            const uint32_t st = ring + uint32_t(vp.s) * C::STAGE;
-            const int n_act = ::min(4, (sp->rows + 31) / 32);  // warps with rows
-#pragma unroll 1
-            for (int i = row; i < (beg + nc - end) * NR * 8; i += 32 * n_act) {
-              const int z = i / (NR * 8), rc = i % (NR * 8);
-              const int rr = z < beg ? z : end + (z - beg);
-              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(st + (rc >> 3) * C::KV_REGION + rr * 128 + ((rc & 7) << 4)),
-                           "r"(0u)
-                           : "memory");
-            }
-            tc::fence_proxy_async_smem();
+            mask[c] = m;
+            none |= uint32_t(!__any_sync(0xffffffffu, m != 0u)) << c;
+            part |= uint32_t(!__all_sync(0xffffffffu, m == ~0u)) << c;
           }
         }
         if (__builtin_expect(unset, 0)) {
-          // references: the maximum of this tile, for rows that have none
+          // references: the maximum of the first 32 columns that hold a key of theirs,
+          // for rows that have none
           if (live) {
-            float mx = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; 32 * c < nc; ++c) {
+            for (int c = 0; 32 * c < nc && unset; ++c) {
               const uint32_t m = c == 0 ? mask[0] : c == 1 ? mask[1] : c == 2 ? mask[2] : mask[3];
-              if (!__any_sync(0xffffffffu, m != 0u)) continue;
+              if ((none >> c) & 1u) continue;
               uint32_t u[32];
+              float mx = -INFINITY;
               tc::tmem_ld32(tl + 32 * c, u);
               tc::tmem_wait_ld();
 #pragma unroll
               for (int e = 0; e < 32; ++e) mx = fmaxf(mx, ((m >> e) & 1u) ? __uint_as_float(u[e]) : -INFINITY);
+              if (m_ref == -INFINITY) m_ref = mx * p.scale_log2;  // scale > 0
+              unset = __any_sync(0xffffffffu, row < sp->rows && m_ref == -INFINITY);
             }
-            if (m_ref == -INFINITY) m_ref = mx * p.scale_log2;  // scale > 0
+          } else {
+            unset = false;
           }
-          unset = __any_sync(0xffffffffu, live && m_ref == -INFINITY);
         }
         const float nmu = m_ref == -INFINITY ? 0.f : -m_ref;
         const uint64_t nmu2 = f32x2(nmu, nmu);
@@ -564,11 +583,12 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
 #pragma unroll 1
         for (int hh = 0; hh < 2; ++hh) {
           uint32_t u[64];
-          if (live && 64 * hh < nc) {
+          const bool some = live && ((none >> (2 * hh)) & 3u) != 3u;  // (columns from nc on are none's)
+          if (some) {
             tc::tmem_ld32(tl + 64 * hh, *reinterpret_cast<uint32_t(*)[32]>(&u[0]));
             tc::tmem_ld32(tl + 64 * hh + 32, *reinterpret_cast<uint32_t(*)[32]>(&u[32]));
             tc::tmem_wait_ld();
-            if (__builtin_expect(!full, 0)) {
+            if (__builtin_expect((part >> (2 * hh)) & 3u, 0)) {
               const uint32_t m0 = hh ? mask[2] : mask[0], m1 = hh ? mask[3] : mask[1];
 #pragma unroll
               for (int e = 0; e < 32; ++e) {
@@ -592,7 +612,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             tc::fence_after_sync();
             arrive_if(empty0 + 8 * v0, lead);
           }
-          if (live && 64 * hh < nc) {
+          if (some) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               uint32_t pk[16];
@@ -606,6 +626,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
               }
               tc::tmem_st16(tl + C::P_COL + 32 * hh + 16 * c, pk);
             }
+            tc::tmem_wait_st();
+          } else if (live && 64 * hh < nc) {
+            const uint32_t zero[16] = {};
+            tc::tmem_st16(tl + C::P_COL + 32 * hh, zero);
+            tc::tmem_st16(tl + C::P_COL + 32 * hh + 16, zero);
             tc::tmem_wait_st();
           }
           tc::fence_before_sync();
@@ -647,16 +672,22 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           const float inv = 1.f / l;
           const int64_t orow = (int64_t(sp->b) * p.T_max + t) * p.Hq + h;
           if (live) {
+            const bool write = real && !((again >> lane) & 1u), wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
+            uint4 *dst = reinterpret_cast<uint4 *>(p.out + orow * D);
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
               uint32_t ov[32];
               tc::tmem_ld32(tl + C::O_COL + c * 32, ov);
               tc::tmem_wait_ld();
-              if (real && !((again >> lane) & 1u)) {
-                uint4 *dst = reinterpret_cast<uint4 *>(p.out + orow * D + c * 32);
-                auto pk = [&](int e) { return pack_bf16x2(__uint_as_float(ov[e]) * inv, __uint_as_float(ov[e + 1]) * inv); };
+              uint32_t pk[16];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) dst[e] = make_uint4(pk(8 * e), pk(8 * e + 2), pk(8 * e + 4), pk(8 * e + 6));
+              for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(__uint_as_float(ov[2 * e]) * inv, __uint_as_float(ov[2 * e + 1]) * inv);
+              if (write && wide) {
+                st_global_v8(dst + 4 * c, pk);
+                st_global_v8(dst + 4 * c + 2, pk + 8);
+              } else if (write) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dst[4 * c + e] = make_uint4(pk[4 * e], pk[4 * e + 1], pk[4 * e + 2], pk[4 * e + 3]);
               }
             }
             if (real && !((again >> lane) & 1u) && p.lse != nullptr) p.lse[orow] = (m_ref + log2f(l)) * LN2;
@@ -695,22 +726,22 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         while (ok && next_item(it, j0, j1, split == 0)) {
           const int32_t *row = p.table != nullptr ? p.table + int64_t(it.b) * p.P : nullptr;
           auto fetch = [&](int j, int h) {
-            if (row == nullptr || j >= j1) return 0;
-            const int pi = (it.slot0(j) >> 6) + h;
+            if (row == nullptr || j >= j1 || 2 * j + h >= it.np) return 0;
+            const int pi = it.slot0(2 * j + h) >> 6;
             return pi < p.P ? __ldg(row + pi) : -1;
           };
           int pg0 = fetch(j0, 0), pg1 = fetch(j0, 1);
           for (int j = j0; j < j1 && ok; ++j) {
-            const int slot = it.slot0(j), halves = it.ncols(j) > 64 ? 2 : 1;
-            // tensor-map coordinate (dim 3) of a 64-slot half: outside the map (zeros)
-            // where the page is missing
+            const int halves = 2 * j + 1 < it.np ? 2 : 1, ha = it.slot0(2 * j), hb = it.slot0(2 * j + 1);
+            // tensor-map coordinate (dim 3) of a half: outside the map (zeros) where the
+            // page is missing
             auto coord = [&](int h, int pg) {
               if (row == nullptr) return it.b;
               if (pg >= 0 && pg < p.num_pages) return pg;
-              if (::max(it.beg(j), slot + 64 * h) < ::min(it.end(j), slot + 64 * h + 64)) flag(p.status, DREAMS_DATA_BAD_PAGE);
+              if (h < halves) flag(p.status, DREAMS_DATA_BAD_PAGE);
               return p.num_pages;
             };
-            const int ca = coord(0, pg0), cb = coord(1, pg1), sa = row != nullptr ? 0 : slot, sb = row != nullptr ? 0 : slot + 64;
+            const int ca = coord(0, pg0), cb = coord(1, pg1), sa = row != nullptr ? 0 : ha, sb = row != nullptr ? 0 : hb;
             pg0 = fetch(j + 1, 0);
             pg1 = fetch(j + 1, 1);
 #pragma unroll 1
@@ -824,7 +855,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             const Pos vp = kp.plus(1);
             pos = kp.plus(2);
             // what the copies bring is waited for ahead of P
-            ok = wait(full0 + 8 * vp.s, vp.ph);
+            ok = wait((it.cut(j) ? ready0 : full0) + 8 * vp.s, vp.ph);
             if ((C::BESIDE || PAIR) && ok && nj < j1) {
               skip(j + 1, nj);
               ok = ok && wait(full0 + 8 * pos.s, pos.ph);
@@ -889,20 +920,41 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           for (int kv = 0; kv < 2; ++kv) {
             ok = __all_sync(0xffffffffu, wait(full0 + 8 * at.s, at.ph));
             if (!ok) break;
+            const uint32_t st = ring + uint32_t(at.s) * C::STAGE + ((lane & 7) << 4);
+            const int halves = 2 * j + 1 < it.np ? 2 : 1;
+            if (kv == 1) {
+              // lanes along a row's 128 bytes, four rows at a time; slots that no row
+              // sees may hold any bits: their V rows become zeros
+              bool cut = false;
+              for (int h = 0; h < halves; ++h) {
+                const int b0 = it.beg(2 * j + h), e0 = it.end(2 * j + h);
+                cut |= b0 > 0 || e0 < 64;
+#pragma unroll 1
+                for (int z = lane >> 3; z < b0 + 64 - e0; z += 4) {
+                  const int rr = 64 * h + (z < b0 ? z : e0 + z - b0);
+#pragma unroll
+                  for (int r = 0; r < NR; ++r)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(st + r * C::KV_REGION + rr * 128), "r"(0u) : "memory");
+                }
+              }
+              if (cut) tc::fence_proxy_async_smem();
+            }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(ready0 + 8 * at.s);
             if (kv == 1 && look) {
-              // lanes along a row's 128 bytes, four rows at a time
-              const int s = it.slot0(j), r0 = it.beg(j) - s, r1 = it.end(j) - s;
-              const uint32_t st = ring + uint32_t(at.s) * C::STAGE + ((lane & 7) << 4);
+              for (int h = 0; h < halves; ++h) {
+                const int r1 = 64 * h + it.end(2 * j + h);
 #pragma unroll 4
-              for (int rr = r0 + (lane >> 3); rr < r1; rr += 4) {
+                for (int rr = 64 * h + it.beg(2 * j + h) + (lane >> 3); rr < r1; rr += 4) {
 #pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                  uint32_t u[4];
-                  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
-                               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                               : "r"(st + r * C::KV_REGION + rr * 128));
+                  for (int r = 0; r < NR; ++r) {
+                    uint32_t u[4];
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                                 : "r"(st + r * C::KV_REGION + rr * 128));
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(u[e]), "r"(0u));
+                    for (int e = 0; e < 4; ++e) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(u[e]), "r"(0u));
+                  }
                 }
               }
             }
@@ -930,7 +982,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     x_next = int(blockIdx.x) / nsplit;
     Item it;
     load_item<PAIR>(P, x_next, it, false);
-    const int per = (it.n + nsplit - 1) / nsplit, j0 = ::min(it.n, split * per), m = ::min(it.n, j0 + per) - j0;
+    const int m = it.first_of(split + 1, nsplit) - it.first_of(split, nsplit);
     const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
     constexpr int CH = D / 4;  // 16-byte columns of a part's row, swizzled by the row
     float *part = reinterpret_cast<float *>(smem + C::NQ * C::Q_BYTES);
@@ -968,7 +1020,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     }
     const bool gave_up = __any_sync(0xffffffffu, state & 1), again = __any_sync(0xffffffffu, state & 2);
     const bool first_has = m > 0;  // (a CTA without tiles has no row descriptions: it joins nothing)
-    const int joiners = it.n > 0 ? ::min(nsplit, (it.n + per - 1) / ::max(1, per)) : 1;
+    const int joiners = ::max(1, ::min(nsplit, it.n));
     if (!gave_up && first_has && warp < 8) {
       for (int row = split * 8 + warp; row < rows_blk; row += joiners * 8) {
         const int off = s_row[row].off, t = s_row[row].t;
@@ -1073,6 +1125,36 @@ dreams_status_t launch(TcParams &P, cudaStream_t stream) {
   return check_launch();
 }
 
+// How many clusters of ns CTAs the current device runs at once (asked once per
+// device); 0: none, or not known.
+template <int D>
+int clusters_at_once(int ns) {
+  static std::atomic<int> known[64][9];  // count + 1
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 0;
+  int n = known[dev][ns].load(std::memory_order_relaxed);
+  if (n == 0) {
+    const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, false>);
+    if (ensure_max_dynamic_smem(kernel, int(Cfg<D, false>::SMEM)) != DREAMS_OK) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(ns));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = Cfg<D, false>::SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(ns);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    known[dev][ns].store(++n, std::memory_order_relaxed);
+  }
+  return n - 1;
+}
+
 }  // namespace
 
 dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaStream_t stream) {
@@ -1083,19 +1165,25 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   const int64_t heads = int64_t(p.B) * p.Hkv;
   const int64_t blocks = (int64_t(p.T_max) + P.TB - 1) / P.TB, pairs = (blocks + 1) / 2;
   test_stall(DREAMS_TEST_ATTENTION, &P.stall_at, &P.wait_ns);
-  // Tiles of a block, and the time of either layout in tiles: a pair of tiles
-  // costs about as much as two tiles of one block, and an item's start and end
-  // about six tiles (the pairs' mostly overlap).
+  // Columns of a block (its keys begin anywhere in a page), and the time of either
+  // layout in tenths of a microsecond, from sweeps of both over 5 to 33 tiles and 8 to
+  // 448 blocks: a CTA of a block takes 13.5
+  // us and 1.5 (head dim 64: 1.3) a tile, a round of them after the other; a pair of
+  // blocks 2 (1.6) a tile, 3 to change items and 4 once. 17 tiles: trees of 16
+  // sequences, 128 pairs 45 us, 256 blocks 83; 9 tiles: a tree's 32 blocks 22 us, over
+  // clusters of 4 15.6.
   const int64_t sms = num_sms();
-  const int64_t tiles = std::max<int64_t>(
-      1, (std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB)) + KT - 1) / KT + (p.sinks > 0 ? 1 : 0));
-  auto waves = [&](int64_t n) { return (n + sms - 1) / sms; };
-  const int64_t pair_cost = blocks > 1 ? waves(heads * pairs) * (2 * tiles + 2) + 4 : INT64_MAX;
+  const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB));
+  const int64_t cols = keys + 63 + (std::min<int64_t>(p.capacity, p.sinks) + 63) / 64 * 64 + 32;
+  const int64_t per_one = kv->D == 128 ? 15 : 13, per_pair = kv->D == 128 ? 20 : 16;
+  auto rounds = [](int64_t n, int64_t fit) { return (n + fit - 1) / fit; };
+  const int64_t pair_cost = blocks > 1 ? rounds(heads * pairs, sms) * (per_pair * cols / KT + 30) + 40 : INT64_MAX;
   int64_t best = INT64_MAX;
   int nsplit = 1;
-  for (int ns = 1; ns <= 8; ns *= 2) {
-    if (ns > 1 && tiles < 2 * ns) break;
-    const int64_t cost = waves(heads * blocks * ns) * ((tiles + ns - 1) / ns + 6);
+  for (int ns = 1; ns <= 8 && (ns == 1 || (ns * KT <= cols && heads * blocks * ns <= sms)); ++ns) {
+    const int64_t fit = ns == 1 ? sms : kv->D == 128 ? clusters_at_once<128>(ns) : clusters_at_once<64>(ns);
+    if (fit < 1) continue;
+    const int64_t cost = rounds(heads * blocks, fit) * (135 + per_one * (cols + (ns - 1) * KT / 2) / (ns * KT));
     if (cost < best) {
       best = cost;
       nsplit = ns;
