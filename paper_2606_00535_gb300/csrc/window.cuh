@@ -46,12 +46,14 @@ __device__ __forceinline__ KeyList key_list(const WinParams &p, int L, int t_fir
 // walk from the node to the root over a checked parent array.
 template <typename I>
 __device__ __forceinline__ unsigned long long tree_row(const WinParams &p, const I *par, int L, int t, int &depth) {
-  depth = 0;
-  for (int a = t; a > 0; a = par[a]) ++depth;
+  depth = -1;
   unsigned long long m = 0ull;
-  int da = depth;
-  for (int a = t; a >= 0; a = par[a], --da)
-    if (depth - da < p.window || int64_t(L) + da < p.sinks) m |= 1ull << a;
+  for (int a = t; a >= 0; a = par[a], ++depth) m |= 1ull << a;
+  if (depth >= p.window) {  // ancestors that the window has left behind
+    int da = depth;
+    for (int a = t; a >= 0; a = par[a], --da)
+      if (depth - da >= p.window && int64_t(L) + da >= p.sinks) m &= ~(1ull << a);
+  }
   return m;
 }
 

@@ -97,8 +97,12 @@ struct Item {
   // the slots of half q that a row may see, from its first one on
   __device__ __forceinline__ int beg(int q) const { return q < nsp ? 0 : ::max(0, lo - slot0(q)); }
   __device__ __forceinline__ int end(int q) const { return ::min(64, (q < nsp ? S1 : hi) - slot0(q)); }
-  // the first tile of a split, all as long as the last or one longer
-  __device__ __forceinline__ int first_of(int split, int of) const { return split * (n / of) + ::min(split, n % of); }
+  // the first tile of a split; some are one longer, the first one last (it has the
+  // tile with the sinks), but the first splits are those with tiles
+  __device__ __forceinline__ int first_of(int split, int of) const {
+    const int q = n / of;
+    return split * q + ::min(q > 0 ? ::max(split - 1, 0) : split, n % of);
+  }
   __device__ __forceinline__ bool part(int q) const { return beg(q) > 0 || end(q) < 64; }
   __device__ __forceinline__ bool cut(int j) const { return part(2 * j) || (2 * j + 1 < np && part(2 * j + 1)); }
   __device__ __forceinline__ int column(int slot) const { return nsp * 64 + slot - lo64; }  // of the window's run
@@ -118,15 +122,15 @@ __device__ __forceinline__ Whole whole_tiles(const WinParams &p, const Item &it,
 }
 
 template <bool PAIR>
-__device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bool report) {
+__device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bool report, const int2 *lens = nullptr) {
   const WinParams &p = P.p;
   // the last blocks first (they have the most keys), all heads of a block together
   const int heads = p.B * p.Hkv;
   const int blk = P.nblk - 1 - x / heads, bg = x % heads;
   it.b = bg / p.Hkv;
   it.g = bg - it.b * p.Hkv;
-  it.T = __ldg(p.q_len + it.b);
-  it.L = __ldg(p.kv_len + it.b);
+  it.T = lens != nullptr ? lens->x : __ldg(p.q_len + it.b);
+  it.L = lens != nullptr ? lens->y : __ldg(p.kv_len + it.b);
   it.nb = it.n = it.ns = 0;
   report = report && it.g == 0 && blk == 0;
   if (it.T < 0 || it.T > p.T_max) {
@@ -366,6 +370,18 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty), ready0 = smem_u32(bar_ready);
   const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), r0 = smem_u32(bar_r), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
                  o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
+  // Without PAIR the item is known: its lengths and parents are on their way early.
+  int2 lens = make_int2(0, 0);
+  int early[2] = {-1, -1};
+  if constexpr (!PAIR) {
+    const int b = (int(blockIdx.x) / p.nsplit) % (p.B * p.Hkv) / p.Hkv;
+    lens = make_int2(__ldg(p.q_len + b), __ldg(p.kv_len + b));
+    if (p.parent != nullptr && warp < 8) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (lane + 32 * k < p.T_max) early[k] = __ldg(p.parent + int64_t(b) * p.T_max + lane + 32 * k);
+    }
+  }
   if (tid == TMA_WARP * 32) {
     for (int i = 0; i < NST; ++i) {
       tc::mbar_init(full0 + 8 * i, 1);
@@ -418,7 +434,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   // the next item with work, and the tiles [j0, j1) of it that are this CTA's
   auto next_item = [&](Item &it, int &j0, int &j1, bool report) {
     while (x_next < P.items) {
-      load_item<PAIR>(P, x_next, it, report);
+      load_item<PAIR>(P, x_next, it, report, PAIR ? nullptr : &lens);
       x_next += PAIR ? int(gridDim.x) : P.items;
       j0 = it.first_of(split, nsplit);
       j1 = it.first_of(split + 1, nsplit);
@@ -488,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         int bad = 0;
         if (p.parent != nullptr) {
           for (int i = lane; i < it.T; i += 32) {
-            const int q = __ldg(p.parent + int64_t(it.b) * p.T_max + i);
+            const int q = PAIR ? __ldg(p.parent + int64_t(it.b) * p.T_max + i) : i < 32 ? early[0] : early[1];
             s_par[warp][i] = int8_t(q);  // (a bad one is not used)
             bad |= i == 0 ? q != -1 : (q < 0 || q >= i);
           }
@@ -981,7 +997,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     // ---------------- join the slots' and the splits' parts
     x_next = int(blockIdx.x) / nsplit;
     Item it;
-    load_item<PAIR>(P, x_next, it, false);
+    load_item<PAIR>(P, x_next, it, false, &lens);
     const int m = it.first_of(split + 1, nsplit) - it.first_of(split, nsplit);
     const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
     constexpr int CH = D / 4;  // 16-byte columns of a part's row, swizzled by the row
@@ -1021,16 +1037,34 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     const bool gave_up = __any_sync(0xffffffffu, state & 1), again = __any_sync(0xffffffffu, state & 2);
     const bool first_has = m > 0;  // (a CTA without tiles has no row descriptions: it joins nothing)
     const int joiners = ::max(1, ::min(nsplit, it.n));
-    if (!gave_up && first_has && warp < 8) {
-      for (int row = split * 8 + warp; row < rows_blk; row += joiners * 8) {
+    if (!gave_up && first_has) {
+      constexpr int WARPS = THREADS / 32, AHEAD = 8;
+      auto sums = [&](int row) {
+        return row < rows_blk && lane < parts ? ld_cluster2(mapa(ml_a + ((lane & 1) * ROWS + row) * 8, lane >> 1)) : make_float2(-INFINITY, 0.f);
+      };
+      float2 next = sums(split * WARPS + warp);
+      for (int row = split * WARPS + warp; row < rows_blk; row += joiners * WARPS) {
+        const float2 ml = next;
+        next = sums(row + joiners * WARPS);
         const int off = s_row[row].off, t = s_row[row].t;
         if (off < 0) continue;  // a malformed tree
         const int h = it.g * p.G + row - (t - it.t00) * p.G;
-        const float2 ml = lane < parts ? ld_cluster2(mapa(ml_a + ((lane & 1) * ROWS + row) * 8, lane >> 1)) : make_float2(-INFINITY, 0.f);
         if (again || __any_sync(0xffffffffu, ml.y > MOST_SUM)) {
           slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc);
           continue;
         }
+        const uint32_t some = __ballot_sync(0xffffffffu, ml.y != 0.f);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f), v[AHEAD];
+        auto fetch = [&](int i0) {  // parts of other CTAs take a while: many at once
+#pragma unroll
+          for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k;
+            v[k] = ((some >> i) & 1u) && lane < CH
+                       ? ld_cluster4(mapa(part_a + (((i & 1) * ROWS + row) * D + ((lane ^ (row & (CH - 1))) << 2)) * 4, i >> 1))
+                       : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+        };
+        fetch(0);
         float M = ml.x;
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
@@ -1038,17 +1072,15 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         float Z = ml.y == 0.f ? 0.f : c * ml.y;
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) Z += __shfl_xor_sync(0xffffffffu, Z, k);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        const bool some = ml.y != 0.f;
-        for (int i = 0; i < parts; ++i) {
-          if (!__shfl_sync(0xffffffffu, int(some), i)) continue;
-          const float ci = __shfl_sync(0xffffffffu, c, i);
-          if (lane < CH) {
-            const float4 v = ld_cluster4(mapa(part_a + (((i & 1) * ROWS + row) * D + ((lane ^ (row & (CH - 1))) << 2)) * 4, i >> 1));
-            acc.x += ci * v.x;
-            acc.y += ci * v.y;
-            acc.z += ci * v.z;
-            acc.w += ci * v.w;
+        for (int i0 = 0; i0 < parts; i0 += AHEAD) {
+          if (i0 > 0) fetch(i0);
+#pragma unroll
+          for (int k = 0; k < AHEAD; ++k) {
+            const float ci = __shfl_sync(0xffffffffu, c, i0 + k);
+            acc.x += ci * v[k].x;
+            acc.y += ci * v[k].y;
+            acc.z += ci * v[k].z;
+            acc.w += ci * v[k].w;
           }
         }
         const float inv = 1.f / Z;
@@ -1171,7 +1203,7 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   // us and 1.5 (head dim 64: 1.3) a tile, a round of them after the other; a pair of
   // blocks 2 (1.6) a tile, 3 to change items and 4 once. 17 tiles: trees of 16
   // sequences, 128 pairs 45 us, 256 blocks 83; 9 tiles: a tree's 32 blocks 22 us, over
-  // clusters of 4 15.6.
+  // clusters of 4 13.7.
   const int64_t sms = num_sms();
   const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB));
   const int64_t cols = keys + 63 + (std::min<int64_t>(p.capacity, p.sinks) + 63) / 64 * 64 + 32;
