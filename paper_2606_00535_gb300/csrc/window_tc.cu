@@ -1199,11 +1199,10 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   test_stall(DREAMS_TEST_ATTENTION, &P.stall_at, &P.wait_ns);
   // Columns of a block (its keys begin anywhere in a page), and the time of either
   // layout in tenths of a microsecond, from sweeps of both over 5 to 33 tiles and 8 to
-  // 448 blocks: a CTA of a block takes 13.5
-  // us and 1.5 (head dim 64: 1.3) a tile, a round of them after the other; a pair of
-  // blocks 2 (1.6) a tile, 3 to change items and 4 once. 17 tiles: trees of 16
-  // sequences, 128 pairs 45 us, 256 blocks 83; 9 tiles: a tree's 32 blocks 22 us, over
-  // clusters of 4 13.7.
+  // 448 blocks: a CTA of a block takes 13.5 us and 1.5 (head dim 64: 1.3) a tile, a
+  // round of them after the other; a pair of blocks 2 (1.6) a tile, 3 to change items
+  // and 4 once. 17 tiles: trees of 16 sequences, 128 pairs 45 us, 256 blocks 83; 9
+  // tiles: a tree's 32 blocks 22 us, over clusters of 4 13.7.
   const int64_t sms = num_sms();
   const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB));
   const int64_t cols = keys + 63 + (std::min<int64_t>(p.capacity, p.sinks) + 63) / 64 * 64 + 32;
