@@ -228,19 +228,14 @@ constexpr int HEAD_FLAGS = 1, HEAD_FOUND = HEAD_FLAGS + FORK_CTAS, FORK_HEAD = H
 constexpr int FORK_SHARED_ROWS = 2048, FORK_UNROLL = 4;
 // One CTA for tables of up to so many entries: its barriers are cheaper; eight
 // keep more loads in flight. (Whole call with copies of next to nothing: 448
-// entries 7.5 us against 9.4, 544 8.5 against 10.6; 12288 14.7 against 11.6.)
+// entries 6.7 us against 9.4, 544 6.9 against 10.6; 12288 14.7 against 11.1.)
 constexpr int FORK_ONE_CELLS = 4096;
 
-template <int CTAS>
-__device__ __forceinline__ void fork_sync() {
-  if (CTAS == 1) {
-    __syncthreads();
-  } else {
-    // (Not the .aligned forms: warps come here from loops that their lanes left
-    // at different turns.)
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-  }
+// (Not the .aligned forms: warps come here from loops that their lanes left at
+// different turns.)
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // The new table, counts and lengths, and the list of pages to copy. A chain of
@@ -254,7 +249,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
                          const ForkState f, int32_t *status) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __shared__ int s_warp[32], s_bad;
-  __shared__ int32_t s_rows[4 * FORK_SHARED_ROWS];
+  __shared__ int32_t s_rows[4 * FORK_SHARED_ROWS], s_list[CTAS == 1 ? FORK_SHARED_ROWS : 1];
   const int rank = CTAS == 1 ? 0 : int(blockIdx.x);
   const int t0 = rank * BOOK_THREADS + int(threadIdx.x);
   constexpr int nt = CTAS * BOOK_THREADS;
@@ -342,22 +337,32 @@ __global__ void __launch_bounds__(BOOK_THREADS)
     }
     if (bad_cell) atomicOr(&s_bad, bad_cell);
     __syncthreads();
-    if (threadIdx.x == 0) f.head[HEAD_FLAGS + rank] = s_bad;
-    fork_sync<CTAS>();
+    if (CTAS == 1) {
+      bad = s_bad;
+    } else {
+      if (threadIdx.x == 0) f.head[HEAD_FLAGS + rank] = s_bad;
+      cluster_sync();
 #pragma unroll
-    for (int c = 0; c < CTAS; ++c) bad |= __ldcg(f.head + HEAD_FLAGS + c);
+      for (int c = 0; c < CTAS; ++c) bad |= __ldcg(f.head + HEAD_FLAGS + c);
+    }
     if (!bad && want > 0) {
       // the free pages of each CTA's part of the pool, no more than there are copies
       const int part = (p.num_pages + CTAS - 1) / CTAS;
       const int lo = ::min(p.num_pages, rank * part);
-      const int n = list_free(p.ref, lo, ::min(p.num_pages, lo + part), want, f.list + int64_t(rank) * p.B, s_warp);
-      if (threadIdx.x == 0) f.head[HEAD_FOUND + rank] = n;
-      fork_sync<CTAS>();
+      int32_t *list = CTAS == 1 && near ? s_list : f.list + int64_t(rank) * p.B;
+      const int n = list_free(p.ref, lo, ::min(p.num_pages, lo + part), want, list, s_warp);
       int have[CTAS], all = 0;
+      if (CTAS == 1) {
+        have[0] = all = n;
+        __syncthreads();
+      } else {
+        if (threadIdx.x == 0) f.head[HEAD_FOUND + rank] = n;
+        cluster_sync();
 #pragma unroll
-      for (int c = 0; c < CTAS; ++c) {
-        have[c] = __ldcg(f.head + HEAD_FOUND + c);
-        all += have[c];
+        for (int c = 0; c < CTAS; ++c) {
+          have[c] = __ldcg(f.head + HEAD_FOUND + c);
+          all += have[c];
+        }
       }
       if (want > all) {
         bad = DREAMS_DATA_NO_PAGES;
@@ -372,7 +377,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
               at -= have[k];
               ++c;
             }
-          const int pg = __ldcg(f.list + int64_t(c) * p.B + at);
+          const int pg = CTAS == 1 ? list[at] : __ldcg(f.list + int64_t(c) * p.B + at);
           page[i] = pg;
           if (rank == 0) {
             // the row that keeps the parent's pages has the one to copy
