@@ -290,3 +290,21 @@ def test_data_flags(dreams):
             out, lse = c.run(dreams, want=dreams.DATA_BAD_PAGE)
             c.B = 1  # the other sequence is whole
             c.check((out[:1], lse[:1]))
+
+
+@pytest.mark.parametrize("sinks", [63, 64, 65, 127, 128, 129, 191, 300, 500])
+@pytest.mark.parametrize("window,kind", [(50, "chunk"), (129, "chunk"), (64, "tree"), (201, "tree")])
+def test_sinks_around_page_ends(dreams, sinks, window, kind):
+    """Sinks and window meet inside a tile of two pages, at its end, and overlap."""
+    c = Case(3 * sinks + window, 8, 2, 128 if sinks % 2 else 64, [450, 700, 90], [130, 33, 140] if kind == "chunk" else [60, 33, 64], window, sinks,
+             tree=kind == "tree", paged=sinks % 3 == 0)
+    c.check(c.run(dreams), n=30)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(28, 4, 128), (16, 1, 64), (32, 8, 128), (20, 10, 64), (32, 32, 128)])
+@pytest.mark.parametrize("window", [90, 400, 1100, 2500])
+def test_one_sequence_over_clusters(dreams, Hq, Hkv, D, window):
+    """A few blocks of one sequence, their tiles split over clusters of every size, some with fewer tiles than CTAs."""
+    for T, tree in ((64, True), (70, False)):
+        c = Case(Hq + window, Hq, Hkv, D, [2600], [T], window, 3, tree=tree, paged=tree)
+        c.check(c.run(dreams), n=40)
