@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(PRUNE_THREADS, 1) kv_prune_kernel(const Cache 
       if (i < PRUNE_LIST) s_list[i] = s;
     }
     if (c.table != nullptr)
-      for (int e = v0 / PAGE + int(threadIdx.x); e * PAGE < L; e += threads) {
+      for (int e = v0 / PAGE + int(threadIdx.x); int64_t(e) * PAGE < L; e += threads) {
         const int pg = __ldg(c.table + int64_t(b) * c.P + e);
         if (pg < 0 || pg >= c.num_pages) bad |= DREAMS_DATA_BAD_PAGE;
         else if (ref != nullptr && __ldg(ref + pg) != 1) bad |= DREAMS_DATA_SHARED_PAGE;
