@@ -71,12 +71,26 @@ struct Cfg {
   static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + 1024, 120 * 1024);
 };
 
+// Division of x in [0, 2^31) by a divisor that the host knows: x m >> (31 + s) with
+// s = ceil(log2 d), m = ceil(2^(31 + s) / d), which is exact (x (m d - 2^(31 + s)) <
+// 2^(31 + s)). The division instructions of an item's set-up took half a microsecond.
+struct Divisor {
+  uint32_t d, m, s;
+  static Divisor of(int64_t d) {
+    uint32_t s = 0;
+    while ((int64_t(1) << s) < d) ++s;
+    return Divisor{uint32_t(d), uint32_t(((uint64_t(1) << (31 + s)) + uint64_t(d) - 1) / uint64_t(d)), s};
+  }
+  __device__ __forceinline__ int div(int x) const { return int((uint64_t(uint32_t(x)) * m) >> (31 + s)); }
+};
+
 struct TcParams {
   CUtensorMap tmap_q, tmap_k, tmap_v;
   WinParams p;
   int32_t TB;      // tokens of a block
   int32_t nblk;    // blocks (or pairs) per sequence and KV head
   int32_t items;   // B * Hkv * nblk
+  Divisor heads, hkv, nsplit, g;  // B * Hkv, Hkv, CTAs of a cluster, query heads per KV head
   int32_t stall_at;
   uint64_t wait_ns;
 };
@@ -97,16 +111,18 @@ struct Item {
   // the slots of half q that a row may see, from its first one on
   __device__ __forceinline__ int beg(int q) const { return q < nsp ? 0 : ::max(0, lo - slot0(q)); }
   __device__ __forceinline__ int end(int q) const { return ::min(64, (q < nsp ? S1 : hi) - slot0(q)); }
-  // the first tile of a split; some are one longer, the first one last (it has the
-  // tile with the sinks), but the first splits are those with tiles
-  __device__ __forceinline__ int first_of(int split, int of) const {
-    const int q = n / of;
-    return split * q + ::min(q > 0 ? ::max(split - 1, 0) : split, n % of);
-  }
   __device__ __forceinline__ bool part(int q) const { return beg(q) > 0 || end(q) < 64; }
   __device__ __forceinline__ bool cut(int j) const { return part(2 * j) || (2 * j + 1 < np && part(2 * j + 1)); }
   __device__ __forceinline__ int column(int slot) const { return nsp * 64 + slot - lo64; }  // of the window's run
   __device__ __forceinline__ int ncols(int j) const { return ::min(KT, (column(hi) - j * KT + 31) & ~31); }
+};
+
+// The first tile of each split; some are one longer, the first one last (it has the tile
+// with the sinks), but the first splits are those with tiles.
+struct Splits {
+  int each, longer;
+  __device__ __forceinline__ Splits(int n, const Divisor &of) : each(of.div(n)), longer(n - each * int(of.d)) {}
+  __device__ __forceinline__ int first(int split) const { return split * each + ::min(each > 0 ? ::max(split - 1, 0) : split, longer); }
 };
 
 // The tiles that every row of a block sees whole: [0, sink) and [from, to).
@@ -125,9 +141,8 @@ template <bool PAIR>
 __device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bool report, const int2 *lens = nullptr) {
   const WinParams &p = P.p;
   // the last blocks first (they have the most keys), all heads of a block together
-  const int heads = p.B * p.Hkv;
-  const int blk = P.nblk - 1 - x / heads, bg = x % heads;
-  it.b = bg / p.Hkv;
+  const int turn = P.heads.div(x), blk = P.nblk - 1 - turn, bg = x - turn * int(P.heads.d);
+  it.b = P.hkv.div(bg);
   it.g = bg - it.b * p.Hkv;
   it.T = lens != nullptr ? lens->x : __ldg(p.q_len + it.b);
   it.L = lens != nullptr ? lens->y : __ldg(p.kv_len + it.b);
@@ -374,7 +389,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   int2 lens = make_int2(0, 0);
   int early[2] = {-1, -1};
   if constexpr (!PAIR) {
-    const int b = (int(blockIdx.x) / p.nsplit) % (p.B * p.Hkv) / p.Hkv;
+    const int x = P.nsplit.div(int(blockIdx.x)), b = P.hkv.div(x - P.heads.div(x) * int(P.heads.d));
     lens = make_int2(__ldg(p.q_len + b), __ldg(p.kv_len + b));
     if (p.parent != nullptr && warp < 8) {
 #pragma unroll
@@ -382,13 +397,18 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         if (lane + 32 * k < p.T_max) early[k] = __ldg(p.parent + int64_t(b) * p.T_max + lane + 32 * k);
     }
   }
-  if (tid == TMA_WARP * 32) {
-    for (int i = 0; i < NST; ++i) {
-      tc::mbar_init(full0 + 8 * i, 1);
-      tc::mbar_init(ready0 + 8 * i, 1);  // the scan
-      tc::mbar_init(empty0 + 8 * i, 3);  // both slots, and the scan
+  if (warp == TMA_WARP) {
+    if (lane < NST) {
+      tc::mbar_init(full0 + 8 * lane, 1);
+      tc::mbar_init(ready0 + 8 * lane, 1);  // the scan
+      tc::mbar_init(empty0 + 8 * lane, 3);  // both slots, and the scan
     }
-    for (int w = 0; w < 2; ++w) {
+    if (lane < SEEN) {
+      s_dirty[lane] = 0;
+      tc::mbar_init(scan0 + 8 * lane, 1);
+    }
+    if (lane >= 16 && lane < 18) {
+      const int w = lane - 16;
       tc::mbar_init(qf0 + 8 * w, 1);
       tc::mbar_init(qe0 + 8 * w, 1);
       tc::mbar_init(s0 + 8 * w, 1);
@@ -398,16 +418,16 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       tc::mbar_init(o0 + 8 * w, 1);
       tc::mbar_init(drain0 + 8 * w, 1);
     }
-    tc::mbar_init(never, 1);  // nothing arrives on it
-    s_abort = s_zero = 0;
-    for (int i = 0; i < SEEN; ++i) {
-      s_dirty[i] = 0;
-      tc::mbar_init(scan0 + 8 * i, 1);
+    if (lane == 18) {
+      tc::mbar_init(never, 1);  // nothing arrives on it
+      s_abort = s_zero = 0;
     }
     tc::fence_barrier_init();
-    tc::prefetch_tmap(&P.tmap_q);
-    tc::prefetch_tmap(&P.tmap_k);
-    tc::prefetch_tmap(&P.tmap_v);
+    if (lane == 0) {
+      tc::prefetch_tmap(&P.tmap_q);
+      tc::prefetch_tmap(&P.tmap_k);
+      tc::prefetch_tmap(&P.tmap_v);
+    }
   }
   if (warp == MMA_WARP) {
     tc::tmem_alloc(smem_u32(&s_tmem), TMEM_COLS);
@@ -429,15 +449,21 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
 
   // The items of this CTA; without PAIR it has one, shared by a cluster.
   const int nsplit = PAIR ? 1 : p.nsplit;
-  const int split = PAIR ? 0 : int(blockIdx.x) % nsplit;
-  int x_next = PAIR ? int(blockIdx.x) : int(blockIdx.x) / nsplit;
+  int x_next = PAIR ? int(blockIdx.x) : P.nsplit.div(int(blockIdx.x));
+  const int split = PAIR ? 0 : int(blockIdx.x) - x_next * nsplit;
   // the next item with work, and the tiles [j0, j1) of it that are this CTA's
   auto next_item = [&](Item &it, int &j0, int &j1, bool report) {
     while (x_next < P.items) {
       load_item<PAIR>(P, x_next, it, report, PAIR ? nullptr : &lens);
       x_next += PAIR ? int(gridDim.x) : P.items;
-      j0 = it.first_of(split, nsplit);
-      j1 = it.first_of(split + 1, nsplit);
+      if (PAIR) {
+        j0 = 0;
+        j1 = it.n;
+      } else {
+        const Splits parts(it.n, P.nsplit);
+        j0 = parts.first(split);
+        j1 = parts.first(split + 1);
+      }
       if (it.nb > 0 && j0 < j1) return true;
     }
     return false;
@@ -520,7 +546,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       int t = 0;
       {
         const int t0 = sp->t0;
-        t = row < sp->rows ? t0 + row / p.G : t0;
+        t = row < sp->rows ? t0 + P.g.div(row) : t0;
         r.off = t;
         r.anc = 0ull;
         if (p.parent != nullptr && row < sp->rows && sp->bad == 0) r.anc = tree_row(p, s_par[warp], sp->L, t, r.off);
@@ -995,10 +1021,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   tc::fence_after_sync();
   if constexpr (!PAIR) {
     // ---------------- join the slots' and the splits' parts
-    x_next = int(blockIdx.x) / nsplit;
+    x_next = P.nsplit.div(int(blockIdx.x));
     Item it;
     load_item<PAIR>(P, x_next, it, false, &lens);
-    const int m = it.first_of(split + 1, nsplit) - it.first_of(split, nsplit);
+    const Splits splits(it.n, P.nsplit);
+    const int m = splits.first(split + 1) - splits.first(split);
     const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
     constexpr int CH = D / 4;  // 16-byte columns of a part's row, swizzled by the row
     float *part = reinterpret_cast<float *>(smem + C::NQ * C::Q_BYTES);
@@ -1202,7 +1229,7 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   // 448 blocks: a CTA of a block takes 13.5 us and 1.5 (head dim 64: 1.3) a tile, a
   // round of them after the other; a pair of blocks 2 (1.6) a tile, 3 to change items
   // and 4 once. 17 tiles: trees of 16 sequences, 128 pairs 45 us, 256 blocks 83; 9
-  // tiles: a tree's 32 blocks 22 us, over clusters of 4 13.7.
+  // tiles: a tree's 32 blocks 22 us, over clusters of 4 13.1.
   const int64_t sms = num_sms();
   const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB));
   const int64_t cols = keys + 63 + (std::min<int64_t>(p.capacity, p.sinks) + 63) / 64 * 64 + 32;
@@ -1226,6 +1253,10 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   const int64_t items = heads * P.nblk;
   if (items * P.p.nsplit > INT_MAX / 2) return DREAMS_ERR_UNSUPPORTED;
   P.items = int(items);
+  P.heads = Divisor::of(heads);
+  P.hkv = Divisor::of(p.Hkv);
+  P.nsplit = Divisor::of(P.p.nsplit);
+  P.g = Divisor::of(p.G);
   if (kv->D == 128) return pair ? launch<128, true>(P, stream) : launch<128, false>(P, stream);
   return pair ? launch<64, true>(P, stream) : launch<64, false>(P, stream);
 }
