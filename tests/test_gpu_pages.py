@@ -271,3 +271,62 @@ def test_fork_past_32_bit_offsets(dreams):
     new = dreams.kv_fork(pool, i32([0, 0]), i32([50, 0]))
     assert new.tolist() == [50, 50] and table.tolist() == [[pages - 1], [pages - 2]] and int(ref[pages - 2]) == 1
     assert (k[pages - 2, :50] == 3).all() and (v[pages - 2, :50] == 4).all() and (k[pages - 2, 50:] == 0).all()
+
+
+@pytest.mark.parametrize("B,P", [(3000, 1), (200, 30), (2500, 2), (700, 60), (65535, 1)])
+def test_forks_of_large_tables(dreams, B, P):
+    """Tables of one CTA and of a cluster, with rows in shared memory and in the workspace, in one turn and in several."""
+    p = Pool(dreams, B, P, B + B // 2 + 2 * P, seed=B + P)
+    rng = p.rng
+    # groups of rows share full pages; every row of a group has its own last page
+    lens = np.zeros(B, np.int32)
+    free = list(rng.permutation(B + B // 2 + 2 * P)[: B + 2 * P])
+    shared = [free.pop() for _ in range(P)]
+    for b in range(B):
+        full = int(rng.integers(0, P))
+        lens[b] = 64 * full + int(rng.integers(0, 64)) if free else 64 * full
+        p.table[b, :full] = shared[:full]
+        if lens[b] % 64:
+            p.table[b, full] = free.pop()
+    np.add.at(p.ref, p.table[p.table >= 0], 1)
+    p.gt.copy_(i32(p.table)), p.gr.copy_(i32(p.ref))
+    for parent in (rng.integers(-1, B, B), (np.arange(B) // 4) * 4 + rng.integers(0, 4, B), np.arange(B)[::-1]):
+        parent = np.minimum(parent, B - 1).astype(np.int32)
+        before = p.table.copy()
+        new, f = p.fork(parent, lens)
+        if f == 0:
+            lens = new
+        else:
+            assert f == dreams.DATA_NO_PAGES
+            np.testing.assert_array_equal(p.table, before)
+    bad = np.arange(B)
+    bad[B // 2] = B
+    assert p.fork(bad, lens)[1] == dreams.DATA_BAD_INDEX
+    full = np.flatnonzero(lens % 64)
+    q = int(full[len(full) // 2])
+    p.table[q, lens[q] // 64] = -1
+    p.gt[q, int(lens[q]) // 64] = -1
+    assert p.fork(np.arange(B), lens)[1] == dreams.DATA_BAD_PAGE
+    p.table[B - 1, P - 1] = p.gt[B - 1, P - 1] = len(p.ref)
+    assert p.fork(np.arange(B), lens)[1] == dreams.DATA_BAD_PAGE
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("B,Hkv,D,v0,n_vis,r,text", [(1, 1, 8, 3, 20000, 9000, 70), (2, 1, 8, 130, 150000, 8193, 300), (1, 2, 16, 60, 9000, 8192, 140000),
+                                                     (160, 4, 128, 1, 90, 30, 40), (1, 80, 128, 9, 300, 200, 60)])
+def test_prune_long(dreams, paged, B, Hkv, D, v0, n_vis, r, text):
+    """Lists and page tables that do not fit into shared memory; more walks than SMs; rows of more than one block."""
+    test_prune(dreams, paged, 1, B, Hkv, D, v0, n_vis, r, text)
+
+
+def test_reserve_many_rows(dreams):
+    """Rows shared by 32 lanes down to one; more free pages wanted than shared memory holds."""
+    for B, P in ((2, 70), (33, 40), (64, 9), (300, 20), (1025, 3), (5000, 2)):
+        p = Pool(dreams, B, P, B * P + 7, seed=B)
+        lens = np.zeros(B, np.int32)
+        n = p.rng.integers(0, 64 * P + 1, B).astype(np.int32)
+        n[B // 2], n[0] = 64 * P, 0
+        lens[B // 3] = n[B // 3] // 2
+        assert p.reserve(lens, n - lens) == 0
+        p.release(np.full(B, 64), n - 64)
+        p.reserve(np.zeros(B, np.int32), n)
