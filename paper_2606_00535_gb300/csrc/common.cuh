@@ -37,6 +37,17 @@ inline dreams_status_t check_launch() {
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Kernels launched with this attribute are set up while the one before them in the
+// stream ends; they start with after_previous(), before their first access to global
+// memory.
+inline cudaLaunchAttribute early_launch() {
+  cudaLaunchAttribute a = {};
+  a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  a.val.programmaticStreamSerializationAllowed = 1;
+  return a;
+}
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 __device__ __forceinline__ void flag(int32_t *status_word, int32_t bits) {
   if (status_word != nullptr) atomicOr(status_word, bits);
 }

@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(BOOK_THREADS) kv_reserve_kernel(const Pool p, 
                                                                   const int32_t *n_new, int32_t *start,
                                                                   int32_t *list_ws, int32_t *status, int g) {
   __shared__ int s_warp[32], s_list[LIST_SHARED];
+  after_previous();
   const int lane = threadIdx.x & (g - 1);
   const int row0 = int(threadIdx.x) / g, rows = BOOK_THREADS / g;
   const unsigned shift = (threadIdx.x & 31) & ~(g - 1);  // the row's lanes within the warp
@@ -196,6 +197,7 @@ __global__ void __launch_bounds__(BOOK_THREADS) kv_reserve_kernel(const Pool p, 
 // One thread per table entry.
 __global__ void __launch_bounds__(256) kv_release_kernel(const Pool p, const int32_t *begin, const int32_t *end,
                                                          int32_t *status) {
+  after_previous();
   const int b = blockIdx.y;
   const int e = blockIdx.x * 256 + threadIdx.x;
   const int64_t lo = __ldg(begin + b), hi = __ldg(end + b);
@@ -248,6 +250,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
     kv_fork_table_kernel(const Pool p, const int32_t *parent, const int32_t *kv_len, int32_t *new_kv_len,
                          const ForkState f, int32_t *status) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  after_previous();
   __shared__ int s_warp[32], s_bad;
   __shared__ int32_t s_rows[4 * FORK_SHARED_ROWS], s_list[CTAS == 1 ? FORK_SHARED_ROWS : 1];
   const int rank = CTAS == 1 ? 0 : int(blockIdx.x);
@@ -428,7 +431,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
 // copy at the copy rate takes).
 constexpr int COPY_PIECE = 1024;
 __global__ void __launch_bounds__(256) kv_fork_copy_kernel(const Cache c, const ForkState f, int pieces) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  after_previous();
   const int lane = threadIdx.x & 31;
   const int64_t runs = int64_t(c.n_layers) * 2, segs = __ldcg(f.head) * runs, items = segs * pieces;
   for (int64_t x0 = blockIdx.x; x0 < items; x0 += int64_t(gridDim.x) * 32) {
@@ -468,6 +471,7 @@ constexpr int APPEND_UNROLL = 4;
 __global__ void __launch_bounds__(256) kv_append_kernel(const Cache c, const uint4 *k_new, const uint4 *v_new,
                                                         int64_t sb16, int64_t st16, const int32_t *kv_len,
                                                         const int32_t *n_new, int T_max, int32_t *status) {
+  after_previous();
   const int b = blockIdx.y;
   const int n = __ldg(n_new + b);
   const int64_t L = __ldg(kv_len + b);
@@ -523,6 +527,7 @@ __global__ void __launch_bounds__(PRUNE_THREADS, 1) kv_prune_kernel(const Cache 
                                                         int32_t *new_kv_len, int32_t *status, int cw, int nblk) {
   extern __shared__ uint4 s_ring[];  // [PRUNE_STAGES][PRUNE_UNROLL][threads]
   constexpr int threads = PRUNE_THREADS;
+  after_previous();
   int *s_list = reinterpret_cast<int *>(s_ring + PRUNE_STAGES * PRUNE_UNROLL * threads), *s_page = s_list + PRUNE_LIST;
   const int b = blockIdx.y;
   const int blk = blockIdx.x % nblk, rest = blockIdx.x / nblk;
@@ -668,23 +673,21 @@ size_t fork_layout(const Pool &p, uint8_t *ws, ForkState *f) {
   return at;
 }
 
-dreams_status_t fork_table(const Pool &p, const int32_t *parent, const int32_t *kv_len, int32_t *new_kv_len,
-                           const ForkState &f, int32_t *status, cudaStream_t stream) {
-  if (int64_t(p.B) * p.P <= FORK_ONE_CELLS) {
-    kv_fork_table_kernel<1><<<1, BOOK_THREADS, 0, stream>>>(p, parent, kv_len, new_kv_len, f, status);
-    return check_launch();
-  }
+template <typename... Params, typename... Args>
+dreams_status_t launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, dreams_stream_t stream,
+                       const Args &...args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(FORK_CTAS);
-  cfg.blockDim = dim3(BOOK_THREADS);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = FORK_CTAS;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute attr[2] = {early_launch()};
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_fork_table_kernel<FORK_CTAS>, p, parent, kv_len, new_kv_len, f, status);
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
   if (e != cudaSuccess) {
     set_last_cuda_error(e);
     return DREAMS_ERR_CUDA;
@@ -715,9 +718,7 @@ extern "C" dreams_status_t dreams_kv_reserve(const dreams_page_pool_t *pool, con
   int32_t *list = start + align_up(size_t(p.B) * 4, 256) / 4;
   int g = 32;
   while (g > 1 && int64_t(p.B) * g > BOOK_THREADS) g /= 2;
-  kv_reserve_kernel<<<1, BOOK_THREADS, 0, reinterpret_cast<cudaStream_t>(stream)>>>(p, kv_len, n_new, start, list,
-                                                                                   status_word, g);
-  return check_launch();
+  return launch(kv_reserve_kernel, dim3(1), BOOK_THREADS, 0, 1, stream, p, kv_len, n_new, start, list, status_word, g);
 }
 
 extern "C" dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, const int32_t *begin, const int32_t *end,
@@ -725,9 +726,7 @@ extern "C" dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, con
   Pool p;
   if (!pool_ok(pool, p) || begin == nullptr || end == nullptr || !aligned4(begin) || !aligned4(end))
     return DREAMS_ERR_INVALID_ARG;
-  kv_release_kernel<<<dim3(unsigned((p.P + 255) / 256), unsigned(p.B)), 256, 0,
-                      reinterpret_cast<cudaStream_t>(stream)>>>(p, begin, end, status_word);
-  return check_launch();
+  return launch(kv_release_kernel, dim3(unsigned((p.P + 255) / 256), unsigned(p.B)), 256, 0, 1, stream, p, begin, end, status_word);
 }
 
 extern "C" size_t dreams_kv_fork_workspace_size(const dreams_page_pool_t *pool) {
@@ -750,26 +749,13 @@ extern "C" dreams_status_t dreams_kv_fork(const dreams_kv_cache_t *kv, const dre
     return DREAMS_ERR_WORKSPACE;
   ForkState f;
   fork_layout(p, static_cast<uint8_t *>(workspace), &f);
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const dreams_status_t st = fork_table(p, parent, kv_len, new_kv_len, f, status_word, s);
+  const bool one = int64_t(p.B) * p.P <= FORK_ONE_CELLS;
+  const dreams_status_t st = launch(one ? kv_fork_table_kernel<1> : kv_fork_table_kernel<FORK_CTAS>, dim3(one ? 1 : FORK_CTAS), BOOK_THREADS, 0,
+                                    one ? 1 : FORK_CTAS, stream, p, parent, kv_len, new_kv_len, f, status_word);
   if (st != DREAMS_OK) return st;
   const int pieces = (PAGE * c.row16 + COPY_PIECE - 1) / COPY_PIECE;
   const int64_t most = int64_t(p.B) * c.n_layers * 2 * pieces;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(std::min<int64_t>(most, int64_t(num_sms()) * 8)));
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_fork_copy_kernel, c, f, pieces);
-  if (e != cudaSuccess) {
-    set_last_cuda_error(e);
-    return DREAMS_ERR_CUDA;
-  }
-  return check_launch();
+  return launch(kv_fork_copy_kernel, dim3(unsigned(std::min<int64_t>(most, int64_t(num_sms()) * 8))), 256, 0, 1, stream, c, f, pieces);
 }
 
 extern "C" dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t layer, const void *k_new,
@@ -790,10 +776,8 @@ extern "C" dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t
   if (blocks > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
   c.k += layer * c.layer16;
   c.v += layer * c.layer16;
-  kv_append_kernel<<<dim3(unsigned(blocks), unsigned(B)), 256, 0, reinterpret_cast<cudaStream_t>(stream)>>>(
-      c, static_cast<const uint4 *>(k_new), static_cast<const uint4 *>(v_new), stride_b / 8, stride_t / 8, kv_len, n_new,
-      T_max, status_word);
-  return check_launch();
+  return launch(kv_append_kernel, dim3(unsigned(blocks), unsigned(B)), 256, 0, 1, stream, c, static_cast<const uint4 *>(k_new),
+                static_cast<const uint4 *>(v_new), stride_b / 8, stride_t / 8, kv_len, n_new, T_max, status_word);
 }
 
 extern "C" dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t B, const int32_t *keep, int32_t v0,
@@ -824,7 +808,6 @@ extern "C" dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t 
   const dreams_status_t st = ensure_max_dynamic_smem(reinterpret_cast<const void *>(kv_prune_kernel), PRUNE_SMEM);
   if (st != DREAMS_OK) return st;
   const dim3 grid(unsigned(int64_t(c.n_layers) * 2 * nblk), unsigned(B));
-  kv_prune_kernel<<<grid, PRUNE_THREADS, PRUNE_SMEM, reinterpret_cast<cudaStream_t>(stream)>>>(
-      c, keep, v0, n_vis, r, kv_len, refcount, new_kv_len, status_word, cw, nblk);
-  return check_launch();
+  return launch(kv_prune_kernel, grid, PRUNE_THREADS, PRUNE_SMEM, 1, stream, c, keep, v0, n_vis, r, kv_len, refcount, new_kv_len, status_word, cw,
+                nblk);
 }

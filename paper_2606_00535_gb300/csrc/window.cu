@@ -400,6 +400,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
   x /= p.nsplit;
   const int g = x % p.Hkv, b = x / p.Hkv;
   if (p.nsplit > 1) cluster_arrive();  // this CTA runs: it may be written to
+  after_previous();
   const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
   const bool report = split == 0 && g == 0;
   int bad = 0;
@@ -491,12 +492,12 @@ dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
   cfg.blockDim = dim3(32 * WARPS);
   cfg.dynamicSmemBytes = RowsCfg<D>::SMEM;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = unsigned(p.nsplit);
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2] = {early_launch()};
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(p.nsplit);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.nsplit > 1 ? 1 : 0;
+  cfg.numAttrs = p.nsplit > 1 ? 2 : 1;
   void *args[] = {&p};
   e = cudaLaunchKernelExC(&cfg, kernel, args);
   if (e != cudaSuccess) {

@@ -385,18 +385,6 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty), ready0 = smem_u32(bar_ready);
   const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), r0 = smem_u32(bar_r), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
                  o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
-  // Without PAIR the item is known: its lengths and parents are on their way early.
-  int2 lens = make_int2(0, 0);
-  int early[2] = {-1, -1};
-  if constexpr (!PAIR) {
-    const int x = P.nsplit.div(int(blockIdx.x)), b = P.hkv.div(x - P.heads.div(x) * int(P.heads.d));
-    lens = make_int2(__ldg(p.q_len + b), __ldg(p.kv_len + b));
-    if (p.parent != nullptr && warp < 8) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (lane + 32 * k < p.T_max) early[k] = __ldg(p.parent + int64_t(b) * p.T_max + lane + 32 * k);
-    }
-  }
   if (warp == TMA_WARP) {
     if (lane < NST) {
       tc::mbar_init(full0 + 8 * lane, 1);
@@ -429,9 +417,22 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       tc::prefetch_tmap(&P.tmap_v);
     }
   }
+  after_previous();  // (ahead of tensor memory too: the kernel before may still be about to take it)
   if (warp == MMA_WARP) {
     tc::tmem_alloc(smem_u32(&s_tmem), TMEM_COLS);
     tc::tmem_relinquish();
+  }
+  // Without PAIR the item is known: its lengths and parents are on their way early.
+  int2 lens = make_int2(0, 0);
+  int early[2] = {-1, -1};
+  if constexpr (!PAIR) {
+    const int x = P.nsplit.div(int(blockIdx.x)), b = P.hkv.div(x - P.heads.div(x) * int(P.heads.d));
+    lens = make_int2(__ldg(p.q_len + b), __ldg(p.kv_len + b));
+    if (p.parent != nullptr && warp < 8) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (lane + 32 * k < p.T_max) early[k] = __ldg(p.parent + int64_t(b) * p.T_max + lane + 32 * k);
+    }
   }
   tc::fence_before_sync();
   __syncthreads();
@@ -1169,12 +1170,12 @@ dreams_status_t launch(TcParams &P, cudaStream_t stream) {
   cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = Cfg<D, PAIR>::SMEM;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = unsigned(P.p.nsplit);
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2] = {early_launch()};
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(P.p.nsplit);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = !PAIR && P.p.nsplit > 1 ? 1 : 0;
+  cfg.numAttrs = !PAIR && P.p.nsplit > 1 ? 2 : 1;
   void *args[] = {&P};
   const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
   if (e != cudaSuccess) {
