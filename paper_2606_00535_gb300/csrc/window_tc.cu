@@ -27,9 +27,15 @@
 //          For grids too small to fill the SMs with pairs.
 // Warps: 0-3 and 4-7 the softmax of slots 0 and 1, 8 the TMA producer, 9 and 10 the
 // MMA issuers of the slots (one thread each, so that one's waits run under the
-// other's MMAs), 11 the scan (below), which also zeroes the V rows that nobody sees. A slot's MMAs complete in order, so the commit
-// that announces S of a tile also says that the P V before it is done: the softmax
-// warpgroup then gives those stages back, and no further commits are needed.
+// other's MMAs), 11 the scan (below), which also zeroes the V rows that nobody sees. A
+// slot's MMAs complete in order, so the commit that announces S of a tile also says
+// that the P V before it is done: the softmax warpgroup then gives those stages back,
+// and no further commits are needed.
+// Bound by the chain of a tile (products, softmax, products), of which two run on an
+// SM: about 3000 clocks for both slots, where the products take 2048 (head dim 128)
+// or the exponentials 1024 (64). 3392 tokens of 32 heads, head dim 128, window 1024: 72
+// us, 36% of the bf16 burst rate on the keys seen; 16 trees of up to 64 nodes, 32/8
+// heads, window 2048: 45 us, 48% of the copy rate.
 // Every mbarrier wait is bounded; a CTA that gives up flags DREAMS_DATA_TIMEOUT,
 // drains its copies and MMAs, frees its tensor memory and leaves unfinished rows
 // untouched.
