@@ -424,8 +424,9 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
  * visible slot and whose entry is out of range is flagged DREAMS_DATA_BAD_PAGE,
  * and its slots read as zeros. What a slot holds does not reach a query that does
  * not see it, infinities and NaN included. Accumulation is fp32; probabilities
- * enter the PV product as bf16, and the output is rounded to bf16 once. One
- * launch, no workspace.
+ * enter the PV product as bf16, and the output is rounded to bf16 once. The sums
+ * are normalised at the end, so finite values of V are good up to 2^87 in
+ * magnitude. One launch, no workspace.
  */
 dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
                                         const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,

@@ -17,7 +17,8 @@
 // tile it sees a key of, and stays; P = 2^(x - m) is as exact at any m, in bf16 and in
 // the f32 sums alike, short of overflow. So the exponentials of a tile start as its
 // scores arrive. A row whose sum ends above 2^100 (a later score exceeds m by some 69
-// nats) is done again from its definition.
+// nats), or above 2^40 (28 nats) with an O that overflowed, is done again from its
+// definition.
 //   PAIR   the slots are two neighbouring blocks of a KV head: every K/V tile is
 //          loaded once for 256 rows. The CTAs are persistent: they walk over the
 //          items with a ring of K/V stages that runs on across them, so the next
@@ -60,7 +61,11 @@ constexpr int THREADS = 384;
 constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 11;  // slot w's MMAs: warp MMA_WARP + w
 constexpr int SEEN = 16;  // items whose scan results are kept (more than the ring can be ahead)
 constexpr uint32_t TMEM_COLS = 512;
-constexpr float MOST_SUM = 1.2676506e30f;  // 2^100: a row's sum above it is done again
+// A row whose sum ends above MOST_SUM (2^100) is done again, and so is one whose O has
+// overflowed with a sum above SAFE_SUM (2^40). |O| is at most the sum times the largest
+// |V|, so below that sum no O overflows for |V| up to 2^87, and above it an infinity or
+// a NaN of O may not be V's.
+constexpr float MOST_SUM = 1.2676506e30f, SAFE_SUM = 1.0995116e12f;
 
 template <int D, bool PAIR>
 struct Cfg {
@@ -716,7 +721,20 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       const bool real = row < sp->rows, tree_ok = sp->bad == 0;
       if constexpr (PAIR) {
         const int h = sp->g * p.G + row - (t - sp->t0) * p.G;
-        const uint32_t again = __ballot_sync(0xffffffffu, any && real && (dirty || l > MOST_SUM));
+        uint32_t again = __ballot_sync(0xffffffffu, any && real && (dirty || l > MOST_SUM));
+        const bool risky = any && real && l > SAFE_SUM;
+        if (__builtin_expect(__any_sync(0xffffffffu, risky), 0)) {
+          uint32_t odd = 0;  // does O hold an infinity or a NaN?
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t ov[32];
+            tc::tmem_ld32(tl + C::O_COL + c * 32, ov);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) odd |= uint32_t((ov[e] & 0x7f800000u) == 0x7f800000u);
+          }
+          again |= __ballot_sync(0xffffffffu, risky && odd != 0u);
+        }
         if (any && tree_ok) {
           const float inv = 1.f / l;
           const int64_t orow = (int64_t(sp->b) * p.T_max + t) * p.Hq + h;
@@ -1115,6 +1133,14 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             acc.y += ci * v[k].y;
             acc.z += ci * v[k].z;
             acc.w += ci * v[k].w;
+          }
+        }
+        if (__builtin_expect(__any_sync(0xffffffffu, ml.y > SAFE_SUM), 0)) {
+          // (a sum of 0 x O is zero, or NaN)
+          const float odd = 0.f * acc.x + 0.f * acc.y + 0.f * acc.z + 0.f * acc.w;
+          if (__any_sync(0xffffffffu, odd != 0.f)) {  // (also where it is NaN)
+            slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc);
+            continue;
           }
         }
         const float inv = 1.f / Z;
