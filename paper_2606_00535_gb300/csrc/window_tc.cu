@@ -59,7 +59,10 @@ constexpr int KT = 128;    // keys of a tile
 constexpr int ROWS = 128;  // query rows of a block
 constexpr int THREADS = 384;
 constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 11;  // slot w's MMAs: warp MMA_WARP + w
-constexpr int SEEN = 16;  // items whose scan results are kept (more than the ring can be ahead)
+// Items whose scan results are kept: more than the scan can be ahead of a slot that has
+// tiles of the item, as it needs stages which that slot gives back. Of a slot that has
+// none it can be ahead by any number of items, so such a slot asks for no result.
+constexpr int SEEN = 16;
 constexpr uint32_t TMEM_COLS = 512;
 // A row whose sum ends above MOST_SUM (2^100) is done again, and so is one whose O has
 // overflowed with a sum above SAFE_SUM (2^40). |O| is at most the sum times the largest
@@ -712,10 +715,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         tc::fence_after_sync();
         if (ok) arrive_if(empty0 + 8 * v1, lead);
       }
-      ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
+      if (any) ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
       if (!ok) break;
       if (PAIR) pos.move(ahead);
-      const bool dirty = *reinterpret_cast<volatile int *>(&s_dirty[seq % SEEN]) != 0;
+      const bool dirty = any && *reinterpret_cast<volatile int *>(&s_dirty[seq % SEEN]) != 0;
       ++seq;
 
       const bool real = row < sp->rows, tree_ok = sp->bad == 0;
