@@ -426,7 +426,11 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
  * not see it, infinities and NaN included. Accumulation is fp32; probabilities
  * enter the PV product as bf16, and the output is rounded to bf16 once. The sums
  * are normalised at the end, so finite values of V are good up to 2^87 in
- * magnitude. One launch, no workspace.
+ * magnitude. With more than 16 query rows per KV head (T_max * Hq / Hkv), rows are
+ * computed one key at a time, about a thousand times slower (0.6 us a key for each
+ * of a block's rows in turn), where their block's tiles hold an infinity or a NaN in
+ * V that not every row sees, and where a row's later scores exceed its first ones by
+ * some 69 nats. One launch, no workspace.
  */
 dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
                                         const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
@@ -573,7 +577,8 @@ dreams_status_t dreams_vocab_argmax_noalloc(const void *logits, dreams_dtype_t d
  * TMA copies of each CTA from its stall_at-th K tile (attention) or k-block
  * (LM head, counted over the CTA's tiles) on, waiting instead on a barrier
  * that nothing arrives on, and every pipeline wait gives up after
- * wait_limit_ns (1 us .. 2 s) instead of 2 s. The kernels then flag
+ * wait_limit_ns (1 us .. 2 s) instead of 2 s (in dreams_window_attention, without
+ * a row computed key by key meanwhile). The kernels then flag
  * DREAMS_DATA_TIMEOUT, wait for the copies and MMAs they did issue, free
  * their tensor memory and exit; output rows they did not finish are left
  * untouched (attention), or unreliable (LM head; rows no tile reached are

@@ -37,7 +37,7 @@
 // or the exponentials 1024 (64). 3392 tokens of 32 heads, head dim 128, window 1024: 72
 // us, 36% of the bf16 burst rate on the keys seen; 16 trees of up to 64 nodes, 32/8
 // heads, window 2048: 45 us, 48% of the copy rate.
-// Every mbarrier wait is bounded; a CTA that gives up flags DREAMS_DATA_TIMEOUT,
+// Every mbarrier wait is bounded (2 s without progress); a CTA that gives up flags DREAMS_DATA_TIMEOUT,
 // drains its copies and MMAs, frees its tensor memory and leaves unfinished rows
 // untouched.
 #include <cuda.h>
@@ -294,14 +294,20 @@ __device__ __forceinline__ bool quick(uint32_t bar, uint32_t parity) {
   asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int *abort, uint64_t limit_ns) {
+// The limit is one without progress: rows that a warp does again key by key (watch[BEAT]
+// counts on) may take longer than that, and the CTA's other warps wait for them.
+constexpr int ABORT = 0, BEAT = 1;
+__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int *watch, uint64_t limit_ns) {
   if (quick(bar, parity)) return true;
   uint64_t t0 = 0;
+  int beat = 0;
   for (;;) {
     if (try_wait(bar, parity)) return true;
     const uint64_t now = tc::global_ns();
-    if (t0 == 0) t0 = now;
-    if (*abort || now - t0 > limit_ns) return false;
+    const int b = watch[BEAT];
+    if (t0 == 0 || b != beat) t0 = now;
+    beat = b;
+    if (watch[ABORT] || now - t0 > limit_ns) return false;
   }
 }
 __device__ __forceinline__ void st_global_v8(void *p, const uint32_t *v) {
@@ -323,9 +329,12 @@ struct Row {
 
 // One row by a whole warp, straight from the definition: used when a tile with
 // partly masked columns held an infinity or a NaN in V (0 x inf would reach rows
-// that do not see it). Slow, and rare.
+// that do not see it), and when a row's sum outgrew its reference. Slow (0.61 us a key,
+// a chain of page entry, K, five shuffles and exponentials), and rare; `beat` is counted
+// on while it lasts.
 template <int D>
-__device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, int t, int h, int off, unsigned long long anc) {
+__device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, int t, int h, int off, unsigned long long anc,
+                                      int *beat) {
   const int lane = threadIdx.x & 31;
   constexpr int E = D / 32;
   float q[E], o[E];
@@ -338,6 +347,7 @@ __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, i
   const KeyList kl = key_list(p, L, p.parent != nullptr ? 0 : t, t);
   float m = -INFINITY, l = 0.f;
   for (int i = 0; i < kl.n; ++i) {
+    if ((i & 63) == 0 && lane == 0) atomicAdd(beat, 1);
     const int s = kl.slot(i);
     if (!sees(p, L, off, anc, s)) continue;
     int64_t at;
@@ -386,7 +396,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST], bar_ready[NST];
   __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_r[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_zero, s_dirty[SEEN];
+  __shared__ int s_watch[2], s_zero, s_dirty[SEEN];
+  int &s_abort = s_watch[ABORT];
   __shared__ int8_t s_par[8][64];
   __shared__ Slot s_slot[8];
   __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
@@ -422,7 +433,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     }
     if (lane == 18) {
       tc::mbar_init(never, 1);  // nothing arrives on it
-      s_abort = s_zero = 0;
+      s_watch[ABORT] = s_watch[BEAT] = s_zero = 0;
     }
     tc::fence_barrier_init();
     if (lane == 0) {
@@ -460,7 +471,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       flag(p.status, DREAMS_DATA_TIMEOUT);
     }
   };
-  auto wait = [&](uint32_t bar, uint32_t parity) { return long_wait(bar, parity & 1u, abort_flag, wait_ns); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return long_wait(bar, parity & 1u, s_watch, wait_ns); };
 
   // The items of this CTA; without PAIR it has one, shared by a cluster.
   const int nsplit = PAIR ? 1 : p.nsplit;
@@ -768,7 +779,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           for (int i = 0; i < 32; ++i) {
             const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, r.off, i), hi = __shfl_sync(0xffffffffu, h, i);
             const unsigned long long ai = __shfl_sync(0xffffffffu, r.anc, i);
-            if ((again >> i) & 1u) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai);
+            if ((again >> i) & 1u) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai, &s_watch[BEAT]);
           }
         }
         tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
@@ -1105,7 +1116,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         if (off < 0) continue;  // a malformed tree
         const int h = it.g * p.G + row - (t - it.t00) * p.G;
         if (again || __any_sync(0xffffffffu, ml.y > MOST_SUM)) {
-          slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc);
+          slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_watch[BEAT]);
           continue;
         }
         const uint32_t some = __ballot_sync(0xffffffffu, ml.y != 0.f);
@@ -1142,7 +1153,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           // (a sum of 0 x O is zero, or NaN)
           const float odd = 0.f * acc.x + 0.f * acc.y + 0.f * acc.z + 0.f * acc.w;
           if (__any_sync(0xffffffffu, odd != 0.f)) {  // (also where it is NaN)
-            slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc);
+            slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_watch[BEAT]);
             continue;
           }
         }

@@ -52,46 +52,82 @@ def test_large_values_under_rising_scores(dreams, layout, D, nats, log2v):
     c.check(c.run(dreams), n=40)
 
 
-def test_one_block_of_a_pair_far_behind(dreams):
-    """A long request of two blocks, whose second block's rows are all done again key by key, and behind it, on the same
-    CTAs, over twenty requests of one block, then one of two blocks again: the second block's warps fall behind by
-    more items than the kernel keeps scan results of."""
-    sms = torch.cuda.get_device_properties(0).multi_processor_count
+class Queue:
+    """On the same CTAs one after the other: a long request of two blocks, whose rows from `slow` on are all done again key
+    by key (their scores rise by 80 nats), `rounds` - 1 short requests of one block, and one of two blocks again."""
     Hq, Hkv, D, T, scale = 32, 8, 64, 64, 0.125
-    assert sms % Hkv == 0
-    B = sms // Hkv * 22 + 1  # the first and the last sequence's heads fall on the same CTAs
-    g = torch.Generator().manual_seed(3)
-    lens, n = [2000] + [3 + b % 30 for b in range(B - 2)] + [70], [T] + [1 + (b * 7) % 32 for b in range(B - 2)] + [T]
-    P = -(-(lens[0] + T) // 64)
-    table, at = torch.full((B, P), -1, dtype=torch.int32), 0
-    for b in range(B):
-        for e in range(-(-(lens[b] + n[b]) // 64)):
-            table[b, e] = at
-            at += 1
-    k, v = (torch.randn((at, 64, Hkv, D), generator=g) for _ in range(2))
-    q = torch.randn((B, T, Hq, D), generator=g)
-    # the first sequence: scores rise by 80 nats for the rows of its second block (sums above 2^100), by about 1 for the others
-    lift = torch.arange(P * 64) * (80.0 / lens[0]) / (scale * D)
-    k[:P] = lift.view(P, 64, 1, 1) + 0.02 * k[:P]
-    q[0, :32] *= 0.1
-    q[0, 32:] = 1.0
-    q, k, v = (x.to(torch.bfloat16) for x in (q, k, v))
-    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
-    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
-    lse = torch.full(q.shape[:3], 7.0, device="cuda")
-    st = i32([0])
-    dreams.window_attention(q.cuda(), dreams.KVCache(k.cuda(), v.cuda(), table.cuda()), i32(n), i32(lens), scale, 10 ** 6, out=out, lse=lse, status=st)
+
+    def __init__(self, rounds, first, slow):
+        sms = torch.cuda.get_device_properties(0).multi_processor_count
+        assert sms % self.Hkv == 0
+        self.B = B = sms // self.Hkv * rounds + 1  # the first and the last sequence's heads fall on the same CTAs
+        g = torch.Generator().manual_seed(3)
+        self.lens = lens = [first] + [3 + b % 30 for b in range(B - 2)] + [70]
+        self.n = n = [self.T] + [1 + (b * 7) % 32 for b in range(B - 2)] + [self.T]
+        P, at = -(-(first + self.T) // 64), 0
+        self.table = torch.full((B, P), -1, dtype=torch.int32)
+        for b in range(B):
+            for e in range(-(-(lens[b] + n[b]) // 64)):
+                self.table[b, e] = at
+                at += 1
+        k, v = (torch.randn((at, 64, self.Hkv, self.D), generator=g) for _ in range(2))
+        q = torch.randn((B, self.T, self.Hq, self.D), generator=g)
+        k[:P] = (torch.arange(P * 64) * (80.0 / first) / (self.scale * self.D)).view(P, 64, 1, 1) + 0.02 * k[:P]
+        q[0, :slow] *= 0.1  # scores of about 1
+        q[0, slow:] = 1.0
+        self.q, self.k, self.v = (x.to(torch.bfloat16) for x in (q, k, v))
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.gpu = self.q.cuda(), self.k.cuda(), self.v.cuda(), self.table.cuda(), i32(n), i32(lens)
+
+    def run(self, dreams):
+        q, k, v, table, n, lens = self.gpu
+        out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full(q.shape[:3], 7.0, device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        dreams.window_attention(q, dreams.KVCache(k, v, table), n, lens, self.scale, 10 ** 6, out=out, lse=lse, status=st)
+        torch.cuda.synchronize()
+        return out, lse, int(st.item())
+
+    def check(self, out, lse):
+        out, lse, B, n = out.double().cpu().numpy(), lse.double().cpu().numpy(), self.B, self.n
+        for b in {0, 1, 2, 19, 20, B // 2, B - 20, B - 2, B - 1}:
+            assert (out[b, n[b]:] == 7.0).all() and (lse[b, n[b]:] == 7.0).all()
+            own = self.table[b, self.table[b] >= 0].long()
+            K, V = (x[own].reshape(-1, self.Hkv, self.D).double().numpy() for x in (self.k, self.v))
+            sel = [(t, h) for t in sorted({0, n[b] // 2, n[b] - 1}) for h in range(0, self.Hq, 5)]
+            ref = S.window_rows(self.q[b].double().numpy(), lambda s, h: (K[s, h], V[s, h]), self.lens[b], self.scale, 10 ** 6, 0,
+                                lambda h: h // 4, None, sel)
+            for (t, h), (o, a, z) in zip(sel, ref):
+                err, tol = np.abs(out[b, t, h] - o), 1.02 * 2.0 ** -8 * (np.abs(o) + a) + 2e-4 * a + 1e-6
+                assert (err <= tol).all(), (b, t, h, float((err / tol).max()))
+                assert abs(lse[b, t, h] - z) <= 1e-4 + 1e-6 * abs(z), (b, t, h)
+        for b in range(B):  # no row was left out
+            assert (lse[b, :n[b]] != 7.0).all()
+
+
+def test_one_block_of_a_pair_far_behind(dreams):
+    """The second block's warps fall behind by more items than the kernel keeps scan results of."""
+    c = Queue(22, 2000, 32)
+    out, lse, st = c.run(dreams)
+    assert st == 0
+    c.check(out, lse)
+
+
+def test_rows_done_again_are_no_stall(dreams):
+    """Warps that redo rows keep the CTA's other warps waiting for much longer than the limit of a wait."""
+    c = Queue(2, 4000, 0)
+    c.run(dreams)
+    t = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    t[0].record()
+    ref, ref_lse, st = c.run(dreams)
+    t[1].record()
     torch.cuda.synchronize()
-    assert int(st.item()) == 0
-    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
-    for b in [0, 1, 2, 19, 20, B // 2, B - 20, B - 2, B - 1]:
-        assert (out[b, n[b]:] == 7.0).all() and (lse[b, n[b]:] == 7.0).all()
-        K, V = (x[table[b, table[b] >= 0].long()].reshape(-1, Hkv, D).double().numpy() for x in (k, v))
-        sel = [(t, h) for t in sorted({0, n[b] // 2, n[b] - 1}) for h in range(0, Hq, 5)]
-        ref = S.window_rows(q[b].double().numpy(), lambda s, h: (K[s, h], V[s, h]), lens[b], scale, 10 ** 6, 0, lambda h: h // 4, None, sel)
-        for (t, h), (o, a, z) in zip(sel, ref):
-            err, tol = np.abs(out[b, t, h] - o), 1.02 * 2.0 ** -8 * (np.abs(o) + a) + 2e-4 * a + 1e-6
-            assert (err <= tol).all(), (b, t, h, float((err / tol).max()))
-            assert abs(lse[b, t, h] - z) <= 1e-4 + 1e-6 * abs(z), (b, t, h)
-    for b in range(B):  # no row of the others was left out
-        assert (lse[b, :n[b]] != 7.0).all()
+    ms = t[0].elapsed_time(t[1])
+    assert st == 0 and ms > 8  # (so the limit below is far above a wait for products or copies)
+    c.check(ref, ref_lse)
+    try:
+        dreams.test_set_stall(dreams.TEST_ATTENTION, 1 << 30, int(ms * 1e6 / 8))  # no copy is withheld
+        out, lse, st = c.run(dreams)
+    finally:
+        dreams.test_set_stall(0, -1)
+    assert st == 0 and torch.equal(out, ref) and torch.equal(lse, ref_lse)
