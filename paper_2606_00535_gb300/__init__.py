@@ -691,18 +691,23 @@ def _launch(name: str, dev: torch.device, stream, *args) -> None:
         raise DreamsError(name, st)
 
 
-def _scratch(kind: str, need: int, workspace: Optional[torch.Tensor], dev: torch.device, stream):
-    """(address, bytes) of the caller's workspace, or of one kept for this call,
-    device and stream; nothing where the call needs none."""
+def _scratch(pool: "PagePool", workspace: Optional[torch.Tensor], dev: torch.device, stream):
+    """(address, bytes) of the caller's workspace, or of the pool's own for this
+    stream; nothing off the GPU, where the launch refuses."""
     if workspace is not None:
-        ws, n = _ws(workspace, dev)
-        return ws, n
-    if need == 0 or dev.type != "cuda":  # off the GPU the launch refuses
+        return _ws(workspace, dev)
+    if dev.type != "cuda":
         return None, 0
     s = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
-    ws = _WS.get((kind, dev.index, s))
-    if ws is None or ws.numel() < need:
-        ws = _workspace(kind, need, dev, stream)
+    ws = pool._by_stream.get(s)
+    if ws is None:
+        if stream is not None and stream.device != dev:
+            raise ValueError(f"stream is on {stream.device}, the tensors on {dev}")
+        # made with the stream current: its memory is then that stream's, so what used it before is done
+        # when the call runs, and what uses it after the pool is gone comes after the call
+        with torch.cuda.stream(stream):
+            ws = torch.empty(max(pool._reserve_bytes, pool._fork_bytes), dtype=torch.uint8, device=dev)
+        ws = pool._by_stream.setdefault(s, ws)
     return ws.data_ptr(), ws.numel()
 
 
@@ -710,7 +715,10 @@ def _scratch(kind: str, need: int, workspace: Optional[torch.Tensor], dev: torch
 class PagePool:
     """The pages of a paged cache: its page table and ``refcount`` (int32
     [num_pages]: how many table entries hold each page; 0 = free). The calls
-    below change both. ``PagePool.empty(kv)`` starts with every page free."""
+    below change both, so calls on one pool from several streams have to be ordered
+    like all uses of its tensors. ``PagePool.empty(kv)`` starts with every page
+    free. The pool owns the workspaces of its calls, one per stream; a captured call
+    uses them at every replay, so the pool has to live as long as the graph."""
     kv: KVCache
     refcount: torch.Tensor
 
@@ -725,6 +733,7 @@ class PagePool:
                             self.kv.pages_per_seq, self.kv.num_pages)
         self._reserve_bytes = int(_lib().dreams_kv_reserve_workspace_size(ctypes.byref(self._c)))
         self._fork_bytes = int(_lib().dreams_kv_fork_workspace_size(ctypes.byref(self._c)))
+        self._by_stream: Dict[int, torch.Tensor] = {}  # workspaces; they hold no state between calls
 
     @classmethod
     def empty(cls, kv: KVCache) -> "PagePool":
@@ -790,7 +799,7 @@ def kv_reserve(pool: PagePool, kv_len: torch.Tensor, n_new: torch.Tensor, worksp
     they have none: free pages, lowest ids first."""
     dev = pool.refcount.device
     kl, nn = _per_seq(kv_len, "kv_len", pool.B, dev), _per_seq(n_new, "n_new", pool.B, dev)
-    ws, ws_bytes = _scratch("reserve", pool._reserve_bytes, workspace, dev, stream)
+    ws, ws_bytes = _scratch(pool, workspace, dev, stream)
     _launch("dreams_kv_reserve", dev, stream, ctypes.byref(pool._c), kl, nn, ws, ws_bytes, _status(status, dev))
 
 
@@ -813,7 +822,7 @@ def kv_fork(pool: PagePool, parent: torch.Tensor, kv_len: torch.Tensor, new_kv_l
     par, kl = _per_seq(parent, "parent", pool.B, dev), _per_seq(kv_len, "kv_len", pool.B, dev)
     if new_kv_len is None:
         new_kv_len = torch.empty(pool.B, dtype=torch.int32, device=dev)
-    ws, ws_bytes = _scratch("fork", pool._fork_bytes, workspace, dev, stream)
+    ws, ws_bytes = _scratch(pool, workspace, dev, stream)
     _launch("dreams_kv_fork", dev, stream, ctypes.byref(pool.kv._c), ctypes.byref(pool._c), par, kl,
             _per_seq(new_kv_len, "new_kv_len", pool.B, dev), ws, ws_bytes, _status(status, dev))
     return new_kv_len
