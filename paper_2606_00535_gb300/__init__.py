@@ -154,6 +154,18 @@ def _stream(stream, dev: torch.device) -> ctypes.c_void_p:
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _new(shape, dtype, dev: torch.device, stream) -> torch.Tensor:
+    """A result of a call on ``stream``. Made with that stream current, so that
+    the memory is that stream's: what used it before is done when the call runs.
+    It is not given out again before what the current stream does with it is done."""
+    if stream is None or dev.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    t.record_stream(torch.cuda.current_stream(dev))
+    return t
+
+
 def _check(name: str, st: int):
     if st != OK:
         raise DreamsError(name, st)
@@ -205,11 +217,11 @@ def _status(status: Optional[torch.Tensor], dev):
     return None if status is None else _ptr(_need_out(status, "status", torch.int32, dev, 1))
 
 
-def _outputs(outputs: Optional[tuple], B: int, max_path: int, dev) -> tuple:
+def _outputs(outputs: Optional[tuple], B: int, max_path: int, dev, stream) -> tuple:
     """(accept_len [B], path [B, max_path], out_tokens [B, max_path],
     new_kv_len [B]): the caller's, checked, or new."""
     if outputs is None:
-        return _walk_outputs(B, max_path, dev)
+        return _walk_outputs(B, max_path, dev, stream)
     if len(outputs) != 4:
         raise ValueError("outputs must be (accept_len, path, out_tokens, new_kv_len)")
     acc, path, toks, nkl = outputs
@@ -359,12 +371,12 @@ def tree_verify_attn(q: torch.Tensor, kv: KVCache, tree: Tree, scale: float, lay
         raise ValueError(f"q must be [B, T_max, Hq, D] with the tree's B = {tree.B}, T_max = {tree.T_max}")
     _cache_covers(kv, tree.B, int(q.shape[3]))
     if out is None:
-        out = torch.empty(tuple(q.shape), dtype=torch.bfloat16, device=dev)
+        out = _new(tuple(q.shape), torch.bfloat16, dev, stream)
     _need(out, "out", torch.bfloat16, dev)
     if tuple(out.shape) != tuple(q.shape):
         raise ValueError("out must have q's shape")
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=dev)
+        lse = _new(q.shape[:3], torch.float32, dev, stream)
     if lse is not None:
         _need(lse, "lse", torch.float32, dev)
         if tuple(lse.shape) != tuple(q.shape[:3]):
@@ -386,7 +398,7 @@ def vocab_argmax(logits: torch.Tensor, out: Optional[torch.Tensor] = None,
     rows, V = int(x.shape[0]), int(x.shape[1])
     dev = logits.device
     if out is None:
-        out = torch.empty(logits.shape[:-1], dtype=torch.int32, device=dev)
+        out = _new(logits.shape[:-1], torch.int32, dev, stream)
     _need_out(out, "out", torch.int32, dev, rows)
     need = int(_lib().dreams_vocab_argmax_workspace_size(rows, V))
     if workspace is None:
@@ -428,7 +440,7 @@ def vocab_sample(logits: torch.Tensor, temperature: float, uniforms: torch.Tenso
     if uniforms.numel() != rows:
         raise ValueError("uniforms must hold one value per row")
     if out is None:
-        out = torch.empty(logits.shape[:-1], dtype=torch.int32, device=dev)
+        out = _new(logits.shape[:-1], torch.int32, dev, stream)
     _need_out(out, "out", torch.int32, dev, rows)
     need = int(_lib().dreams_vocab_sample_workspace_size(rows, V))
     if workspace is None:
@@ -461,12 +473,12 @@ def attention(q: torch.Tensor, kv: KVCache, q_len: torch.Tensor, kv_len: torch.T
             raise ValueError(f"{n} holds {t.numel()} entries, q has {B} sequences")
     _cache_covers(kv, B, int(q.shape[3]))
     if out is None:
-        out = torch.empty(tuple(q.shape), dtype=torch.bfloat16, device=dev)
+        out = _new(tuple(q.shape), torch.bfloat16, dev, stream)
     _need(out, "out", torch.bfloat16, dev)
     if tuple(out.shape) != tuple(q.shape):
         raise ValueError("out must have q's shape")
-    lse = torch.empty((B, T_max, Hq), dtype=torch.float32, device=dev) if want_lse else None
-    ent = torch.empty((B, T_max, Hq), dtype=torch.float32, device=dev) if want_entropy else None
+    lse = _new((B, T_max, Hq), torch.float32, dev, stream) if want_lse else None
+    ent = _new((B, T_max, Hq), torch.float32, dev, stream) if want_entropy else None
     need = int(_lib().dreams_attention_workspace_size(ctypes.byref(kv._c), B, T_max, Hq, mode, int(want_entropy)))
     if workspace is None:
         workspace = _workspace("attention", need, dev, stream)
@@ -492,10 +504,10 @@ def lm_head_argmax(hidden: torch.Tensor, weight: torch.Tensor, out: Optional[tor
     V = int(weight.shape[0])
     dev = hidden.device
     if out is None:
-        out = torch.empty(rows, dtype=torch.int32, device=dev)
+        out = _new(rows, torch.int32, dev, stream)
     _need_out(out, "out", torch.int32, dev, rows)
     if out_max is None and want_max:
-        out_max = torch.empty(rows, dtype=torch.float32, device=dev)
+        out_max = _new(rows, torch.float32, dev, stream)
     if out_max is not None:
         _need_out(out_max, "out_max", torch.float32, dev, rows)
     need = int(_lib().dreams_lm_head_argmax_workspace_size(rows))
@@ -517,8 +529,8 @@ def visual_importance(attn: torch.Tensor, v0: int, n_vis: int, r: int, workspace
         raise TypeError("attn must be a contiguous [B, H, Q, K] float32/bfloat16 tensor")
     B, H, Q, K = (int(x) for x in attn.shape)
     dev = attn.device
-    imp = torch.empty((B, n_vis), dtype=torch.float32, device=dev)
-    keep = torch.empty((B, r), dtype=torch.int32, device=dev)
+    imp = _new((B, n_vis), torch.float32, dev, stream)
+    keep = _new((B, r), torch.int32, dev, stream)
     need = int(_lib().dreams_visual_importance_workspace_size(B, H, Q, n_vis))
     if workspace is None:
         workspace = _workspace("importance", need, dev, stream)
@@ -528,11 +540,11 @@ def visual_importance(attn: torch.Tensor, v0: int, n_vis: int, r: int, workspace
     return imp, keep
 
 
-def _walk_outputs(B: int, max_path: int, dev):
-    return (torch.empty(B, dtype=torch.int32, device=dev),
-            torch.empty((B, max_path), dtype=torch.int32, device=dev),
-            torch.empty((B, max_path), dtype=torch.int32, device=dev),
-            torch.empty(B, dtype=torch.int32, device=dev))
+def _walk_outputs(B: int, max_path: int, dev, stream):
+    return (_new(B, torch.int32, dev, stream),
+            _new((B, max_path), torch.int32, dev, stream),
+            _new((B, max_path), torch.int32, dev, stream),
+            _new(B, torch.int32, dev, stream))
 
 
 def accept_path(argmax: torch.Tensor, tree: Tree, max_path: int, status: Optional[torch.Tensor] = None,
@@ -540,7 +552,7 @@ def accept_path(argmax: torch.Tensor, tree: Tree, max_path: int, status: Optiona
     """Greedy acceptance over the trees. Returns a dict of device tensors."""
     dev = tree.parent.device
     _need_out(argmax, "argmax", torch.int32, dev, tree.B * tree.T_max)
-    acc, path, toks, nkl = _walk_outputs(tree.B, max_path, dev)
+    acc, path, toks, nkl = _walk_outputs(tree.B, max_path, dev, stream)
     _call("dreams_accept_path", dev, _ptr(argmax), ctypes.byref(tree._c), max_path, _ptr(acc), _ptr(path),
           _ptr(toks), _ptr(nkl), _status(status, dev), _stream(stream, dev))
     return {"accept_len": acc, "path": path, "out_tokens": toks, "new_kv_len": nkl}
@@ -586,7 +598,7 @@ def verify_step(logits: torch.Tensor, tree: Tree, kv: KVCache, max_path: int,
     V = int(logits.shape[2])
     if argmax_out is not None:
         _need_out(argmax_out, "argmax_out", torch.int32, dev, tree.B * tree.T_max)
-    acc, path, toks, nkl = _outputs(outputs, tree.B, max_path, dev)
+    acc, path, toks, nkl = _outputs(outputs, tree.B, max_path, dev, stream)
     st = _status(status, dev)
     _cache_covers(kv, tree.B)
     need = verify_step_workspace_size(tree, V)
@@ -619,7 +631,7 @@ def verify_step_sampled(logits: torch.Tensor, tree: Tree, kv: KVCache, max_path:
     V = int(logits.shape[2])
     if sample_out is not None:
         _need_out(sample_out, "sample_out", torch.int32, dev, tree.B * tree.T_max)
-    acc, path, toks, nkl = _outputs(outputs, tree.B, max_path, dev)
+    acc, path, toks, nkl = _outputs(outputs, tree.B, max_path, dev, stream)
     st = _status(status, dev)
     _cache_covers(kv, tree.B)
     need = verify_step_sampled_workspace_size(tree, V)
@@ -658,7 +670,7 @@ def verify_step_speculative(target_logits: torch.Tensor, draft_logits: torch.Ten
         if tuple(t.shape) != (tree.B, tree.T_max):
             raise ValueError(f"{n} must be [B, T_max]")
     V = int(target_logits.shape[2])
-    acc, path, toks, nkl = _outputs(outputs, tree.B, max_path, dev)
+    acc, path, toks, nkl = _outputs(outputs, tree.B, max_path, dev, stream)
     st = _status(status, dev)
     _cache_covers(kv, tree.B)
     _call("dreams_verify_step_speculative", dev,
@@ -775,14 +787,14 @@ def window_attention(q: torch.Tensor, kv: KVCache, q_len: torch.Tensor, kv_len: 
             raise ValueError("parent must be [B, T_max]")
         par = parent.data_ptr()
     if out is None:
-        out = torch.empty((B, T_max, Hq, D), dtype=torch.bfloat16, device=dev)
+        out = _new((B, T_max, Hq, D), torch.bfloat16, dev, stream)
     else:
         _need(out, "out", torch.bfloat16, dev)
         if out.shape != q.shape:
             raise ValueError("out must have q's shape")
     if lse is None:
         if want_lse:
-            lse = torch.empty((B, T_max, Hq), dtype=torch.float32, device=dev)
+            lse = _new((B, T_max, Hq), torch.float32, dev, stream)
     else:
         _need(lse, "lse", torch.float32, dev)
         if lse.shape != q.shape[:3]:
@@ -821,7 +833,7 @@ def kv_fork(pool: PagePool, parent: torch.Tensor, kv_len: torch.Tensor, new_kv_l
     dev = pool.refcount.device
     par, kl = _per_seq(parent, "parent", pool.B, dev), _per_seq(kv_len, "kv_len", pool.B, dev)
     if new_kv_len is None:
-        new_kv_len = torch.empty(pool.B, dtype=torch.int32, device=dev)
+        new_kv_len = _new(pool.B, torch.int32, dev, stream)
     ws, ws_bytes = _scratch(pool, workspace, dev, stream)
     _launch("dreams_kv_fork", dev, stream, ctypes.byref(pool.kv._c), ctypes.byref(pool._c), par, kl,
             _per_seq(new_kv_len, "new_kv_len", pool.B, dev), ws, ws_bytes, _status(status, dev))
@@ -868,7 +880,7 @@ def kv_prune(kv: KVCache, keep: torch.Tensor, v0: int, n_vis: int, kv_len: torch
             raise ValueError("refcount goes with a paged cache")
         _need_out(refcount, "refcount", torch.int32, dev, kv.num_pages)
     if new_kv_len is None:
-        new_kv_len = torch.empty(B, dtype=torch.int32, device=dev)
+        new_kv_len = _new(B, torch.int32, dev, stream)
     _launch("dreams_kv_prune", dev, stream, ctypes.byref(kv._c), B, keep.data_ptr() if r else None, v0, n_vis, r, kl,
             None if refcount is None else refcount.data_ptr(), _per_seq(new_kv_len, "new_kv_len", B, dev),
             _status(status, dev))

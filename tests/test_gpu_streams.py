@@ -61,6 +61,29 @@ def test_page_calls_beside_a_busy_stream(dreams, B, P):
         p.same()
 
 
+def test_results_beside_a_busy_stream(dreams):
+    """The results that the calls make themselves."""
+    g = torch.Generator().manual_seed(1)
+    side = torch.cuda.Stream()
+    p = Pool(dreams, 40, 6, 300, Hkv=2, D=64, seed=9)
+    lens = p.rng.integers(80, 64 * 6 - 2, 40).astype(np.int32)
+    p.reserve(np.zeros(40, np.int32), lens + 2)
+    for x in (p.gk, p.gv):
+        x.copy_(torch.randn(x.shape, generator=g).to(torch.bfloat16))
+    q = torch.randn((40, 2, 8, 64), generator=g).to(torch.bfloat16).cuda()
+    gl, two, keep = i32(lens), i32(np.full(40, 2)), i32(np.tile(np.arange(5, 35), (40, 1)))
+    ref, ref_lse = dreams.window_attention(q, p.kv, two, gl, 0.125, 100, 3, want_lse=True)
+    for _ in range(4):
+        torch.cuda.synchronize()
+        held = busy(5)
+        out, lse = dreams.window_attention(q, p.kv, two, gl, 0.125, 100, 3, want_lse=True, stream=side)
+        new = dreams.kv_prune(dreams.KVCache(p.gk.clone(), p.gv.clone(), p.gt), keep, 5, 70, gl, stream=side)
+        side.synchronize()
+        assert torch.equal(out, ref) and torch.equal(lse, ref_lse)
+        assert torch.equal(new, gl - 40)
+        del held
+
+
 def test_pools_of_two_threads(dreams):
     """Each thread has a pool and a stream of its own."""
     errors = []

@@ -16,6 +16,10 @@ CUDA = torch.device("cuda", 0)
 class OnGpu(torch.Tensor):
     """A CPU tensor that says it is on the GPU."""
     device = CUDA
+    recorded = ()
+
+    def record_stream(self, s):
+        self.recorded += (s.cuda_stream,)
 
 
 def gpu(t):
@@ -29,12 +33,15 @@ class World:
         libbuild.build()
         dreams._lib()
         self.now, self.made, self.calls = self.MAIN, {}, []
+        self.empties = []  # the tensors made without a fill
         empty, zeros = torch.empty, torch.zeros
 
         def make(real):
             def f(*shape, device=None, **kw):
                 t = gpu(real(*shape, **kw))
                 self.made[t.data_ptr()] = self.now
+                if real is empty:
+                    self.empties.append((t, self.now))
                 return t
             return f
 
@@ -109,3 +116,43 @@ def test_a_callers_workspace_is_used(world, call):
     CALLS[call](p, i, workspace=mine, stream=world.side(22))
     at, n = world.workspace()
     assert (at if isinstance(at, int) else at.value) == mine.data_ptr() and n == mine.numel() * 4
+
+
+def _results(world):
+    """Every call that makes its results, as functions of the stream."""
+    z = lambda *s, dt=torch.bfloat16: gpu(torch.Tensor(*s).to(dt).zero_())  # noqa: E731
+    f, i = (lambda *s: z(*s, dt=torch.float32)), (lambda *s: z(*s, dt=torch.int32))
+    p, q, two, logits = world.pool(), z(2, 3, 4, 64), i(2), f(2, 3, 40)
+    tree = dreams.Tree(i(2, 3), i(2, 3), two, two)
+    p._by_stream.update({world.MAIN: i(1000), 22: i(1000)})
+    return {
+        "window_attention": lambda s: dreams.window_attention(q, p.kv, two, two, 0.1, 8, want_lse=True, stream=s),
+        "kv_fork": lambda s: dreams.kv_fork(p, two, two, stream=s),
+        "kv_prune": lambda s: dreams.kv_prune(p.kv, i(2, 3), 0, 4, two, stream=s),
+        "tree_verify_attn": lambda s: dreams.tree_verify_attn(q, p.kv, tree, 0.1, want_lse=True, stream=s),
+        "attention": lambda s: dreams.attention(q, p.kv, two, two, 0.1, dreams.ATTN_CAUSAL, want_lse=True, want_entropy=True, stream=s),
+        "vocab_argmax": lambda s: dreams.vocab_argmax(logits, stream=s),
+        "vocab_sample": lambda s: dreams.vocab_sample(logits, 1.0, f(6), stream=s),
+        "lm_head_argmax": lambda s: dreams.lm_head_argmax(z(3, 64), z(40, 64), want_max=True, stream=s),
+        "visual_importance": lambda s: dreams.visual_importance(f(2, 2, 3, 9), 1, 5, 2, stream=s),
+        "accept_path": lambda s: dreams.accept_path(i(2, 3), tree, 2, stream=s),
+        "verify_step": lambda s: dreams.verify_step(logits, tree, p.kv, 2, stream=s),
+        "verify_step_sampled": lambda s: dreams.verify_step_sampled(logits, tree, p.kv, 2, 1.0, f(2, 3), stream=s),
+        "verify_step_speculative": lambda s: dreams.verify_step_speculative(logits, logits, tree, p.kv, 2, 1.0, f(2, 3), f(2, 3), stream=s)}
+
+
+RESULTS = {"window_attention": 2, "kv_fork": 1, "kv_prune": 1, "tree_verify_attn": 2, "attention": 3, "vocab_argmax": 1, "vocab_sample": 1,
+           "lm_head_argmax": 2, "visual_importance": 2, "accept_path": 4, "verify_step": 4, "verify_step_sampled": 4, "verify_step_speculative": 4}
+
+
+@pytest.mark.parametrize("name", RESULTS)
+def test_results_belong_to_the_stream_of_the_call(world, name):
+    """Made under the call's stream, and held back for the current one, which reads them."""
+    call = _results(world)[name]
+    for s, handle in ((None, world.MAIN), (world.side(22), 22)):
+        world.empties.clear()
+        call(s)
+        assert len(world.empties) == RESULTS[name]
+        for t, under in world.empties:
+            assert under == handle
+            assert t.recorded == (() if s is None else (world.MAIN,))
