@@ -22,7 +22,7 @@ import os
 import re
 import threading
 from dataclasses import dataclass
-from typing import Dict, Optional, Tuple
+from typing import Dict, List, Optional, Tuple
 
 import torch
 
@@ -307,8 +307,11 @@ class Tree:
 
 
 # Zero-filled workspaces, one per (function, device, stream); the kernels
-# leave them zero-filled after each call.
+# leave them zero-filled after each call. One that has become too small is kept
+# (a captured graph may have its address); each new one is at least twice as
+# large, so that all of them together are less than twice the last.
 _WS: Dict[Tuple[str, int, int], torch.Tensor] = {}
+_WS_OUTGROWN: List[torch.Tensor] = []
 
 
 def _workspace(kind: str, nbytes: int, device: torch.device, stream) -> Optional[torch.Tensor]:
@@ -318,7 +321,11 @@ def _workspace(kind: str, nbytes: int, device: torch.device, stream) -> Optional
            (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
     ws = _WS.get(key)
     if ws is None or ws.numel() < nbytes:
-        ws = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        if ws is not None:
+            _WS_OUTGROWN.append(ws)
+            nbytes = max(nbytes, 2 * ws.numel())
+        with torch.cuda.stream(stream):  # filled on the stream that uses it
+            ws = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         _WS[key] = ws
     return ws
 

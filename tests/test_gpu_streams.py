@@ -84,6 +84,21 @@ def test_results_beside_a_busy_stream(dreams):
         del held
 
 
+def test_argmax_beside_a_busy_stream(dreams):
+    """Its workspace has to be zero-filled when it runs, on a stream that has made none yet too."""
+    g = torch.Generator().manual_seed(2)
+    for rows in (7, 80, 300):
+        logits = torch.randn((rows, 50000), generator=g).cuda()
+        arg = torch.argmax(logits, 1).to(torch.int32)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        held = busy(5)
+        top = dreams.vocab_argmax(logits, stream=side)
+        side.synchronize()
+        assert torch.equal(top, arg)
+        del held
+
+
 def test_pools_of_two_threads(dreams):
     """Each thread has a pool and a stream of its own."""
     errors = []

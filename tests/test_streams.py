@@ -33,15 +33,14 @@ class World:
         libbuild.build()
         dreams._lib()
         self.now, self.made, self.calls = self.MAIN, {}, []
-        self.empties = []  # the tensors made without a fill
+        self.empties, self.fills = [], []  # the tensors made without a fill, and with one
         empty, zeros = torch.empty, torch.zeros
 
         def make(real):
             def f(*shape, device=None, **kw):
                 t = gpu(real(*shape, **kw))
                 self.made[t.data_ptr()] = self.now
-                if real is empty:
-                    self.empties.append((t, self.now))
+                (self.empties if real is empty else self.fills).append((t, self.now))
                 return t
             return f
 
@@ -59,6 +58,7 @@ class World:
         patch.setattr(dreams, "_launch", lambda name, dev, stream, *a: self.calls.append((name, stream, a)))
         patch.setattr(dreams, "_call", lambda name, dev, *a: self.calls.append((name, None, a)))
         patch.setattr(dreams, "_WS", {})
+        patch.setattr(dreams, "_WS_OUTGROWN", [], raising=False)
 
     def side(self, handle):
         return types.SimpleNamespace(cuda_stream=handle, device=CUDA)
@@ -131,7 +131,7 @@ def _results(world):
         "kv_prune": lambda s: dreams.kv_prune(p.kv, i(2, 3), 0, 4, two, stream=s),
         "tree_verify_attn": lambda s: dreams.tree_verify_attn(q, p.kv, tree, 0.1, want_lse=True, stream=s),
         "attention": lambda s: dreams.attention(q, p.kv, two, two, 0.1, dreams.ATTN_CAUSAL, want_lse=True, want_entropy=True, stream=s),
-        "vocab_argmax": lambda s: dreams.vocab_argmax(logits, stream=s),
+        "vocab_argmax": lambda s: dreams.vocab_argmax(f(3, 300000), stream=s),
         "vocab_sample": lambda s: dreams.vocab_sample(logits, 1.0, f(6), stream=s),
         "lm_head_argmax": lambda s: dreams.lm_head_argmax(z(3, 64), z(40, 64), want_max=True, stream=s),
         "visual_importance": lambda s: dreams.visual_importance(f(2, 2, 3, 9), 1, 5, 2, stream=s),
@@ -156,3 +156,28 @@ def test_results_belong_to_the_stream_of_the_call(world, name):
         for t, under in world.empties:
             assert under == handle
             assert t.recorded == (() if s is None else (world.MAIN,))
+
+
+@pytest.mark.parametrize("name", ["vocab_argmax", "vocab_sample", "lm_head_argmax", "visual_importance", "verify_step", "verify_step_sampled"])
+def test_zero_filled_workspaces_are_filled_on_the_stream_of_the_call(world, name):
+    call = _results(world)[name]
+    for s, handle in ((None, world.MAIN), (world.side(22), 22)):
+        world.fills.clear()
+        call(s)
+        assert [under for _, under in world.fills] == [handle]
+        call(s)  # kept, and left zero-filled by the kernels
+        assert len(world.fills) == 1
+
+
+def test_an_outgrown_workspace_is_kept(world):
+    """A captured call has its address. They do not pile up: each is at least twice as large as the one before."""
+    sizes, kept = [], []
+    for rows in (3, 5, 9, 40, 41, 42, 43, 200, 201):
+        world.fills.clear()
+        dreams.vocab_argmax(gpu(torch.Tensor(rows, 300000).zero_()))
+        for t, _ in world.fills:
+            sizes.append(t.numel())
+            kept.append(t.data_ptr())
+    alive = [t.data_ptr() for t in list(dreams._WS.values()) + dreams._WS_OUTGROWN]
+    assert sorted(alive) == sorted(kept) and len(kept) > 1
+    assert all(b >= 2 * a for a, b in zip(sizes, sizes[1:]))
