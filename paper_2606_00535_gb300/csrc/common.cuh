@@ -39,7 +39,8 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 // Kernels launched with this attribute are set up while the one before them in the
 // stream ends; they start with after_previous(), before their first access to global
-// memory.
+// memory. They read it with ordinary loads: __ldg is for data that nothing writes while
+// the kernel lives, and the kernel before may still be writing when this one begins.
 inline cudaLaunchAttribute early_launch() {
   cudaLaunchAttribute a = {};
   a.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -38,7 +38,7 @@ struct Cache {
 // 16-byte offset of slot s of sequence b within a layer; -1: no page.
 __device__ __forceinline__ int64_t slot16(const Cache &c, int b, int s) {
   if (c.table == nullptr) return (int64_t(b) * c.capacity + s) * c.row16;
-  const int pg = __ldg(c.table + int64_t(b) * c.P + (s >> 6));
+  const int pg = c.table[int64_t(b) * c.P + (s >> 6)];
   if (pg < 0 || pg >= c.num_pages) return -1;
   return (int64_t(pg) * PAGE + (s & (PAGE - 1))) * c.row16;
 }
@@ -112,7 +112,7 @@ struct RowSpan {
   int e0, e1, bad;  // the entries that the new tokens touch
 };
 __device__ __forceinline__ RowSpan row_span(const Pool &p, const int32_t *kv_len, const int32_t *n_new, int b) {
-  const int64_t L = __ldg(kv_len + b), n = __ldg(n_new + b);
+  const int64_t L = kv_len[b], n = n_new[b];
   if (L < 0 || n < 0 || L + n > int64_t(p.P) * PAGE) return {0, 0, DREAMS_DATA_BAD_KV_LEN};
   return {int(L / PAGE), n > 0 ? int((L + n + PAGE - 1) / PAGE) : int(L / PAGE), 0};
 }
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(256) kv_release_kernel(const Pool p, const int
   after_previous();
   const int b = blockIdx.y;
   const int e = blockIdx.x * 256 + threadIdx.x;
-  const int64_t lo = __ldg(begin + b), hi = __ldg(end + b);
+  const int64_t lo = begin[b], hi = end[b];
   if (lo < 0 || hi > int64_t(p.P) * PAGE) {
     if (e == 0) flag(status, DREAMS_DATA_BAD_KV_LEN);
     return;
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
   {
     int bad = 0;
     for (int i = threadIdx.x; i < p.B; i += BOOK_THREADS) {
-      int q = __ldg(parent + i);
+      int q = parent[i];
       if (q < -1 || q >= p.B) {
         bad |= DREAMS_DATA_BAD_INDEX;
         q = -1;
@@ -474,8 +474,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const Cache c, const uin
                                                         const int32_t *n_new, int T_max, int32_t *status) {
   after_previous();
   const int b = blockIdx.y;
-  const int n = __ldg(n_new + b);
-  const int64_t L = __ldg(kv_len + b);
+  const int n = n_new[b];
+  const int64_t L = kv_len[b];
   if (n < 0 || n > T_max || L < 0 || L + n > c.capacity) {
     if (blockIdx.x == 0 && threadIdx.x == 0) flag(status, DREAMS_DATA_BAD_KV_LEN);
     return;
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(PRUNE_THREADS, 1) kv_prune_kernel(const Cache 
   const int b = blockIdx.y;
   const int blk = blockIdx.x % nblk, rest = blockIdx.x / nblk;
   const bool reporter = blockIdx.x == 0 && threadIdx.x == 0;
-  const int L = __ldg(kv_len + b);
+  const int L = kv_len[b];
   const int32_t *list = keep + int64_t(b) * r;
   __shared__ int s_bad;
   if (threadIdx.x == 0) s_bad = 0;
@@ -543,15 +543,15 @@ __global__ void __launch_bounds__(PRUNE_THREADS, 1) kv_prune_kernel(const Cache 
     bad = DREAMS_DATA_BAD_KV_LEN;
   } else {
     for (int i = threadIdx.x; i < r; i += threads) {
-      const int s = __ldg(list + i), before = i ? __ldg(list + i - 1) : v0 - 1;
+      const int s = list[i], before = i ? list[i - 1] : v0 - 1;
       if (s <= before || s >= v0 + n_vis) bad |= DREAMS_DATA_BAD_INDEX;
       if (i < PRUNE_LIST) s_list[i] = s;
     }
     if (c.table != nullptr)
       for (int e = v0 / PAGE + int(threadIdx.x); int64_t(e) * PAGE < L; e += threads) {
-        const int pg = __ldg(c.table + int64_t(b) * c.P + e);
+        const int pg = c.table[int64_t(b) * c.P + e];
         if (pg < 0 || pg >= c.num_pages) bad |= DREAMS_DATA_BAD_PAGE;
-        else if (ref != nullptr && __ldg(ref + pg) != 1) bad |= DREAMS_DATA_SHARED_PAGE;
+        else if (ref != nullptr && ref[pg] != 1) bad |= DREAMS_DATA_SHARED_PAGE;
         if (e - v0 / PAGE < PRUNE_PAGES) s_page[e - v0 / PAGE] = pg;
       }
   }

@@ -91,7 +91,7 @@ __device__ __forceinline__ bool load_rows(const WinParams &p, RowsShared &sh, in
   if (p.parent != nullptr) {
     int bad = 0;
     for (int i = tid; i < T; i += 32 * WARPS) {
-      const int par = __ldg(p.parent + int64_t(b) * p.T_max + i);
+      const int par = p.parent[int64_t(b) * p.T_max + i];
       sh.par[i] = par;
       bad |= i == 0 ? par != -1 : (par < 0 || par >= i);
     }
@@ -132,7 +132,7 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
   auto look = [&](int j) {
     const int i = i0 + (warp + j * WARPS) * KT + (lane & 15);
     nslot = j < my && i < i1 ? kl.slot(i) : -1;
-    if (p.table != nullptr && nslot >= 0) npage = __ldg(p.table + int64_t(b) * p.P + (nslot >> 6));
+    if (p.table != nullptr && nslot >= 0) npage = p.table[int64_t(b) * p.P + (nslot >> 6)];
   };
   // Copies of 16 bytes: lanes CH to a key, 32 / CH keys at a time. A key is known by
   // its row (slot and page, without the head): below 2^32 in any memory.
@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
   const int g = x % p.Hkv, b = x / p.Hkv;
   if (p.nsplit > 1) cluster_arrive();  // this CTA runs: it may be written to
   after_previous();
-  const int T = __ldg(p.q_len + b), L = __ldg(p.kv_len + b);
+  const int T = p.q_len[b], L = p.kv_len[b];
   const bool report = split == 0 && g == 0;
   int bad = 0;
   if (T < 0 || T > p.T_max) bad = DREAMS_DATA_BAD_TREE_LEN;

@@ -158,8 +158,8 @@ __device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bo
   const int turn = P.heads.div(x), blk = P.nblk - 1 - turn, bg = x - turn * int(P.heads.d);
   it.b = P.hkv.div(bg);
   it.g = bg - it.b * p.Hkv;
-  it.T = lens != nullptr ? lens->x : __ldg(p.q_len + it.b);
-  it.L = lens != nullptr ? lens->y : __ldg(p.kv_len + it.b);
+  it.T = lens != nullptr ? lens->x : p.q_len[it.b];
+  it.L = lens != nullptr ? lens->y : p.kv_len[it.b];
   it.nb = it.n = it.ns = 0;
   report = report && it.g == 0 && blk == 0;
   if (it.T < 0 || it.T > p.T_max) {
@@ -354,7 +354,7 @@ __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, i
     if (p.table == nullptr) {
       at = (int64_t(b) * p.capacity + s) * p.Hkv + g;
     } else {
-      const int pg = __ldg(p.table + int64_t(b) * p.P + (s >> 6));
+      const int pg = p.table[int64_t(b) * p.P + (s >> 6)];
       at = pg >= 0 && pg < p.num_pages ? (int64_t(pg) * 64 + (s & 63)) * p.Hkv + g : -1;
     }
     float x = 0.f, v[E];
@@ -452,11 +452,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   int early[2] = {-1, -1};
   if constexpr (!PAIR) {
     const int x = P.nsplit.div(int(blockIdx.x)), b = P.hkv.div(x - P.heads.div(x) * int(P.heads.d));
-    lens = make_int2(__ldg(p.q_len + b), __ldg(p.kv_len + b));
+    lens = make_int2(p.q_len[b], p.kv_len[b]);
     if (p.parent != nullptr && warp < 8) {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-        if (lane + 32 * k < p.T_max) early[k] = __ldg(p.parent + int64_t(b) * p.T_max + lane + 32 * k);
+        if (lane + 32 * k < p.T_max) early[k] = p.parent[int64_t(b) * p.T_max + lane + 32 * k];
     }
   }
   tc::fence_before_sync();
@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         int bad = 0;
         if (p.parent != nullptr) {
           for (int i = lane; i < it.T; i += 32) {
-            const int q = PAIR ? __ldg(p.parent + int64_t(it.b) * p.T_max + i) : i < 32 ? early[0] : early[1];
+            const int q = PAIR ? p.parent[int64_t(it.b) * p.T_max + i] : i < 32 ? early[0] : early[1];
             s_par[warp][i] = int8_t(q);  // (a bad one is not used)
             bad |= i == 0 ? q != -1 : (q < 0 || q >= i);
           }
@@ -809,7 +809,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           auto fetch = [&](int j, int h) {
             if (row == nullptr || j >= j1 || 2 * j + h >= it.np) return 0;
             const int pi = it.slot0(2 * j + h) >> 6;
-            return pi < p.P ? __ldg(row + pi) : -1;
+            return pi < p.P ? row[pi] : -1;
           };
           int pg0 = fetch(j0, 0), pg1 = fetch(j0, 1);
           for (int j = j0; j < j1 && ok; ++j) {
