@@ -287,28 +287,26 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // Waiting for what has happened takes half as long without the hint (135 clocks
-// against 270), and an MMA
-// issuer does it four times a tile.
+// against 270), and an MMA issuer does it four times a tile.
 __device__ __forceinline__ bool quick(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// The limit is one without progress: rows that a warp does again key by key (watch[BEAT]
-// counts on) may take longer than that, and the CTA's other warps wait for them.
-constexpr int ABORT = 0, BEAT = 1;
-__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int *watch, uint64_t limit_ns) {
-  if (quick(bar, parity)) return true;
+// The limit is one without progress: rows that a warp does again key by key may take
+// longer than that, and the CTA's other warps wait for them. `beat` is the last time that
+// such a warp gave. The loop is out of line, as few waits outlast the first two tries.
+__device__ __noinline__ bool patient(uint32_t bar, uint32_t parity, volatile int *abort, volatile int64_t *beat, uint64_t limit_ns) {
   uint64_t t0 = 0;
-  int beat = 0;
   for (;;) {
     if (try_wait(bar, parity)) return true;
     const uint64_t now = tc::global_ns();
-    const int b = watch[BEAT];
-    if (t0 == 0 || b != beat) t0 = now;
-    beat = b;
-    if (watch[ABORT] || now - t0 > limit_ns) return false;
+    if (t0 == 0) t0 = now;
+    if (*abort || (now - t0 > limit_ns && int64_t(now) - *beat > int64_t(limit_ns))) return false;
   }
+}
+__device__ __forceinline__ bool long_wait(uint32_t bar, uint32_t parity, volatile int *abort, volatile int64_t *beat, uint64_t limit_ns) {
+  return quick(bar, parity) || try_wait(bar, parity) || patient(bar, parity, abort, beat, limit_ns);
 }
 __device__ __forceinline__ void st_global_v8(void *p, const uint32_t *v) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
@@ -329,12 +327,12 @@ struct Row {
 
 // One row by a whole warp, straight from the definition: used when a tile with
 // partly masked columns held an infinity or a NaN in V (0 x inf would reach rows
-// that do not see it), and when a row's sum outgrew its reference. Slow (0.61 us a key,
-// a chain of page entry, K, five shuffles and exponentials), and rare; `beat` is counted
-// on while it lasts.
+// that do not see it), and when a row's sum outgrew its reference. Slow (0.58 us a key,
+// a chain of page entry, K, five shuffles and exponentials), and rare; `beat` is given the
+// time while it lasts.
 template <int D>
 __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, int t, int h, int off, unsigned long long anc,
-                                      int *beat) {
+                                      volatile int64_t *beat) {
   const int lane = threadIdx.x & 31;
   constexpr int E = D / 32;
   float q[E], o[E];
@@ -347,7 +345,7 @@ __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, i
   const KeyList kl = key_list(p, L, p.parent != nullptr ? 0 : t, t);
   float m = -INFINITY, l = 0.f;
   for (int i = 0; i < kl.n; ++i) {
-    if ((i & 63) == 0 && lane == 0) atomicAdd(beat, 1);
+    if ((i & 63) == 0 && lane == 0) *beat = int64_t(tc::global_ns());
     const int s = kl.slot(i);
     if (!sees(p, L, off, anc, s)) continue;
     int64_t at;
@@ -384,6 +382,20 @@ __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, i
   if (lane == 0 && p.lse != nullptr) p.lse[row] = (m + log2f(l)) * LN2;
 }
 
+// Does this thread's row of O hold an infinity or a NaN? By a whole warp.
+template <int D>
+__device__ __noinline__ bool overflowed(uint32_t o_at) {
+  uint32_t odd = 0;
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t ov[32];
+    tc::tmem_ld32(o_at + c * 32, ov);
+    tc::tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) odd |= uint32_t((ov[e] & 0x7f800000u) == 0x7f800000u);
+  }
+  return odd != 0u;
+}
 
 template <int D, bool PAIR>
 __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_constant__ TcParams P) {
@@ -396,8 +408,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST], bar_ready[NST];
   __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_r[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_watch[2], s_zero, s_dirty[SEEN];
-  int &s_abort = s_watch[ABORT];
+  __shared__ int s_abort, s_zero, s_dirty[SEEN];
+  __shared__ int64_t s_beat;
   __shared__ int8_t s_par[8][64];
   __shared__ Slot s_slot[8];
   __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
@@ -433,7 +445,8 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     }
     if (lane == 18) {
       tc::mbar_init(never, 1);  // nothing arrives on it
-      s_watch[ABORT] = s_watch[BEAT] = s_zero = 0;
+      s_abort = s_zero = 0;
+      s_beat = 0;
     }
     tc::fence_barrier_init();
     if (lane == 0) {
@@ -464,14 +477,13 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   tc::fence_after_sync();
   const uint32_t tmem = s_tmem;
   volatile int *abort_flag = &s_abort;
-  const uint64_t wait_ns = P.wait_ns;
   auto give_up = [&]() {
     if (*abort_flag == 0) {
       *abort_flag = 1;
       flag(p.status, DREAMS_DATA_TIMEOUT);
     }
   };
-  auto wait = [&](uint32_t bar, uint32_t parity) { return long_wait(bar, parity & 1u, s_watch, wait_ns); };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return long_wait(bar, parity & 1u, abort_flag, &s_beat, P.wait_ns); };
 
   // The items of this CTA; without PAIR it has one, shared by a cluster.
   const int nsplit = PAIR ? 1 : p.nsplit;
@@ -725,29 +737,20 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         ++oc;
         tc::fence_after_sync();
         if (ok) arrive_if(empty0 + 8 * v1, lead);
+        ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
       }
-      if (any) ok = ok && __all_sync(0xffffffffu, wait(scan0 + 8 * (seq % SEEN), uint32_t(seq / SEEN)));
       if (!ok) break;
       if (PAIR) pos.move(ahead);
-      const bool dirty = any && *reinterpret_cast<volatile int *>(&s_dirty[seq % SEEN]) != 0;
+      const bool dirty = *reinterpret_cast<volatile int *>(&s_dirty[seq % SEEN]) != 0;  // (of use where `any`)
       ++seq;
 
       const bool real = row < sp->rows, tree_ok = sp->bad == 0;
       if constexpr (PAIR) {
         const int h = sp->g * p.G + row - (t - sp->t0) * p.G;
-        uint32_t again = __ballot_sync(0xffffffffu, any && real && (dirty || l > MOST_SUM));
-        const bool risky = any && real && l > SAFE_SUM;
-        if (__builtin_expect(__any_sync(0xffffffffu, risky), 0)) {
-          uint32_t odd = 0;  // does O hold an infinity or a NaN?
-#pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t ov[32];
-            tc::tmem_ld32(tl + C::O_COL + c * 32, ov);
-            tc::tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) odd |= uint32_t((ov[e] & 0x7f800000u) == 0x7f800000u);
-          }
-          again |= __ballot_sync(0xffffffffu, risky && odd != 0u);
+        uint32_t again = __ballot_sync(0xffffffffu, any && real && (dirty || l > SAFE_SUM));
+        if (__builtin_expect(again != 0u, 0)) {
+          const bool odd = overflowed<D>(tl + C::O_COL);
+          again &= __ballot_sync(0xffffffffu, dirty || l > MOST_SUM || odd);
         }
         if (any && tree_ok) {
           const float inv = 1.f / l;
@@ -779,7 +782,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           for (int i = 0; i < 32; ++i) {
             const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, r.off, i), hi = __shfl_sync(0xffffffffu, h, i);
             const unsigned long long ai = __shfl_sync(0xffffffffu, r.anc, i);
-            if ((again >> i) & 1u) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai, &s_watch[BEAT]);
+            if ((again >> i) & 1u) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai, &s_beat);
           }
         }
         tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
@@ -829,7 +832,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
             for (int kv = 0; kv < 2 && ok; ++kv) {
               if (kv == 0 && P.stall_at >= 0 && ktiles >= P.stall_at) {
                 // test hook: this copy is never issued
-                tc::mbar_wait(never, 0, abort_flag, wait_ns);
+                tc::mbar_wait(never, 0, abort_flag, P.wait_ns);
                 ok = false;
                 break;
               }
@@ -1116,7 +1119,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         if (off < 0) continue;  // a malformed tree
         const int h = it.g * p.G + row - (t - it.t00) * p.G;
         if (again || __any_sync(0xffffffffu, ml.y > MOST_SUM)) {
-          slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_watch[BEAT]);
+          slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
           continue;
         }
         const uint32_t some = __ballot_sync(0xffffffffu, ml.y != 0.f);
@@ -1153,7 +1156,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           // (a sum of 0 x O is zero, or NaN)
           const float odd = 0.f * acc.x + 0.f * acc.y + 0.f * acc.z + 0.f * acc.w;
           if (__any_sync(0xffffffffu, odd != 0.f)) {  // (also where it is NaN)
-            slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_watch[BEAT]);
+            slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
             continue;
           }
         }
