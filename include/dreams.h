@@ -478,7 +478,9 @@ dreams_status_t dreams_kv_reserve(const dreams_page_pool_t *pool, const int32_t 
  * the new length, end = capacity) and the end of a sequence (0, capacity) are all
  * this call. begin[b] >= end[b] gives nothing back; begin[b] < 0 or end[b] >
  * capacity is flagged BAD_KV_LEN and skips the sequence, an entry outside
- * [-1, num_pages) is flagged BAD_PAGE and stays. One launch.
+ * [-1, num_pages) is flagged BAD_PAGE and stays. An entry whose page has count 0
+ * (or has it once the call's other entries are taken off) is flagged BAD_PAGE and
+ * becomes -1, while the count stays 0. One launch.
  */
 dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, const int32_t *begin, const int32_t *end,
                                   int32_t *status_word, dreams_stream_t stream);

@@ -98,7 +98,10 @@ def release(table, ref, begin, end):
             if table[b, e] < 0 or table[b, e] >= len(ref):
                 flags |= BAD_PAGE
                 continue
-            ref[table[b, e]] -= 1
+            if ref[table[b, e]] > 0:
+                ref[table[b, e]] -= 1
+            else:
+                flags |= BAD_PAGE
             table[b, e] = -1
     return table, ref, flags
 

@@ -213,8 +213,11 @@ __global__ void __launch_bounds__(256) kv_release_kernel(const Pool p, const int
     flag(status, DREAMS_DATA_BAD_PAGE);
     return;
   }
-  atomicSub(p.ref + pg, 1);
   *at = -1;
+  if (atomicSub(p.ref + pg, 1) <= 0) {  // a page that by its count nobody holds: the count stays
+    atomicAdd(p.ref + pg, 1);
+    flag(status, DREAMS_DATA_BAD_PAGE);
+  }
 }
 
 // ------------------------------------------------------------------ fork
