@@ -414,7 +414,8 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
  *     lse[b, t, h]    = log sum_s exp(scale * <q, K[b, s, g]>)    (may be NULL)
  * over the slots s it sees; every query sees itself. window >= 1, sinks >= 0; a
  * window of at least kv_len + q_len is plain causal (tree) attention. q, out,
- * lse, layer and scale as for dreams_attention, 1 <= T_max <= 2^20. q_len[b] in
+ * lse, layer and scale as for dreams_attention, 1 <= T_max <= 2^20; q_stride_t is
+ * ignored when T_max == 1. q_len[b] in
  * [0, T_max]: 0 is an idle sequence (nothing is read or written). Rows
  * t >= q_len[b] of out and lse are left untouched, as are the rows of a sequence
  * with bad lengths or a bad tree.
@@ -511,9 +512,9 @@ dreams_status_t dreams_kv_fork(const dreams_kv_cache_t *kv, const dreams_page_po
  * for t < n_new[b]. k_new, v_new: bf16, element (b, t, g, d) at b * stride_b +
  * t * stride_t + g * D + d (so views of a fused projection; the same strides for
  * both, multiples of 8 elements, stride_t >= Hkv * D; stride_b is ignored when
- * B == 1), 16-byte aligned, n_new[b] in [0, T_max]. Bad lengths skip the sequence
- * (BAD_KV_LEN), a slot whose page is missing is skipped (BAD_PAGE). The rows do
- * not overlap the cache. One launch.
+ * B == 1, stride_t when T_max == 1), 16-byte aligned, n_new[b] in [0, T_max].
+ * Bad lengths skip the sequence (BAD_KV_LEN), a slot whose page is missing is
+ * skipped (BAD_PAGE). The rows do not overlap the cache. One launch.
  */
 dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t layer, const void *k_new, const void *v_new,
                                  int64_t stride_b, int64_t stride_t, const int32_t *kv_len, const int32_t *n_new,

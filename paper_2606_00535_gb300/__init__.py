@@ -355,13 +355,15 @@ def _cache_covers(kv: "KVCache", B: int, D: Optional[int] = None) -> None:
 def _q_strides(q: torch.Tensor, name: str = "q", heads: str = "Hq") -> Tuple[int, int]:
     """(sequence stride, token stride) in elements of a bf16 [B, T, Hq, D]
     query tensor whose head rows are dense (a view into a fused QKV output
-    qualifies)."""
+    qualifies). The strides of dimensions of one token, head or column say
+    nothing, and are not looked at."""
     if not isinstance(q, torch.Tensor) or q.dtype != torch.bfloat16 or q.dim() != 4:
         raise TypeError(f"{name} must be a 4-D bfloat16 tensor [B, T, {heads}, D]")
     sb, st, sh, sd = q.stride()
-    if sd != 1 or sh != q.shape[3]:
+    _, T, H, D = q.shape
+    if (sd != 1 and D > 1) or (sh != D and H > 1):
         raise ValueError(f"{name}'s head rows must be dense (strides [.., .., D, 1])")
-    return sb, st
+    return sb, st if T > 1 else H * D
 
 
 def tree_verify_attn(q: torch.Tensor, kv: KVCache, tree: Tree, scale: float, layer: int = 0,
@@ -857,10 +859,13 @@ def kv_append(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, kv_len: tor
     kv_len + n_new - 1 of one layer."""
     dev = kv.k.device
     sb, stt = _q_strides(k_new, "k_new", "Hkv")
-    if k_new.shape != v_new.shape or v_new.dtype != torch.bfloat16 or k_new.stride() != v_new.stride() or \
-            k_new.device != dev or v_new.device != dev:
-        raise ValueError("k_new and v_new must share shape, strides, bfloat16 and the cache's device")
     B, T_max, Hkv, D = k_new.shape
+    if k_new.shape != v_new.shape or v_new.dtype != torch.bfloat16 or k_new.device != dev or v_new.device != dev:
+        raise ValueError("k_new and v_new must share shape, bfloat16 and the cache's device")
+    if k_new.stride() != v_new.stride():
+        vb, vt = _q_strides(v_new, "v_new", "Hkv")
+        if vt != stt or (vb != sb and B > 1):
+            raise ValueError("k_new and v_new must share their strides")
     if Hkv != kv.Hkv:
         raise ValueError(f"k_new has {Hkv} heads, the cache {kv.Hkv}")
     _cache_covers(kv, B, D)

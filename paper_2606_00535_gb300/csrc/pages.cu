@@ -771,8 +771,9 @@ extern "C" dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t
       kv_len == nullptr || n_new == nullptr || B < 1 || B > 65535 || T_max < 1 || T_max > (1 << 20) ||
       !aligned16(k_new) || !aligned16(v_new) || !aligned4(kv_len) || !aligned4(n_new))
     return DREAMS_ERR_INVALID_ARG;
-  if (B == 1) stride_b = stride_t;  // not used
   const int64_t row = int64_t(kv->Hkv) * kv->D;
+  if (T_max == 1) stride_t = row;  // not used
+  if (B == 1) stride_b = stride_t;
   if (stride_t < row || stride_b < row || stride_t % 8 != 0 || stride_b % 8 != 0 || stride_t >= (int64_t(1) << 38) ||
       stride_b >= (int64_t(1) << 38))
     return DREAMS_ERR_INVALID_ARG;

@@ -537,7 +537,8 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
       (reinterpret_cast<uintptr_t>(lse) & 3))
     return DREAMS_ERR_INVALID_ARG;
   if (!isfinite(scale) || !(scale > 0.f)) return DREAMS_ERR_INVALID_ARG;
-  if (B == 1) q_stride_b = q_stride_t;  // not used
+  if (T_max == 1) q_stride_t = int64_t(Hq) * kv->D;  // not used
+  if (B == 1) q_stride_b = q_stride_t;
   if (q_stride_t < int64_t(Hq) * kv->D || q_stride_b < int64_t(Hq) * kv->D || q_stride_t % 8 != 0 ||
       q_stride_b % 8 != 0 || q_stride_t >= (int64_t(1) << 38) || q_stride_b >= (int64_t(1) << 38))
     return DREAMS_ERR_INVALID_ARG;
