@@ -425,7 +425,8 @@ dreams_status_t dreams_visual_importance(const void *attn, dreams_dtype_t dtype,
  * visible slot and whose entry is out of range is flagged DREAMS_DATA_BAD_PAGE,
  * and its slots read as zeros. What a slot holds does not reach a query that does
  * not see it, infinities and NaN included. Accumulation is fp32; probabilities
- * enter the PV product as bf16, and the output is rounded to bf16 once. The sums
+ * enter the PV product as bf16 (as the sum of two bf16 with at most 8 query rows per
+ * KV head), and the output is rounded to bf16 once. The sums
  * are normalised at the end, so finite values of V are good up to 2^87 in
  * magnitude. With more than 16 query rows per KV head (T_max * Hq / Hkv), rows are
  * computed one key at a time, about a thousand times slower (0.6 us a key for each

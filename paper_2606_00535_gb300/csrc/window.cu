@@ -16,7 +16,13 @@
 // is split over a cluster, whose CTAs push their parts into each other's shared memory
 // and join them there, in list order. More rows go to window_tc.cu. Head dim 128: 64
 // sequences of 8 KV heads, window 4096, 161 us, 95% of the copy rate; one of 4, window
-// 1024, 6.8 us, a chain of dependent loads.
+// 1024, 6.3 us, a chain of dependent loads.
+//
+// P enters P V as bf16, which makes the outputs' error against 64 bits 1.2 to 1.4 times
+// that of f32 probabilities. With at most 8 rows (FOLD) half of an instruction's 16 is
+// free: it takes what is left of P, and the halves are added at the end, so that 16 bits
+// of P count. With 9 to 16 rows that would be a second product (the batch above 171 us
+// with one), so there P is one bf16, as in window_tc.cu.
 #include <limits.h>
 #include <math.h>
 
@@ -115,11 +121,12 @@ __device__ __forceinline__ bool load_rows(const WinParams &p, RowsShared &sh, in
 
 // Attention of the rows over keys [i0, i1) of the list. Afterwards sh.ml holds each
 // warp's (m, l) per row, and `ring` its unnormalised outputs [warp][row][D] in f32.
-template <int D>
+template <int D, bool FOLD>
 __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, uint8_t *smem, const KeyList &kl, int b, int g, int L, int T,
                                             int i0, int i1) {
   using C = RowsCfg<D>;
-  constexpr int CH = D / 8;  // 16-byte columns of a key
+  constexpr int CH = D / 8;         // 16-byte columns of a key
+  constexpr int H = FOLD ? 1 : 2;  // rows of a thread
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int ntiles = (i1 - i0 + KT - 1) / KT;
 
@@ -168,13 +175,13 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
   };
   look(0);
 
-  // this thread's part of Q: rows lane / 4 and lane / 4 + 8
+  // this thread's part of Q: rows lane / 4 and (H = 2) lane / 4 + 8
   const int r0 = lane >> 2, c0 = (lane & 3) * 2;
   uint32_t qf[D / 16][4];
-  int off[2];
-  unsigned long long anc[2];
+  int off[H];
+  unsigned long long anc[H];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < H; ++h) {
     const int r = r0 + 8 * h, t = r / p.G;
     off[h] = t < T ? t : -1;
     anc[h] = 0ull;
@@ -187,12 +194,18 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
     for (int kk = 0; kk < D / 16; ++kk) {
       qf[kk][h] = t < T ? *reinterpret_cast<const uint32_t *>(src + kk * 16) : 0u;
       qf[kk][h + 2] = t < T ? *reinterpret_cast<const uint32_t *>(src + kk * 16 + 8) : 0u;
+      if (FOLD) qf[kk][1] = qf[kk][3] = 0u;
     }
   }
   float o[D / 8][4];
 #pragma unroll
   for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[H], l[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    m[h] = -INFINITY;
+    l[h] = 0.f;
+  }
 
   const int off_max = T - 1;
   uint32_t st_in = ring, st = ring;  // the stages of the copy and of the tile
@@ -230,24 +243,24 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 2 * H; ++e) {
           const int i = ib + n * 8 + c0 + (e & 1);
           if (i >= i1 || off[e >> 1] < 0 || !sees(p, L, off[e >> 1], anc[e >> 1], kl.slot(i))) s[n][e] = -INFINITY;
         }
     }
     uint32_t pf[4];
-    float mx[2];
+    float mx[H];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
+    for (int h = 0; h < H; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
 #pragma unroll
     for (int k = 1; k < 4; k <<= 1)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], k));
+      for (int h = 0; h < H; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], k));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) mx[h] = fmaxf(m[h], mx[h] * p.scale_log2);
-    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+    for (int h = 0; h < H; ++h) mx[h] = fmaxf(m[h], mx[h] * p.scale_log2);
+    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[H - 1] > m[H - 1])) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < H; ++h) {
         const float corr = mx[h] == m[h] ? 1.f : tc::ex2(m[h] - mx[h]);  // (also where both are -inf)
         m[h] = mx[h];
         l[h] *= corr;
@@ -255,18 +268,30 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
         for (int n = 0; n < D / 8; ++n) {
           o[n][2 * h] *= corr;
           o[n][2 * h + 1] *= corr;
+          if (FOLD) {
+            o[n][2] *= corr;
+            o[n][3] *= corr;
+          }
         }
       }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < H; ++h) {
       const float nm = m[h] == -INFINITY ? 0.f : -m[h];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         const float p0 = tc::ex2(fmaf(s[n][2 * h], p.scale_log2, nm));
         const float p1 = tc::ex2(fmaf(s[n][2 * h + 1], p.scale_log2, nm));
         l[h] += p0 + p1;
-        pf[2 * n + h] = pack_bf16x2(p0, p1);
+        if (FOLD) {
+          const uint32_t hi = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);
+          pf[2 * n] = hi;
+          // (what is left may be zero, and zero times an infinity in V a NaN: 2^-20 of P is below its error)
+          pf[2 * n + 1] = pack_bf16x2(fmaxf(p0 - __uint_as_float(hi << 16), p0 * 0x1p-20f),
+                                      fmaxf(p1 - __uint_as_float(hi & 0xffff0000u), p1 * 0x1p-20f));
+        } else {
+          pf[2 * n + h] = pack_bf16x2(p0, p1);
+        }
       }
     }
     // O += P V
@@ -298,7 +323,7 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
       }
     } else {
 #pragma unroll 1
-      for (int r = 0; r < RB; ++r) {
+      for (int r = 0; r < 8 * H; ++r) {
         const RowInfo ri = sh.row[r];
         uint32_t keep[2];
 #pragma unroll
@@ -319,7 +344,7 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
           mma16816(a1, pf, vb[2] & keep[0], vb[3] & keep[1]);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            if (r0 + 8 * h == r) {
+            if (r0 + (FOLD ? 0 : 8 * h) == r) {
               o[n][2 * h] += a0[2 * h];
               o[n][2 * h + 1] += a0[2 * h + 1];
               o[n + 1][2 * h] += a1[2 * h];
@@ -335,7 +360,7 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
 
   float *so = reinterpret_cast<float *>(smem);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < H; ++h) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
     const int r = r0 + 8 * h;
@@ -343,7 +368,8 @@ __device__ __forceinline__ void stream_keys(const WinParams &p, RowsShared &sh, 
     if (off[h] >= 0) {
 #pragma unroll
       for (int n = 0; n < D / 8; ++n)
-        *reinterpret_cast<float2 *>(so + (warp * RB + r) * D + n * 8 + c0) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+        *reinterpret_cast<float2 *>(so + (warp * RB + r) * D + n * 8 + c0) =
+            FOLD ? make_float2(o[n][0] + o[n][2], o[n][1] + o[n][3]) : make_float2(o[n][2 * h], o[n][2 * h + 1]);
     }
   }
   __syncthreads();
@@ -391,7 +417,7 @@ __device__ __forceinline__ void emit(const WinParams &p, int b, int g, int u, fl
   if (d == 0 && p.lse != nullptr) p.lse[row] = (M + log2f(Z)) * LN2;
 }
 
-template <int D>
+template <int D, bool FOLD>
 __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams p) {
   using C = RowsCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -417,7 +443,7 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
   const KeyList kl = key_list(p, L, 0, T - 1);
   const int64_t per = ((int64_t(kl.n) + p.nsplit - 1) / p.nsplit + KT - 1) / KT * KT;
   const int i0 = int(::min(int64_t(kl.n), split * per)), i1 = int(::min(int64_t(kl.n), i0 + per));
-  stream_keys<D>(p, sh, smem, kl, b, g, L, T, i0, i1);
+  stream_keys<D, FOLD>(p, sh, smem, kl, b, g, L, T, i0, i1);
   const int units = T * p.G * (D / 4);
   if (p.nsplit == 1) {
     for (int u = tid; u < units; u += 32 * WARPS) {
@@ -469,9 +495,9 @@ int split_of(int64_t lists, int64_t keys) {
   return n;
 }
 
-template <int D>
+template <int D, bool FOLD>
 dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
-  const void *kernel = reinterpret_cast<const void *>(window_rows_kernel<D>);
+  const void *kernel = reinterpret_cast<const void *>(window_rows_kernel<D, FOLD>);
   const dreams_status_t st = ensure_max_dynamic_smem(kernel, RowsCfg<D>::SMEM);
   if (st != DREAMS_OK) return st;
   // clusters of 16 have to be asked for, once per device
@@ -573,5 +599,6 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
   p.status = status_word;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (int64_t(T_max) * p.G > RB) return launch_tc(p, kv, s);
-  return kv->D == 128 ? launch_rows<128>(p, s) : launch_rows<64>(p, s);
+  if (int64_t(T_max) * p.G <= 8) return kv->D == 128 ? launch_rows<128, true>(p, s) : launch_rows<64, true>(p, s);
+  return kv->D == 128 ? launch_rows<128, false>(p, s) : launch_rows<64, false>(p, s);
 }

@@ -16,7 +16,10 @@
 // Softmax without a running maximum: a row's reference m is the maximum of the first
 // tile it sees a key of, and stays; P = 2^(x - m) is as exact at any m, in bf16 and in
 // the f32 sums alike, short of overflow. So the exponentials of a tile start as its
-// scores arrive. A row whose sum ends above 2^100 (a later score exceeds m by some 69
+// scores arrive. P enters P V as one bf16: the outputs' error against 64 bits is then 1.2
+// to 1.4 times that of f32 probabilities (the one rounding of the output is most of
+// either), and a product with what is left of P would add half of Q K^T and P V to the
+// tensor pipe. A row whose sum ends above 2^100 (a later score exceeds m by some 69
 // nats), or above 2^40 (28 nats) with an O that overflowed, is done again from its
 // definition.
 //   PAIR   the slots are two neighbouring blocks of a KV head: every K/V tile is

@@ -131,3 +131,37 @@ def test_rows_done_again_are_no_stall(dreams):
     finally:
         dreams.test_set_stall(0, -1)
     assert st == 0 and torch.equal(out, ref) and torch.equal(lse, ref_lse)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(28, 4, 128), (8, 2, 64), (8, 1, 128), (3, 3, 64)])
+@pytest.mark.parametrize("kv_len", [[0, 1, 2, 5], [40, 700, 3000, 63]])
+@pytest.mark.parametrize("tree", [False, True])
+def test_eight_rows_keep_sixteen_bits_of_the_probabilities(dreams, Hq, Hkv, D, kv_len, tree):
+    """At most 8 rows per KV head: outputs closer than one bf16 a probability could give them.
+
+    Tolerance: the probabilities are held to 2^-16 (two bf16, the second rounded), at most 2^-20 of one is added so that
+    none of the two is zero, and the f32 parts cost 2e-4 at most, all relative to A = sum_j a_j |V_j|; the one rounding of the
+    output is 2^-8 |O|. A single bf16 would cost up to 2^-8 A."""
+    n = 8 // (Hq // Hkv) if tree else 1
+    c = Case(77 + D, Hq, Hkv, D, kv_len, [n] * 4, 2500, 2, tree=tree, paged=D == 64)
+    out, lse = (x.double().cpu().numpy() for x in c.run(dreams))
+    K, V = (x[0].double().numpy() for x in (c.k, c.v))
+    for b in range(4):
+        sel = [(t, h) for t in range(n) for h in range(0, Hq, 3)]
+        ref = S.window_rows(c.q[b].double().numpy(), lambda s, g: (K[b, s, g], V[b, s, g]), kv_len[b], c.scale, 2500, 2,
+                            lambda h: h // (Hq // Hkv), c.parent[b] if tree else None, sel)
+        for (t, h), (o, a, z) in zip(sel, ref):
+            err, tol = np.abs(out[b, t, h] - o), 1.02 * 2.0 ** -8 * np.abs(o) + (2e-4 + 2.0 ** -16 + 2.0 ** -20) * a + 1e-6
+            assert (err <= tol).all(), (b, t, h, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("T,L", [(1, 0), (1, 5), (3, 300), (4, 15)])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf")])
+def test_an_infinity_that_a_row_sees_is_its_output(dreams, T, L, bad):
+    """An infinity in V of a seen slot makes that element infinite, of that sign, whatever the weight; the others stay."""
+    c = Case(5, 8, 2, 128, [L], [T], 200, 1)
+    c.v[0, 0, L, :, 7] = bad  # the first new slot: every query sees it
+    out, lse = c.run(dreams)
+    assert (out[0, :T, :, 7] == bad).all()
+    rest = [i for i in range(128) if i != 7]
+    assert torch.isfinite(out[0, :T, :, rest]).all() and torch.isfinite(lse[0, :T]).all()
