@@ -165,3 +165,40 @@ def test_an_infinity_that_a_row_sees_is_its_output(dreams, T, L, bad):
     assert (out[0, :T, :, 7] == bad).all()
     rest = [i for i in range(128) if i != 7]
     assert torch.isfinite(out[0, :T, :, rest]).all() and torch.isfinite(lse[0, :T]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("stall_at", [0, 1, 30])
+def test_a_pairs_wait_runs_out_then_recovers(dreams, D, stall_at):
+    """Copies withheld (the test hook) in the layout of tests/test_gpu_window_timeout.py that its shapes do not reach: more
+    blocks than SMs, so pairs of them. Two items for some CTAs, about 25 tiles each: rows of an item whose tiles all came
+    are those of the normal call, the others are untouched."""
+    g = torch.Generator().manual_seed(6)
+    B, T, Hq, Hkv, L = 24, 64, 32, 8, 3001
+    q = torch.randn((B, T, Hq, D), generator=g).to(torch.bfloat16).cuda()
+    k, v = (torch.randn((B, L + T + 63, Hkv, D), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    kv = dreams.KVCache(k, v)
+    n, lens = (torch.full((B,), x, dtype=torch.int32, device="cuda") for x in (T, L))
+
+    def run():
+        out = torch.full(q.shape, 0x7F7F, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+        lse = torch.full(q.shape[:3], -7.0, device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        dreams.window_attention(q, kv, n, lens, D ** -0.5, 3000, 4, out=out, lse=lse, status=st)
+        torch.cuda.synchronize()
+        return out.view(torch.int16), lse, int(st.item())
+
+    ref, ref_lse, st = run()
+    assert st == 0 and not (ref == 0x7F7F).any()
+    try:
+        dreams.test_set_stall(dreams.TEST_ATTENTION, stall_at, 20_000_000)
+        out, lse, st = run()
+    finally:
+        dreams.test_set_stall(0, -1)
+    assert st == dreams.DATA_TIMEOUT
+    done = lse != -7.0
+    assert torch.equal(out[done], ref[done]) and torch.equal(lse[done], ref_lse[done])
+    assert (out[~done] == 0x7F7F).all()
+    assert not done.any() if stall_at < 2 else done.any() and not done.all()
+    out, lse, st = run()
+    assert st == 0 and torch.equal(out, ref) and torch.equal(lse, ref_lse)
