@@ -232,8 +232,10 @@ struct ForkState {
 constexpr int HEAD_FLAGS = 1, HEAD_FOUND = HEAD_FLAGS + FORK_CTAS, FORK_HEAD = HEAD_FOUND + FORK_CTAS;
 constexpr int FORK_SHARED_ROWS = 2048, FORK_UNROLL = 4;
 // One CTA for tables of up to so many entries: its barriers are cheaper; eight
-// keep more loads in flight. (Whole call with copies of next to nothing: 448
-// entries 6.7 us against 9.4, 544 6.9 against 10.6; 12288 14.7 against 11.1.)
+// keep more loads in flight. Whole call with copies of one row each, us on the GPU:
+//   entries    448   1024   2048   3072   4096   6144   8192  12288
+//   one CTA    4.4    5.0    5.5    6.2    6.7    8.4    9.4   12.1
+//   eight      5.6    6.2    6.2    6.2    6.5    6.6    6.7    7.1
 constexpr int FORK_ONE_CELLS = 4096;
 
 // (Not the .aligned forms: warps come here from loops that their lanes left at

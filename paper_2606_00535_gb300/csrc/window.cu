@@ -480,14 +480,19 @@ __global__ void __launch_bounds__(32 * WARPS) window_rows_kernel(const WinParams
 
 // ------------------------------------------------------------------ host side
 // CTAs of a list: as many as still run at the same time, two to an SM. One CTA takes
-// 15 us for 1024 keys whatever else runs; with all places taken the copies are bound by
+// 14 us for 1024 keys whatever else runs; with all places taken the copies are bound by
 // HBM, and further splits only add joins. Measured on the GPU for 8 KV heads, window
 // 4096, head dim 128, in us:
 //   lists        8     64    128    512
-//   1 CTA     61.4   63.1   63.6  162.0
-//   2         34.3   35.8   43.7  176.2
-//   4         20.1   25.4   50.6  174.5
-//   8         13.2   32.3   59.5  211.1
+//   1 CTA     57.5   59.6   60.4  160.5
+//   2         31.8   33.8   44.6  175.7
+//   4         18.4   24.4   50.2  179.7
+//   8         12.0   30.7   60.2  211.9
+//   16         9.7   50.0   96.9  360.6
+// Keys are counted by the cache's capacity, as the lengths are on the device: a short
+// sequence in a large cache gets CTAs without keys. One of 50 tokens, window 4096, takes
+// 3.4 us in a cache of 64 slots and 5.4 in one of 32768, one of 300 5.1 and 5.6; from
+// some thousand on, and with 64 sequences, there is no difference.
 constexpr int MAX_SPLIT = 16;
 int split_of(int64_t lists, int64_t keys) {
   int n = 1;

@@ -36,10 +36,11 @@
 // that the P V before it is done: the softmax warpgroup then gives those stages back,
 // and no further commits are needed.
 // Bound by the chain of a tile (products, softmax, products), of which two run on an
-// SM: about 3000 clocks for both slots, where the products take 2048 (head dim 128)
-// or the exponentials 1024 (64). 3392 tokens of 32 heads, head dim 128, window 1024: 72
-// us, 36% of the bf16 burst rate on the keys seen; 16 trees of up to 64 nodes, 32/8
-// heads, window 2048: 45 us, 48% of the copy rate.
+// SM: about 4000 clocks for both slots, where the products take 2048, with head dim 128
+// (1.93 us a tile of a pair at 2070 MHz, from windows of 2048 to 8192); 2900 with head
+// dim 64 (1.41 us), where products and exponentials take 1024 each. 3392 tokens of 32
+// heads, head dim 128, window 1024: 73 us, 35% of the bf16 burst rate on the keys seen;
+// 16 trees of up to 64 nodes, 32/8 heads, window 2048: 45 us, 48% of the copy rate.
 // Every mbarrier wait is bounded (2 s without progress); a CTA that gives up flags DREAMS_DATA_TIMEOUT,
 // drains its copies and MMAs, frees its tensor memory and leaves unfinished rows
 // untouched.
@@ -1281,8 +1282,14 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   // layout in tenths of a microsecond, from sweeps of both over 5 to 33 tiles and 8 to
   // 448 blocks: a CTA of a block takes 13.5 us and 1.5 (head dim 64: 1.3) a tile, a
   // round of them after the other; a pair of blocks 2 (1.6) a tile, 3 to change items
-  // and 4 once. 17 tiles: trees of 16 sequences, 128 pairs 45 us, 256 blocks 83; 9
-  // tiles: a tree's 32 blocks 22 us, over clusters of 4 13.1.
+  // and 4 once. 17 tiles: trees of 16 sequences, 128 pairs 45 us, 256 blocks 85; 9
+  // tiles: a tree's 32 blocks 22 us, over clusters of 4 13.5.
+  // A later sweep of both (32 to 864 blocks, windows of 512 to 4096) has pairs as said (1.4
+  // a tile with head dim 64), a CTA of a block at 12.6 and 1.5 (64: 15.4 and 0.85), and
+  // one of a cluster of 4 at 10 and 1.2: the rule overrates clusters by 3 to 6 us. It took
+  // the slower layout at 5 of 96 points, all near where the two cross: 18.3 us against
+  // 15.7 (64 blocks, 5 tiles), 14.6 against 11.8 (32 blocks, 5 tiles, head dim 64), and 4
+  // to 7% at 17 tiles of 96 to 152 blocks with head dim 64.
   const int64_t sms = num_sms();
   const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB));
   const int64_t cols = keys + 63 + (std::min<int64_t>(p.capacity, p.sinks) + 63) / 64 * 64 + 32;
