@@ -79,7 +79,7 @@ typedef enum dreams_dtype { DREAMS_F32 = 0, DREAMS_BF16 = 1 } dreams_dtype_t;
 #define DREAMS_DATA_BAD_PARENT 0x1   /* parent[0] != -1 or parent[i] outside [0, i) */
 #define DREAMS_DATA_BAD_TREE_LEN 0x2 /* tree_len outside [1, T_max] */
 #define DREAMS_DATA_BAD_KV_LEN 0x4   /* kv_len < 0 or kv_len + tree_len > capacity */
-#define DREAMS_DATA_BAD_PAGE 0x8     /* page-table entry outside [0, num_pages) */
+#define DREAMS_DATA_BAD_PAGE 0x8     /* page-table entry outside [0, num_pages), or given back with count 0 */
 #define DREAMS_DATA_BAD_PATH 0x10    /* path[0] != 0 or not strictly increasing */
 #define DREAMS_DATA_TIMEOUT 0x20     /* a kernel gave up waiting on its own pipeline (2 s) */
 #define DREAMS_DATA_NO_PAGES 0x40    /* the page pool has too few free pages for the call */
