@@ -541,6 +541,139 @@ dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t B, const in
                                 int32_t *status_word, dreams_stream_t stream);
 
 /*
+ * Rotary positions: what turns each pair of dimensions of a head by an angle that
+ * grows with the token's position.
+ *   n_pairs  rotated pairs; the dimensions from 2 n_pairs on stay as they are
+ *   phase    device [n_pairs]: how far a pair turns per position, in turns times
+ *            2^64, modulo 2^64 (a frequency of f radians: f / (2 pi) 2^64). The
+ *            angle at any position is then one integer product, exact however far
+ *            the position; scalings for long contexts are other phases.
+ *   axis     device [n_pairs], or NULL (all 0): which of a call's position axes a
+ *            pair goes by (visual tokens: time, row, column). A value that is no
+ *            axis of the call is flagged DREAMS_DATA_BAD_INDEX and counts as 0.
+ *   layout   DREAMS_ROPE_HALF: pair i is dimensions (i, i + n_pairs);
+ *            DREAMS_ROPE_INTERLEAVED: (2 i, 2 i + 1)
+ *   factor   finite; the cosines and sines are multiplied by it
+ */
+#define DREAMS_ROPE_HALF 0
+#define DREAMS_ROPE_INTERLEAVED 1
+typedef struct dreams_rotary {
+  const uint64_t *phase;
+  const int32_t *axis;
+  int32_t n_pairs;
+  int32_t layout;
+  float factor;
+} dreams_rotary_t;
+
+/*
+ * Turns the rows of a tensor x [B, T, H, D] by their positions: for pair (u, v) of
+ * a row at position p, with the pair's angle a = 2 pi (p phase / 2^64),
+ *     u' = factor (u cos a - v sin a),   v' = factor (v cos a + u sin a)
+ * or, with transpose != 0, by the transposed map (-a in place of a): the gradient
+ * with respect to x of an output's, and with factor 1 the inverse. Products and
+ * sums are f32, the result is rounded to x's type once. Element (b, t, h, d) of x
+ * is at b * x_stride[0] + t * x_stride[1] + h * x_stride[2] + d, of out alike; both
+ * have the same type (f32 or bf16). out may be x itself (the same pointer and
+ * strides), else they do not overlap. Strides and pointers may have any alignment
+ * of whole elements; rows of 16-byte multiples, 16-byte aligned, take 16-byte
+ * accesses. D even, at most 512, 1 <= n_pairs <= D / 2.
+ * positions: device [n_axes, B, T], any values (negative ones turn backwards); or
+ * NULL (n_axes 1): token t of sequence b is at start[b] + t, start device [B], NULL
+ * = 0. 1 <= n_axes <= 4. One launch.
+ */
+dreams_status_t dreams_rope(const void *x, const int64_t *x_stride, void *out, const int64_t *out_stride,
+                            dreams_dtype_t dtype, int32_t B, int32_t T, int32_t H, int32_t D,
+                            const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes,
+                            const int32_t *start, int32_t transpose, int32_t *status_word, dreams_stream_t stream);
+
+/*
+ * dreams_kv_append with the rotation applied on the way: new rows of one layer,
+ *     slot kv_len[b] + t  <-  turned k_new[b, t], v_new[b, t]
+ * and q_out[b, t] <- turned q[b, t], for t < n_new[b], in one launch. q NULL: K and
+ * V alone (q_out NULL, Hq 0). q, k_new and v_new: bf16, element (b, t, h, d) at b *
+ * stride[0] + t * stride[1] + h * D + d, so views of one fused projection; each has
+ * its own strides (multiples of 8 elements, at least a row; stride[0] is ignored
+ * when B == 1, stride[1] when T_max == 1). q_out: dense bf16 [B, T_max, Hq, D], or
+ * q itself where q is dense. All are 16-byte aligned and overlap neither the cache
+ * nor, but for that, each other. Positions: positions ([n_axes, B, T_max]); or
+ * parent ([B, T_max], T_max <= 64): the rows are the nodes of a draft tree, node t
+ * at kv_len[b] + its depth; or neither (both NULL, n_axes 1): kv_len[b] + t.
+ * kv->D any multiple of 8 up to 512. Rows t >= n_new[b] of q_out are left
+ * untouched. Bad lengths (BAD_KV_LEN) or a bad tree (BAD_PARENT; its first n_new[b]
+ * entries) skip the sequence; a slot whose page is missing is skipped (BAD_PAGE),
+ * its q row is not. One launch.
+ */
+dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer, const void *q,
+                                      const int64_t *q_stride, void *q_out, int32_t Hq, const void *k_new,
+                                      const int64_t *k_stride, const void *v_new, const int64_t *v_stride,
+                                      const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes,
+                                      const int32_t *parent, const int32_t *kv_len, const int32_t *n_new, int32_t B,
+                                      int32_t T_max, int32_t *status_word, dreams_stream_t stream);
+
+/*
+ * Full pages of a cache in 8 bits. k, v: e4m3 codes (one byte a value, no infinities),
+ * [n_layers, num_pages, 64, Hkv, D], layers layer_stride bytes apart; exps:
+ * [n_layers, num_pages, Hkv, 2], dense: for each page and head the powers of two of
+ * K and of V. A cached value is code * 2^exp, which bf16 holds exactly (powers of
+ * two cost e4m3 no precision, and the attention works on the very values that are
+ * stored). DREAMS_KV8_NOT_FINITE in place of a power: the values held an infinity
+ * or a NaN; all 64 rows then count as NaN, whatever the codes. Codes 0x7f and 0xff
+ * are not used. The pages have a table and a pool of their own (dreams_kv_reserve,
+ * _release and _fork work on it; a fork takes lengths that are multiples of 64).
+ * Slots 0 .. len8[b] - 1 of a sequence are here, len8[b] a multiple of 64; later
+ * ones are in its bf16 cache, whose pages for slots below len8[b] can be given back.
+ * k, v and layer_stride 16-byte aligned, exps 4-byte aligned.
+ */
+#define DREAMS_KV8_NOT_FINITE 32767
+typedef struct dreams_kv8_cache {
+  void *k;
+  void *v;
+  int16_t *exps;
+  int32_t n_layers;
+  int64_t layer_stride;
+  int32_t Hkv;
+  int32_t D; /* 64 or 128 */
+  const int32_t *page_table; /* [B, pages_per_seq], -1 = no page */
+  int32_t pages_per_seq;
+  int32_t num_pages;
+} dreams_kv8_cache_t;
+
+/*
+ * Puts the pages that lie wholly inside slots begin[b] .. end[b] - 1 of the bf16
+ * cache kv into 8 bits, in all layers (begin = len8, end = kv_len: every page that
+ * has filled up since). Of each page and head, K and V apart, exp is the smallest
+ * power with max |x| <= 448 * 2^exp, not below -96 nor above 119 (above 448 * 2^119
+ * values become that), and a code is x / 2^exp rounded to nearest even. Pages of kv8 for
+ * them have to be there (dreams_kv_reserve) and belong to the sequence alone. new_len8[b]
+ * (not the same array as begin or end) = the end of the last page done, begin[b] where
+ * there is none. begin[b] < 0 or no multiple of 64, end[b] < begin[b] or beyond either
+ * cache flags BAD_KV_LEN, skips the sequence and gives new_len8 = begin. A page that is
+ * missing in either cache is flagged BAD_PAGE and skipped; new_len8[b] then ends before
+ * the first such page. Both caches have the same n_layers, Hkv and D. One launch.
+ */
+dreams_status_t dreams_kv_quantize(const dreams_kv_cache_t *kv, const dreams_kv8_cache_t *kv8, int32_t B,
+                                   const int32_t *begin, const int32_t *end, int32_t *new_len8, int32_t *status_word,
+                                   dreams_stream_t stream);
+
+/*
+ * dreams_window_attention over a cache whose first len8[b] slots are in 8 bits: slot
+ * s < len8[b] is read from kv8, any other from kv (contiguous or paged). Everything
+ * else is as there: causal queries and draft trees, window (INT32_MAX: every slot is
+ * seen) and sinks, lengths, bad data and untouched rows, finite values up to 2^87 in
+ * magnitude, the roundings. len8[b] < 0, no multiple of 64, above kv_len[b] or above
+ * kv8's capacity flags BAD_KV_LEN and skips the sequence. A visible slot whose page
+ * is missing in the cache that holds it is flagged BAD_PAGE and reads as zeros. Rows
+ * that see a page marked DREAMS_KV8_NOT_FINITE become NaN, others do not. One launch,
+ * no workspace.
+ */
+dreams_status_t dreams_kv8_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
+                                     const dreams_kv8_cache_t *kv8, const dreams_kv_cache_t *kv, int32_t layer,
+                                     const int32_t *parent, const int32_t *q_len, const int32_t *kv_len,
+                                     const int32_t *len8, int32_t B, int32_t T_max, int32_t Hq, float scale,
+                                     int32_t window, int32_t sinks, void *out, float *lse, int32_t *status_word,
+                                     dreams_stream_t stream);
+
+/*
  * Row-wise argmax for callers that cannot allocate device memory. The paper
  * has no counterpart to this call; it exists for integration. Some callers
  * cannot allocate, or cannot hand out a workspace, when the argmax runs: a

@@ -18,11 +18,12 @@ equal its own greedy prediction; here the drafts form a tree.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import re
 import threading
 from dataclasses import dataclass
-from typing import Dict, List, Optional, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -66,6 +67,18 @@ class _PagePool(ctypes.Structure):
                 ("pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
 
 
+class _Rotary(ctypes.Structure):
+    _fields_ = [("phase", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("n_pairs", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("factor", ctypes.c_float)]
+
+
+class _KV8Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("exps", ctypes.c_void_p),
+                ("n_layers", ctypes.c_int32), ("layer_stride", ctypes.c_int64), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("pages_per_seq", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 _LOCK = threading.Lock()
 
@@ -82,6 +95,7 @@ def _lib() -> ctypes.CDLL:
                 p, i32, i64, sz, f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                                         ctypes.c_float)
                 pkv, ptr, ppl = ctypes.POINTER(_KVCache), ctypes.POINTER(_Tree), ctypes.POINTER(_PagePool)
+                pi64, prt, pk8 = ctypes.POINTER(i64), ctypes.POINTER(_Rotary), ctypes.POINTER(_KV8Cache)
                 sig = {
                     "dreams_tree_verify_attn_workspace_size": (sz, [pkv, ptr, i32]),
                     "dreams_tree_verify_attn_launches": (i32, [pkv, ptr, i32]),
@@ -119,6 +133,13 @@ def _lib() -> ctypes.CDLL:
                     "dreams_kv_fork": (ctypes.c_int, [pkv, ppl, p, p, p, p, sz, p, p]),
                     "dreams_kv_append": (ctypes.c_int, [pkv, i32, p, p, i64, i64, p, p, i32, i32, p, p]),
                     "dreams_kv_prune": (ctypes.c_int, [pkv, i32, p, i32, i32, i32, p, p, p, p, p]),
+                    "dreams_rope": (ctypes.c_int, [p, pi64, p, pi64, ctypes.c_int, i32, i32, i32, i32, prt, p, i32, p, i32, p,
+                                                   p]),
+                    "dreams_kv_append_rope": (ctypes.c_int, [pkv, i32, p, pi64, p, i32, p, pi64, p, pi64, prt, p, i32, p,
+                                                             p, p, i32, i32, p, p]),
+                    "dreams_kv_quantize": (ctypes.c_int, [pkv, pk8, i32, p, p, p, p, p]),
+                    "dreams_kv8_attention": (ctypes.c_int, [p, i64, i64, pk8, pkv, i32, p, p, p, p, i32, i32, i32, f32,
+                                                            i32, i32, p, p, p, p]),
                     "dreams_test_set_stall": (ctypes.c_int, [i32, i32, i64]),
                     "dreams_status_string": (ctypes.c_char_p, [ctypes.c_int]),
                     "dreams_version": (i32, []),
@@ -283,6 +304,52 @@ class KVCache:
                            self.D, self.capacity,
                            None if self.page_table is None else self.page_table.data_ptr(),
                            self.page_size, self.pages_per_seq, self.num_pages)
+
+
+@dataclass
+class KV8Cache:
+    """Full pages of one or more layers' K/V in 8 bits: ``k, v`` codes
+    (float8_e4m3fn) ``[num_pages, 64, Hkv, D]`` (or with a leading layer dim),
+    ``exps`` int16 ``[num_pages, Hkv, 2]`` (likewise), the powers of two of K and
+    V of each page and head, and their ``page_table`` int32 ``[B, pages_per_seq]``.
+    A cached value is code * 2^exp; an exp of KV8_NOT_FINITE marks 64 rows that held
+    an infinity or a NaN. ``PagePool`` takes it like a ``KVCache``, with lengths in
+    multiples of 64."""
+    k: torch.Tensor
+    v: torch.Tensor
+    exps: torch.Tensor
+    page_table: torch.Tensor
+
+    def __post_init__(self):
+        if self.k.shape != self.v.shape:
+            raise ValueError("k and v shapes differ")
+        dev = self.k.device
+        _need(self.k, "k", torch.float8_e4m3fn, dev)
+        _need(self.v, "v", torch.float8_e4m3fn, dev)
+        _need(self.exps, "exps", torch.int16, dev)
+        _need(self.page_table, "page_table", torch.int32, dev)
+        nd = self.k.dim()
+        if nd not in (4, 5) or self.k.shape[-3] != 64:
+            raise ValueError("k must be [num_pages, 64, Hkv, D], or with a leading layer dim")
+        if self.page_table.dim() != 2:
+            raise ValueError("page_table must be [B, pages_per_seq]")
+        if tuple(self.exps.shape) != (*self.k.shape[:-3], self.k.shape[-2], 2):
+            raise ValueError("exps must be [num_pages, Hkv, 2], or with k's leading layer dim")
+        self.n_layers = self.k.shape[0] if nd == 5 else 1
+        self.num_pages, _, self.Hkv, self.D = (int(x) for x in self.k.shape[-4:])
+        self.layer_stride = self.num_pages * 64 * self.Hkv * self.D if nd == 5 else 0
+        self.B, self.pages_per_seq = (int(x) for x in self.page_table.shape)
+        self.page_size, self.capacity = 64, self.pages_per_seq * 64
+        self._c8 = _KV8Cache(self.k.data_ptr(), self.v.data_ptr(), self.exps.data_ptr(), self.n_layers,
+                             self.layer_stride, self.Hkv, self.D, self.page_table.data_ptr(), self.pages_per_seq,
+                             self.num_pages)
+        # the same pages as kv_fork takes them: rows of half as many 16-bit values
+        self._c = _KVCache(self.k.data_ptr(), self.v.data_ptr(), self.n_layers, self.layer_stride // 2, self.Hkv,
+                           self.D // 2, self.capacity, self.page_table.data_ptr(), 64, self.pages_per_seq,
+                           self.num_pages)
+
+
+KV8_NOT_FINITE = 32767  # in place of a power: the page's values of that head held an infinity or a NaN
 
 
 @dataclass
@@ -740,7 +807,7 @@ class PagePool:
     like all uses of its tensors. ``PagePool.empty(kv)`` starts with every page
     free. The pool owns the workspaces of its calls, one per stream; a captured call
     uses them at every replay, so the pool has to live as long as the graph."""
-    kv: KVCache
+    kv: Union[KVCache, KV8Cache]
     refcount: torch.Tensor
 
     def __post_init__(self):
@@ -757,7 +824,7 @@ class PagePool:
         self._by_stream: Dict[int, torch.Tensor] = {}  # workspaces; they hold no state between calls
 
     @classmethod
-    def empty(cls, kv: KVCache) -> "PagePool":
+    def empty(cls, kv: Union[KVCache, KV8Cache]) -> "PagePool":
         if kv.page_table is None:
             raise ValueError("a page pool needs a paged cache")
         kv.page_table.fill_(-1)
@@ -897,6 +964,256 @@ def kv_prune(kv: KVCache, keep: torch.Tensor, v0: int, n_vis: int, kv_len: torch
             None if refcount is None else refcount.data_ptr(), _per_seq(new_kv_len, "new_kv_len", B, dev),
             _status(status, dev))
     return new_kv_len
+
+
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+
+
+@dataclass
+class Rotary:
+    """Rotary positions: ``phase`` (int64 [n_pairs], the bits of an unsigned
+    number): how far a pair turns per position, in turns times 2^64; ``layout``
+    ROPE_HALF (pairs (i, i + n_pairs)) or ROPE_INTERLEAVED ((2 i, 2 i + 1));
+    ``factor`` multiplies the cosines and sines; ``axis`` (int32 [n_pairs], or
+    None): the position axis each pair goes by. ``Rotary.make`` works the phases out."""
+    phase: torch.Tensor
+    layout: int = ROPE_HALF
+    factor: float = 1.0
+    axis: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        dev = self.phase.device
+        _need(self.phase, "phase", torch.int64, dev)
+        if self.phase.dim() != 1 or self.phase.numel() < 1:
+            raise ValueError("phase must be [n_pairs]")
+        if self.layout not in (ROPE_HALF, ROPE_INTERLEAVED):
+            raise ValueError("layout must be ROPE_HALF or ROPE_INTERLEAVED")
+        if not math.isfinite(self.factor):
+            raise ValueError("factor must be finite")
+        self.n_pairs = int(self.phase.numel())
+        if self.axis is not None:
+            _need(self.axis, "axis", torch.int32, dev)
+            if self.axis.shape != self.phase.shape:
+                raise ValueError("axis must be [n_pairs]")
+        self._c = _Rotary(self.phase.data_ptr(), None if self.axis is None else self.axis.data_ptr(), self.n_pairs,
+                          self.layout, self.factor)
+
+    @classmethod
+    def make(cls, rot_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none",
+             factor: float = 1.0, original: int = 4096, fast: float = 32.0, slow: float = 1.0,
+             frequencies: Optional[Sequence[float]] = None, gain: Optional[float] = None,
+             axis: Optional[Sequence[int]] = None, device="cuda") -> "Rotary":
+        """The first ``rot_dim`` dimensions of a head, pair i at base^(-2 i /
+        rot_dim) radians a position (or at ``frequencies``), scaled for a context
+        ``factor`` times as long:
+          none, linear   f, f / factor (positions interpolated)
+          ntk            the base times factor^(rot_dim / (rot_dim - 2)): the fastest
+                         pair as it was, the slowest ``factor`` times slower
+          yarn           pairs that turn more than ``fast`` times over ``original``
+                         positions keep f, those below ``slow`` take f / factor,
+                         linearly between; cos and sin times 0.1 ln(factor) + 1
+        ``gain`` sets that multiplier of cos and sin instead."""
+        if rot_dim < 2 or rot_dim % 2:
+            raise ValueError("rot_dim must be even and positive")
+        if layout not in ("half", "interleaved"):
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        if scaling not in ("none", "linear", "ntk", "yarn"):
+            raise ValueError("scaling must be 'none', 'linear', 'ntk' or 'yarn'")
+        if not (math.isfinite(factor) and factor > 0 and math.isfinite(base) and base > 0):
+            raise ValueError("base and factor must be finite and positive")
+        if scaling == "yarn" and not (original > 0 and fast > slow):
+            raise ValueError("yarn needs original > 0 and fast > slow")
+        n = rot_dim // 2
+        if scaling == "ntk":
+            if rot_dim == 2:
+                raise ValueError("ntk needs more than one pair")
+            base = base * factor ** (rot_dim / (rot_dim - 2))
+        f = [base ** (-2.0 * i / rot_dim) for i in range(n)] if frequencies is None else [float(x) for x in frequencies]
+        if len(f) != n or not all(math.isfinite(x) for x in f):
+            raise ValueError(f"frequencies must hold {n} finite values")
+        mult = 1.0
+        if scaling == "linear":
+            f = [x / factor for x in f]
+        elif scaling == "yarn":
+            keep = [min(1.0, max(0.0, (original * abs(x) / (2.0 * math.pi) - slow) / (fast - slow))) for x in f]
+            f = [x * (k + (1.0 - k) / factor) for x, k in zip(f, keep)]
+            mult = 0.1 * math.log(factor) + 1.0
+        phase = []
+        for x in f:  # turns x 2^64, modulo 2^64, as a signed number of the same bits
+            u = round(math.fmod(x / (2.0 * math.pi), 1.0) * 2.0 ** 64) % 2 ** 64
+            phase.append(u - 2 ** 64 if u >= 2 ** 63 else u)
+        if axis is not None and (len(axis) != n or any(not 0 <= a <= 3 for a in axis)):
+            raise ValueError(f"axis must hold {n} values from 0 to 3")
+        return cls(torch.tensor(phase, dtype=torch.int64, device=device),
+                   ROPE_HALF if layout == "half" else ROPE_INTERLEAVED, mult if gain is None else float(gain),
+                   None if axis is None else torch.tensor(list(axis), dtype=torch.int32, device=device))
+
+
+_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
+def _positions(positions: Optional[torch.Tensor], B: int, T: int, dev) -> Tuple[Optional[int], int]:
+    """Address and axes of positions [B, T] or [n_axes, B, T]."""
+    if positions is None:
+        return None, 1
+    _need(positions, "positions", torch.int32, dev)
+    if positions.dim() not in (2, 3) or tuple(positions.shape[-2:]) != (B, T):
+        raise ValueError(f"positions must be [B, T] or [n_axes, B, T] with B = {B}, T = {T}")
+    return positions.data_ptr(), 1 if positions.dim() == 2 else int(positions.shape[0])
+
+
+def rope(x: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = None,
+         start: Optional[torch.Tensor] = None, transpose: bool = False, out: Optional[torch.Tensor] = None,
+         status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Turns the rows of ``x`` (bf16 or f32 [B, T, H, D], any strides with dense
+    rows) by their positions: ``positions`` (int32 [B, T] or [n_axes, B, T]), or
+    ``start`` (int32 [B]) + t, or t. ``transpose``: by the transposed map, which is
+    the gradient with respect to x of an output's (and with factor 1 the inverse).
+    Returns ``out``, which may be ``x``."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 4:
+        raise TypeError("x must be a 4-D bfloat16 or float32 tensor [B, T, H, D]")
+    dev = x.device
+    B, T, H, D = x.shape
+    if x.stride(3) != 1 and D > 1:
+        raise ValueError("x's rows must be dense (last stride 1)")
+    if rotary.phase.device != dev:
+        raise ValueError(f"the rotary table is on {rotary.phase.device}, x on {dev}")
+    pos, axes = _positions(positions, B, T, dev)
+    if positions is not None and start is not None:
+        raise ValueError("give positions or start, not both")
+    st = None if start is None else _per_seq(start, "start", B, dev)
+    if out is None:
+        out = _new((B, T, H, D), x.dtype, dev, stream)
+    elif not isinstance(out, torch.Tensor) or out.dtype != x.dtype or out.device != dev or out.shape != x.shape:
+        raise ValueError("out must have x's type, shape and device")
+    elif out.stride(3) != 1 and D > 1:
+        raise ValueError("out's rows must be dense (last stride 1)")
+    _launch("dreams_rope", dev, stream, x.data_ptr(), _I64x3(*x.stride()[:3]), out.data_ptr(),
+            _I64x3(*out.stride()[:3]), F32 if x.dtype == torch.float32 else BF16, B, T, H, D,
+            ctypes.byref(rotary._c), pos, axes, st, int(bool(transpose)), _status(status, dev))
+    return out
+
+
+def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary: Rotary, kv_len: torch.Tensor,
+                   n_new: torch.Tensor, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                   positions: Optional[torch.Tensor] = None, parent: Optional[torch.Tensor] = None, layer: int = 0,
+                   status: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """kv_append with the rotation on the way: turned rows of ``k_new`` and those
+    of ``v_new`` (bf16 [B, T_max, Hkv, D], head rows dense, strides of their own)
+    go to slots kv_len .. kv_len + n_new - 1 of one layer, and turned rows of ``q``
+    (bf16 [B, T_max, Hq, D]) to ``q_out`` (dense; may be ``q``), which is returned.
+    Positions: ``positions`` (int32 [B, T_max] or [n_axes, B, T_max]); or
+    ``parent`` (int32 [B, T_max]): kv_len + a tree node's depth; or kv_len + t."""
+    dev = kv.k.device
+    kb, kt = _q_strides(k_new, "k_new", "Hkv")
+    vb, vt = _q_strides(v_new, "v_new", "Hkv")
+    B, T_max, Hkv, D = k_new.shape
+    if k_new.shape != v_new.shape or k_new.device != dev or v_new.device != dev:
+        raise ValueError("k_new and v_new must share their shape and the cache's device")
+    if Hkv != kv.Hkv:
+        raise ValueError(f"k_new has {Hkv} heads, the cache {kv.Hkv}")
+    _cache_covers(kv, B)
+    if kv.D != D:
+        raise ValueError(f"k_new's head dim {D} differs from the cache's {kv.D}")
+    if rotary.phase.device != dev:
+        raise ValueError(f"the rotary table is on {rotary.phase.device}, the cache on {dev}")
+    kl, nn = _per_seq(kv_len, "kv_len", B, dev), _per_seq(n_new, "n_new", B, dev)
+    pos, axes = _positions(positions, B, T_max, dev)
+    par = None
+    if parent is not None:
+        if positions is not None:
+            raise ValueError("give positions or parent, not both")
+        _need(parent, "parent", torch.int32, dev)
+        if tuple(parent.shape) != (B, T_max):
+            raise ValueError("parent must be [B, T_max]")
+        par = parent.data_ptr()
+    Hq, qs = 0, None
+    if q is not None:
+        qb, qt = _q_strides(q)
+        if q.device != dev or tuple(q.shape[:2]) != (B, T_max) or q.shape[3] != D:
+            raise ValueError("q must be [B, T_max, Hq, D] on the cache's device, with k_new's B, T_max and D")
+        Hq, qs = int(q.shape[2]), _I64x2(qb, qt)
+        if q_out is None:
+            q_out = _new((B, T_max, Hq, D), torch.bfloat16, dev, stream)
+        else:
+            _need(q_out, "q_out", torch.bfloat16, dev)
+            if q_out.shape != q.shape:
+                raise ValueError("q_out must have q's shape")
+    elif q_out is not None:
+        raise ValueError("q_out goes with q")
+    _launch("dreams_kv_append_rope", dev, stream, ctypes.byref(kv._c), layer, None if q is None else q.data_ptr(), qs,
+            None if q_out is None else q_out.data_ptr(), Hq, k_new.data_ptr(), _I64x2(kb, kt), v_new.data_ptr(),
+            _I64x2(vb, vt), ctypes.byref(rotary._c), pos, axes, par, kl, nn, B, T_max, _status(status, dev))
+    return q_out
+
+
+def _both_caches(kv8: KV8Cache, kv: KVCache, B: int) -> None:
+    if kv8.k.device != kv.k.device:
+        raise ValueError(f"the 8-bit cache is on {kv8.k.device}, the bf16 one on {kv.k.device}")
+    if (kv8.n_layers, kv8.Hkv, kv8.D) != (kv.n_layers, kv.Hkv, kv.D):
+        raise ValueError("the two caches must share their layers, heads and head dim")
+    _cache_covers(kv, B)
+    if kv8.B < B:
+        raise ValueError(f"the 8-bit cache holds {kv8.B} sequences, the call addresses {B}")
+
+
+def kv_quantize(kv: KVCache, kv8: KV8Cache, begin: torch.Tensor, end: torch.Tensor,
+                new_len8: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                stream=None) -> torch.Tensor:
+    """Puts the pages that lie wholly inside slots begin .. end - 1 of ``kv`` into
+    8 bits, in all layers (begin: the slots in 8 bits so far, end: kv_len); kv8 has
+    pages for them (kv_reserve on its pool). Returns the slots in 8 bits after it."""
+    dev = kv.k.device
+    B = int(begin.numel())
+    _both_caches(kv8, kv, B)
+    bg, en = _per_seq(begin, "begin", B, dev), _per_seq(end, "end", B, dev)
+    if new_len8 is None:
+        new_len8 = _new(B, torch.int32, dev, stream)
+    _launch("dreams_kv_quantize", dev, stream, ctypes.byref(kv._c), ctypes.byref(kv8._c8), B, bg, en,
+            _per_seq(new_len8, "new_len8", B, dev), _status(status, dev))
+    return new_len8
+
+
+def kv8_attention(q: torch.Tensor, kv8: KV8Cache, kv: KVCache, q_len: torch.Tensor, kv_len: torch.Tensor,
+                  len8: torch.Tensor, scale: float, window: Optional[int] = None, sinks: int = 0,
+                  parent: Optional[torch.Tensor] = None, layer: int = 0, out: Optional[torch.Tensor] = None,
+                  lse: Optional[torch.Tensor] = None, want_lse: bool = False, status: Optional[torch.Tensor] = None,
+                  stream=None):
+    """window_attention over a cache whose first ``len8`` slots of each sequence
+    (multiples of 64) are in ``kv8`` and whose later ones are in ``kv``; without
+    ``window`` every slot is seen. Returns (out, lse or None); rows past q_len are
+    left untouched."""
+    dev = q.device
+    sb, stt = _q_strides(q)
+    B, T_max, Hq, D = q.shape
+    ql, kl, l8 = (_per_seq(t, n, B, dev) for t, n in ((q_len, "q_len"), (kv_len, "kv_len"), (len8, "len8")))
+    _cache_covers(kv, B, D)
+    _both_caches(kv8, kv, B)
+    if kv.k.device != dev:
+        raise ValueError(f"the KV cache is on {kv.k.device}, q on {dev}")
+    par = None
+    if parent is not None:
+        _need(parent, "parent", torch.int32, dev)
+        if tuple(parent.shape) != (B, T_max):
+            raise ValueError("parent must be [B, T_max]")
+        par = parent.data_ptr()
+    if out is None:
+        out = _new((B, T_max, Hq, D), torch.bfloat16, dev, stream)
+    else:
+        _need(out, "out", torch.bfloat16, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    if lse is None:
+        if want_lse:
+            lse = _new((B, T_max, Hq), torch.float32, dev, stream)
+    else:
+        _need(lse, "lse", torch.float32, dev)
+        if lse.shape != q.shape[:3]:
+            raise ValueError("lse must be [B, T_max, Hq]")
+    _launch("dreams_kv8_attention", dev, stream, q.data_ptr(), sb, stt, ctypes.byref(kv8._c8), ctypes.byref(kv._c),
+            layer, par, ql, kl, l8, B, T_max, Hq, float(scale), 2 ** 31 - 1 if window is None else window, sinks,
+            out.data_ptr(), None if lse is None else lse.data_ptr(), _status(status, dev))
+    return out, lse
 
 
 VERIFY_STEP_SPECULATIVE_LAUNCHES = 1  # one cluster per sequence: walk, residual sums, bonus, compaction

@@ -35,6 +35,19 @@ inline dreams_status_t check_launch() {
   return DREAMS_OK;
 }
 
+// Division of x in [0, 2^31) by a divisor that the host knows: x m >> (31 + s) with
+// s = ceil(log2 d), m = ceil(2^(31 + s) / d), which is exact (x (m d - 2^(31 + s)) <
+// 2^(31 + s)). The division instructions of an item's set-up took half a microsecond.
+struct Divisor {
+  uint32_t d, m, s;
+  static Divisor of(int64_t d) {
+    uint32_t s = 0;
+    while ((int64_t(1) << s) < d) ++s;
+    return Divisor{uint32_t(d), uint32_t(((uint64_t(1) << (31 + s)) + uint64_t(d) - 1) / uint64_t(d)), s};
+  }
+  __device__ __forceinline__ int div(int x) const { return int((uint64_t(uint32_t(x)) * m) >> (31 + s)); }
+};
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Kernels launched with this attribute are set up while the one before them in the

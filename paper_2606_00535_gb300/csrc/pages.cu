@@ -10,12 +10,11 @@
 
 #include <algorithm>
 
-#include "common.cuh"
+#include "cache.cuh"
 
 namespace dreams {
 namespace {
 
-constexpr int PAGE = 64;
 constexpr int BOOK_THREADS = 1024;
 constexpr int FORK_CTAS = 8;  // one portable cluster
 
@@ -24,33 +23,6 @@ struct Pool {
   int32_t *ref;
   int32_t B, P, num_pages;
 };
-
-struct Cache {
-  uint4 *k, *v;  // 16-byte columns
-  int32_t n_layers;
-  int64_t layer16;  // layer stride in 16-byte units
-  int32_t row16;    // Hkv * D / 8: 16-byte columns of a slot
-  int32_t capacity;
-  const int32_t *table;  // nullptr: contiguous
-  int32_t P, num_pages;
-};
-
-// 16-byte offset of slot s of sequence b within a layer; -1: no page.
-__device__ __forceinline__ int64_t slot16(const Cache &c, int b, int s) {
-  if (c.table == nullptr) return (int64_t(b) * c.capacity + s) * c.row16;
-  const int pg = c.table[int64_t(b) * c.P + (s >> 6)];
-  if (pg < 0 || pg >= c.num_pages) return -1;
-  return (int64_t(pg) * PAGE + (s & (PAGE - 1))) * c.row16;
-}
-
-__device__ __forceinline__ uint4 ld_stream(const uint4 *p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p)
-               : "memory");
-  return v;
-}
 
 // Exclusive prefix sum of one value per thread over the block, and the total.
 __device__ __forceinline__ int block_scan(int x, int *s_warp, int &total) {
@@ -627,30 +599,6 @@ __global__ void __launch_bounds__(PRUNE_THREADS, 1) kv_prune_kernel(const Cache 
 // ------------------------------------------------------------------ host side
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-bool cache_ok(const dreams_kv_cache_t *kv, Cache &c) {
-  if (kv == nullptr || kv->k == nullptr || kv->v == nullptr || kv->n_layers < 1 || kv->Hkv < 1 || kv->D < 8 ||
-      kv->D % 8 != 0 || kv->capacity < 1 || kv->layer_stride < 0)
-    return false;
-  if (!aligned16(kv->k) || !aligned16(kv->v) || (kv->layer_stride * 2) % 16 != 0) return false;
-  if (int64_t(kv->Hkv) * (kv->D / 8) > (1 << 20)) return false;
-  if (kv->page_table != nullptr &&
-      (kv->page_size != PAGE || kv->pages_per_seq < 1 || kv->num_pages < 1 || !aligned4(kv->page_table) ||
-       int64_t(kv->pages_per_seq) * PAGE != kv->capacity))
-    return false;
-  c.k = static_cast<uint4 *>(kv->k);
-  c.v = static_cast<uint4 *>(kv->v);
-  c.n_layers = kv->n_layers;
-  c.layer16 = kv->layer_stride * 2 / 16;
-  c.row16 = kv->Hkv * (kv->D / 8);
-  c.capacity = kv->capacity;
-  c.table = kv->page_table;
-  c.P = kv->pages_per_seq;
-  c.num_pages = kv->num_pages;
-  return true;
-}
-
 bool pool_ok(const dreams_page_pool_t *pool, Pool &p) {
   if (pool == nullptr || pool->page_table == nullptr || pool->refcount == nullptr || !aligned4(pool->page_table) ||
       !aligned4(pool->refcount) || pool->B < 1 || pool->B > 65535 || pool->pages_per_seq < 1 || pool->num_pages < 1 ||
@@ -679,28 +627,6 @@ size_t fork_layout(const Pool &p, uint8_t *ws, ForkState *f) {
   return at;
 }
 
-template <typename... Params, typename... Args>
-dreams_status_t launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, dreams_stream_t stream,
-                       const Args &...args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(unsigned(threads));
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = reinterpret_cast<cudaStream_t>(stream);
-  cudaLaunchAttribute attr[2] = {early_launch()};
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = unsigned(cluster);
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
-  if (e != cudaSuccess) {
-    set_last_cuda_error(e);
-    return DREAMS_ERR_CUDA;
-  }
-  return check_launch();
-}
-
 }  // namespace
 }  // namespace dreams
 
@@ -724,7 +650,7 @@ extern "C" dreams_status_t dreams_kv_reserve(const dreams_page_pool_t *pool, con
   int32_t *list = start + align_up(size_t(p.B) * 4, 256) / 4;
   int g = 32;
   while (g > 1 && int64_t(p.B) * g > BOOK_THREADS) g /= 2;
-  return launch(kv_reserve_kernel, dim3(1), BOOK_THREADS, 0, 1, stream, p, kv_len, n_new, start, list, status_word, g);
+  return launch(early_launch(), kv_reserve_kernel, dim3(1), BOOK_THREADS, 0, 1, stream, p, kv_len, n_new, start, list, status_word, g);
 }
 
 extern "C" dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, const int32_t *begin, const int32_t *end,
@@ -732,7 +658,7 @@ extern "C" dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, con
   Pool p;
   if (!pool_ok(pool, p) || begin == nullptr || end == nullptr || !aligned4(begin) || !aligned4(end))
     return DREAMS_ERR_INVALID_ARG;
-  return launch(kv_release_kernel, dim3(unsigned((p.P + 255) / 256), unsigned(p.B)), 256, 0, 1, stream, p, begin, end, status_word);
+  return launch(early_launch(), kv_release_kernel, dim3(unsigned((p.P + 255) / 256), unsigned(p.B)), 256, 0, 1, stream, p, begin, end, status_word);
 }
 
 extern "C" size_t dreams_kv_fork_workspace_size(const dreams_page_pool_t *pool) {
@@ -756,12 +682,12 @@ extern "C" dreams_status_t dreams_kv_fork(const dreams_kv_cache_t *kv, const dre
   ForkState f;
   fork_layout(p, static_cast<uint8_t *>(workspace), &f);
   const bool one = int64_t(p.B) * p.P <= FORK_ONE_CELLS;
-  const dreams_status_t st = launch(one ? kv_fork_table_kernel<1> : kv_fork_table_kernel<FORK_CTAS>, dim3(one ? 1 : FORK_CTAS), BOOK_THREADS, 0,
+  const dreams_status_t st = launch(early_launch(), one ? kv_fork_table_kernel<1> : kv_fork_table_kernel<FORK_CTAS>, dim3(one ? 1 : FORK_CTAS), BOOK_THREADS, 0,
                                     one ? 1 : FORK_CTAS, stream, p, parent, kv_len, new_kv_len, f, status_word);
   if (st != DREAMS_OK) return st;
   const int pieces = (PAGE * c.row16 + COPY_PIECE - 1) / COPY_PIECE;
   const int64_t most = int64_t(p.B) * c.n_layers * 2 * pieces;
-  return launch(kv_fork_copy_kernel, dim3(unsigned(std::min<int64_t>(most, int64_t(num_sms()) * 8))), 256, 0, 1, stream, c, f, pieces);
+  return launch(early_launch(), kv_fork_copy_kernel, dim3(unsigned(std::min<int64_t>(most, int64_t(num_sms()) * 8))), 256, 0, 1, stream, c, f, pieces);
 }
 
 extern "C" dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t layer, const void *k_new,
@@ -783,7 +709,7 @@ extern "C" dreams_status_t dreams_kv_append(const dreams_kv_cache_t *kv, int32_t
   if (blocks > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
   c.k += layer * c.layer16;
   c.v += layer * c.layer16;
-  return launch(kv_append_kernel, dim3(unsigned(blocks), unsigned(B)), 256, 0, 1, stream, c, static_cast<const uint4 *>(k_new),
+  return launch(early_launch(), kv_append_kernel, dim3(unsigned(blocks), unsigned(B)), 256, 0, 1, stream, c, static_cast<const uint4 *>(k_new),
                 static_cast<const uint4 *>(v_new), stride_b / 8, stride_t / 8, kv_len, n_new, T_max, status_word);
 }
 
@@ -815,6 +741,6 @@ extern "C" dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t 
   const dreams_status_t st = ensure_max_dynamic_smem(reinterpret_cast<const void *>(kv_prune_kernel), PRUNE_SMEM);
   if (st != DREAMS_OK) return st;
   const dim3 grid(unsigned(int64_t(c.n_layers) * 2 * nblk), unsigned(B));
-  return launch(kv_prune_kernel, grid, PRUNE_THREADS, PRUNE_SMEM, 1, stream, c, keep, v0, n_vis, r, kv_len, refcount, new_kv_len, status_word, cw,
+  return launch(early_launch(), kv_prune_kernel, grid, PRUNE_THREADS, PRUNE_SMEM, 1, stream, c, keep, v0, n_vis, r, kv_len, refcount, new_kv_len, status_word, cw,
                 nblk);
 }

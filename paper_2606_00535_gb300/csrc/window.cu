@@ -540,24 +540,22 @@ dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
   return check_launch();
 }
 
-bool shapes_ok(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max, int32_t Hq, int32_t window, int32_t sinks,
+}  // namespace
+}  // namespace dreams
+
+namespace dreams {
+namespace win {
+
+static bool shapes_ok(const dreams_kv_cache_t *kv, int32_t B, int32_t T_max, int32_t Hq, int32_t window, int32_t sinks,
                bool tree) {
   return kv != nullptr && B >= 1 && B <= 65535 && T_max >= 1 && T_max <= (tree ? 64 : 1 << 20) && kv->Hkv >= 1 &&
          kv->Hkv <= 65535 && Hq >= kv->Hkv && Hq % kv->Hkv == 0 && Hq / kv->Hkv <= 128 && kv->capacity >= 1 &&
          kv->n_layers >= 1 && window >= 1 && sinks >= 0;
 }
 
-}  // namespace
-}  // namespace dreams
-
-using namespace dreams;
-
-extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
-                                                   const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
-                                                   const int32_t *q_len, const int32_t *kv_len, int32_t B,
-                                                   int32_t T_max, int32_t Hq, float scale, int32_t window,
-                                                   int32_t sinks, void *out, float *lse, int32_t *status_word,
-                                                   dreams_stream_t stream) {
+dreams_status_t window_args(const void *q, int64_t q_stride_b, int64_t q_stride_t, const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
+                            const int32_t *q_len, const int32_t *kv_len, int32_t B, int32_t T_max, int32_t Hq, float scale, int32_t window,
+                            int32_t sinks, void *out, float *lse, int32_t *status_word, WinParams &p) {
   if (q == nullptr || out == nullptr || kv == nullptr || q_len == nullptr || kv_len == nullptr || kv->k == nullptr ||
       kv->v == nullptr || !shapes_ok(kv, B, T_max, Hq, window, sinks, parent != nullptr))
     return DREAMS_ERR_INVALID_ARG;
@@ -578,7 +576,7 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
     if (kv->pages_per_seq < 1 || kv->num_pages < 1 || int64_t(kv->pages_per_seq) * 64 != kv->capacity)
       return DREAMS_ERR_INVALID_ARG;
   }
-  WinParams p{};
+  p = WinParams{};
   p.q = static_cast<const __nv_bfloat16 *>(q);
   p.sb = q_stride_b;
   p.st = q_stride_t;
@@ -602,6 +600,24 @@ extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stri
   p.sinks = sinks;
   p.scale_log2 = scale * LOG2E;
   p.status = status_word;
+  return DREAMS_OK;
+}
+
+}  // namespace win
+}  // namespace dreams
+
+using namespace dreams;
+
+extern "C" dreams_status_t dreams_window_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,
+                                                   const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
+                                                   const int32_t *q_len, const int32_t *kv_len, int32_t B,
+                                                   int32_t T_max, int32_t Hq, float scale, int32_t window,
+                                                   int32_t sinks, void *out, float *lse, int32_t *status_word,
+                                                   dreams_stream_t stream) {
+  WinParams p;
+  const dreams_status_t st =
+      win::window_args(q, q_stride_b, q_stride_t, kv, layer, parent, q_len, kv_len, B, T_max, Hq, scale, window, sinks, out, lse, status_word, p);
+  if (st != DREAMS_OK) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (int64_t(T_max) * p.G > RB) return launch_tc(p, kv, s);
   if (int64_t(T_max) * p.G <= 8) return kv->D == 128 ? launch_rows<128, true>(p, s) : launch_rows<64, true>(p, s);

@@ -78,6 +78,11 @@ __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t cta) {
   return r;
 }
 
+// The checks of dreams_window_attention's arguments, and its parameters from them.
+dreams_status_t window_args(const void *q, int64_t q_stride_b, int64_t q_stride_t, const dreams_kv_cache_t *kv, int32_t layer, const int32_t *parent,
+                            const int32_t *q_len, const int32_t *kv_len, int32_t B, int32_t T_max, int32_t Hq, float scale, int32_t window,
+                            int32_t sinks, void *out, float *lse, int32_t *status_word, WinParams &p);
+
 // Blocks of 128 rows on the fifth-generation tensor cores (window_tc.cu).
 dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaStream_t stream);
 
