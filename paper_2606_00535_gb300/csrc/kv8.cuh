@@ -54,4 +54,9 @@ __device__ __forceinline__ float code_value(uint32_t code) {
   return __uint_as_float(u) * 0x1p120f;
 }
 
+namespace win {
+// Blocks of 128 rows over a cache in 8 bits (window_tc.cu).
+dreams_status_t launch_tc8(const WinParams &p, const Kv8 &c, int D, cudaStream_t stream);
+}  // namespace win
+
 }  // namespace dreams

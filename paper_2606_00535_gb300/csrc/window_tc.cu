@@ -51,8 +51,10 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "tmap.cuh"
+#include "kv8.cuh"
 #include "window.cuh"
 
 namespace dreams {
@@ -61,8 +63,8 @@ namespace {
 
 constexpr int KT = 128;    // keys of a tile
 constexpr int ROWS = 128;  // query rows of a block
-constexpr int THREADS = 384;
 constexpr int TMA_WARP = 8, MMA_WARP = 9, SCAN_WARP = 11;  // slot w's MMAs: warp MMA_WARP + w
+constexpr int CODE_WARP = 12, CODE_WARPS = 4;              // EIGHT: those that turn codes into bf16
 // Items whose scan results are kept: more than the scan can be ahead of a slot that has
 // tiles of the item, as it needs stages which that slot gives back. Of a slot that has
 // none it can be ahead by any number of items, so such a slot asks for no result.
@@ -74,8 +76,9 @@ constexpr uint32_t TMEM_COLS = 512;
 // a NaN of O may not be V's.
 constexpr float MOST_SUM = 1.2676506e30f, SAFE_SUM = 1.0995116e12f;
 
-template <int D, bool PAIR>
+template <int D, bool PAIR, bool EIGHT>
 struct Cfg {
+  static constexpr int THREADS = EIGHT ? 512 : 384;
   static constexpr int NR = D / 64;  // 128-byte column regions of a row
   static constexpr uint32_t Q_REGION = ROWS * 128, KV_REGION = KT * 128;
   static constexpr uint32_t Q_BYTES = NR * Q_REGION;
@@ -85,8 +88,11 @@ struct Cfg {
   // next Q K^T can start once the scores are in registers; with 128 P goes over S.
   static constexpr bool BESIDE = D == 64;
   static constexpr uint32_t P_COL = BESIDE ? 128 : 0, O_COL = BESIDE ? 192 : 128;
-  static constexpr int NST = D == 64 ? 8 : 5;
-  static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + 1024, 120 * 1024);
+  static constexpr int NST = D == 64 ? 8 : EIGHT ? 4 : 5;
+  // EIGHT: stages of codes, two pages of K or V each
+  static constexpr int NCODE = !EIGHT ? 0 : D == 64 ? 4 : 2;
+  static constexpr uint32_t CODES = KT * D;
+  static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + size_t(NCODE) * CODES + 1024, 120 * 1024);
 };
 
 struct TcParams {
@@ -99,12 +105,18 @@ struct TcParams {
   int32_t stall_at;
   uint64_t wait_ns;
 };
+struct Tc8Params : TcParams {
+  CUtensorMap tmap_k8, tmap_v8;
+  Kv8 c;
+};
+template <bool EIGHT>
+using ParamsOf = std::conditional_t<EIGHT, Tc8Params, TcParams>;
 
 // An item: a pair of blocks, or one block, of a sequence and KV head. Its keys are
 // np half tiles of up to 64 slots, the nsp sink ones first; tile j is the halves
 // 2j and 2j + 1. A key's column is its place in that row of halves.
 struct Item {
-  int b, g, L, T;
+  int b, g, L, T, L8;      // L8: slots in 8 bits
   int t00, t01, tl0, tl1;  // first and last token of each block
   int nb;                  // blocks present (0: nothing to do)
   int lo, lo64, S1, hi;
@@ -112,6 +124,7 @@ struct Item {
   int e0, a1;              // block 0 reads tiles [0, e0), block 1 [0, ns) and [a1, n)
   __device__ __forceinline__ bool need0(int j) const { return j < e0; }
   __device__ __forceinline__ bool need1(int j) const { return nb == 2 && j < n && (j < ns || j >= a1); }
+  __device__ __forceinline__ bool codes(int q) const { return q < np && slot0(q) < L8; }
   __device__ __forceinline__ int slot0(int q) const { return q < nsp ? q * 64 : lo64 + (q - nsp) * 64; }
   // the slots of half q that a row may see, from its first one on
   __device__ __forceinline__ int beg(int q) const { return q < nsp ? 0 : ::max(0, lo - slot0(q)); }
@@ -142,22 +155,37 @@ __device__ __forceinline__ Whole whole_tiles(const WinParams &p, const Item &it,
   return Whole{it.S1 / KT, (it.nsp + (from + 63) / 64 + 1) / 2, (it.nsp + (to > 0 ? to / 64 : 0)) / 2};
 }
 
-template <bool PAIR>
-__device__ __forceinline__ void load_item(const TcParams &P, int x, Item &it, bool report, const int2 *lens = nullptr) {
+// What is known of a sequence.
+struct Lens {
+  int T, L, L8;
+};
+template <bool EIGHT>
+__device__ __forceinline__ Lens lens_of(const ParamsOf<EIGHT> &P, int b) {
+  Lens l{P.p.q_len[b], P.p.kv_len[b], 0};
+  if constexpr (EIGHT) l.L8 = P.c.len8[b];
+  return l;
+}
+
+template <bool PAIR, bool EIGHT>
+__device__ __forceinline__ void load_item(const ParamsOf<EIGHT> &P, int x, Item &it, bool report, const Lens *lens = nullptr) {
   const WinParams &p = P.p;
   // the last blocks first (they have the most keys), all heads of a block together
   const int turn = P.heads.div(x), blk = P.nblk - 1 - turn, bg = x - turn * int(P.heads.d);
   it.b = P.hkv.div(bg);
   it.g = bg - it.b * p.Hkv;
-  it.T = lens != nullptr ? lens->x : p.q_len[it.b];
-  it.L = lens != nullptr ? lens->y : p.kv_len[it.b];
+  const Lens l = lens != nullptr ? *lens : lens_of<EIGHT>(P, it.b);
+  it.T = l.T;
+  it.L = l.L;
+  it.L8 = l.L8;
   it.nb = it.n = it.ns = 0;
   report = report && it.g == 0 && blk == 0;
   if (it.T < 0 || it.T > p.T_max) {
     if (report) flag(p.status, DREAMS_DATA_BAD_TREE_LEN);
     return;
   }
-  if (it.L < 0 || int64_t(it.L) + it.T > p.capacity) {
+  bool odd = it.L < 0 || int64_t(it.L) + it.T > p.capacity;
+  if constexpr (EIGHT) odd = odd || len8_bad(P.c, it.L8, it.L);
+  if (odd) {
     if (report) flag(p.status, DREAMS_DATA_BAD_KV_LEN);
     return;
   }
@@ -321,9 +349,10 @@ struct Row {
 // that do not see it), and when a row's sum outgrew its reference. Slow (0.58 us a key,
 // a chain of page entry, K, five shuffles and exponentials), and rare; `beat` is given the
 // time while it lasts.
-template <int D>
-__device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, int t, int h, int off, unsigned long long anc,
+template <int D, bool EIGHT>
+__device__ __noinline__ void slow_row(const ParamsOf<EIGHT> &P, int b, int g, int L, int t, int h, int off, unsigned long long anc,
                                       volatile int64_t *beat) {
+  const WinParams &p = P.p;
   const int lane = threadIdx.x & 31;
   constexpr int E = D / 32;
   float q[E], o[E];
@@ -340,7 +369,16 @@ __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, i
     const int s = kl.slot(i);
     if (!sees(p, L, off, anc, s)) continue;
     int64_t at;
-    if (p.table == nullptr) {
+    bool codes = false;
+    uint32_t exps = 0;
+    if constexpr (EIGHT) codes = s < P.c.len8[b];
+    if (codes) {
+      if constexpr (EIGHT) {
+        const int pg = P.c.table[int64_t(b) * P.c.P + (s >> 6)];
+        at = pg >= 0 && pg < P.c.num_pages ? (int64_t(pg) * 64 + (s & 63)) * p.Hkv + g : -1;
+        if (at >= 0) exps = P.c.exps[int64_t(pg) * p.Hkv + g];
+      }
+    } else if (p.table == nullptr) {
       at = (int64_t(b) * p.capacity + s) * p.Hkv + g;
     } else {
       const int pg = p.table[int64_t(b) * p.P + (s >> 6)];
@@ -349,8 +387,19 @@ __device__ __noinline__ void slow_row(const WinParams &p, int b, int g, int L, i
     float x = 0.f, v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      x += at >= 0 ? q[e] * __bfloat162float(p.k[at * D + lane * E + e]) : 0.f;
-      v[e] = at >= 0 ? __bfloat162float(p.v[at * D + lane * E + e]) : 0.f;
+      float kx = 0.f, vx = 0.f;
+      if (at >= 0) {
+        const int64_t i = at * D + lane * E + e;
+        if constexpr (EIGHT) {
+          kx = codes ? code_value(P.c.k[i]) * power(k_exp(exps)) : __bfloat162float(p.k[i]);
+          vx = codes ? code_value(P.c.v[i]) * power(v_exp(exps)) : __bfloat162float(p.v[i]);
+        } else {
+          kx = __bfloat162float(p.k[i]);
+          vx = __bfloat162float(p.v[i]);
+        }
+      }
+      x += q[e] * kx;
+      v[e] = vx;
     }
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) x += __shfl_xor_sync(0xffffffffu, x, k);
@@ -388,9 +437,9 @@ __device__ __noinline__ bool overflowed(uint32_t o_at) {
   return odd != 0u;
 }
 
-template <int D, bool PAIR>
-__global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_constant__ TcParams P) {
-  using C = Cfg<D, PAIR>;
+template <int D, bool PAIR, bool EIGHT>
+__global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_kernel(const __grid_constant__ ParamsOf<EIGHT> P) {
+  using C = Cfg<D, PAIR, EIGHT>;
   using Pos = Place<C::NST>;
   const WinParams &p = P.p;
   constexpr int NST = C::NST, NR = C::NR;
@@ -398,6 +447,9 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST], bar_ready[NST];
   __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_r[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
+  // EIGHT: codes' stages, their powers, and bf16 pages that copies bring
+  __shared__ __align__(8) uint64_t bar_code[EIGHT ? C::NCODE : 1], bar_taken[EIGHT ? C::NCODE : 1], bar_wide[EIGHT ? NST : 1];
+  __shared__ uint32_t s_exp[EIGHT ? C::NCODE : 1][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
   __shared__ int64_t s_beat;
@@ -409,15 +461,21 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t base = smem_u32(smem);
   auto q_s = [&](int w) { return base + uint32_t(PAIR ? w : 0) * C::Q_BYTES; };
-  const uint32_t ring = base + C::NQ * C::Q_BYTES;
+  const uint32_t ring = base + C::NQ * C::Q_BYTES, codes = ring + uint32_t(NST) * C::STAGE;
+  const uint32_t code0 = smem_u32(bar_code), taken0 = smem_u32(bar_taken), wide0 = smem_u32(bar_wide);
   const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty), ready0 = smem_u32(bar_ready);
   const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), r0 = smem_u32(bar_r), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
                  o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
   if (warp == TMA_WARP) {
     if (lane < NST) {
-      tc::mbar_init(full0 + 8 * lane, 1);
+      tc::mbar_init(full0 + 8 * lane, EIGHT ? CODE_WARPS : 1);
+      if constexpr (EIGHT) tc::mbar_init(wide0 + 8 * lane, 1);
       tc::mbar_init(ready0 + 8 * lane, 1);  // the scan
       tc::mbar_init(empty0 + 8 * lane, 3);  // both slots, and the scan
+    }
+    if (EIGHT && lane < C::NCODE) {
+      tc::mbar_init(code0 + 8 * lane, 1);
+      tc::mbar_init(taken0 + 8 * lane, CODE_WARPS);
     }
     if (lane < SEEN) {
       s_dirty[lane] = 0;
@@ -444,6 +502,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
       tc::prefetch_tmap(&P.tmap_q);
       tc::prefetch_tmap(&P.tmap_k);
       tc::prefetch_tmap(&P.tmap_v);
+      if constexpr (EIGHT) {
+        tc::prefetch_tmap(&P.tmap_k8);
+        tc::prefetch_tmap(&P.tmap_v8);
+      }
     }
   }
   after_previous();  // (ahead of tensor memory too: the kernel before may still be about to take it)
@@ -452,11 +514,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     tc::tmem_relinquish();
   }
   // Without PAIR the item is known: its lengths and parents are on their way early.
-  int2 lens = make_int2(0, 0);
+  Lens lens{0, 0, 0};
   int early[2] = {-1, -1};
   if constexpr (!PAIR) {
     const int x = P.nsplit.div(int(blockIdx.x)), b = P.hkv.div(x - P.heads.div(x) * int(P.heads.d));
-    lens = make_int2(p.q_len[b], p.kv_len[b]);
+    lens = lens_of<EIGHT>(P, b);
     if (p.parent != nullptr && warp < 8) {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
@@ -483,7 +545,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
   // the next item with work, and the tiles [j0, j1) of it that are this CTA's
   auto next_item = [&](Item &it, int &j0, int &j1, bool report) {
     while (x_next < P.items) {
-      load_item<PAIR>(P, x_next, it, report, PAIR ? nullptr : &lens);
+      load_item<PAIR, EIGHT>(P, x_next, it, report, PAIR ? nullptr : &lens);
       x_next += PAIR ? int(gridDim.x) : P.items;
       if (PAIR) {
         j0 = 0;
@@ -773,7 +835,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           for (int i = 0; i < 32; ++i) {
             const int ti = __shfl_sync(0xffffffffu, t, i), oi = __shfl_sync(0xffffffffu, r.off, i), hi = __shfl_sync(0xffffffffu, h, i);
             const unsigned long long ai = __shfl_sync(0xffffffffu, r.anc, i);
-            if ((again >> i) & 1u) slow_row<D>(p, sp->b, sp->g, sp->L, ti, hi, oi, ai, &s_beat);
+            if ((again >> i) & 1u) slow_row<D, EIGHT>(P, sp->b, sp->g, sp->L, ti, hi, oi, ai, &s_beat);
           }
         }
         tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
@@ -795,28 +857,49 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         Pos at{0, 0};
         bool wrapped = false, ok = true;
         int issued = 0, ktiles = 0;
+        uint32_t used = 0, phases = 0;  // EIGHT: ring stages that copies have written, and the phases of their barriers
+        Place<(EIGHT ? C::NCODE : 1)> cp{0, 0};
         uint32_t nq[2] = {0, 0};
         Item it;
         int j0, j1;
         while (ok && next_item(it, j0, j1, split == 0)) {
           const int32_t *row = p.table != nullptr ? p.table + int64_t(it.b) * p.P : nullptr;
           auto fetch = [&](int j, int h) {
-            if (row == nullptr || j >= j1 || 2 * j + h >= it.np) return 0;
+            if (j >= j1 || 2 * j + h >= it.np) return 0;
             const int pi = it.slot0(2 * j + h) >> 6;
+            if constexpr (EIGHT) {
+              if (it.codes(2 * j + h)) return P.c.table[int64_t(it.b) * P.c.P + pi];
+            }
+            if (row == nullptr) return 0;
             return pi < p.P ? row[pi] : -1;
+          };
+          auto powers = [&](int j, int h, int pg) -> uint32_t {
+            if constexpr (EIGHT) {
+              if (j < j1 && it.codes(2 * j + h) && pg >= 0 && pg < P.c.num_pages) return P.c.exps[int64_t(pg) * p.Hkv + it.g];
+            }
+            return 0u;
           };
           int pg0 = fetch(j0, 0), pg1 = fetch(j0, 1);
           for (int j = j0; j < j1 && ok; ++j) {
             const int halves = 2 * j + 1 < it.np ? 2 : 1, ha = it.slot0(2 * j), hb = it.slot0(2 * j + 1);
             // tensor-map coordinate (dim 3) of a half: outside the map (zeros) where the
             // page is missing
+            const bool c0 = EIGHT && it.codes(2 * j), c1 = EIGHT && it.codes(2 * j + 1);
             auto coord = [&](int h, int pg) {
+              if constexpr (EIGHT) {
+                if (h == 0 ? c0 : c1) {
+                  if (pg >= 0 && pg < P.c.num_pages) return pg;
+                  flag(p.status, DREAMS_DATA_BAD_PAGE);
+                  return P.c.num_pages;
+                }
+              }
               if (row == nullptr) return it.b;
               if (pg >= 0 && pg < p.num_pages) return pg;
               if (h < halves) flag(p.status, DREAMS_DATA_BAD_PAGE);
               return p.num_pages;
             };
             const int ca = coord(0, pg0), cb = coord(1, pg1), sa = row != nullptr ? 0 : ha, sb = row != nullptr ? 0 : hb;
+            const uint32_t x0 = powers(j, 0, pg0), x1 = powers(j, 1, pg1);  // (waited for where they are used)
             pg0 = fetch(j + 1, 0);
             pg1 = fetch(j + 1, 1);
 #pragma unroll 1
@@ -827,19 +910,41 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
                 ok = false;
                 break;
               }
-              if (wrapped && !wait(empty0 + 8 * at.s, at.ph ^ 1u)) {
-                ok = false;
-                break;
+              if constexpr (EIGHT) {
+                if (c0 || c1) {  // codes' stages do not wait for the ring
+                  if (issued >= C::NCODE && !wait(taken0 + 8 * cp.s, cp.ph ^ 1u)) {
+                    ok = false;
+                    break;
+                  }
+                  const uint32_t st = codes + uint32_t(cp.s) * C::CODES, bar = code0 + 8 * cp.s;
+                  s_exp[cp.s][0] = x0;
+                  s_exp[cp.s][1] = x1;
+                  tc::mbar_arrive_expect_tx(bar, uint32_t(int(c0) + int(c1)) * 64 * D);
+                  const CUtensorMap *map = kv == 0 ? &P.tmap_k8 : &P.tmap_v8;
+                  if (c0) tc::tma_load_4d(st, map, bar, 0, it.g, 0, ca);
+                  if (c1) tc::tma_load_4d(st + 64 * D, map, bar, 0, it.g, 0, cb);
+                  ++issued;
+                  cp = cp.plus(1);
+                }
               }
-              const uint32_t st = ring + uint32_t(at.s) * C::STAGE, bar = full0 + 8 * at.s;
-              tc::mbar_arrive_expect_tx(bar, uint32_t(NR * halves * 8192));
-              const CUtensorMap *map = kv == 0 ? &P.tmap_k : &P.tmap_v;
+              const int wide = halves - int(c0) - int(c1);
+              if (!EIGHT || wide > 0) {
+                if (wrapped && !wait(empty0 + 8 * at.s, at.ph ^ 1u)) {
+                  ok = false;
+                  break;
+                }
+                const uint32_t st = ring + uint32_t(at.s) * C::STAGE, bar = (EIGHT ? wide0 : full0) + 8 * at.s;
+                tc::mbar_arrive_expect_tx(bar, uint32_t(NR * wide * 8192));
+                const CUtensorMap *map = kv == 0 ? &P.tmap_k : &P.tmap_v;
 #pragma unroll
-              for (int r = 0; r < NR; ++r) {
-                tc::tma_load_4d(st + r * C::KV_REGION, map, bar, r * 64, it.g, sa, ca);
-                if (halves == 2) tc::tma_load_4d(st + r * C::KV_REGION + 8192, map, bar, r * 64, it.g, sb, cb);
+                for (int r = 0; r < NR; ++r) {
+                  if (!EIGHT || !c0) tc::tma_load_4d(st + r * C::KV_REGION, map, bar, r * 64, it.g, sa, ca);
+                  if (halves == 2 && !c1) tc::tma_load_4d(st + r * C::KV_REGION + 8192, map, bar, r * 64, it.g, sb, cb);
+                }
+                if (!EIGHT) ++issued;
+                used |= 1u << at.s;
+                phases ^= 1u << at.s;
               }
-              ++issued;
               at = at.plus(1);
               wrapped |= at.s == 0;
               if (kv == 1) break;
@@ -864,7 +969,13 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         }
         if (!ok) give_up();
         // no copy may still be landing when the CTA ends
-        for (int i = ::max(0, issued - NST); i < issued; ++i) tc::mbar_wait(full0 + 8 * (i % NST), (i / NST) & 1, &s_zero);
+        if constexpr (EIGHT) {
+          for (int i = ::max(0, issued - C::NCODE); i < issued; ++i) tc::mbar_wait(code0 + 8 * (i % C::NCODE), (i / C::NCODE) & 1, &s_zero);
+          for (int s = 0; s < NST; ++s)
+            if ((used >> s) & 1u) tc::mbar_wait(wide0 + 8 * s, ((phases >> s) & 1u) ^ 1u, &s_zero);
+        } else {
+          for (int i = ::max(0, issued - NST); i < issued; ++i) tc::mbar_wait(full0 + 8 * (i % NST), (i / NST) & 1, &s_zero);
+        }
         for (int w = 0; w < C::NQ; ++w)
           if (nq[w] > 0) tc::mbar_wait(qf0 + 8 * w, (nq[w] - 1) & 1u, &s_zero);
       }
@@ -979,6 +1090,90 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         tc::mma_commit(drain0 + 8 * w);
         tc::mbar_wait(drain0 + 8 * w, 0, &s_zero);
       }
+    } else if (warp >= CODE_WARP) {
+      if constexpr (EIGHT) {
+        // ---------------- codes to bf16, on their way into the ring: each warp 16 rows of
+        // a page, 16 codes at a time. A code times its page's power is exact in bf16, so
+        // what follows does not know of codes; pages in bf16 are waited for here.
+        const int cw = warp - CODE_WARP;
+        Pos at{0, 0};
+        Place<C::NCODE> cp{0, 0};
+        bool wrapped = false, ok = true;
+        uint32_t phases = 0;
+        Item it;
+        int j0, j1;
+        while (ok && next_item(it, j0, j1, false)) {
+          for (int j = j0; j < j1 && ok; ++j) {
+            const bool c0 = it.codes(2 * j), c1 = it.codes(2 * j + 1), wide = !c0 || (2 * j + 1 < it.np && !c1);
+#pragma unroll 1
+            for (int kv = 0; kv < 2; ++kv) {
+              if (wrapped) ok = __all_sync(0xffffffffu, wait(empty0 + 8 * at.s, at.ph ^ 1u));
+              if (ok && (c0 || c1)) {
+                ok = __all_sync(0xffffffffu, wait(code0 + 8 * cp.s, cp.ph));
+                if (!ok) break;
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                  if (!(h == 0 ? c0 : c1)) continue;
+                  const uint32_t ex = *reinterpret_cast<volatile uint32_t *>(&s_exp[cp.s][h]);
+                  const int e = kv == 0 ? k_exp(ex) : v_exp(ex);
+                  // 2^(120 + e), in two factors where bf16 ends before
+                  const bool marked = e == DREAMS_KV8_NOT_FINITE;
+                  const uint32_t f = marked ? 0x7fffu : uint32_t(::min(::max(247 + e, 0), 254)) << 7, up = f | f << 16;
+                  const uint32_t f2 = uint32_t(::min(120 + e, 254)) << 7, up2 = f2 | f2 << 16;
+                  constexpr int CH = D / 16, RS = 32 / CH;  // 16-byte pieces of a row; rows side by side
+                  const int ch = lane % CH;
+                  const uint32_t from = codes + uint32_t(cp.s) * C::CODES + h * 64 * D + lane * 16;
+                  const uint32_t to = ring + uint32_t(at.s) * C::STAGE + (ch >> 2) * C::KV_REGION + h * 8192;
+                  uint32_t u[16 / RS][4];
+#pragma unroll
+                  for (int i = 0; i < 16 / RS; ++i)
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(u[i][0]), "=r"(u[i][1]), "=r"(u[i][2]), "=r"(u[i][3])
+                                 : "r"(from + (16 * cw + RS * i) * D));
+#pragma unroll
+                  for (int i = 0; i < 16 / RS; ++i) {
+                    const int rr = 16 * cw + RS * i + lane / CH;
+                    uint32_t v[8];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                      v[2 * k] = mul_bf16x2(codes_x2<sel_of(0, 1)>(u[i][k]), up);
+                      v[2 * k + 1] = mul_bf16x2(codes_x2<sel_of(2, 3)>(u[i][k]), up);
+                    }
+                    if (__builtin_expect(e > 7 && !marked, 0)) {
+#pragma unroll
+                      for (int k = 0; k < 8; ++k) v[k] = mul_bf16x2(v[k], up2);
+                    }
+                    // the second region's lanes write their second half first: no two of eight meet in a bank
+                    const int swap = (ch >> 2) & 1;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                      const bool hi = (k ^ swap) != 0;
+                      const uint32_t dst = to + rr * 128 + (uint32_t((2 * (ch & 3) + int(hi)) ^ (rr & 7)) << 4);
+                      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(hi ? v[4] : v[0]), "r"(hi ? v[5] : v[1]), "r"(hi ? v[6] : v[2]),
+                                   "r"(hi ? v[7] : v[3])
+                                   : "memory");
+                    }
+                  }
+                }
+                tc::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(taken0 + 8 * cp.s);
+                cp = cp.plus(1);
+              }
+              if (ok && wide) {
+                ok = __all_sync(0xffffffffu, wait(wide0 + 8 * at.s, (phases >> at.s) & 1u));
+                phases ^= 1u << at.s;
+              }
+              if (!ok) break;
+              __syncwarp();
+              if (lane == 0) tc::mbar_arrive(full0 + 8 * at.s);
+              at = at.plus(1);
+              wrapped |= at.s == 0;
+            }
+          }
+        }
+        if (!ok) give_up();
+      }
     } else {
       // ---------------- the scan: where rows see a tile in part, an infinity or a
       // NaN in V would reach the others (0 x inf); such items are done again row by row
@@ -1056,7 +1251,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     // ---------------- join the slots' and the splits' parts
     x_next = P.nsplit.div(int(blockIdx.x));
     Item it;
-    load_item<PAIR>(P, x_next, it, false, &lens);
+    load_item<PAIR, EIGHT>(P, x_next, it, false, &lens);
     const Splits splits(it.n, P.nsplit);
     const int m = splits.first(split + 1) - splits.first(split);
     const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
@@ -1098,7 +1293,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
     const bool first_has = m > 0;  // (a CTA without tiles has no row descriptions: it joins nothing)
     const int joiners = ::max(1, ::min(nsplit, it.n));
     if (!gave_up && first_has) {
-      constexpr int WARPS = THREADS / 32, AHEAD = 8;
+      constexpr int WARPS = C::THREADS / 32, AHEAD = 8;
       auto sums = [&](int row) {
         return row < rows_blk && lane < parts ? ld_cluster2(mapa(ml_a + ((lane & 1) * ROWS + row) * 8, lane >> 1)) : make_float2(-INFINITY, 0.f);
       };
@@ -1110,7 +1305,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
         if (off < 0) continue;  // a malformed tree
         const int h = it.g * p.G + row - (t - it.t00) * p.G;
         if (again || __any_sync(0xffffffffu, ml.y > MOST_SUM)) {
-          slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
+          slow_row<D, EIGHT>(P, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
           continue;
         }
         const uint32_t some = __ballot_sync(0xffffffffu, ml.y != 0.f);
@@ -1147,7 +1342,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_tc_kernel(const __grid_cons
           // (a sum of 0 x O is zero, or NaN)
           const float odd = 0.f * acc.x + 0.f * acc.y + 0.f * acc.z + 0.f * acc.w;
           if (__any_sync(0xffffffffu, odd != 0.f)) {  // (also where it is NaN)
-            slow_row<D>(p, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
+            slow_row<D, EIGHT>(P, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
             continue;
           }
         }
@@ -1199,16 +1394,32 @@ bool q_map(CUtensorMap *m, const WinParams &p, int D, int TB) {
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool PAIR>
-dreams_status_t launch(TcParams &P, cudaStream_t stream) {
-  const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR>);
-  const dreams_status_t st = ensure_max_dynamic_smem(kernel, int(Cfg<D, PAIR>::SMEM));
+// Codes of one layer's K or V: (D, 1 head, 64 slots, 1) boxes of (D, Hkv, 64, num_pages),
+// rows one behind the other.
+bool code_map(CUtensorMap *m, const uint8_t *base, const WinParams &p, const Kv8 &c, int D) {
+  EncodeTiledFn enc = encode_tiled();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[4] = {cuuint64_t(D), cuuint64_t(p.Hkv), 64, cuuint64_t(c.num_pages)};
+  const cuuint64_t strides[3] = {cuuint64_t(D), cuuint64_t(p.Hkv) * D, cuuint64_t(64) * p.Hkv * D};
+  const cuuint32_t box[4] = {cuuint32_t(D), 1, 64, 1}, one[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool PAIR, bool EIGHT>
+dreams_status_t launch(ParamsOf<EIGHT> &P, cudaStream_t stream) {
+  using C = Cfg<D, PAIR, EIGHT>;
+  const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR, EIGHT>);
+  const dreams_status_t st = ensure_max_dynamic_smem(kernel, int(C::SMEM));
   if (st != DREAMS_OK) return st;
   if (!kv_map(&P.tmap_k, P.p.k, P.p, D) || !kv_map(&P.tmap_v, P.p.v, P.p, D) || !q_map(&P.tmap_q, P.p, D, P.TB)) return DREAMS_ERR_UNSUPPORTED;
+  if constexpr (EIGHT) {
+    if (!code_map(&P.tmap_k8, P.c.k, P.p, P.c, D) || !code_map(&P.tmap_v8, P.c.v, P.p, P.c, D)) return DREAMS_ERR_UNSUPPORTED;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(PAIR ? unsigned(std::min(P.items, num_sms())) : unsigned(P.items) * unsigned(P.p.nsplit));
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = Cfg<D, PAIR>::SMEM;
+  cfg.blockDim = dim3(C::THREADS);
+  cfg.dynamicSmemBytes = C::SMEM;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2] = {early_launch()};
   attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -1227,19 +1438,20 @@ dreams_status_t launch(TcParams &P, cudaStream_t stream) {
 
 // How many clusters of ns CTAs the current device runs at once (asked once per
 // device); 0: none, or not known.
-template <int D>
+template <int D, bool EIGHT>
 int clusters_at_once(int ns) {
+  using C = Cfg<D, false, EIGHT>;
   static std::atomic<int> known[64][9];  // count + 1
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 0;
   int n = known[dev][ns].load(std::memory_order_relaxed);
   if (n == 0) {
-    const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, false>);
-    if (ensure_max_dynamic_smem(kernel, int(Cfg<D, false>::SMEM)) != DREAMS_OK) return 0;
+    const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, false, EIGHT>);
+    if (ensure_max_dynamic_smem(kernel, int(C::SMEM)) != DREAMS_OK) return 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ns));
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Cfg<D, false>::SMEM;
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = unsigned(ns);
@@ -1255,12 +1467,9 @@ int clusters_at_once(int ns) {
   return n - 1;
 }
 
-}  // namespace
-
-dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaStream_t stream) {
-  TcParams P;
-  memset(&P, 0, sizeof(P));
-  P.p = p;
+template <bool EIGHT>
+dreams_status_t launch_blocks(ParamsOf<EIGHT> &P, int D, cudaStream_t stream) {
+  const WinParams &p = P.p;
   P.TB = std::max(1, ROWS / p.G);
   const int64_t heads = int64_t(p.B) * p.Hkv;
   const int64_t blocks = (int64_t(p.T_max) + P.TB - 1) / P.TB, pairs = (blocks + 1) / 2;
@@ -1280,13 +1489,13 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   const int64_t sms = num_sms();
   const int64_t keys = std::min<int64_t>(p.capacity, int64_t(p.window) + std::min<int64_t>(p.T_max, P.TB));
   const int64_t cols = keys + 63 + (std::min<int64_t>(p.capacity, p.sinks) + 63) / 64 * 64 + 32;
-  const int64_t per_one = kv->D == 128 ? 15 : 13, per_pair = kv->D == 128 ? 20 : 16;
+  const int64_t per_one = D == 128 ? 15 : 13, per_pair = D == 128 ? 20 : 16;
   auto rounds = [](int64_t n, int64_t fit) { return (n + fit - 1) / fit; };
   const int64_t pair_cost = blocks > 1 ? rounds(heads * pairs, sms) * (per_pair * cols / KT + 30) + 40 : INT64_MAX;
   int64_t best = INT64_MAX;
   int nsplit = 1;
   for (int ns = 1; ns <= 8 && (ns == 1 || (ns * KT <= cols && heads * blocks * ns <= sms)); ++ns) {
-    const int64_t fit = ns == 1 ? sms : kv->D == 128 ? clusters_at_once<128>(ns) : clusters_at_once<64>(ns);
+    const int64_t fit = ns == 1 ? sms : D == 128 ? clusters_at_once<128, EIGHT>(ns) : clusters_at_once<64, EIGHT>(ns);
     if (fit < 1) continue;
     const int64_t cost = rounds(heads * blocks, fit) * (135 + per_one * (cols + (ns - 1) * KT / 2) / (ns * KT));
     if (cost < best) {
@@ -1304,8 +1513,25 @@ dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaS
   P.hkv = Divisor::of(p.Hkv);
   P.nsplit = Divisor::of(P.p.nsplit);
   P.g = Divisor::of(p.G);
-  if (kv->D == 128) return pair ? launch<128, true>(P, stream) : launch<128, false>(P, stream);
-  return pair ? launch<64, true>(P, stream) : launch<64, false>(P, stream);
+  if (D == 128) return pair ? launch<128, true, EIGHT>(P, stream) : launch<128, false, EIGHT>(P, stream);
+  return pair ? launch<64, true, EIGHT>(P, stream) : launch<64, false, EIGHT>(P, stream);
+}
+
+}  // namespace
+
+dreams_status_t launch_tc(const WinParams &p, const dreams_kv_cache_t *kv, cudaStream_t stream) {
+  TcParams P;
+  memset(&P, 0, sizeof(P));
+  P.p = p;
+  return launch_blocks<false>(P, kv->D, stream);
+}
+
+dreams_status_t launch_tc8(const WinParams &p, const Kv8 &c, int D, cudaStream_t stream) {
+  Tc8Params P;
+  memset(&P, 0, sizeof(P));
+  P.p = p;
+  P.c = c;
+  return launch_blocks<true>(P, D, stream);
 }
 
 }  // namespace win
