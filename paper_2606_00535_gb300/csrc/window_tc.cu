@@ -92,6 +92,9 @@ struct Cfg {
   // EIGHT: stages of codes, two pages of K or V each
   static constexpr int NCODE = !EIGHT ? 0 : D == 64 ? 4 : 2;
   static constexpr uint32_t CODES = KT * D;
+  // (the producer, which waits for no stage of the ring where it copies nothing into one, is
+  // never a whole phase of the ring ahead of what its barriers can tell)
+  static_assert(NCODE < NST, "stages of codes");
   static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + size_t(NCODE) * CODES + 1024, 120 * 1024);
 };
 
@@ -336,6 +339,62 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   uint32_t r;
   asm("shl.b32 %0, %1, %2;" : "=r"(r) : "r"(0xffffffffu), "r"(::max(n, 0)));  // (a shift by 32 or more leaves nothing)
   return ~r;
+}
+
+// A lane's codes of a page (16 of each of 16 / RS rows) times 2^e, as bf16 into the ring:
+// `from` its first 8 codes, the other 8 `flip` bytes on; `to` their place.
+__device__ __forceinline__ uint32_t factor_of(int e) {  // 2^(120 + e), e <= 7, or NaN; twice
+  const uint32_t f = e == DREAMS_KV8_NOT_FINITE ? 0x7fffu : uint32_t(247 + ::max(e, -247)) << 7;
+  return f | f << 16;
+}
+template <int D>
+__device__ __forceinline__ void widen(uint32_t from, uint32_t to, int e0, int e1, uint32_t flip) {  // two pages
+  constexpr int RS = 32 / (D / 16), N = 16 / RS;  // rows side by side; rows of a lane
+  uint32_t u[2][N][4];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[h][i][0]), "=r"(u[h][i][1]) : "r"(from + 64 * D * h + RS * D * i));
+      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[h][i][2]), "=r"(u[h][i][3]) : "r"(from + 64 * D * h + RS * D * i + flip));
+    }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t up = factor_of(h == 0 ? e0 : e1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t v[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = mul_bf16x2(codes_x2<sel_of(0, 1)>(u[h][i][k]), up);
+        v[2 * k + 1] = mul_bf16x2(codes_x2<sel_of(2, 3)>(u[h][i][k]), up);
+      }
+      // (rows 4 on have the third bit of their swizzle turned)
+      const uint32_t dst = (to ^ (RS == 4 && (i & 1) ? 64u : 0u)) + 8192 * h + RS * 128 * i;
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst ^ 16u), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    }
+  }
+}
+// The same for one page, of any power: beyond 2^7 the factor is beyond bf16, and comes in two.
+template <int D>
+__device__ __noinline__ void widen_rare(uint32_t from, uint32_t to, int e, uint32_t flip) {
+  constexpr int RS = 32 / (D / 16), N = 16 / RS;
+  const bool large = e > 7 && e != DREAMS_KV8_NOT_FINITE;
+  const uint32_t up = large ? 0x7f007f00u : factor_of(e), f2 = large ? uint32_t(::min(120 + e, 254)) << 7 : 0x3f80u, up2 = f2 | f2 << 16;
+#pragma unroll 1
+  for (int i = 0; i < N; ++i) {
+    const uint32_t dst = (to ^ (RS == 4 && (i & 1) ? 64u : 0u)) + RS * 128 * i;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint32_t a, b;
+      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(a), "=r"(b) : "r"(from + RS * D * i + (k == 0 ? 0u : flip)));
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst ^ (16u * k)), "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(0, 1)>(a), up), up2)),
+                   "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(2, 3)>(a), up), up2)), "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(0, 1)>(b), up), up2)),
+                   "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(2, 3)>(b), up), up2))
+                   : "memory");
+    }
+  }
 }
 
 // A query row: its position (less L) and, in a tree, the new slots it sees.
@@ -1093,9 +1152,14 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     } else if (warp >= CODE_WARP) {
       if constexpr (EIGHT) {
         // ---------------- codes to bf16, on their way into the ring: each warp 16 rows of
-        // a page, 16 codes at a time. A code times its page's power is exact in bf16, so
-        // what follows does not know of codes; pages in bf16 are waited for here.
-        const int cw = warp - CODE_WARP;
+        // a page. A code times its page's power is exact in bf16, so what follows does not
+        // know of codes; pages in bf16 are waited for here.
+        // A lane's 16 codes of a row are two runs of 8, each 16 bytes of the ring; which of
+        // them is first differs between lanes, so that no two of eight meet in a bank.
+        constexpr int CH = D / 16;
+        const int ch = lane % CH, row = 16 * (warp - CODE_WARP) + lane / CH, part = D == 128 ? ((ch >> 2) ^ (row & 1)) : 0;
+        const uint32_t mine = codes + uint32_t(row * D + ch * 16 + part * 8), flip = part != 0 ? uint32_t(-8) : 8u;
+        const uint32_t put = ring + (ch >> 2) * C::KV_REGION + row * 128 + (uint32_t((2 * (ch & 3) + part) ^ (row & 7)) << 4);
         Pos at{0, 0};
         Place<C::NCODE> cp{0, 0};
         bool wrapped = false, ok = true;
@@ -1107,66 +1171,40 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
             const bool c0 = it.codes(2 * j), c1 = it.codes(2 * j + 1), wide = !c0 || (2 * j + 1 < it.np && !c1);
 #pragma unroll 1
             for (int kv = 0; kv < 2; ++kv) {
-              if (wrapped) ok = __all_sync(0xffffffffu, wait(empty0 + 8 * at.s, at.ph ^ 1u));
-              if (ok && (c0 || c1)) {
-                ok = __all_sync(0xffffffffu, wait(code0 + 8 * cp.s, cp.ph));
-                if (!ok) break;
-#pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                  if (!(h == 0 ? c0 : c1)) continue;
-                  const uint32_t ex = *reinterpret_cast<volatile uint32_t *>(&s_exp[cp.s][h]);
-                  const int e = kv == 0 ? k_exp(ex) : v_exp(ex);
-                  // 2^(120 + e), in two factors where bf16 ends before
-                  const bool marked = e == DREAMS_KV8_NOT_FINITE;
-                  const uint32_t f = marked ? 0x7fffu : uint32_t(::min(::max(247 + e, 0), 254)) << 7, up = f | f << 16;
-                  const uint32_t f2 = uint32_t(::min(120 + e, 254)) << 7, up2 = f2 | f2 << 16;
-                  constexpr int CH = D / 16, RS = 32 / CH;  // 16-byte pieces of a row; rows side by side
-                  const int ch = lane % CH;
-                  const uint32_t from = codes + uint32_t(cp.s) * C::CODES + h * 64 * D + lane * 16;
-                  const uint32_t to = ring + uint32_t(at.s) * C::STAGE + (ch >> 2) * C::KV_REGION + h * 8192;
-                  uint32_t u[16 / RS][4];
-#pragma unroll
-                  for (int i = 0; i < 16 / RS; ++i)
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
-                                 : "=r"(u[i][0]), "=r"(u[i][1]), "=r"(u[i][2]), "=r"(u[i][3])
-                                 : "r"(from + (16 * cw + RS * i) * D));
-#pragma unroll
-                  for (int i = 0; i < 16 / RS; ++i) {
-                    const int rr = 16 * cw + RS * i + lane / CH;
-                    uint32_t v[8];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                      v[2 * k] = mul_bf16x2(codes_x2<sel_of(0, 1)>(u[i][k]), up);
-                      v[2 * k + 1] = mul_bf16x2(codes_x2<sel_of(2, 3)>(u[i][k]), up);
-                    }
-                    if (__builtin_expect(e > 7 && !marked, 0)) {
-#pragma unroll
-                      for (int k = 0; k < 8; ++k) v[k] = mul_bf16x2(v[k], up2);
-                    }
-                    // the second region's lanes write their second half first: no two of eight meet in a bank
-                    const int swap = (ch >> 2) & 1;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                      const bool hi = (k ^ swap) != 0;
-                      const uint32_t dst = to + rr * 128 + (uint32_t((2 * (ch & 3) + int(hi)) ^ (rr & 7)) << 4);
-                      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(hi ? v[4] : v[0]), "r"(hi ? v[5] : v[1]), "r"(hi ? v[6] : v[2]),
-                                   "r"(hi ? v[7] : v[3])
-                                   : "memory");
-                    }
-                  }
+              const uint32_t code = code0 + 8 * cp.s, empty = empty0 + 8 * at.s;
+              if (c0) {  // (the first half is in 8 bits where the second is)
+                // both at once, as either takes a while to answer
+                const bool a = quick(code, cp.ph), b = !wrapped || quick(empty, at.ph ^ 1u);
+                ok = (a || wait(code, cp.ph)) && (b || wait(empty, at.ph ^ 1u));
+              } else if (wrapped) {
+                ok = wait(empty, at.ph ^ 1u);
+              }
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              if (c0) {
+                const uint32_t from = mine + uint32_t(cp.s) * C::CODES, to = put + uint32_t(at.s) * C::STAGE;
+                const uint32_t x0 = *reinterpret_cast<volatile uint32_t *>(&s_exp[cp.s][0]), x1 = *reinterpret_cast<volatile uint32_t *>(&s_exp[cp.s][1]);
+                const int e0 = kv == 0 ? k_exp(x0) : v_exp(x0), e1 = kv == 0 ? k_exp(x1) : v_exp(x1);
+                const bool large = (e0 > 7 && e0 != DREAMS_KV8_NOT_FINITE) || (e1 > 7 && e1 != DREAMS_KV8_NOT_FINITE);
+                if (__builtin_expect(large || !c1, 0)) {
+                  widen_rare<D>(from, to, e0, flip);
+                  if (c1) widen_rare<D>(from + 64 * D, to + 8192, e1, flip);
+                } else {
+                  widen<D>(from, to, e0, e1, flip);
                 }
                 tc::fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(taken0 + 8 * cp.s);
-                cp = cp.plus(1);
               }
-              if (ok && wide) {
+              if (wide) {
                 ok = __all_sync(0xffffffffu, wait(wide0 + 8 * at.s, (phases >> at.s) & 1u));
                 phases ^= 1u << at.s;
+                if (!ok) break;
               }
-              if (!ok) break;
               __syncwarp();
-              if (lane == 0) tc::mbar_arrive(full0 + 8 * at.s);
+              if (lane == 0) {
+                tc::mbar_arrive(full0 + 8 * at.s);
+                if (c0) tc::mbar_arrive(taken0 + 8 * cp.s);
+              }
+              if (c0) cp = cp.plus(1);
               at = at.plus(1);
               wrapped |= at.s == 0;
             }
