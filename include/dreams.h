@@ -572,7 +572,7 @@ typedef struct dreams_rotary {
  * or, with transpose != 0, by the transposed map (-a in place of a): the gradient
  * with respect to x of an output's, and with factor 1 the inverse. Products and
  * sums are f32, the result is rounded to x's type once. Element (b, t, h, d) of x
- * is at b * x_stride[0] + t * x_stride[1] + h * x_stride[2] + d, of out alike; both
+ * is at b * x_stride_b + t * x_stride_t + h * x_stride_h + d, of out alike; both
  * have the same type (f32 or bf16). out may be x itself (the same pointer and
  * strides), else they do not overlap. Strides and pointers may have any alignment
  * of whole elements; rows of 16-byte multiples, 16-byte aligned, take 16-byte
@@ -581,8 +581,8 @@ typedef struct dreams_rotary {
  * NULL (n_axes 1): token t of sequence b is at start[b] + t, start device [B], NULL
  * = 0. 1 <= n_axes <= 4. One launch.
  */
-dreams_status_t dreams_rope(const void *x, const int64_t *x_stride, void *out, const int64_t *out_stride,
-                            dreams_dtype_t dtype, int32_t B, int32_t T, int32_t H, int32_t D,
+dreams_status_t dreams_rope(const void *x, int64_t x_stride_b, int64_t x_stride_t, int64_t x_stride_h, void *out,
+                            int64_t out_stride_b, int64_t out_stride_t, int64_t out_stride_h, dreams_dtype_t dtype, int32_t B, int32_t T, int32_t H, int32_t D,
                             const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes,
                             const int32_t *start, int32_t transpose, int32_t *status_word, dreams_stream_t stream);
 
@@ -591,9 +591,9 @@ dreams_status_t dreams_rope(const void *x, const int64_t *x_stride, void *out, c
  *     slot kv_len[b] + t  <-  turned k_new[b, t], v_new[b, t]
  * and q_out[b, t] <- turned q[b, t], for t < n_new[b], in one launch. q NULL: K and
  * V alone (q_out NULL, Hq 0). q, k_new and v_new: bf16, element (b, t, h, d) at b *
- * stride[0] + t * stride[1] + h * D + d, so views of one fused projection; each has
- * its own strides (multiples of 8 elements, at least a row; stride[0] is ignored
- * when B == 1, stride[1] when T_max == 1). q_out: dense bf16 [B, T_max, Hq, D], or
+ * stride_b + t * stride_t + h * D + d, so views of one fused projection; each has
+ * its own strides (multiples of 8 elements, at least a row; stride_b is ignored
+ * when B == 1, stride_t when T_max == 1). q_out: dense bf16 [B, T_max, Hq, D], or
  * q itself where q is dense. All are 16-byte aligned and overlap neither the cache
  * nor, but for that, each other. Positions: positions ([n_axes, B, T_max]); or
  * parent ([B, T_max], T_max <= 64): the rows are the nodes of a draft tree, node t
@@ -603,10 +603,10 @@ dreams_status_t dreams_rope(const void *x, const int64_t *x_stride, void *out, c
  * entries) skip the sequence; a slot whose page is missing is skipped (BAD_PAGE),
  * its q row is not. One launch.
  */
-dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer, const void *q,
-                                      const int64_t *q_stride, void *q_out, int32_t Hq, const void *k_new,
-                                      const int64_t *k_stride, const void *v_new, const int64_t *v_stride,
-                                      const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes,
+dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer, const void *q, int64_t q_stride_b,
+                                      int64_t q_stride_t, void *q_out, int32_t Hq, const void *k_new,
+                                      int64_t k_stride_b, int64_t k_stride_t, const void *v_new, int64_t v_stride_b,
+                                      int64_t v_stride_t, const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes,
                                       const int32_t *parent, const int32_t *kv_len, const int32_t *n_new, int32_t B,
                                       int32_t T_max, int32_t *status_word, dreams_stream_t stream);
 

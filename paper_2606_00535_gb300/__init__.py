@@ -95,7 +95,7 @@ def _lib() -> ctypes.CDLL:
                 p, i32, i64, sz, f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
                                         ctypes.c_float)
                 pkv, ptr, ppl = ctypes.POINTER(_KVCache), ctypes.POINTER(_Tree), ctypes.POINTER(_PagePool)
-                pi64, prt, pk8 = ctypes.POINTER(i64), ctypes.POINTER(_Rotary), ctypes.POINTER(_KV8Cache)
+                prt, pk8 = ctypes.POINTER(_Rotary), ctypes.POINTER(_KV8Cache)
                 sig = {
                     "dreams_tree_verify_attn_workspace_size": (sz, [pkv, ptr, i32]),
                     "dreams_tree_verify_attn_launches": (i32, [pkv, ptr, i32]),
@@ -133,10 +133,10 @@ def _lib() -> ctypes.CDLL:
                     "dreams_kv_fork": (ctypes.c_int, [pkv, ppl, p, p, p, p, sz, p, p]),
                     "dreams_kv_append": (ctypes.c_int, [pkv, i32, p, p, i64, i64, p, p, i32, i32, p, p]),
                     "dreams_kv_prune": (ctypes.c_int, [pkv, i32, p, i32, i32, i32, p, p, p, p, p]),
-                    "dreams_rope": (ctypes.c_int, [p, pi64, p, pi64, ctypes.c_int, i32, i32, i32, i32, prt, p, i32, p, i32, p,
-                                                   p]),
-                    "dreams_kv_append_rope": (ctypes.c_int, [pkv, i32, p, pi64, p, i32, p, pi64, p, pi64, prt, p, i32, p,
-                                                             p, p, i32, i32, p, p]),
+                    "dreams_rope": (ctypes.c_int, [p, i64, i64, i64, p, i64, i64, i64, ctypes.c_int, i32, i32, i32, i32, prt, p,
+                                                   i32, p, i32, p, p]),
+                    "dreams_kv_append_rope": (ctypes.c_int, [pkv, i32, p, i64, i64, p, i32, p, i64, i64, p, i64, i64, prt,
+                                                             p, i32, p, p, p, i32, i32, p, p]),
                     "dreams_kv_quantize": (ctypes.c_int, [pkv, pk8, i32, p, p, p, p, p]),
                     "dreams_kv8_attention": (ctypes.c_int, [p, i64, i64, pk8, pkv, i32, p, p, p, p, i32, i32, i32, f32,
                                                             i32, i32, p, p, p, p]),
@@ -833,6 +833,8 @@ class PagePool:
 
 def _per_seq(t: torch.Tensor, name: str, B: int, dev) -> int:
     """Address of an int32 array with an entry for each of B sequences."""
+    if type(t) is torch.Tensor and t.dtype is torch.int32 and t.device == dev and t.numel() >= B and t.is_contiguous():
+        return t.data_ptr()
     _need(t, name, torch.int32, dev)
     if t.numel() < B:
         raise ValueError(f"{name} holds {t.numel()} entries, the call addresses {B} sequences")
@@ -967,6 +969,7 @@ def kv_prune(kv: KVCache, keep: torch.Tensor, v0: int, n_vis: int, kv_len: torch
 
 
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+_ROPE_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 @dataclass
@@ -997,6 +1000,7 @@ class Rotary:
                 raise ValueError("axis must be [n_pairs]")
         self._c = _Rotary(self.phase.data_ptr(), None if self.axis is None else self.axis.data_ptr(), self.n_pairs,
                           self.layout, self.factor)
+        self._ref = ctypes.byref(self._c)
 
     @classmethod
     def make(cls, rot_dim: int, base: float = 10000.0, layout: str = "half", scaling: str = "none",
@@ -1049,9 +1053,6 @@ class Rotary:
                    None if axis is None else torch.tensor(list(axis), dtype=torch.int32, device=device))
 
 
-_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
-
-
 def _positions(positions: Optional[torch.Tensor], B: int, T: int, dev) -> Tuple[Optional[int], int]:
     """Address and axes of positions [B, T] or [n_axes, B, T]."""
     if positions is None:
@@ -1070,27 +1071,30 @@ def rope(x: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = No
     ``start`` (int32 [B]) + t, or t. ``transpose``: by the transposed map, which is
     the gradient with respect to x of an output's (and with factor 1 the inverse).
     Returns ``out``, which may be ``x``."""
-    if not isinstance(x, torch.Tensor) or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() != 4:
+    if not isinstance(x, torch.Tensor) or x.dtype not in _ROPE_TYPES or x.dim() != 4:
         raise TypeError("x must be a 4-D bfloat16 or float32 tensor [B, T, H, D]")
-    dev = x.device
+    dev, dtype = x.device, x.dtype
     B, T, H, D = x.shape
-    if x.stride(3) != 1 and D > 1:
+    sb, stt, sh, sd = x.stride()
+    if sd != 1 and D > 1:
         raise ValueError("x's rows must be dense (last stride 1)")
     if rotary.phase.device != dev:
         raise ValueError(f"the rotary table is on {rotary.phase.device}, x on {dev}")
-    pos, axes = _positions(positions, B, T, dev)
+    pos, axes = (None, 1) if positions is None else _positions(positions, B, T, dev)
     if positions is not None and start is not None:
         raise ValueError("give positions or start, not both")
-    st = None if start is None else _per_seq(start, "start", B, dev)
     if out is None:
-        out = _new((B, T, H, D), x.dtype, dev, stream)
-    elif not isinstance(out, torch.Tensor) or out.dtype != x.dtype or out.device != dev or out.shape != x.shape:
-        raise ValueError("out must have x's type, shape and device")
-    elif out.stride(3) != 1 and D > 1:
-        raise ValueError("out's rows must be dense (last stride 1)")
-    _launch("dreams_rope", dev, stream, x.data_ptr(), _I64x3(*x.stride()[:3]), out.data_ptr(),
-            _I64x3(*out.stride()[:3]), F32 if x.dtype == torch.float32 else BF16, B, T, H, D,
-            ctypes.byref(rotary._c), pos, axes, st, int(bool(transpose)), _status(status, dev))
+        out = _new((B, T, H, D), dtype, dev, stream)
+        ob, ot, oh = T * H * D, H * D, D
+    else:
+        if not isinstance(out, torch.Tensor) or out.dtype != dtype or out.device != dev or out.shape != x.shape:
+            raise ValueError("out must have x's type, shape and device")
+        ob, ot, oh, od = out.stride()
+        if od != 1 and D > 1:
+            raise ValueError("out's rows must be dense (last stride 1)")
+    _launch("dreams_rope", dev, stream, x.data_ptr(), sb, stt, sh, out.data_ptr(), ob, ot, oh, _ROPE_TYPES[dtype], B, T, H,
+            D, rotary._ref, pos, axes, None if start is None else _per_seq(start, "start", B, dev), 1 if transpose else 0,
+            None if status is None else _status(status, dev))
     return out
 
 
@@ -1118,7 +1122,7 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
     if rotary.phase.device != dev:
         raise ValueError(f"the rotary table is on {rotary.phase.device}, the cache on {dev}")
     kl, nn = _per_seq(kv_len, "kv_len", B, dev), _per_seq(n_new, "n_new", B, dev)
-    pos, axes = _positions(positions, B, T_max, dev)
+    pos, axes = (None, 1) if positions is None else _positions(positions, B, T_max, dev)
     par = None
     if parent is not None:
         if positions is not None:
@@ -1127,12 +1131,12 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
         if tuple(parent.shape) != (B, T_max):
             raise ValueError("parent must be [B, T_max]")
         par = parent.data_ptr()
-    Hq, qs = 0, None
+    Hq = qb = qt = 0
     if q is not None:
         qb, qt = _q_strides(q)
-        if q.device != dev or tuple(q.shape[:2]) != (B, T_max) or q.shape[3] != D:
+        if q.device != dev or q.shape[:2] != k_new.shape[:2] or q.shape[3] != D:
             raise ValueError("q must be [B, T_max, Hq, D] on the cache's device, with k_new's B, T_max and D")
-        Hq, qs = int(q.shape[2]), _I64x2(qb, qt)
+        Hq = q.shape[2]
         if q_out is None:
             q_out = _new((B, T_max, Hq, D), torch.bfloat16, dev, stream)
         else:
@@ -1141,9 +1145,9 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
                 raise ValueError("q_out must have q's shape")
     elif q_out is not None:
         raise ValueError("q_out goes with q")
-    _launch("dreams_kv_append_rope", dev, stream, ctypes.byref(kv._c), layer, None if q is None else q.data_ptr(), qs,
-            None if q_out is None else q_out.data_ptr(), Hq, k_new.data_ptr(), _I64x2(kb, kt), v_new.data_ptr(),
-            _I64x2(vb, vt), ctypes.byref(rotary._c), pos, axes, par, kl, nn, B, T_max, _status(status, dev))
+    _launch("dreams_kv_append_rope", dev, stream, ctypes.byref(kv._c), layer, None if q is None else q.data_ptr(), qb, qt,
+            None if q_out is None else q_out.data_ptr(), Hq, k_new.data_ptr(), kb, kt, v_new.data_ptr(), vb, vt,
+            rotary._ref, pos, axes, par, kl, nn, B, T_max, None if status is None else _status(status, dev))
     return q_out
 
 

@@ -320,16 +320,17 @@ dreams_status_t launch_rope(RopeParams &p, bool inter, bool append, dreams_strea
 
 using namespace dreams;
 
-extern "C" dreams_status_t dreams_rope(const void *x, const int64_t *x_stride, void *out, const int64_t *out_stride, dreams_dtype_t dtype,
-                                       int32_t B, int32_t T, int32_t H, int32_t D, const dreams_rotary_t *rotary, const int32_t *positions,
+extern "C" dreams_status_t dreams_rope(const void *x, int64_t x_stride_b, int64_t x_stride_t, int64_t x_stride_h, void *out, int64_t out_stride_b,
+                                       int64_t out_stride_t, int64_t out_stride_h, dreams_dtype_t dtype, int32_t B, int32_t T, int32_t H, int32_t D, const dreams_rotary_t *rotary, const int32_t *positions,
                                        int32_t n_axes, const int32_t *start, int32_t transpose, int32_t *status_word, dreams_stream_t stream) {
-  if (x == nullptr || out == nullptr || x_stride == nullptr || out_stride == nullptr || (dtype != DREAMS_F32 && dtype != DREAMS_BF16) || B < 1 ||
+  if (x == nullptr || out == nullptr || (dtype != DREAMS_F32 && dtype != DREAMS_BF16) || B < 1 ||
       B > 65535 || T < 1 || T > (1 << 30) || H < 1 || H > (1 << 20) || D < 2 || D % 2 != 0 || D > 512 || !rotary_ok(rotary, D) || n_axes < 1 ||
       n_axes > 4 || !aligned4(positions) || !aligned4(start) || (positions != nullptr && start != nullptr) || (positions == nullptr && n_axes != 1))
     return DREAMS_ERR_INVALID_ARG;
   const int es = dtype == DREAMS_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(x) % es != 0 || reinterpret_cast<uintptr_t>(out) % es != 0) return DREAMS_ERR_INVALID_ARG;
   const int32_t size[3] = {B, T, H};
+  const int64_t x_stride[3] = {x_stride_b, x_stride_t, x_stride_h}, out_stride[3] = {out_stride_b, out_stride_t, out_stride_h};
   int64_t xs[3], ys[3];
   uint64_t odd = (reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) & 15u;
   for (int i = 0; i < 3; ++i) {  // (the stride of a dimension of one says nothing)
@@ -365,23 +366,23 @@ extern "C" dreams_status_t dreams_rope(const void *x, const int64_t *x_stride, v
   return wide ? launch_rope<__nv_bfloat16, 8>(p, inter, false, stream) : launch_rope<__nv_bfloat16, 1>(p, inter, false, stream);
 }
 
-extern "C" dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer, const void *q, const int64_t *q_stride, void *q_out,
-                                                 int32_t Hq, const void *k_new, const int64_t *k_stride, const void *v_new, const int64_t *v_stride,
-                                                 const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes, const int32_t *parent,
+extern "C" dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer, const void *q, int64_t q_stride_b, int64_t q_stride_t,
+                                                 void *q_out, int32_t Hq, const void *k_new, int64_t k_stride_b, int64_t k_stride_t,
+                                                 const void *v_new, int64_t v_stride_b, int64_t v_stride_t, const dreams_rotary_t *rotary, const int32_t *positions, int32_t n_axes, const int32_t *parent,
                                                  const int32_t *kv_len, const int32_t *n_new, int32_t B, int32_t T_max, int32_t *status_word,
                                                  dreams_stream_t stream) {
   Cache c;
-  if (!cache_ok(kv, c) || layer < 0 || layer >= kv->n_layers || k_new == nullptr || v_new == nullptr || k_stride == nullptr || v_stride == nullptr ||
+  if (!cache_ok(kv, c) || layer < 0 || layer >= kv->n_layers || k_new == nullptr || v_new == nullptr ||
       kv_len == nullptr || n_new == nullptr || B < 1 || B > 65535 || T_max < 1 || T_max > (parent != nullptr ? 64 : 1 << 20) || !aligned16(k_new) ||
       !aligned16(v_new) || !aligned4(kv_len) || !aligned4(n_new) || !aligned4(parent) || !aligned4(positions) || n_axes < 1 || n_axes > 4 ||
       (positions != nullptr && parent != nullptr) || (positions == nullptr && n_axes != 1) || kv->D > 512 || !rotary_ok(rotary, kv->D))
     return DREAMS_ERR_INVALID_ARG;
   if (q == nullptr ? (q_out != nullptr || Hq != 0)
-                   : (q_out == nullptr || q_stride == nullptr || Hq < 1 || Hq > (1 << 20) || !aligned16(q) || !aligned16(q_out)))
+                   : (q_out == nullptr || Hq < 1 || Hq > (1 << 20) || !aligned16(q) || !aligned16(q_out)))
     return DREAMS_ERR_INVALID_ARG;
   const int64_t D = kv->D;
   int64_t s[3][2] = {};
-  const int64_t *given[3] = {q_stride, k_stride, v_stride};
+  const int64_t given[3][2] = {{q_stride_b, q_stride_t}, {k_stride_b, k_stride_t}, {v_stride_b, v_stride_t}};
   for (int i = q == nullptr ? 1 : 0; i < 3; ++i) {
     const int64_t row = (i == 0 ? Hq : kv->Hkv) * D;
     s[i][1] = T_max == 1 ? row : given[i][1];

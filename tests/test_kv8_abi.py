@@ -11,7 +11,6 @@ from paper_2606_00535_gb300 import build as libbuild
 P = 0x1000  # placeholder, never dereferenced: every call below fails validation
 INV, UNS = dreams.ERR_INVALID_ARG, dreams.ERR_UNSUPPORTED
 needs_no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="host-validation cases use placeholder pointers")
-S3, S2 = (lambda *s: (ctypes.c_int64 * 3)(*s)), (lambda *s: (ctypes.c_int64 * 2)(*s))
 
 
 @pytest.fixture(scope="module")
@@ -47,10 +46,10 @@ BAD_ROTARY = [dict(phase=None), dict(phase=P + 4), dict(axis=P + 2), dict(n_pair
 def test_rope_refusals(lib):
     def call(x=P, xs=(4096, 512, 128), out=2 * P, ys=(4096, 512, 128), dtype=1, B=2, T=8, H=4, D=128, r=None, pos=None, axes=1, start=None):
         r = rotary() if r is None else r
-        return lib.dreams_rope(x, None if xs is None else S3(*xs), out, None if ys is None else S3(*ys), dtype, B, T, H, D, ctypes.byref(r), pos,
+        return lib.dreams_rope(x, *xs, out, *ys, dtype, B, T, H, D, ctypes.byref(r), pos,
                                axes, start, 0, None, None)
 
-    for kw in [dict(x=None), dict(out=None), dict(xs=None), dict(ys=None), dict(dtype=2), dict(B=0), dict(B=65536), dict(T=0), dict(H=0), dict(D=0),
+    for kw in [dict(x=None), dict(out=None), dict(dtype=2), dict(B=0), dict(B=65536), dict(T=0), dict(H=0), dict(D=0),
                dict(D=127), dict(D=514), dict(x=P + 1), dict(out=P + 1), dict(x=P + 2, dtype=0), dict(axes=0), dict(axes=5, pos=P), dict(axes=2),
                dict(pos=P, start=P), dict(pos=P + 2), dict(start=P + 1), dict(xs=(-1, 512, 128)), dict(xs=(1 << 38, 512, 128)), dict(ys=(4096, 512, 64)),
                dict(ys=(4096, 0, 128)), dict(ys=(2048, 512, 128)), dict(ys=(4096, 511, 128)), dict(out=P, xs=(8192, 512, 128)),
@@ -63,12 +62,11 @@ def test_append_rope_refusals(lib):
     def call(kv=None, layer=0, q=P, qs=(8 * 512, 512), qo=2 * P, Hq=4, k=P, ks=(8 * 256, 256), v=P, vs=(8 * 256, 256), r=None, pos=None, axes=1, par=None,
              kl=P, n=P, B=2, T=8):
         kv, r = cache() if kv is None else kv, rotary() if r is None else r
-        two = lambda s: None if s is None else S2(*s)  # noqa: E731
-        return lib.dreams_kv_append_rope(ctypes.byref(kv), layer, q, two(qs), qo, Hq, k, two(ks), v, two(vs), ctypes.byref(r), pos, axes, par, kl, n, B,
+        return lib.dreams_kv_append_rope(ctypes.byref(kv), layer, q, *qs, qo, Hq, k, *ks, v, *vs, ctypes.byref(r), pos, axes, par, kl, n, B,
                                          T, None, None)
 
-    for kw in [dict(layer=2), dict(layer=-1), dict(q=None), dict(qo=None), dict(qs=None), dict(Hq=0), dict(q=None, qo=None), dict(q=P + 8), dict(qo=P + 8),
-               dict(k=None), dict(v=None), dict(ks=None), dict(vs=None), dict(k=P + 8), dict(v=P + 8), dict(qs=(4096, 504)), dict(qs=(4096, 516)),
+    for kw in [dict(layer=2), dict(layer=-1), dict(q=None), dict(qo=None), dict(Hq=0), dict(q=None, qo=None), dict(q=P + 8), dict(qo=P + 8),
+               dict(k=None), dict(v=None), dict(k=P + 8), dict(v=P + 8), dict(qs=(4096, 504)), dict(qs=(4096, 516)),
                dict(ks=(8 * 256, 248)), dict(vs=(248, 256)), dict(vs=(1 << 38, 256)), dict(q=P, qo=P, qs=(8192, 1024)), dict(pos=P, par=P),
                dict(axes=2), dict(axes=0), dict(axes=5, pos=P), dict(par=P, T=65, qs=(65 * 512, 512)), dict(par=P + 1), dict(pos=P + 2), dict(kl=None),
                dict(n=None), dict(kl=P + 2), dict(n=P + 1), dict(B=0), dict(B=65536), dict(T=0), dict(T=(1 << 20) + 1), dict(kv=cache(D=12)),
