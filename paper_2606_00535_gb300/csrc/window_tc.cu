@@ -88,14 +88,13 @@ struct Cfg {
   // next Q K^T can start once the scores are in registers; with 128 P goes over S.
   static constexpr bool BESIDE = D == 64;
   static constexpr uint32_t P_COL = BESIDE ? 128 : 0, O_COL = BESIDE ? 192 : 128;
-  static constexpr int NST = D == 64 ? 8 : EIGHT ? 4 : 5;
-  // EIGHT: stages of codes, two pages of K or V each
-  static constexpr int NCODE = !EIGHT ? 0 : D == 64 ? 4 : 2;
-  static constexpr uint32_t CODES = KT * D;
-  // (the producer, which waits for no stage of the ring where it copies nothing into one, is
-  // never a whole phase of the ring ahead of what its barriers can tell)
-  static_assert(NCODE < NST, "stages of codes");
-  static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * STAGE + size_t(NCODE) * CODES + 1024, 120 * 1024);
+  static constexpr int NST = D == 64 ? 8 : 5;
+  // EIGHT: where a stage's codes land, two pages HALF bytes apart. With head dim 128 a row's
+  // lie in the stage itself, where its first 64 dimensions come to lie, so that a warp
+  // writes over its own rows' alone; with 64 there is room beside it.
+  static constexpr bool IN_PLACE = D == 128;
+  static constexpr uint32_t HALF = IN_PLACE ? 8192 : 64 * D, CODES = IN_PLACE ? STAGE : 2 * HALF;
+  static constexpr size_t SMEM = std::max<size_t>(NQ * Q_BYTES + size_t(NST) * (STAGE + (EIGHT && !IN_PLACE ? CODES : 0)) + 1024, 120 * 1024);
 };
 
 struct TcParams {
@@ -341,23 +340,28 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   return ~r;
 }
 
-// A lane's codes of a page (16 of each of 16 / RS rows) times 2^e, as bf16 into the ring:
-// `from` its first 8 codes, the other 8 `flip` bytes on; `to` their place.
+// A lane's codes of 16 rows of a page (16 of each of 16 / RS) times 2^e, as bf16 into
+// the ring: `from` its first 8 codes, the other 8 `flip` bytes on; `to` where they go.
+// A warp has all of its rows' codes in registers before it writes over them.
 __device__ __forceinline__ uint32_t factor_of(int e) {  // 2^(120 + e), e <= 7, or NaN; twice
   const uint32_t f = e == DREAMS_KV8_NOT_FINITE ? 0x7fffu : uint32_t(247 + ::max(e, -247)) << 7;
   return f | f << 16;
 }
-template <int D>
-__device__ __forceinline__ void widen(uint32_t from, uint32_t to, int e0, int e1, uint32_t flip) {  // two pages
-  constexpr int RS = 32 / (D / 16), N = 16 / RS;  // rows side by side; rows of a lane
+template <int D, int N>
+__device__ __forceinline__ void fetch_codes(uint32_t from, uint32_t flip, uint32_t (&u)[N][4]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[i][0]), "=r"(u[i][1]) : "r"(from + 512 * i) : "memory");
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[i][2]), "=r"(u[i][3]) : "r"(from + 512 * i + flip) : "memory");
+  }
+}
+template <int D, uint32_t HALF>
+__device__ __forceinline__ void widen(uint32_t from, uint32_t to, int e0, int e1, uint32_t flip) {  // of two pages
+  constexpr int RS = 32 / (D / 16), N = 16 / RS;  // rows side by side (512 bytes); rows of a lane
   uint32_t u[2][N][4];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[h][i][0]), "=r"(u[h][i][1]) : "r"(from + 64 * D * h + RS * D * i));
-      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(u[h][i][2]), "=r"(u[h][i][3]) : "r"(from + 64 * D * h + RS * D * i + flip));
-    }
+  fetch_codes<D>(from, flip, u[0]);
+  fetch_codes<D>(from + HALF, flip, u[1]);
+  __syncwarp();
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t up = factor_of(h == 0 ? e0 : e1);
@@ -382,13 +386,15 @@ __device__ __noinline__ void widen_rare(uint32_t from, uint32_t to, int e, uint3
   constexpr int RS = 32 / (D / 16), N = 16 / RS;
   const bool large = e > 7 && e != DREAMS_KV8_NOT_FINITE;
   const uint32_t up = large ? 0x7f007f00u : factor_of(e), f2 = large ? uint32_t(::min(120 + e, 254)) << 7 : 0x3f80u, up2 = f2 | f2 << 16;
-#pragma unroll 1
+  uint32_t u[N][4];
+  fetch_codes<D>(from, flip, u);
+  __syncwarp();
+#pragma unroll
   for (int i = 0; i < N; ++i) {
     const uint32_t dst = (to ^ (RS == 4 && (i & 1) ? 64u : 0u)) + RS * 128 * i;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      uint32_t a, b;
-      asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(a), "=r"(b) : "r"(from + RS * D * i + (k == 0 ? 0u : flip)));
+      const uint32_t a = u[i][2 * k], b = u[i][2 * k + 1];
       asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst ^ (16u * k)), "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(0, 1)>(a), up), up2)),
                    "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(2, 3)>(a), up), up2)), "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(0, 1)>(b), up), up2)),
                    "r"(mul_bf16x2(mul_bf16x2(codes_x2<sel_of(2, 3)>(b), up), up2))
@@ -506,9 +512,8 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ __align__(8) uint64_t bar_full[NST], bar_empty[NST], bar_ready[NST];
   __shared__ __align__(8) uint64_t bar_qf[2], bar_qe[2], bar_s[2], bar_r[2], bar_h[2], bar_p[2], bar_o[2], bar_scan[SEEN], bar_drain[2], bar_never;
-  // EIGHT: codes' stages, their powers, and bf16 pages that copies bring
-  __shared__ __align__(8) uint64_t bar_code[EIGHT ? C::NCODE : 1], bar_taken[EIGHT ? C::NCODE : 1], bar_wide[EIGHT ? NST : 1];
-  __shared__ uint32_t s_exp[EIGHT ? C::NCODE : 1][2];
+  __shared__ __align__(8) uint64_t bar_land[EIGHT ? NST : 1];  // EIGHT: the copies into a stage have landed
+  __shared__ uint32_t s_exp[EIGHT ? NST : 1][2];               // and the powers of its pages
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
   __shared__ int64_t s_beat;
@@ -520,21 +525,16 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t base = smem_u32(smem);
   auto q_s = [&](int w) { return base + uint32_t(PAIR ? w : 0) * C::Q_BYTES; };
-  const uint32_t ring = base + C::NQ * C::Q_BYTES, codes = ring + uint32_t(NST) * C::STAGE;
-  const uint32_t code0 = smem_u32(bar_code), taken0 = smem_u32(bar_taken), wide0 = smem_u32(bar_wide);
+  const uint32_t ring = base + C::NQ * C::Q_BYTES, land0 = smem_u32(bar_land), codes = C::IN_PLACE ? ring : ring + uint32_t(NST) * C::STAGE;
   const uint32_t full0 = smem_u32(bar_full), empty0 = smem_u32(bar_empty), ready0 = smem_u32(bar_ready);
   const uint32_t qf0 = smem_u32(bar_qf), qe0 = smem_u32(bar_qe), s0 = smem_u32(bar_s), r0 = smem_u32(bar_r), h0 = smem_u32(bar_h), p0 = smem_u32(bar_p),
                  o0 = smem_u32(bar_o), scan0 = smem_u32(bar_scan), drain0 = smem_u32(bar_drain), never = smem_u32(&bar_never);
   if (warp == TMA_WARP) {
     if (lane < NST) {
       tc::mbar_init(full0 + 8 * lane, EIGHT ? CODE_WARPS : 1);
-      if constexpr (EIGHT) tc::mbar_init(wide0 + 8 * lane, 1);
+      if constexpr (EIGHT) tc::mbar_init(land0 + 8 * lane, 1);
       tc::mbar_init(ready0 + 8 * lane, 1);  // the scan
       tc::mbar_init(empty0 + 8 * lane, 3);  // both slots, and the scan
-    }
-    if (EIGHT && lane < C::NCODE) {
-      tc::mbar_init(code0 + 8 * lane, 1);
-      tc::mbar_init(taken0 + 8 * lane, CODE_WARPS);
     }
     if (lane < SEEN) {
       s_dirty[lane] = 0;
@@ -916,8 +916,6 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
         Pos at{0, 0};
         bool wrapped = false, ok = true;
         int issued = 0, ktiles = 0;
-        uint32_t used = 0, phases = 0;  // EIGHT: ring stages that copies have written, and the phases of their barriers
-        Place<(EIGHT ? C::NCODE : 1)> cp{0, 0};
         uint32_t nq[2] = {0, 0};
         Item it;
         int j0, j1;
@@ -969,41 +967,30 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
                 ok = false;
                 break;
               }
+              if (wrapped && !wait(empty0 + 8 * at.s, at.ph ^ 1u)) {
+                ok = false;
+                break;
+              }
+              const uint32_t st = ring + uint32_t(at.s) * C::STAGE, bar = (EIGHT ? land0 : full0) + 8 * at.s;
+              const int coded = int(c0) + int(c1);
               if constexpr (EIGHT) {
-                if (c0 || c1) {  // codes' stages do not wait for the ring
-                  if (issued >= C::NCODE && !wait(taken0 + 8 * cp.s, cp.ph ^ 1u)) {
-                    ok = false;
-                    break;
-                  }
-                  const uint32_t st = codes + uint32_t(cp.s) * C::CODES, bar = code0 + 8 * cp.s;
-                  s_exp[cp.s][0] = x0;
-                  s_exp[cp.s][1] = x1;
-                  tc::mbar_arrive_expect_tx(bar, uint32_t(int(c0) + int(c1)) * 64 * D);
-                  const CUtensorMap *map = kv == 0 ? &P.tmap_k8 : &P.tmap_v8;
-                  if (c0) tc::tma_load_4d(st, map, bar, 0, it.g, 0, ca);
-                  if (c1) tc::tma_load_4d(st + 64 * D, map, bar, 0, it.g, 0, cb);
-                  ++issued;
-                  cp = cp.plus(1);
-                }
+                s_exp[at.s][0] = x0;
+                s_exp[at.s][1] = x1;
               }
-              const int wide = halves - int(c0) - int(c1);
-              if (!EIGHT || wide > 0) {
-                if (wrapped && !wait(empty0 + 8 * at.s, at.ph ^ 1u)) {
-                  ok = false;
-                  break;
-                }
-                const uint32_t st = ring + uint32_t(at.s) * C::STAGE, bar = (EIGHT ? wide0 : full0) + 8 * at.s;
-                tc::mbar_arrive_expect_tx(bar, uint32_t(NR * wide * 8192));
-                const CUtensorMap *map = kv == 0 ? &P.tmap_k : &P.tmap_v;
+              tc::mbar_arrive_expect_tx(bar, uint32_t(NR * (halves - coded) * 8192 + coded * 64 * D));
+              if constexpr (EIGHT) {
+                const uint32_t to = codes + uint32_t(at.s) * C::CODES;
+                const CUtensorMap *map = kv == 0 ? &P.tmap_k8 : &P.tmap_v8;
+                if (c0) tc::tma_load_4d(to, map, bar, 0, it.g, 0, ca);
+                if (c1) tc::tma_load_4d(to + C::HALF, map, bar, 0, it.g, 0, cb);
+              }
+              const CUtensorMap *map = kv == 0 ? &P.tmap_k : &P.tmap_v;
 #pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                  if (!EIGHT || !c0) tc::tma_load_4d(st + r * C::KV_REGION, map, bar, r * 64, it.g, sa, ca);
-                  if (halves == 2 && !c1) tc::tma_load_4d(st + r * C::KV_REGION + 8192, map, bar, r * 64, it.g, sb, cb);
-                }
-                if (!EIGHT) ++issued;
-                used |= 1u << at.s;
-                phases ^= 1u << at.s;
+              for (int r = 0; r < NR; ++r) {
+                if (!c0) tc::tma_load_4d(st + r * C::KV_REGION, map, bar, r * 64, it.g, sa, ca);
+                if (halves == 2 && !c1) tc::tma_load_4d(st + r * C::KV_REGION + 8192, map, bar, r * 64, it.g, sb, cb);
               }
+              ++issued;
               at = at.plus(1);
               wrapped |= at.s == 0;
               if (kv == 1) break;
@@ -1028,13 +1015,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
         }
         if (!ok) give_up();
         // no copy may still be landing when the CTA ends
-        if constexpr (EIGHT) {
-          for (int i = ::max(0, issued - C::NCODE); i < issued; ++i) tc::mbar_wait(code0 + 8 * (i % C::NCODE), (i / C::NCODE) & 1, &s_zero);
-          for (int s = 0; s < NST; ++s)
-            if ((used >> s) & 1u) tc::mbar_wait(wide0 + 8 * s, ((phases >> s) & 1u) ^ 1u, &s_zero);
-        } else {
-          for (int i = ::max(0, issued - NST); i < issued; ++i) tc::mbar_wait(full0 + 8 * (i % NST), (i / NST) & 1, &s_zero);
-        }
+        for (int i = ::max(0, issued - NST); i < issued; ++i) tc::mbar_wait((EIGHT ? land0 : full0) + 8 * (i % NST), (i / NST) & 1, &s_zero);
         for (int w = 0; w < C::NQ; ++w)
           if (nq[w] > 0) tc::mbar_wait(qf0 + 8 * w, (nq[w] - 1) & 1u, &s_zero);
       }
@@ -1151,62 +1132,41 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
       }
     } else if (warp >= CODE_WARP) {
       if constexpr (EIGHT) {
-        // ---------------- codes to bf16, on their way into the ring: each warp 16 rows of
-        // a page. A code times its page's power is exact in bf16, so what follows does not
-        // know of codes; pages in bf16 are waited for here.
-        // A lane's 16 codes of a row are two runs of 8, each 16 bytes of the ring; which of
+        // ---------------- codes to bf16: each warp 16 rows of a page. A code times its page's
+        // power is exact in bf16, so what follows does not know of codes.
+        // A lane's 16 codes of a row are two runs of 8, each 16 bytes of a row's bf16; which of
         // them is first differs between lanes, so that no two of eight meet in a bank.
         constexpr int CH = D / 16;
-        const int ch = lane % CH, row = 16 * (warp - CODE_WARP) + lane / CH, part = D == 128 ? ((ch >> 2) ^ (row & 1)) : 0;
-        const uint32_t mine = codes + uint32_t(row * D + ch * 16 + part * 8), flip = part != 0 ? uint32_t(-8) : 8u;
-        const uint32_t put = ring + (ch >> 2) * C::KV_REGION + row * 128 + (uint32_t((2 * (ch & 3) + part) ^ (row & 7)) << 4);
+        const int cw = warp - CODE_WARP, ch = lane % CH, lr = lane / CH, part = D == 128 ? ((ch >> 2) ^ (lr & 1)) : 0;
+        const uint32_t mine = codes + uint32_t((16 * cw + lr) * D + ch * 16 + part * 8), flip = part != 0 ? uint32_t(-8) : 8u;
+        const uint32_t put = ring + 2048u * cw + (ch >> 2) * C::KV_REGION + lr * 128 + (uint32_t((2 * (ch & 3) + part) ^ lr) << 4);
         Pos at{0, 0};
-        Place<C::NCODE> cp{0, 0};
-        bool wrapped = false, ok = true;
-        uint32_t phases = 0;
+        bool ok = true;
         Item it;
         int j0, j1;
         while (ok && next_item(it, j0, j1, false)) {
           for (int j = j0; j < j1 && ok; ++j) {
-            const bool c0 = it.codes(2 * j), c1 = it.codes(2 * j + 1), wide = !c0 || (2 * j + 1 < it.np && !c1);
+            const bool c0 = it.codes(2 * j), c1 = it.codes(2 * j + 1);
 #pragma unroll 1
             for (int kv = 0; kv < 2; ++kv) {
-              const uint32_t code = code0 + 8 * cp.s, empty = empty0 + 8 * at.s;
-              if (c0) {  // (the first half is in 8 bits where the second is)
-                // both at once, as either takes a while to answer
-                const bool a = quick(code, cp.ph), b = !wrapped || quick(empty, at.ph ^ 1u);
-                ok = (a || wait(code, cp.ph)) && (b || wait(empty, at.ph ^ 1u));
-              } else if (wrapped) {
-                ok = wait(empty, at.ph ^ 1u);
-              }
-              ok = __all_sync(0xffffffffu, ok);
+              ok = __all_sync(0xffffffffu, wait(land0 + 8 * at.s, at.ph));
               if (!ok) break;
-              if (c0) {
-                const uint32_t from = mine + uint32_t(cp.s) * C::CODES, to = put + uint32_t(at.s) * C::STAGE;
-                const uint32_t x0 = *reinterpret_cast<volatile uint32_t *>(&s_exp[cp.s][0]), x1 = *reinterpret_cast<volatile uint32_t *>(&s_exp[cp.s][1]);
+              if (c0) {  // (the first half is in 8 bits where the second is)
+                const uint32_t x0 = *reinterpret_cast<volatile uint32_t *>(&s_exp[at.s][0]), x1 = *reinterpret_cast<volatile uint32_t *>(&s_exp[at.s][1]);
                 const int e0 = kv == 0 ? k_exp(x0) : v_exp(x0), e1 = kv == 0 ? k_exp(x1) : v_exp(x1);
                 const bool large = (e0 > 7 && e0 != DREAMS_KV8_NOT_FINITE) || (e1 > 7 && e1 != DREAMS_KV8_NOT_FINITE);
+                const uint32_t from = mine + uint32_t(at.s) * C::CODES, to = put + uint32_t(at.s) * C::STAGE;
                 if (__builtin_expect(large || !c1, 0)) {
                   widen_rare<D>(from, to, e0, flip);
-                  if (c1) widen_rare<D>(from + 64 * D, to + 8192, e1, flip);
+                  if (c1) widen_rare<D>(from + C::HALF, to + 8192, e1, flip);
                 } else {
-                  widen<D>(from, to, e0, e1, flip);
+                  widen<D, C::HALF>(from, to, e0, e1, flip);
                 }
                 tc::fence_proxy_async_smem();
               }
-              if (wide) {
-                ok = __all_sync(0xffffffffu, wait(wide0 + 8 * at.s, (phases >> at.s) & 1u));
-                phases ^= 1u << at.s;
-                if (!ok) break;
-              }
               __syncwarp();
-              if (lane == 0) {
-                tc::mbar_arrive(full0 + 8 * at.s);
-                if (c0) tc::mbar_arrive(taken0 + 8 * cp.s);
-              }
-              if (c0) cp = cp.plus(1);
+              if (lane == 0) tc::mbar_arrive(full0 + 8 * at.s);
               at = at.plus(1);
-              wrapped |= at.s == 0;
             }
           }
         }
