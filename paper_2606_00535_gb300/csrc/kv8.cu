@@ -11,7 +11,8 @@
 // rounding. Blocks are persistent, as which pages there are is known on the device
 // alone: each counts the pages of 256 sequences at a time by a prefix sum and walks
 // over (page, layer, head), heads side by side, so that neighbours read neighbouring
-// parts of the same rows.
+// parts of the same rows. 3392 tokens of 32 layers of 32 heads: 425 us, 94% of the copy rate;
+// one page of 8 layers of 8 heads for each of 16 sequences 11.1 us, of which 7.6 are the bytes.
 #include <limits.h>
 
 #include <algorithm>
@@ -23,6 +24,11 @@ namespace dreams {
 namespace {
 
 constexpr int THREADS = 256;
+// Blocks of an SM, all of which run: 3392 tokens of 32 heads and layers, head dim 128, take
+// 425 us with 4, 471 with 3 and 579 with 6 (spills); 16 x 1000 to 3000 of 8 heads and layers,
+// head dim 64, 149 with 6 and 166 with 4.
+template <int D>
+constexpr int RESIDENT = D == 64 ? 6 : 4;
 
 struct QuantParams {
   Cache c;
@@ -61,7 +67,7 @@ __device__ __forceinline__ uint32_t to_codes(uint32_t w, float scale) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(THREADS) kv_quantize_kernel(const QuantParams p) {
+__global__ void __launch_bounds__(THREADS, RESIDENT<D>) kv_quantize_kernel(const QuantParams p) {
   constexpr int COLS = D / 8, ROWS = THREADS / COLS, N = PAGE / ROWS;  // 16-byte columns; rows of a pass; passes
   __shared__ int s_first[THREADS + 1], s_warp[THREADS / 32];
   __shared__ uint32_t s_max[2][THREADS / 32];  // K's in the low half, V's in the high one
@@ -197,6 +203,6 @@ extern "C" dreams_status_t dreams_kv_quantize(const dreams_kv_cache_t *kv, const
   p.new_len8 = new_len8;
   p.status = status_word;
   const int64_t most = int64_t(B) * std::min<int64_t>(kv8->pages_per_seq, kv->capacity / PAGE) * kv->n_layers * kv->Hkv;
-  const dim3 grid(unsigned(std::max<int64_t>(1, std::min<int64_t>(most, int64_t(num_sms()) * 6))));
+  const dim3 grid(unsigned(std::max<int64_t>(1, std::min<int64_t>(most, int64_t(num_sms()) * (kv->D == 128 ? RESIDENT<128> : RESIDENT<64>)))));
   return launch(early_launch(), kv->D == 128 ? kv_quantize_kernel<128> : kv_quantize_kernel<64>, grid, THREADS, 0, 1, stream, p);
 }
