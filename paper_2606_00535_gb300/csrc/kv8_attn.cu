@@ -1,9 +1,13 @@
 // kv8_attn.cu -- attention over a cache whose full pages are held in 8 bits.
 //
-// More than 16 query rows of a KV head go to window_tc.cu.
+// Many rows of a KV head go to window_tc.cu: more than 32, with head dim 64 more than 64.
+// Up to there they are blocks of 16 rows, each with a list of keys of its own, which the
+// second block finds in L2. 8 sequences of 1000 to 8000 tokens, 8 KV heads, in us, here and
+// there: 20 rows 53.4 and 79.0, 48 rows 72.2 and 80.2 (all of 4000 tokens: 86.0 and 46.1), 64
+// rows 88.0 and 80.1; head dim 64, 48 rows 46.7 and 58.0, 64 rows 57.4 and 57.9. (One CTA
+// for both blocks of 32 rows, K and V read once: 59.5 against 55.0.)
 //
-// Few rows (at most 16 of a KV head: single tokens, short drafts), bound by reading K
-// and V once. As in window.cu, a CTA takes part of the keys of a sequence and KV head, its
+// Few rows (single tokens, short drafts), bound by reading K and V once. As in window.cu, a CTA takes part of the keys of a sequence and KV head, its
 // warps take tiles in turn, each with its own ring of cp.async stages, scores and P V run
 // on m16n8k16 tensor instructions, and a cluster's CTAs join their parts in shared
 // memory. What differs is the tiles. Keys come in runs, the sinks and the window, each
@@ -45,6 +49,7 @@ constexpr int MAX_RANKED = 128;
 struct AttnParams {
   WinParams p;
   Kv8 c;
+  int32_t blocks;  // of 16 rows, of a KV head
   int32_t ranked;  // sequences are taken longest first
 };
 
@@ -55,7 +60,7 @@ struct Cfg8 {
   static constexpr int TILE = 32 * ROW8;         // K or V of a tile
   static constexpr int WARP_BYTES = STAGES * 2 * TILE;
   static constexpr int RING = WARPS * WARP_BYTES;  // afterwards the warps' outputs [WARPS][16][D] f32
-  static constexpr int SMEM = RING + RB * D * 4;   // and what the CTAs of a cluster push here
+  static constexpr int SMEM = RING + RB * D * 4;  // and what the CTAs of a cluster push here
   static_assert(RING >= WARPS * RB * D * 4, "partials fit");
 };
 
@@ -207,7 +212,7 @@ __device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], flo
 // row, and `smem` its unnormalised outputs [warp][row][D] in f32.
 template <int D, bool FOLD>
 __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh, uint32_t (*s_exp)[6], uint8_t *smem, const Tiles &tl, int b, int g, int L, int T,
-                                             int j0, int j1) {
+                                             int first, int j0, int j1) {
   using C = Cfg8<D>;
   const WinParams &p = P.p;
   constexpr int H = FOLD ? 1 : 2;  // rows of a thread
@@ -268,33 +273,29 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
   look(0);
 
   const int r0 = lane >> 2, c = lane & 3;  // this thread's rows: r0 and (H = 2) r0 + 8
-  int off[H];
-  unsigned long long anc[H];
-  const __nv_bfloat16 *src[H];  // its part of Q: dimensions 4 c .. 4 c + 3 of each 16
-#pragma unroll
-  for (int h = 0; h < H; ++h) {
-    const int r = r0 + 8 * h, t = r / p.G;
-    off[h] = t < T ? t : -1;
-    anc[h] = 0ull;
-    if (p.parent != nullptr) {
-      off[h] = sh.row[r].off;
-      anc[h] = sh.row[r].anc;
-    }
-    src[h] = t < T ? p.q + b * p.sb + t * p.st + int64_t(g * p.G + r - t * p.G) * D + 4 * c : nullptr;
-  }
+  // (in registers where they have room: 64 sequences of up to 32768 tokens 352 us with one
+  // row, 392 from shared memory; with two rows 523 and 481)
+  const RowInfo own = FOLD ? sh.row[r0] : RowInfo{};
+  auto info = [&](int h) { return FOLD ? own : sh.row[r0 + 8 * h]; };
+  // its part of Q: dimensions 4 c .. 4 c + 3 of each 16
+  auto src = [&](int h) -> const __nv_bfloat16 * {
+    const int r = first + r0 + 8 * h, t = r / p.G;
+    return t < T ? p.q + b * p.sb + t * p.st + int64_t(g * p.G + r - t * p.G) * D + 4 * c : nullptr;
+  };
   float o[D / 8][2 * H];
+  float m[H], l[H];
 #pragma unroll
   for (int n = 0; n < D / 8; ++n)
 #pragma unroll
     for (int e = 0; e < 2 * H; ++e) o[n][e] = 0.f;
-  float m[H], l[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) {
     m[h] = -INFINITY;
     l[h] = 0.f;
   }
 
-  const int off_max = T - 1;
+  // what the rows see differs between the first token and the last
+  const int off_min = first / p.G, off_max = ::min(T - 1, (first + RB - 1) / p.G);
   int in = 0, at = 0;  // the stages of the copy and of the tile
   auto step = [&](int i) {  // the tile after it is copied; this one is there
     cp_wait<C::STAGES - 2>();
@@ -313,11 +314,12 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
     float rq[H];                                       // scale of a row's scores
 #pragma unroll
     for (int h = 0; h < H; ++h) {
+      const __nv_bfloat16 *from = src(h);
       uint2 w[D / 16];
       uint32_t bits = 0;
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        w[kk] = src[h] != nullptr ? *reinterpret_cast<const uint2 *>(src[h] + kk * 16) : make_uint2(0u, 0u);
+        w[kk] = from != nullptr ? *reinterpret_cast<const uint2 *>(from + kk * 16) : make_uint2(0u, 0u);
         bits = __vmaxu2(bits, __vmaxu2(w[kk].x & 0x7fff7fffu, w[kk].y & 0x7fff7fffu));
       }
       bits = ::max(bits & 0xffffu, bits >> 16);
@@ -374,14 +376,18 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
         }
       }
       // does every row see every key of the tile?
-      if (!(t.slot >= t.lo && t.slot + 32 <= t.hi && (t.sink || int64_t(L) + off_max - t.slot < p.window))) {
+      if (!(t.slot >= t.lo && t.slot + 32 <= t.hi && (t.sink || int64_t(L) + (p.parent != nullptr ? T - 1 : off_max) - t.slot < p.window))) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int h = 0; h < H; ++h) {
+          const RowInfo ri = info(h);
 #pragma unroll
-          for (int e = 0; e < 2 * H; ++e) {
-            const int slot = t.slot + n * 8 + 2 * c + (e & 1);
-            if (slot < t.lo || slot >= t.hi || off[e >> 1] < 0 || !sees(p, L, off[e >> 1], anc[e >> 1], slot)) s[n][e] = -INFINITY;
-          }
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int slot = t.slot + n * 8 + 2 * c + e;
+              if (slot < t.lo || slot >= t.hi || ri.off < 0 || !sees(p, L, ri.off, ri.anc, slot)) s[n][2 * h + e] = -INFINITY;
+            }
+        }
       }
       soften<D, 4, H>(s, m, l, o);
       float fv[H];
@@ -431,61 +437,22 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
     to_order<D, 2 * H>(o);
     uint32_t qf[D / 16][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      const __nv_bfloat16 *from = h < H ? src(h % H) : nullptr;
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        const uint2 w = h < H && src[h % H] != nullptr ? *reinterpret_cast<const uint2 *>(src[h % H] + kk * 16) : make_uint2(0u, 0u);
+        const uint2 w = from != nullptr ? *reinterpret_cast<const uint2 *>(from + kk * 16) : make_uint2(0u, 0u);
         qf[kk][h] = w.x;
         qf[kk][h + 2] = w.y;
       }
+    }
 #pragma unroll 1
     for (; i < my; ++i) {
       step(i);
       const Tile t = tile_of(tl, j0 + warp + i * WARPS);
       const uint32_t st = ring + at * 2 * C::TILE;
-      float x[2][4] = {}, s[2][2 * H];
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const int key = n * 8 + r0;
-          uint32_t k0, k1;
-          asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];"
-                       : "=r"(k0), "=r"(k1)
-                       : "r"(st + key * C::ROW16 + (((2 * kk + (c >> 1)) ^ (key & 7)) << 4) + (c & 1) * 8));
-          mma16816(x[n], qf[kk], k0, k1);
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int e = 0; e < 2 * H; ++e) s[n][e] = x[n][e] * p.scale_log2;
       const bool all = t.slot >= t.lo && t.slot + 16 <= t.hi &&
-                       (t.sink || (int64_t(L) + off_max - t.slot < p.window && (p.parent != nullptr ? t.slot + 15 < L : t.slot + 15 <= L)));
-      if (!all) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 2 * H; ++e) {
-            const int slot = t.slot + n * 8 + 2 * c + (e & 1);
-            if (slot < t.lo || slot >= t.hi || off[e >> 1] < 0 || !sees(p, L, off[e >> 1], anc[e >> 1], slot)) s[n][e] = -INFINITY;
-          }
-      }
-      soften<D, 2, H>(s, m, l, o);
-      uint32_t pf[4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        if constexpr (FOLD) {
-          const uint32_t hi = __byte_perm(__float_as_uint(s[n][0]), __float_as_uint(s[n][1]), 0x7632);
-          pf[2 * n] = hi;
-          // (what is left may be zero, and zero times an infinity in V a NaN: 2^-20 of P is below its error)
-          pf[2 * n + 1] = pack_bf16x2(fmaxf(s[n][0] - __uint_as_float(hi << 16), s[n][0] * 0x1p-20f),
-                                      fmaxf(s[n][1] - __uint_as_float(hi & 0xffff0000u), s[n][1] * 0x1p-20f));
-        } else {
-          pf[2 * n] = pack_bf16x2(s[n][0], s[n][1]);
-          pf[2 * n + 1] = pack_bf16x2(s[n][2], s[n][3]);
-        }
-      }
+                       (t.sink || (int64_t(L) + (p.parent != nullptr ? T - 1 : off_max) - t.slot < p.window && (p.parent != nullptr ? t.slot + 15 < L : t.slot + 15 <= L + off_min)));
       const int vkey = lane & 15, vhalf = lane >> 4;
       const uint32_t vrow = st + C::TILE + vkey * C::ROW16;
       // 0 x inf and 0 x NaN are NaN: where a key that not every row sees holds one, each
@@ -503,6 +470,51 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           for (int k = 0; k < 4; ++k) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(u[k]), "r"(0u));
         }
         odd = __any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0u);
+      }
+      float x[2][4] = {}, s[2][2 * H];
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const int key = n * 8 + r0;
+          uint32_t k0, k1;
+          asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];"
+                       : "=r"(k0), "=r"(k1)
+                       : "r"(st + key * C::ROW16 + (((2 * kk + (c >> 1)) ^ (key & 7)) << 4) + (c & 1) * 8));
+          mma16816(x[n], qf[kk], k0, k1);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 2 * H; ++e) s[n][e] = x[n][e] * p.scale_log2;
+      if (!all) {
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          const RowInfo ri = info(h);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int slot = t.slot + n * 8 + 2 * c + e;
+              if (slot < t.lo || slot >= t.hi || ri.off < 0 || !sees(p, L, ri.off, ri.anc, slot)) s[n][2 * h + e] = -INFINITY;
+            }
+        }
+      }
+      soften<D, 2, H>(s, m, l, o);
+      uint32_t pf[4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        if constexpr (FOLD) {
+          const uint32_t hi = __byte_perm(__float_as_uint(s[n][0]), __float_as_uint(s[n][1]), 0x7632);
+          pf[2 * n] = hi;
+          // (what is left may be zero, and zero times an infinity in V a NaN: 2^-20 of P is below its error)
+          pf[2 * n + 1] = pack_bf16x2(fmaxf(s[n][0] - __uint_as_float(hi << 16), s[n][0] * 0x1p-20f),
+                                      fmaxf(s[n][1] - __uint_as_float(hi & 0xffff0000u), s[n][1] * 0x1p-20f));
+        } else {
+          pf[2 * n] = pack_bf16x2(s[n][0], s[n][1]);
+          pf[2 * n + 1] = pack_bf16x2(s[n][2], s[n][3]);
+        }
       }
 #pragma unroll 1
       for (int r = odd ? 0 : -1; r < (odd ? 8 * H : 0); ++r) {
@@ -547,7 +559,7 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
     const int r = r0 + 8 * h;
     if (c == 0) sh.ml[warp][r] = make_float2(m[h] - LIFT, l[h]);
-    if (off[h] >= 0) {
+    if (info(h).off >= 0) {
       float *to = so + (warp * RB + r) * D;
 #pragma unroll
       for (int n = 0; n < D / 8; n += 2) {
@@ -618,27 +630,30 @@ __global__ void __launch_bounds__(32 * WARPS) kv8_rows_kernel(const AttnParams P
   int x = blockIdx.x;
   const int split = x % p.nsplit;
   x /= p.nsplit;
+  const int first = x % P.blocks * RB;  // of the KV head's rows
+  x /= P.blocks;
   const int g = x % p.Hkv;
   int b = x / p.Hkv;
   if (p.nsplit > 1) cluster_arrive();  // this CTA runs: it may be written to
   after_previous();
   if (P.ranked) b = by_length(p, b);
   const int T = p.q_len[b], L = p.kv_len[b], L8 = P.c.len8[b];
-  const bool report = split == 0 && g == 0;
+  const bool report = split == 0 && g == 0 && first == 0;
   int bad = 0;
   if (T < 0 || T > p.T_max) bad = DREAMS_DATA_BAD_TREE_LEN;
   else if (L < 0 || int64_t(L) + T > p.capacity || len8_bad(P.c, L8, L)) bad = DREAMS_DATA_BAD_KV_LEN;
   if (bad && report && tid == 0) flag(p.status, bad);
   // (all CTAs of a cluster come to the same answer; none leaves while it may be written to)
-  if (bad || T == 0 || !load_rows(p, sh, b, L, T, report)) {
+  if (bad || T * p.G <= first || !load_rows(p, sh, b, L, T, report, first)) {
     if (p.nsplit > 1) cluster_wait();
     return;
   }
-  const Tiles tl(key_list(p, L, 0, T - 1), L8, L + T);
+  const int last = ::min(T - 1, (first + RB - 1) / p.G);
+  const Tiles tl(key_list(p, L, first / p.G, last), L8, L + (p.parent != nullptr ? T : last + 1));
   const int per = (tl.n + p.nsplit - 1) / p.nsplit;
   const int j0 = ::min(tl.n, split * per), j1 = ::min(tl.n, j0 + per);
-  stream_tiles<D, FOLD>(P, sh, s_exp, smem, tl, b, g, L, T, j0, j1);
-  finish_rows<D>(p, sh, smem, Cfg8<D>::RING, b, g, T, split);
+  stream_tiles<D, FOLD>(P, sh, s_exp, smem, tl, b, g, L, T, first, j0, j1);
+  finish_rows<D>(p, sh, smem, Cfg8<D>::RING, b, g, T, split, first);
 }
 
 // ------------------------------------------------------------------ host side
@@ -662,14 +677,15 @@ constexpr int MAX_SPLIT = 16;
 int split_of(int B, int64_t lists, int64_t keys) {
   const int64_t fit = 2 * int64_t(num_sms());
   int n = 1;
-  while (n < MAX_SPLIT && lists * n * 2 <= fit && keys / n > WARPS * 32) n *= 2;
+  while (n < MAX_SPLIT && lists * n * 2 <= (n == MAX_SPLIT / 2 ? fit / 2 : fit) && keys / n > WARPS * 32) n *= 2;
   if (B > 1 && n < MAX_SPLIT && lists * n <= fit && keys / (2 * n) >= 1000) n *= 2;
   return n;
 }
 
 template <int D, bool FOLD>
 dreams_status_t launch_rows(AttnParams P, cudaStream_t stream) {
-  const int64_t lists = int64_t(P.p.B) * P.p.Hkv;
+  P.blocks = int32_t((int64_t(P.p.T_max) * P.p.G + RB - 1) / RB);
+  const int64_t lists = int64_t(P.p.B) * P.p.Hkv * P.blocks;
   P.p.nsplit = split_of(P.p.B, lists, std::min<int64_t>(P.p.capacity, int64_t(P.p.window) - 1 + P.p.T_max + P.p.sinks));
   P.ranked = P.p.B > 1 && P.p.B <= MAX_RANKED && lists * P.p.nsplit > 2 * int64_t(num_sms());
   return launch_lists(early_launch(), kv8_rows_kernel<D, FOLD>, Cfg8<D>::SMEM, lists, P.p.nsplit, stream, P);
@@ -701,6 +717,6 @@ extern "C" dreams_status_t dreams_kv8_attention(const void *q, int64_t q_stride_
   const int64_t few = int64_t(T_max) * P.p.G;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (few <= 8) return kv->D == 128 ? launch_rows<128, true>(P, s) : launch_rows<64, true>(P, s);
-  if (few <= RB) return kv->D == 128 ? launch_rows<128, false>(P, s) : launch_rows<64, false>(P, s);
+  if (few <= (kv->D == 128 ? 2 : 4) * RB) return kv->D == 128 ? launch_rows<128, false>(P, s) : launch_rows<64, false>(P, s);
   return win::launch_tc8(P.p, P.c, kv->D, s);
 }

@@ -54,8 +54,9 @@ struct RowsShared {
   float2 part[16][RB];     // those of a list's parts
 };
 
-// The queries of a sequence and KV head; false (flagged by `report`): a bad tree.
-__device__ __forceinline__ bool load_rows(const WinParams &p, RowsShared &sh, int b, int L, int T, bool report) {
+// The queries of a sequence and KV head, from row `first` on; false (flagged by
+// `report`): a bad tree.
+__device__ __forceinline__ bool load_rows(const WinParams &p, RowsShared &sh, int b, int L, int T, bool report, int first = 0) {
   const int tid = threadIdx.x;
   __syncthreads();  // the last part's readers are done
   if (p.parent != nullptr) {
@@ -71,7 +72,7 @@ __device__ __forceinline__ bool load_rows(const WinParams &p, RowsShared &sh, in
     }
   }
   if (tid < RB) {
-    const int t = tid / p.G;
+    const int t = (first + tid) / p.G;
     RowInfo r{-1, 0ull};
     if (t < T) {
       r.off = t;
@@ -117,8 +118,8 @@ __device__ __forceinline__ float4 join_warps(const RowsShared &sh, const uint8_t
 }
 
 template <int D>
-__device__ __forceinline__ void emit(const WinParams &p, int b, int g, int u, float4 v, float M, float Z) {
-  const int r = u / (D / 4), d = (u % (D / 4)) * 4, t = r / p.G;
+__device__ __forceinline__ void emit(const WinParams &p, int b, int g, int u, float4 v, float M, float Z, int first) {
+  const int r = first + u / (D / 4), d = (u % (D / 4)) * 4, t = r / p.G;
   const int64_t row = (int64_t(b) * p.T_max + t) * p.Hq + g * p.G + (r - t * p.G);
   const float inv = __frcp_rn(Z);
   *reinterpret_cast<uint2 *>(p.out + row * D + d) = make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
@@ -129,14 +130,15 @@ __device__ __forceinline__ void emit(const WinParams &p, int b, int g, int u, fl
 // cluster's CTAs, and writes the rows out. Behind ring_bytes there is room for RB * D * 4
 // bytes that the CTAs push.
 template <int D>
-__device__ __forceinline__ void finish_rows(const WinParams &p, RowsShared &sh, uint8_t *smem, uint32_t ring_bytes, int b, int g, int T, int split) {
+__device__ __forceinline__ void finish_rows(const WinParams &p, RowsShared &sh, uint8_t *smem, uint32_t ring_bytes, int b, int g, int T, int split,
+                                            int first = 0) {
   const int tid = threadIdx.x;
-  const int units = T * p.G * (D / 4);
+  const int units = ::min(RB, T * p.G - first) * (D / 4);
   if (p.nsplit == 1) {
     for (int u = tid; u < units; u += 32 * WARPS) {
       float M, Z;
       const float4 v = join_warps<D>(sh, smem, u, M, Z);
-      emit<D>(p, b, g, u, v, M, Z);
+      emit<D>(p, b, g, u, v, M, Z, first);
     }
     return;
   }
@@ -161,7 +163,7 @@ __device__ __forceinline__ void finish_rows(const WinParams &p, RowsShared &sh, 
     float M, Z;
     const float4 v = join<4>(
         p.nsplit, [&](int c) { return sh.part[c][u / (D / 4)]; }, [&](int c) { return in[c * room + u / p.nsplit]; }, M, Z);
-    emit<D>(p, b, g, u, v, M, Z);
+    emit<D>(p, b, g, u, v, M, Z, first);
   }
 }
 
