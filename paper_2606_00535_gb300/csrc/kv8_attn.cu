@@ -53,9 +53,13 @@ struct AttnParams {
   int32_t ranked;  // sequences are taken longest first
 };
 
-template <int D>
+template <int D, bool FOLD>
 struct Cfg8 {
-  static constexpr int STAGES = D == 128 ? 3 : 6;
+  // CTAs of an SM. With head dim 64 a tile is half the bytes for the same softmax, and one row
+  // to a thread leaves room for four: 64 sequences of 1500 to 32768 tokens 212 us, 264 with two.
+  // (With two rows: 326 and 327, and 38 equal ones 236 and 189.)
+  static constexpr int PER_SM = D == 64 && FOLD ? 4 : 2;
+  static constexpr int STAGES = D == 128 || FOLD ? 3 : 6;
   static constexpr int ROW8 = D, ROW16 = 2 * D;  // bytes of a key
   static constexpr int TILE = 32 * ROW8;         // K or V of a tile
   static constexpr int WARP_BYTES = STAGES * 2 * TILE;
@@ -213,7 +217,7 @@ __device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], flo
 template <int D, bool FOLD>
 __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh, uint32_t (*s_exp)[6], uint8_t *smem, const Tiles &tl, int b, int g, int L, int T,
                                              int first, int j0, int j1) {
-  using C = Cfg8<D>;
+  using C = Cfg8<D, FOLD>;
   const WinParams &p = P.p;
   constexpr int H = FOLD ? 1 : 2;  // rows of a thread
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -620,8 +624,10 @@ __device__ __noinline__ int by_length(const WinParams &p, int r) {
   return s_at;
 }
 
+// (0 CTAs in the bounds: none are asked for. Asking for two changes the code of head dim
+// 128, and a batch of 64 takes 402 us for 347.)
 template <int D, bool FOLD>
-__global__ void __launch_bounds__(32 * WARPS) kv8_rows_kernel(const AttnParams P) {
+__global__ void __launch_bounds__(32 * WARPS, Cfg8<D, FOLD>::PER_SM == 4 ? 4 : 0) kv8_rows_kernel(const AttnParams P) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ RowsShared sh;
   __shared__ uint32_t s_exp[WARPS][6];
@@ -653,14 +659,15 @@ __global__ void __launch_bounds__(32 * WARPS) kv8_rows_kernel(const AttnParams P
   const int per = (tl.n + p.nsplit - 1) / p.nsplit;
   const int j0 = ::min(tl.n, split * per), j1 = ::min(tl.n, j0 + per);
   stream_tiles<D, FOLD>(P, sh, s_exp, smem, tl, b, g, L, T, first, j0, j1);
-  finish_rows<D>(p, sh, smem, Cfg8<D>::RING, b, g, T, split, first);
+  finish_rows<D>(p, sh, smem, Cfg8<D, FOLD>::RING, b, g, T, split, first);
 }
 
 // ------------------------------------------------------------------ host side
-// CTAs of a list, and the order of the lists. Two CTAs fit an SM. One takes 9 us for 1000
-// keys whatever else runs, and with all places taken the copies are bound by HBM, so
-// lists are split while all CTAs still run at the same time, and once more for
-// several sequences of which each part keeps 1000 keys, as their lengths may differ.
+// CTAs of a list, and the order of the lists. One CTA takes 9 us for 1000 keys whatever
+// else runs, and with all places taken the copies are bound by HBM, so lists are split
+// while all CTAs (`fit` places) still run at the same time, 16 to a list only while each
+// has an SM of its own, and once more for several sequences of which each part keeps
+// 1000 keys, as their lengths may differ.
 // Where not all CTAs run at the same time, the longest sequences go first. Measured on
 // the GPU for 8 KV heads, head dim 128, lengths spread from a to b, in us; (r): longest first
 //   lists          8      16       64       64        128        256          512     1024
@@ -674,10 +681,9 @@ __global__ void __launch_bounds__(32 * WARPS) kv8_rows_kernel(const AttnParams P
 // CTA a pass over the lengths and B comparisons for each of them: with 256 sequences of
 // equal length 132.0 us against 128.0, of lengths up to 4000 239.7 against 227.0.
 constexpr int MAX_SPLIT = 16;
-int split_of(int B, int64_t lists, int64_t keys) {
-  const int64_t fit = 2 * int64_t(num_sms());
+int split_of(int64_t fit, int B, int64_t lists, int64_t keys) {
   int n = 1;
-  while (n < MAX_SPLIT && lists * n * 2 <= (n == MAX_SPLIT / 2 ? fit / 2 : fit) && keys / n > WARPS * 32) n *= 2;
+  while (n < MAX_SPLIT && lists * n * 2 <= (n == MAX_SPLIT / 2 ? num_sms() : fit) && keys / n > WARPS * 32) n *= 2;
   if (B > 1 && n < MAX_SPLIT && lists * n <= fit && keys / (2 * n) >= 1000) n *= 2;
   return n;
 }
@@ -686,9 +692,10 @@ template <int D, bool FOLD>
 dreams_status_t launch_rows(AttnParams P, cudaStream_t stream) {
   P.blocks = int32_t((int64_t(P.p.T_max) * P.p.G + RB - 1) / RB);
   const int64_t lists = int64_t(P.p.B) * P.p.Hkv * P.blocks;
-  P.p.nsplit = split_of(P.p.B, lists, std::min<int64_t>(P.p.capacity, int64_t(P.p.window) - 1 + P.p.T_max + P.p.sinks));
-  P.ranked = P.p.B > 1 && P.p.B <= MAX_RANKED && lists * P.p.nsplit > 2 * int64_t(num_sms());
-  return launch_lists(early_launch(), kv8_rows_kernel<D, FOLD>, Cfg8<D>::SMEM, lists, P.p.nsplit, stream, P);
+  const int64_t fit = int64_t(Cfg8<D, FOLD>::PER_SM) * num_sms();
+  P.p.nsplit = split_of(fit, P.p.B, lists, std::min<int64_t>(P.p.capacity, int64_t(P.p.window) - 1 + P.p.T_max + P.p.sinks));
+  P.ranked = P.p.B > 1 && P.p.B <= MAX_RANKED && lists * P.p.nsplit > fit;
+  return launch_lists(early_launch(), kv8_rows_kernel<D, FOLD>, Cfg8<D, FOLD>::SMEM, lists, P.p.nsplit, stream, P);
 }
 
 }  // namespace
