@@ -579,7 +579,7 @@ typedef struct dreams_rotary {
  * accesses. D even, at most 512, 1 <= n_pairs <= D / 2.
  * positions: device [n_axes, B, T], any values (negative ones turn backwards); or
  * NULL (n_axes 1): token t of sequence b is at start[b] + t, start device [B], NULL
- * = 0. 1 <= n_axes <= 4. One launch.
+ * = 0. 1 <= n_axes <= 4, B <= 65535. One launch.
  */
 dreams_status_t dreams_rope(const void *x, int64_t x_stride_b, int64_t x_stride_t, int64_t x_stride_h, void *out,
                             int64_t out_stride_b, int64_t out_stride_t, int64_t out_stride_h, dreams_dtype_t dtype, int32_t B, int32_t T, int32_t H, int32_t D,
@@ -709,12 +709,13 @@ dreams_status_t dreams_vocab_argmax_noalloc(const void *logits, dreams_dtype_t d
  * the GPU, and this hook lets a test make such a wait run out without any
  * fault. While stall_at >= 0, every later launch of the kernels selected by
  * `kernels` (DREAMS_TEST_ATTENTION: dreams_tree_verify_attn,
- * dreams_attention and, for more than 16 rows per KV head,
- * dreams_window_attention; DREAMS_TEST_LM_HEAD: dreams_lm_head_argmax) withholds the
+ * dreams_attention and, where blocks of rows go to the tensor cores' tcgen05 (more than
+ * 16 rows per KV head; dreams_kv8_attention: more than 32, with head dim 64 more than
+ * 64), dreams_window_attention and dreams_kv8_attention; DREAMS_TEST_LM_HEAD: dreams_lm_head_argmax) withholds the
  * TMA copies of each CTA from its stall_at-th K tile (attention) or k-block
  * (LM head, counted over the CTA's tiles) on, waiting instead on a barrier
  * that nothing arrives on, and every pipeline wait gives up after
- * wait_limit_ns (1 us .. 2 s) instead of 2 s (in dreams_window_attention, without
+ * wait_limit_ns (1 us .. 2 s) instead of 2 s (in these two, without
  * a row computed key by key meanwhile). The kernels then flag
  * DREAMS_DATA_TIMEOUT, wait for the copies and MMAs they did issue, free
  * their tensor memory and exit; output rows they did not finish are left

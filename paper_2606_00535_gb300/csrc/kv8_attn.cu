@@ -394,10 +394,9 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
         }
       }
       soften<D, 4, H>(s, m, l, o);
-      float fv[H];
-#pragma unroll
-      for (int h = 0; h < H; ++h) fv[h] = power(v_exp(w));
-      if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {  // a row that sees none of the page stays as it is
+      const float fv = power(v_exp(w));
+      if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
+        // the rows that see some of the page become NaN; the others stay as they are, whatever the codes
 #pragma unroll
         for (int h = 0; h < H; ++h) {
           float any = 0.f;
@@ -405,8 +404,10 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           for (int n = 0; n < 4; ++n) any += s[n][2 * h] + s[n][2 * h + 1];
           any += __shfl_xor_sync(0xffffffffu, any, 1);
           any += __shfl_xor_sync(0xffffffffu, any, 2);
-          if (any == 0.f) fv[h] = 0.f;
+          if (any != 0.f) l[h] = fv;
         }
+        at = at + 1 == C::STAGES ? 0 : at + 1;
+        continue;
       }
       uint32_t p0[4], p1[4];
 #pragma unroll
@@ -429,8 +430,8 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
         mma_f16(a1, p1, codes_to_f16x2(y[2] >> 16), codes_to_f16x2(y[3] >> 16));
 #pragma unroll
         for (int e = 0; e < 2 * H; ++e) {
-          o[n][e] = fmaf(a0[e], fv[e >> 1], o[n][e]);
-          o[n + 1][e] = fmaf(a1[e], fv[e >> 1], o[n + 1][e]);
+          o[n][e] = fmaf(a0[e], fv, o[n][e]);
+          o[n + 1][e] = fmaf(a1[e], fv, o[n + 1][e]);
         }
       }
       at = at + 1 == C::STAGES ? 0 : at + 1;

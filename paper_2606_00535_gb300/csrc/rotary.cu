@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeParams p) {
   for (int i = tid; i < p.NT * p.n; i += THREADS) {
     const int j = p.pairs.div(i), q = i - j * p.n;
     if (t0 + j >= n) break;
-    int pos = L + t0 + j;
+    int64_t pos = int64_t(L) + t0 + j;
     if (APPEND && p.parent != nullptr) pos = s_pos[j];
     if (p.positions != nullptr) {
       int ax = p.axis != nullptr ? p.axis[q] : 0;
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(const RopeParams p) {
       }
       pos = p.positions[(int64_t(ax) * p.B + b) * p.T + t0 + j];
     }
-    const uint64_t turns = p.phase[q] * uint64_t(int64_t(pos));
+    const uint64_t turns = p.phase[q] * uint64_t(pos);
     float sn, cs;
     sincospif(float(int32_t(turns >> 32)) * 0x1p-31f, &sn, &cs);
     const int at = q / V, e = q % V;

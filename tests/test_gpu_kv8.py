@@ -365,6 +365,27 @@ def test_pages_that_were_not_finite(dreams, T, j):
     c.check(c.run(dreams), nan=lambda b, t: b == 0 and 300 + t - last < window)
 
 
+@pytest.mark.parametrize("T", [1, 4, 9, 70])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("j", [0, 1])
+def test_what_was_not_finite_before(dreams, T, bad, j):
+    """The same through kv_quantize, whose codes of such values stand for nothing."""
+    window = 2 ** 31 - 1 if T == 1 else 100
+    c = Case(T, 8, 2, 128, [300, 300], [T, T], [256, 256], window)
+    z, bf = int(c.table8[0, 3]), torch.randn((1, 1, 64, 2, 128)).to(torch.bfloat16)
+    k, v = bf.clone(), bf.clone()
+    (k, v)[j][0, 0, 60] = bad
+    one = torch.full((1, 4), -1, dtype=torch.int32, device="cuda")
+    one[0, 3] = 0
+    kv8 = dreams.KV8Cache(codes8((1, 1, 64, 2, 128)), codes8((1, 1, 64, 2, 128)), torch.zeros((1, 1, 2, 2), dtype=torch.int16, device="cuda"), one)
+    assert dreams.kv_quantize(dreams.KVCache(k.cuda(), v.cuda(), one), kv8, i32([192]), i32([256])).tolist() == [256]
+    c.k8[:, z], c.v8[:, z], c.exps[:, z] = kv8.k[:, 0].view(torch.uint8).cpu(), kv8.v[:, 0].view(torch.uint8).cpu(), kv8.exps[:, 0].cpu()
+    assert (c.exps[0, z, :, j] == R.NOT_FINITE).all() and (c.exps[0, z, :, 1 - j] < 0).all()
+    for x, y, e in ((c.vals[0], c.k8, c.exps[:, :, :, 0]), (c.vals[1], c.v8, c.exps[:, :, :, 1])):
+        x[0, 0, 192:256] = R.decode(y[0, z].numpy(), e[0, z].numpy()[None, :, None])
+    c.check(c.run(dreams), nan=lambda b, t: b == 0 and 300 + t - 255 < window)
+
+
 @pytest.mark.parametrize("T", [1, 40])
 def test_missing_pages_read_as_zeros(dreams, T):
     for table, e in (("table8", 1), ("table8", 3), ("table", 4), ("table", 5)):
@@ -379,7 +400,7 @@ def test_missing_pages_read_as_zeros(dreams, T):
 def test_bad_data(dreams, T):
     """Bad sequences are flagged and left untouched, the others computed."""
     for kw, want in ((dict(len8=[32, 128]), dreams.DATA_BAD_KV_LEN), (dict(len8=[-64, 128]), dreams.DATA_BAD_KV_LEN), (dict(len8=[320, 128]), dreams.DATA_BAD_KV_LEN),
-                     (dict(kv_len=[-1, 130]), dreams.DATA_BAD_KV_LEN), (dict(kv_len=[10 ** 6, 130]), dreams.DATA_BAD_KV_LEN),
+                     (dict(kv_len=[-1, 130]), dreams.DATA_BAD_KV_LEN), (dict(len8=[2 ** 31 - 64, 128]), dreams.DATA_BAD_KV_LEN), (dict(kv_len=[10 ** 6, 130]), dreams.DATA_BAD_KV_LEN),
                      (dict(q_len=[-1, T]), dreams.DATA_BAD_TREE_LEN), (dict(q_len=[T + 1, T]), dreams.DATA_BAD_TREE_LEN)):
         c = Case(T, 8, 2, 128, [300, 130], [T, T], [256, 128])
         for k, v in kw.items():

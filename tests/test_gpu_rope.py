@@ -79,8 +79,9 @@ def test_far_and_negative_positions(dreams):
     pos = [0, 1, -1, 10 ** 6, -10 ** 6, 2 ** 31 - 1, -2 ** 31, 123456789]
     x = torch.randn((1, len(pos), 2, 64), device="cuda")
     check(dreams.rope(x, r, positions=i32([pos]))[0], x[0], phases_of(r), pos, "half")
-    # starts that carry past 2^31 go on from -2^31, as 32-bit positions do
     assert torch.equal(dreams.rope(x, r, start=i32([7])), dreams.rope(x, r, positions=i32([[7 + t for t in range(len(pos))]])))
+    for start in (2 ** 31 - 3, -2 ** 31, -4):  # (tokens past 2^31 go on from it)
+        check(dreams.rope(x, r, start=i32([start]))[0], x[0], phases_of(r), [start + t for t in range(len(pos))], "half")
 
 
 def test_axes(dreams):
