@@ -110,6 +110,8 @@ struct TcParams {
 struct Tc8Params : TcParams {
   CUtensorMap tmap_k8, tmap_v8;
   Kv8 c;
+  Divisor seqs;    // B
+  int32_t ranked;  // pairs: those with the most tiles first
 };
 template <bool EIGHT>
 using ParamsOf = std::conditional_t<EIGHT, Tc8Params, TcParams>;
@@ -169,12 +171,8 @@ __device__ __forceinline__ Lens lens_of(const ParamsOf<EIGHT> &P, int b) {
 }
 
 template <bool PAIR, bool EIGHT>
-__device__ __forceinline__ void load_item(const ParamsOf<EIGHT> &P, int x, Item &it, bool report, const Lens *lens = nullptr) {
+__device__ __forceinline__ void load_item(const ParamsOf<EIGHT> &P, int blk, Item &it, bool report, const Lens *lens) {
   const WinParams &p = P.p;
-  // the last blocks first (they have the most keys), all heads of a block together
-  const int turn = P.heads.div(x), blk = P.nblk - 1 - turn, bg = x - turn * int(P.heads.d);
-  it.b = P.hkv.div(bg);
-  it.g = bg - it.b * p.Hkv;
   const Lens l = lens != nullptr ? *lens : lens_of<EIGHT>(P, it.b);
   it.T = l.T;
   it.L = l.L;
@@ -212,6 +210,34 @@ __device__ __forceinline__ void load_item(const ParamsOf<EIGHT> &P, int x, Item 
   const int lo1 = ::max(0, it.L + (tree ? 0 : it.t01) - p.window + 1);
   it.a1 = one_run ? 0 : ::max(it.ns, (it.nsp + (lo1 - it.lo64) / 64) / 2);
   it.e0 = (it.nsp + (it.L + it.tl0 - it.lo64) / 64) / 2 + 1;
+}
+
+// EIGHT: the pairs of blocks of all sequences in order of their tiles, most first.
+constexpr int MAX_RANKED = 256;
+__device__ __forceinline__ void rank_items(const Tc8Params &P, int *tiles, uint8_t *order) {
+  const int i = threadIdx.x, n = P.nblk * P.p.B;
+  int mine = -1;
+  if (i < n) {
+    Item it;
+    const int turn = P.seqs.div(i);
+    it.b = i - turn * P.p.B;
+    it.g = 0;
+    load_item<true, true>(P, P.nblk - 1 - turn, it, false, nullptr);
+    mine = it.nb > 0 ? it.n : 0;
+  }
+  if (i < MAX_RANKED) tiles[i] = mine;
+  tc::fence_proxy_async_smem();  // (copies will land there)
+  __syncthreads();
+  if (i < n) {
+    int before = 0;
+#pragma unroll 4
+    for (int k = 0; 4 * k < n; ++k) {
+      const int4 x = reinterpret_cast<const int4 *>(tiles)[k];
+      before += int(x.x > mine || (x.x == mine && 4 * k < i)) + int(x.y > mine || (x.y == mine && 4 * k + 1 < i)) +
+                int(x.z > mine || (x.z == mine && 4 * k + 2 < i)) + int(x.w > mine || (x.w == mine && 4 * k + 3 < i));
+    }
+    order[before] = uint8_t(i);
+  }
 }
 
 // An arrival by the threads for which `yes` holds, without a branch.
@@ -517,6 +543,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
   __shared__ int64_t s_beat;
+  __shared__ uint8_t s_order[EIGHT && PAIR ? MAX_RANKED : 1];
   __shared__ int8_t s_par[8][64];
   __shared__ Slot s_slot[8];
   __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
@@ -572,11 +599,29 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     tc::tmem_alloc(smem_u32(&s_tmem), TMEM_COLS);
     tc::tmem_relinquish();
   }
+  if constexpr (EIGHT && PAIR) {
+    if (P.ranked) rank_items(P, reinterpret_cast<int *>(smem + C::NQ * C::Q_BYTES), s_order);
+  }
+  // (block, sequence) and KV head of item x
+  auto place = [&](int x, int &turn, int &b, int &g) {
+    if constexpr (EIGHT && PAIR) {
+      const int e = P.hkv.div(x), i = P.ranked ? s_order[e] : e;
+      turn = P.seqs.div(i);
+      b = i - turn * p.B;
+      g = x - e * p.Hkv;
+    } else {
+      turn = P.heads.div(x);
+      const int bg = x - turn * int(P.heads.d);
+      b = P.hkv.div(bg);
+      g = bg - b * p.Hkv;
+    }
+  };
   // Without PAIR the item is known: its lengths and parents are on their way early.
   Lens lens{0, 0, 0};
   int early[2] = {-1, -1};
   if constexpr (!PAIR) {
-    const int x = P.nsplit.div(int(blockIdx.x)), b = P.hkv.div(x - P.heads.div(x) * int(P.heads.d));
+    int turn, b, g;
+    place(P.nsplit.div(int(blockIdx.x)), turn, b, g);
     lens = lens_of<EIGHT>(P, b);
     if (p.parent != nullptr && warp < 8) {
 #pragma unroll
@@ -604,8 +649,18 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   // the next item with work, and the tiles [j0, j1) of it that are this CTA's
   auto next_item = [&](Item &it, int &j0, int &j1, bool report) {
     while (x_next < P.items) {
-      load_item<PAIR, EIGHT>(P, x_next, it, report, PAIR ? nullptr : &lens);
-      x_next += PAIR ? int(gridDim.x) : P.items;
+      // the last blocks first (they have the most keys), all heads of a block together
+      int turn;
+      place(x_next, turn, it.b, it.g);
+      load_item<PAIR, EIGHT>(P, P.nblk - 1 - turn, it, report, PAIR ? nullptr : &lens);
+      if constexpr (EIGHT && PAIR) {
+        // CTAs take items in order, then in reverse, and so on: who had the longest of a
+        // round has the shortest of the next
+        const int n = gridDim.x, of = x_next / n + 1;
+        x_next = of * n + ((of & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+      } else {
+        x_next += PAIR ? int(gridDim.x) : P.items;
+      }
       if (PAIR) {
         j0 = 0;
         j1 = it.n;
@@ -1249,7 +1304,9 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     // ---------------- join the slots' and the splits' parts
     x_next = P.nsplit.div(int(blockIdx.x));
     Item it;
-    load_item<PAIR, EIGHT>(P, x_next, it, false, &lens);
+    int turn;
+    place(x_next, turn, it.b, it.g);
+    load_item<PAIR, EIGHT>(P, P.nblk - 1 - turn, it, false, &lens);
     const Splits splits(it.n, P.nsplit);
     const int m = splits.first(split + 1) - splits.first(split);
     const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
@@ -1511,6 +1568,10 @@ dreams_status_t launch_blocks(ParamsOf<EIGHT> &P, int D, cudaStream_t stream) {
   P.hkv = Divisor::of(p.Hkv);
   P.nsplit = Divisor::of(P.p.nsplit);
   P.g = Divisor::of(p.G);
+  if constexpr (EIGHT) {
+    P.seqs = Divisor::of(p.B);
+    P.ranked = pair && items > sms && P.nblk * p.B <= MAX_RANKED;
+  }
   if (D == 128) return pair ? launch<128, true, EIGHT>(P, stream) : launch<128, false, EIGHT>(P, stream);
   return pair ? launch<64, true, EIGHT>(P, stream) : launch<64, false, EIGHT>(P, stream);
 }
