@@ -26,6 +26,9 @@
 //          loaded once for 256 rows. The CTAs are persistent: they walk over the
 //          items with a ring of K/V stages that runs on across them, so the next
 //          item's loads and first Q K^T overlap the epilogue of the last.
+//   CLUSTER  pairs over 8-bit pages, on clusters of two CTAs: pair A, one of the longest, is cut
+//          so that the first CTA's part of it is as long as the second's and pair B, one
+//          of the shortest, together; A's parts are joined through distributed shared memory.
 //   !PAIR  both slots work on one block, alternate tiles; a block's tiles may be
 //          split over a cluster of CTAs, joined through distributed shared memory.
 //          For grids too small to fill the SMs with pairs.
@@ -111,7 +114,8 @@ struct Tc8Params : TcParams {
   CUtensorMap tmap_k8, tmap_v8;
   Kv8 c;
   Divisor seqs;    // B
-  int32_t ranked;  // pairs: those with the most tiles first
+  int32_t ranked;    // pairs: those with the most tiles first
+  int32_t clusters;  // CLUSTER: that run at once
 };
 template <bool EIGHT>
 using ParamsOf = std::conditional_t<EIGHT, Tc8Params, TcParams>;
@@ -214,7 +218,8 @@ __device__ __forceinline__ void load_item(const ParamsOf<EIGHT> &P, int blk, Ite
 
 // EIGHT: the pairs of blocks of all sequences in order of their tiles, most first.
 constexpr int MAX_RANKED = 256;
-__device__ __forceinline__ void rank_items(const Tc8Params &P, int *tiles, uint8_t *order) {
+constexpr int CHANGE = 2, LEAST = 4;  // CLUSTER: what a change of items costs, and the least part that a join is worth, in tiles
+__device__ __forceinline__ void rank_items(const Tc8Params &P, int *tiles, uint8_t *order) {  // tiles: of entry i, for what follows too
   const int i = threadIdx.x, n = P.nblk * P.p.B;
   int mine = -1;
   if (i < n) {
@@ -305,6 +310,13 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
   float2 v;
   asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void st_cluster2(uint32_t addr, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
+}
+__device__ __forceinline__ void st_cluster4(uint32_t addr, const uint32_t *v) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 // tcgen05.mma of kind::f16 with the descriptors' low words in registers: the high
 // word (stride offset 1024 bytes, 128-byte swizzle) is the same for every operand.
@@ -528,7 +540,7 @@ __device__ __noinline__ bool overflowed(uint32_t o_at) {
   return odd != 0u;
 }
 
-template <int D, bool PAIR, bool EIGHT>
+template <int D, bool PAIR, bool EIGHT, bool CLUSTER>
 __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_kernel(const __grid_constant__ ParamsOf<EIGHT> P) {
   using C = Cfg<D, PAIR, EIGHT>;
   using Pos = Place<C::NST>;
@@ -544,6 +556,8 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   __shared__ int s_abort, s_zero, s_dirty[SEEN];
   __shared__ int64_t s_beat;
   __shared__ uint8_t s_order[EIGHT && PAIR ? MAX_RANKED : 1];
+  __shared__ int s_first, s_cut;  // CLUSTER: does this CTA have tiles of B; where A is cut, 0: not
+  __shared__ uint32_t s_other;    // of the other CTA, 1: gave up, 2: done again row by row
   __shared__ int8_t s_par[8][64];
   __shared__ Slot s_slot[8];
   __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
@@ -600,7 +614,20 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     tc::tmem_relinquish();
   }
   if constexpr (EIGHT && PAIR) {
-    if (P.ranked) rank_items(P, reinterpret_cast<int *>(smem + C::NQ * C::Q_BYTES), s_order);
+    if (P.ranked) {
+      int *tiles = reinterpret_cast<int *>(smem + C::NQ * C::Q_BYTES);
+      rank_items(P, tiles, s_order);
+      if constexpr (CLUSTER) {
+        __syncthreads();
+        if (tid == 0) {
+          const int n = gridDim.x >> 1, a = blockIdx.x >> 1, b = 2 * n - 1 - a;
+          const int na = tiles[s_order[P.hkv.div(a)]], nb = b < P.items ? tiles[s_order[P.hkv.div(b)]] : 0;
+          const int cut = (na + nb + (nb > 0 ? CHANGE : 0) + 1) / 2;
+          s_cut = na - cut >= LEAST ? cut : 0;
+          s_first = nb;
+        }
+      }
+    }
   }
   // (block, sequence) and KV head of item x
   auto place = [&](int x, int &turn, int &b, int &g) {
@@ -644,36 +671,54 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
 
   // The items of this CTA; without PAIR it has one, shared by a cluster.
   const int nsplit = PAIR ? 1 : p.nsplit;
-  int x_next = PAIR ? int(blockIdx.x) : P.nsplit.div(int(blockIdx.x));
-  const int split = PAIR ? 0 : int(blockIdx.x) - x_next * nsplit;
+  int x_next = CLUSTER ? int(blockIdx.x & 1) ^ 1 : PAIR ? int(blockIdx.x) : P.nsplit.div(int(blockIdx.x));
+  const int split = CLUSTER ? int(blockIdx.x & 1) : PAIR ? 0 : int(blockIdx.x) - x_next * nsplit;
   // the next item with work, and the tiles [j0, j1) of it that are this CTA's
   auto next_item = [&](Item &it, int &j0, int &j1, bool report) {
-    while (x_next < P.items) {
-      // the last blocks first (they have the most keys), all heads of a block together
-      int turn;
-      place(x_next, turn, it.b, it.g);
-      load_item<PAIR, EIGHT>(P, P.nblk - 1 - turn, it, report, PAIR ? nullptr : &lens);
-      if constexpr (EIGHT && PAIR) {
-        // CTAs take items in order, then in reverse, and so on: who had the longest of a
-        // round has the shortest of the next
-        const int n = gridDim.x, of = x_next / n + 1;
-        x_next = of * n + ((of & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
-      } else {
-        x_next += PAIR ? int(gridDim.x) : P.items;
+    if constexpr (CLUSTER) {  // x_next: 0 B, 1 A, 2 nothing
+      while (x_next < 2) {
+        const int n = gridDim.x >> 1, a = blockIdx.x >> 1, x = x_next == 1 ? a : 2 * n - 1 - a;
+        const bool second = x_next++ == 1 && split == 1;
+        if (x >= P.items || (second && s_cut == 0)) continue;
+        int turn;
+        place(x, turn, it.b, it.g);
+        load_item<PAIR, EIGHT>(P, P.nblk - 1 - turn, it, report && !second, nullptr);
+        j0 = second ? s_cut : 0;
+        j1 = x == a && !second && s_cut > 0 ? s_cut : it.n;
+        if (it.nb > 0 && j0 < j1) return true;
       }
-      if (PAIR) {
-        j0 = 0;
-        j1 = it.n;
-      } else {
-        const Splits parts(it.n, P.nsplit);
-        j0 = parts.first(split);
-        j1 = parts.first(split + 1);
+    } else {
+      while (x_next < P.items) {
+        // the last blocks first (they have the most keys), all heads of a block together
+        int turn;
+        place(x_next, turn, it.b, it.g);
+        load_item<PAIR, EIGHT>(P, P.nblk - 1 - turn, it, report, PAIR ? nullptr : &lens);
+        if constexpr (EIGHT && PAIR) {
+          // CTAs take items in order, then in reverse, and so on: who had the longest of a
+          // round has the shortest of the next
+          const int n = gridDim.x, of = x_next / n + 1;
+          x_next = of * n + ((of & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+        } else {
+          x_next += PAIR ? int(gridDim.x) : P.items;
+        }
+        if (PAIR) {
+          j0 = 0;
+          j1 = it.n;
+        } else {
+          const Splits parts(it.n, P.nsplit);
+          j0 = parts.first(split);
+          j1 = parts.first(split + 1);
+        }
+        if (it.nb > 0 && j0 < j1) return true;
       }
-      if (it.nb > 0 && j0 < j1) return true;
     }
     return false;
   };
 
+  // CLUSTER: this thread's row at the item's end
+  Row kept{-1, 0ull};
+  int kept_t = 0;
+  float2 kept_ml = make_float2(-INFINITY, 0.f);
   if (warp < 8) {
     // ---------------- softmax warpgroup w: the rows of slot w
     // What an item is lies in shared memory, one copy per warp, and is read where
@@ -691,6 +736,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
       int j, jend, gap, to;  // tiles j .. jend-1 but for [gap, to), which only the other slot reads
       int wfrom, wto;        // tiles that all rows see whole
       bool live;             // does this warp have rows?
+      bool whole = true;     // are all of the item's tiles this CTA's?
       int ahead;             // stages from here to the next item
       {
         Item it;
@@ -705,15 +751,21 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
         wto = wh.to;
         j = j0;
         jend = j1;
+        if (CLUSTER) whole = j1 - j0 == it.n;
         gap = to = INT_MAX;
         if (PAIR) {
           if (!here) jend = j;
-          else if (w == 0) jend = it.e0;
+          else if (w == 0) jend = CLUSTER ? ::min(j1, it.e0) : it.e0;
           else if (it.a1 > it.ns) {
             gap = it.ns;
             to = it.a1;
           }
-          if (here && j >= gap) j = to;
+          if (CLUSTER) {
+            to = ::min(to, j1);
+            if (here && j >= gap) j = ::max(j, to);
+          } else if (here && j >= gap) {
+            j = to;
+          }
         } else {
           j = ::min(j1, j0 + w);
         }
@@ -740,7 +792,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
             bad |= i == 0 ? q != -1 : (q < 0 || q >= i);
           }
           bad = __any_sync(0xffffffffu, bad);
-          if (bad && lead && w == 0 && it.g == 0 && split == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
+          if (bad && lead && w == 0 && it.g == 0 && (CLUSTER ? j0 : split) == 0) flag(p.status, DREAMS_DATA_BAD_PARENT);
         }
         if (lane == 0) sp->bad = bad;
         __syncwarp();
@@ -894,7 +946,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
         if (!PAIR) pos = pos.plus(2);
         else if (nj != j + 1) {
           pos.move(2 * (nj - j - 1));
-          if (!C::BESIDE) v1 = -1;  // (before a gap the issuer's commit gives V back)
+          if (!C::BESIDE && (!CLUSTER || nj < jend)) v1 = -1;  // (before a gap the issuer's commit gives V back)
         }
         ahead -= 2 * (nj - j);
         j = nj;
@@ -912,7 +964,11 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
       ++seq;
 
       const bool real = row < sp->rows, tree_ok = sp->bad == 0;
-      if constexpr (PAIR) {
+      if (CLUSTER && !whole) {
+        kept = Row{tree_ok ? r.off : -1, r.anc};
+        kept_t = t;
+        if (any && live) kept_ml = make_float2(m_ref, l);
+      } else if constexpr (PAIR) {
         const int h = sp->g * p.G + row - (t - sp->t0) * p.G;
         uint32_t again = __ballot_sync(0xffffffffu, any && real && (dirty || l > SAFE_SUM));
         if (__builtin_expect(again != 0u, 0)) {
@@ -974,7 +1030,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
         uint32_t nq[2] = {0, 0};
         Item it;
         int j0, j1;
-        while (ok && next_item(it, j0, j1, split == 0)) {
+        while (ok && next_item(it, j0, j1, CLUSTER || split == 0)) {
           const int32_t *row = p.table != nullptr ? p.table + int64_t(it.b) * p.P : nullptr;
           auto fetch = [&](int j, int h) {
             if (j >= j1 || 2 * j + h >= it.np) return 0;
@@ -1107,8 +1163,9 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
           auto next_of = [&](int j) {
             int k = j + (PAIR ? 1 : 2);
             if (!PAIR) return ::min(j1, k);
-            if (w == 0) return k < it.e0 ? k : j1;
-            return k >= it.ns ? ::max(k, it.a1) : k;
+            if (w == 0) return k < (CLUSTER ? ::min(j1, it.e0) : it.e0) ? k : j1;
+            const int to = k >= it.ns ? ::max(k, it.a1) : k;
+            return CLUSTER ? ::min(j1, to) : to;
           };
           // tiles [a, e) are the other slot's: this one gives them back unread
           Pos pos = at;  // K of the first tile not dealt with
@@ -1300,6 +1357,111 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
+  if constexpr (CLUSTER) {
+    // ---------------- join the two parts of A: CTA w finishes block w, whose other part is
+    // pushed into its ring once both are done with theirs
+    if (s_cut > 0) {
+      Item it;
+      int turn;
+      place(blockIdx.x >> 1, turn, it.b, it.g);
+      load_item<PAIR, EIGHT>(P, P.nblk - 1 - turn, it, false, nullptr);
+      constexpr int CH = D / 4;  // 16-byte columns of a part's row, swizzled by the row
+      float *part = reinterpret_cast<float *>(smem + C::NQ * C::Q_BYTES);
+      float2 *mls = reinterpret_cast<float2 *>(part + ROWS * D);
+      static_assert(size_t(NST) * C::STAGE >= ROWS * (D * 4 + sizeof(float2)), "a part fits");
+      const int w = (warp >> 2) & 1, row = 32 * (warp & 3) + lane;
+      const int rows = w < it.nb ? ((w ? it.tl1 : it.tl0) - (w ? it.t01 : it.t00) + 1) * p.G : 0;
+      const bool live = warp < 8 && 32 * (warp & 3) < rows, mine = w == split;
+      const bool dirty = s_dirty[split == 1 && s_first > 0 ? 1 : 0] != 0;
+      const uint32_t tl = tmem + (uint32_t(32 * (warp & 3)) << 16) + 256u * w + C::O_COL;
+      cluster_sync();
+      if (tid == 0) st_cluster(mapa(smem_u32(&s_other), split ^ 1), (s_abort ? 1u : 0u) | (dirty ? 2u : 0u));
+      if (live && !mine) {
+        st_cluster2(mapa(smem_u32(mls + row), split ^ 1), kept_ml);
+        if (__any_sync(0xffffffffu, kept_ml.y != 0.f)) {
+          const uint32_t to = mapa(smem_u32(part + row * D), split ^ 1);
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t ov[32];
+            tc::tmem_ld32(tl + c * 32, ov);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) st_cluster4(to + (((c * 8 + e) ^ (row & (CH - 1))) << 4), ov + 4 * e);
+          }
+        }
+      }
+      __syncwarp();
+      cluster_sync();
+      const uint32_t state = s_other | (s_abort ? 1u : 0u) | (dirty ? 2u : 0u);
+      if (live && mine && !(state & 1u)) {
+        const float2 own = kept_ml, far = mls[row];
+        const bool real = row < rows && kept.off >= 0;  // (not of a malformed tree)
+        const float M = fmaxf(own.x, far.x), c0 = own.y == 0.f ? 0.f : tc::ex2(own.x - M), c1 = far.y == 0.f ? 0.f : tc::ex2(far.x - M);
+        const float Z = c0 * own.y + c1 * far.y;
+        // columns 32 c .. 32 c + 31 of the row, both parts
+        auto both = [&](int c, float (&o)[32]) {
+          uint32_t ov[32];
+          tc::tmem_ld32(tl + c * 32, ov);
+          tc::tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float4 f = *reinterpret_cast<const float4 *>(part + row * D + (((c * 8 + e) ^ (row & (CH - 1))) << 2));
+            const float fv[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float a = own.y == 0.f ? 0.f : c0 * __uint_as_float(ov[4 * e + k]);  // (a part without keys may be anything)
+              o[4 * e + k] = far.y == 0.f ? a : a + c1 * fv[k];
+            }
+          }
+        };
+        const bool wild = own.y > SAFE_SUM || far.y > SAFE_SUM;
+        bool redo = (state & 2u) || own.y > MOST_SUM || far.y > MOST_SUM;
+        if (__builtin_expect(__any_sync(0xffffffffu, wild), 0)) {
+          float odd = 0.f;  // (a sum of 0 x O is zero, or NaN)
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            both(c, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) odd += 0.f * o[e];
+          }
+          redo = redo || (wild && odd != 0.f);
+        }
+        const uint32_t again = __ballot_sync(0xffffffffu, real && redo);
+        const int h = it.g * p.G + row - (kept_t - (w ? it.t01 : it.t00)) * p.G;
+        const int64_t orow = (int64_t(it.b) * p.T_max + kept_t) * p.Hq + h;
+        const bool write = real && !redo, wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
+        const float inv = 1.f / Z;
+        uint4 *dst = reinterpret_cast<uint4 *>(p.out + orow * D);
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float o[32];
+          both(c, o);
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) pk[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
+          if (write && wide) {
+            st_global_v8(dst + 4 * c, pk);
+            st_global_v8(dst + 4 * c + 2, pk + 8);
+          } else if (write) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dst[4 * c + e] = make_uint4(pk[4 * e], pk[4 * e + 1], pk[4 * e + 2], pk[4 * e + 3]);
+          }
+        }
+        if (write && p.lse != nullptr) p.lse[orow] = (M + log2f(Z)) * LN2;
+        if (__builtin_expect(again != 0u, 0)) {
+          for (int i = 0; i < 32; ++i) {
+            const int ti = __shfl_sync(0xffffffffu, kept_t, i), oi = __shfl_sync(0xffffffffu, kept.off, i), hi = __shfl_sync(0xffffffffu, h, i);
+            const unsigned long long ai = __shfl_sync(0xffffffffu, kept.anc, i);
+            if ((again >> i) & 1u) slow_row<D, EIGHT>(P, it.b, it.g, it.L, ti, hi, oi, ai, &s_beat);
+          }
+        }
+      }
+      tc::fence_before_sync();
+      __syncthreads();
+      tc::fence_after_sync();
+    }
+  }
   if constexpr (!PAIR) {
     // ---------------- join the slots' and the splits' parts
     x_next = P.nsplit.div(int(blockIdx.x));
@@ -1461,10 +1623,10 @@ bool code_map(CUtensorMap *m, const uint8_t *base, const WinParams &p, const Kv8
              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool PAIR, bool EIGHT>
+template <int D, bool PAIR, bool EIGHT, bool CLUSTER = false>
 dreams_status_t launch(ParamsOf<EIGHT> &P, cudaStream_t stream) {
   using C = Cfg<D, PAIR, EIGHT>;
-  const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR, EIGHT>);
+  const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR, EIGHT, CLUSTER>);
   const dreams_status_t st = ensure_max_dynamic_smem(kernel, int(C::SMEM));
   if (st != DREAMS_OK) return st;
   if (!kv_map(&P.tmap_k, P.p.k, P.p, D) || !kv_map(&P.tmap_v, P.p.v, P.p, D) || !q_map(&P.tmap_q, P.p, D, P.TB)) return DREAMS_ERR_UNSUPPORTED;
@@ -1472,7 +1634,8 @@ dreams_status_t launch(ParamsOf<EIGHT> &P, cudaStream_t stream) {
     if (!code_map(&P.tmap_k8, P.c.k, P.p, P.c, D) || !code_map(&P.tmap_v8, P.c.v, P.p, P.c, D)) return DREAMS_ERR_UNSUPPORTED;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(PAIR ? unsigned(std::min(P.items, num_sms())) : unsigned(P.items) * unsigned(P.p.nsplit));
+  if constexpr (CLUSTER) cfg.gridDim = dim3(2u * unsigned(std::min(P.items, P.clusters)));
+  else cfg.gridDim = dim3(PAIR ? unsigned(std::min(P.items, num_sms())) : unsigned(P.items) * unsigned(P.p.nsplit));
   cfg.blockDim = dim3(C::THREADS);
   cfg.dynamicSmemBytes = C::SMEM;
   cfg.stream = stream;
@@ -1481,7 +1644,7 @@ dreams_status_t launch(ParamsOf<EIGHT> &P, cudaStream_t stream) {
   attr[1].val.clusterDim.x = unsigned(P.p.nsplit);
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = !PAIR && P.p.nsplit > 1 ? 2 : 1;
+  cfg.numAttrs = P.p.nsplit > 1 ? 2 : 1;
   void *args[] = {&P};
   const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
   if (e != cudaSuccess) {
@@ -1493,15 +1656,15 @@ dreams_status_t launch(ParamsOf<EIGHT> &P, cudaStream_t stream) {
 
 // How many clusters of ns CTAs the current device runs at once (asked once per
 // device); 0: none, or not known.
-template <int D, bool EIGHT>
+template <int D, bool EIGHT, bool PAIR = false>
 int clusters_at_once(int ns) {
-  using C = Cfg<D, false, EIGHT>;
+  using C = Cfg<D, PAIR, EIGHT>;
   static std::atomic<int> known[64][9];  // count + 1
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 0;
   int n = known[dev][ns].load(std::memory_order_relaxed);
   if (n == 0) {
-    const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, false, EIGHT>);
+    const void *kernel = reinterpret_cast<const void *>(window_tc_kernel<D, PAIR, EIGHT, PAIR>);
     if (ensure_max_dynamic_smem(kernel, int(C::SMEM)) != DREAMS_OK) return 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ns));
@@ -1558,8 +1721,25 @@ dreams_status_t launch_blocks(ParamsOf<EIGHT> &P, int D, cudaStream_t stream) {
       nsplit = ns;
     }
   }
-  const bool pair = pair_cost <= best;
-  P.p.nsplit = pair ? 1 : nsplit;
+  bool pair = pair_cost <= best, cluster = false;
+  if constexpr (EIGHT) {
+    // Pairs of blocks on clusters of two CTAs. Up to a pair for each cluster that runs at
+    // once, each is cut in half: 12.5 us and 2.45 a tile of a CTA (head dim 64: 11.5 and 1.95).
+    // Above, where at least one SM in eight would have nothing to do and the lengths may
+    // differ, the halves of the longest have the shortest beside them. Against pairs or
+    // blocks as above, trees of 64 nodes, 8 KV heads, head dim 128, us:
+    //   pairs                  32          64         96         128        152
+    //   of 1500 to 6000   57.5 59.8  117.2 68.1  112.5 74.7  113.0 93.3  117.1 107.3
+    //   of 4000           44.8 47.9   85.4 52.2   80.7 86.4   80.9 88.5   88.1  93.5
+    //   of 2000 to 3000   34.3 38.6   65.5 42.2   61.9 56.3   62.4 69.6   65.7  75.6
+    // (At 128 and 152 all SMs run, and a tile takes 2.35 us where it takes 2.15 with 128.)
+    P.clusters = D == 128 ? clusters_at_once<128, true, true>(2) : clusters_at_once<64, true, true>(2);
+    const int64_t n = heads * pairs;
+    if (blocks > 1 && n <= P.clusters) cluster = 10 * (D == 128 ? 125 : 115) + (D == 128 ? 245 : 195) * cols / (2 * KT) < 10 * std::min(best, pair_cost);
+    else cluster = pair && p.B > 1 && n <= std::min<int64_t>(2 * P.clusters, sms - sms / 8);
+  }
+  pair = pair || cluster;
+  P.p.nsplit = cluster ? 2 : pair ? 1 : nsplit;
   P.nblk = int(pair ? pairs : blocks);
   const int64_t items = heads * P.nblk;
   if (items * P.p.nsplit > INT_MAX / 2) return DREAMS_ERR_UNSUPPORTED;
@@ -1570,7 +1750,8 @@ dreams_status_t launch_blocks(ParamsOf<EIGHT> &P, int D, cudaStream_t stream) {
   P.g = Divisor::of(p.G);
   if constexpr (EIGHT) {
     P.seqs = Divisor::of(p.B);
-    P.ranked = pair && items > sms && P.nblk * p.B <= MAX_RANKED;
+    P.ranked = cluster || (pair && items > sms && int64_t(P.nblk) * p.B <= MAX_RANKED);
+    if (cluster) return D == 128 ? launch<128, true, true, true>(P, stream) : launch<64, true, true, true>(P, stream);
   }
   if (D == 128) return pair ? launch<128, true, EIGHT>(P, stream) : launch<128, false, EIGHT>(P, stream);
   return pair ? launch<64, true, EIGHT>(P, stream) : launch<64, false, EIGHT>(P, stream);
