@@ -649,7 +649,8 @@ typedef struct dreams_kv8_cache {
  * there is none. begin[b] < 0 or no multiple of 64, end[b] < begin[b] or beyond either
  * cache flags BAD_KV_LEN, skips the sequence and gives new_len8 = begin. A page that is
  * missing in either cache is flagged BAD_PAGE and skipped; new_len8[b] then ends before
- * the first such page. Both caches have the same n_layers, Hkv and D. One launch.
+ * the first such page. Both caches have the same n_layers, Hkv and D. One launch. More than
+ * 2^23 - 1 pages to a sequence of kv8 are DREAMS_ERR_UNSUPPORTED.
  */
 dreams_status_t dreams_kv_quantize(const dreams_kv_cache_t *kv, const dreams_kv8_cache_t *kv8, int32_t B,
                                    const int32_t *begin, const int32_t *end, int32_t *new_len8, int32_t *status_word,

@@ -185,7 +185,8 @@ extern "C" dreams_status_t dreams_kv_quantize(const dreams_kv_cache_t *kv, const
       !aligned4(end) || !aligned4(new_len8) || new_len8 == begin || new_len8 == end || kv8->n_layers != kv->n_layers || kv8->Hkv != kv->Hkv ||
       kv8->D != kv->D)
     return DREAMS_ERR_INVALID_ARG;
-  if (kv->D != 64 && kv->D != 128) return DREAMS_ERR_UNSUPPORTED;
+  // (a block counts the pages of THREADS sequences in 32 bits)
+  if ((kv->D != 64 && kv->D != 128) || kv8->pages_per_seq > INT_MAX / THREADS) return DREAMS_ERR_UNSUPPORTED;
   QuantParams p{};
   p.c = c;
   p.k8 = static_cast<uint8_t *>(kv8->k);

@@ -7,10 +7,11 @@
 // rows 88.0 and 80.1; head dim 64, 48 rows 46.7 and 58.0, 64 rows 57.4 and 57.9. (One CTA
 // for both blocks of 32 rows, K and V read once: 59.5 against 55.0.)
 //
-// Few rows (single tokens, short drafts), bound by reading K and V once. As in window.cu, a CTA takes part of the keys of a sequence and KV head, its
-// warps take tiles in turn, each with its own ring of cp.async stages, scores and P V run
-// on m16n8k16 tensor instructions, and a cluster's CTAs join their parts in shared
-// memory. What differs is the tiles. Keys come in runs, the sinks and the window, each
+// Few rows (single tokens, short drafts), bound by reading K and V once. As in window.cu, a
+// CTA takes part of the keys of a sequence and KV head, its warps take tiles in turn, each
+// with its own ring of cp.async stages, scores and P V run on m16n8k16 tensor
+// instructions, and a cluster's CTAs join their parts in shared memory. What differs is
+// the tiles. Keys come in runs, the sinks and the window, each
 // of them first in 8 bits, then in bf16; a tile is 32 codes' or 16 bf16 keys, which take
 // the same bytes of a stage, lies in one page, and has one power of K and one of V.
 //   Scores of codes are e4m3 products (32 dimensions an instruction), Q being two codes:
@@ -28,8 +29,8 @@
 //   its sums change places once.
 // In bf16 tiles P is one bf16, or two with FOLD, as in window.cu.
 // Bound by HBM when the GPU is full: 38 sequences of 16384 tokens, 8 KV heads of 128
-// dimensions, 204 us, 94% of the copy rate (253 us with both operands made bf16 by integer
-// instructions, which kept the ALU busy 47% of the time). 64 of 1500 to 32768, 382 us, 89%.
+// dimensions, 206 us, 93% of the copy rate (253 us with both operands made bf16 by integer
+// instructions, which kept the ALU busy 47% of the time). 64 of 1500 to 32768, 351 us, 97%.
 #include <limits.h>
 #include <math.h>
 
@@ -672,15 +673,16 @@ __global__ void __launch_bounds__(32 * WARPS, Cfg8<D, FOLD>::PER_SM == 4 ? 4 : 0
 // Where not all CTAs run at the same time, the longest sequences go first. Measured on
 // the GPU for 8 KV heads, head dim 128, lengths spread from a to b, in us; (r): longest first
 //   lists          8      16       64       64        128        256          512     1024
-//   lengths     8000  -8000    -4000   -32768     -32768     -32768       -32768    -8192
-//   1 CTA       75.0   74.1     40.2    288.9      289.4   (r)334.4     (r)382.1 (r)203.9
-//   2           43.0   42.4     24.6    150.5      177.6   (r)197.2     (r)382.1 (r)236.7
-//   4           25.5   24.9     17.4     96.1   (r)107.7   (r)207.2     (r)410.0 (r)300.6
-//   8           15.8   16.0  (r)20.0  (r)63.2   (r)123.1   (r)245.3     (r)491.5 (r)434.9
-//   16          13.2   17.5     42.0     96.3      189.5      380.1        763.5    823.5
-// (512 lists as they come: 574.5 with one CTA each, 440.0 with four.) The ranks cost every
-// CTA a pass over the lengths and B comparisons for each of them: with 256 sequences of
-// equal length 132.0 us against 128.0, of lengths up to 4000 239.7 against 227.0.
+//   lengths     8000   1000-     300-    1500-      1500-      1500-        1500-     500-
+//                       8000     4000    32768      32768      32768        32768     8192
+//   1 CTA       72.4   72.1     39.3    283.2      281.6   (r)347.3     (r)351.6 (r)201.8
+//   2           40.9   40.9     23.7    145.7   (r)170.4   (r)185.4     (r)367.1 (r)229.7
+//   4           23.9   23.9     16.7     91.7   (r)103.9   (r)202.7     (r)392.7 (r)284.9
+//   8           14.6   15.1  (r)19.0  (r)61.6   (r)119.4   (r)236.7     (r)460.3 (r)406.4
+//   16          11.8   16.4  (r)40.7  (r)92.5   (r)181.2   (r)360.6     (r)707.2 (r)791.0
+// The price: lists of equal length that a split makes more than fit (19 sequences of 16384:
+// 147 us for 108). The ranks cost every CTA a pass over the lengths and B comparisons for
+// each of them, nothing where the lengths are alike: 128 sequences at most.
 constexpr int MAX_SPLIT = 16;
 int split_of(int64_t fit, int B, int64_t lists, int64_t keys) {
   int n = 1;

@@ -38,6 +38,15 @@
 // slot's MMAs complete in order, so the commit that announces S of a tile also says
 // that the P V before it is done: the softmax warpgroup then gives those stages back,
 // and no further commits are needed.
+//   EIGHT  pages below a sequence's len8 come as codes, and four warps more, 12-15, turn
+//          them into bf16 between the copy and everything else (a code times its page's
+//          power of two is exact in bf16). They take about 1200 clocks of a tile of 4400 and
+//          slow the softmax, whose schedulers they share, from 2000 to 2500 (head dim 64: 2500
+//          to 3200): the bytes are half, and the time 10 to 15% above that of the
+//          same pairs in bf16. Work is laid out anew instead: pairs in order of their tiles,
+//          or cut between two CTAs (CLUSTER). 16 trees of up to 64 nodes on 1500 to 6000 tokens,
+//          32/8 heads: 93 us (as in bf16, one pair a CTA: 112); four chunks of 701 to 999
+//          tokens on as many, head dim 64: 213 us (pairs as they come: 255).
 // Bound by the chain of a tile (products, softmax, products), of which two run on an
 // SM: about 4000 clocks for both slots, where the products take 2048, with head dim 128
 // (1.93 us a tile of a pair at 2070 MHz, from windows of 2048 to 8192); 2900 with head
@@ -218,7 +227,11 @@ __device__ __forceinline__ void load_item(const ParamsOf<EIGHT> &P, int blk, Ite
 
 // EIGHT: the pairs of blocks of all sequences in order of their tiles, most first.
 constexpr int MAX_RANKED = 256;
-constexpr int CHANGE = 2, LEAST = 4;  // CLUSTER: what a change of items costs, and the least part that a join is worth, in tiles
+// CLUSTER: what a change of items costs, and the least part that is worth a join, in tiles.
+// (The least 8: 12 trees on 300 to 1500 tokens 39.6 us, 30.8 with 4; 2: 16 on 2000 to 3000
+// 72.1, 69.9 with 4. A change 5: 16 on 1500 to 6000 98.6, 93.8 with 2; 0: 92.7, but head dim
+// 64 on 300 to 1500 35.4 for 33.9.)
+constexpr int CHANGE = 2, LEAST = 4;
 __device__ __forceinline__ void rank_items(const Tc8Params &P, int *tiles, uint8_t *order) {  // tiles: of entry i, for what follows too
   const int i = threadIdx.x, n = P.nblk * P.p.B;
   int mine = -1;

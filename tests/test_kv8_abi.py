@@ -84,6 +84,7 @@ def test_quantize_refusals(lib):
                dict(kv=cache(n_layers=3))] + [dict(kv8=cache8(**b)) for b in BAD_KV8]:
         assert call(**kw) == INV, kw
     assert call(kv=cache(D=96), kv8=cache8(D=96)) == UNS
+    assert call(kv8=cache8(pages_per_seq=1 << 23)) == UNS
 
 
 BAD_KV8 = [dict(k=None), dict(v=None), dict(exps=None), dict(k=P + 8), dict(v=P + 4), dict(exps=P + 2), dict(n_layers=0), dict(n_layers=1),
