@@ -1053,14 +1053,38 @@ class Rotary:
                    None if axis is None else torch.tensor(list(axis), dtype=torch.int32, device=device))
 
 
-def _positions(positions: Optional[torch.Tensor], B: int, T: int, dev) -> Tuple[Optional[int], int]:
+# The calls below run once a layer of a decode step, and there the host is what takes
+# longest: each attribute of a tensor is asked for once.
+def _rows(x: torch.Tensor, name: str, heads: str) -> Tuple[int, int, int, int, int, int]:
+    """B, T, H, D of a bf16 tensor with dense head rows, and its sequence and token strides."""
+    if not isinstance(x, torch.Tensor) or x.dtype is not torch.bfloat16 or x.dim() != 4:
+        raise TypeError(f"{name} must be a 4-D bfloat16 tensor [B, T, {heads}, D]")
+    B, T, H, D = x.shape
+    sb, st, sh, sd = x.stride()
+    if (sd != 1 and D > 1) or (sh != D and H > 1):
+        raise ValueError(f"{name}'s head rows must be dense (strides [.., .., D, 1])")
+    return B, T, H, D, sb, st if T > 1 else H * D
+
+
+def _given(t: torch.Tensor, name: str, dtype, dev, shape: Tuple[int, ...]) -> int:
+    """Address of a dense tensor of this type, device and shape."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+        return t.data_ptr()
+    _need(t, name, dtype, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _positions(positions: torch.Tensor, B: int, T: int, dev) -> Tuple[int, int]:
     """Address and axes of positions [B, T] or [n_axes, B, T]."""
-    if positions is None:
-        return None, 1
     _need(positions, "positions", torch.int32, dev)
-    if positions.dim() not in (2, 3) or tuple(positions.shape[-2:]) != (B, T):
+    s = positions.shape
+    if s == (B, T):
+        return positions.data_ptr(), 1
+    if len(s) != 3 or s[1] != B or s[2] != T:
         raise ValueError(f"positions must be [B, T] or [n_axes, B, T] with B = {B}, T = {T}")
-    return positions.data_ptr(), 1 if positions.dim() == 2 else int(positions.shape[0])
+    return positions.data_ptr(), s[0]
 
 
 def rope(x: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = None,
@@ -1071,9 +1095,9 @@ def rope(x: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = No
     ``start`` (int32 [B]) + t, or t. ``transpose``: by the transposed map, which is
     the gradient with respect to x of an output's (and with factor 1 the inverse).
     Returns ``out``, which may be ``x``."""
-    if not isinstance(x, torch.Tensor) or x.dtype not in _ROPE_TYPES or x.dim() != 4:
+    if not isinstance(x, torch.Tensor) or x.dim() != 4 or (dtype := x.dtype) not in _ROPE_TYPES:
         raise TypeError("x must be a 4-D bfloat16 or float32 tensor [B, T, H, D]")
-    dev, dtype = x.device, x.dtype
+    dev = x.device
     B, T, H, D = x.shape
     sb, stt, sh, sd = x.stride()
     if sd != 1 and D > 1:
@@ -1109,10 +1133,9 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
     Positions: ``positions`` (int32 [B, T_max] or [n_axes, B, T_max]); or
     ``parent`` (int32 [B, T_max]): kv_len + a tree node's depth; or kv_len + t."""
     dev = kv.k.device
-    kb, kt = _q_strides(k_new, "k_new", "Hkv")
-    vb, vt = _q_strides(v_new, "v_new", "Hkv")
-    B, T_max, Hkv, D = k_new.shape
-    if k_new.shape != v_new.shape or k_new.device != dev or v_new.device != dev:
+    B, T_max, Hkv, D, kb, kt = _rows(k_new, "k_new", "Hkv")
+    vB, vT, vH, vD, vb, vt = _rows(v_new, "v_new", "Hkv")
+    if vB != B or vT != T_max or vH != Hkv or vD != D or k_new.device != dev or v_new.device != dev:
         raise ValueError("k_new and v_new must share their shape and the cache's device")
     if Hkv != kv.Hkv:
         raise ValueError(f"k_new has {Hkv} heads, the cache {kv.Hkv}")
@@ -1127,26 +1150,22 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
     if parent is not None:
         if positions is not None:
             raise ValueError("give positions or parent, not both")
-        _need(parent, "parent", torch.int32, dev)
-        if tuple(parent.shape) != (B, T_max):
-            raise ValueError("parent must be [B, T_max]")
-        par = parent.data_ptr()
+        par = _given(parent, "parent", torch.int32, dev, (B, T_max))
     Hq = qb = qt = 0
+    to = None
     if q is not None:
-        qb, qt = _q_strides(q)
-        if q.device != dev or q.shape[:2] != k_new.shape[:2] or q.shape[3] != D:
+        qB, qT, Hq, qD, qb, qt = _rows(q, "q", "Hq")
+        if qB != B or qT != T_max or qD != D or q.device != dev:
             raise ValueError("q must be [B, T_max, Hq, D] on the cache's device, with k_new's B, T_max and D")
-        Hq = q.shape[2]
         if q_out is None:
             q_out = _new((B, T_max, Hq, D), torch.bfloat16, dev, stream)
+            to = q_out.data_ptr()
         else:
-            _need(q_out, "q_out", torch.bfloat16, dev)
-            if q_out.shape != q.shape:
-                raise ValueError("q_out must have q's shape")
+            to = _given(q_out, "q_out", torch.bfloat16, dev, (B, T_max, Hq, D))
     elif q_out is not None:
         raise ValueError("q_out goes with q")
     _launch("dreams_kv_append_rope", dev, stream, ctypes.byref(kv._c), layer, None if q is None else q.data_ptr(), qb, qt,
-            None if q_out is None else q_out.data_ptr(), Hq, k_new.data_ptr(), kb, kt, v_new.data_ptr(), vb, vt,
+            to, Hq, k_new.data_ptr(), kb, kt, v_new.data_ptr(), vb, vt,
             rotary._ref, pos, axes, par, kl, nn, B, T_max, None if status is None else _status(status, dev))
     return q_out
 
@@ -1154,7 +1173,7 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
 def _both_caches(kv8: KV8Cache, kv: KVCache, B: int) -> None:
     if kv8.k.device != kv.k.device:
         raise ValueError(f"the 8-bit cache is on {kv8.k.device}, the bf16 one on {kv.k.device}")
-    if (kv8.n_layers, kv8.Hkv, kv8.D) != (kv.n_layers, kv.Hkv, kv.D):
+    if kv8.n_layers != kv.n_layers or kv8.Hkv != kv.Hkv or kv8.D != kv.D:
         raise ValueError("the two caches must share their layers, heads and head dim")
     _cache_covers(kv, B)
     if kv8.B < B:
@@ -1173,8 +1192,11 @@ def kv_quantize(kv: KVCache, kv8: KV8Cache, begin: torch.Tensor, end: torch.Tens
     bg, en = _per_seq(begin, "begin", B, dev), _per_seq(end, "end", B, dev)
     if new_len8 is None:
         new_len8 = _new(B, torch.int32, dev, stream)
-    _launch("dreams_kv_quantize", dev, stream, ctypes.byref(kv._c), ctypes.byref(kv8._c8), B, bg, en,
-            _per_seq(new_len8, "new_len8", B, dev), _status(status, dev))
+        new = new_len8.data_ptr()
+    else:
+        new = _per_seq(new_len8, "new_len8", B, dev)
+    _launch("dreams_kv_quantize", dev, stream, ctypes.byref(kv._c), ctypes.byref(kv8._c8), B, bg, en, new,
+            None if status is None else _status(status, dev))
     return new_len8
 
 
@@ -1188,35 +1210,28 @@ def kv8_attention(q: torch.Tensor, kv8: KV8Cache, kv: KVCache, q_len: torch.Tens
     ``window`` every slot is seen. Returns (out, lse or None); rows past q_len are
     left untouched."""
     dev = q.device
-    sb, stt = _q_strides(q)
-    B, T_max, Hq, D = q.shape
-    ql, kl, l8 = (_per_seq(t, n, B, dev) for t, n in ((q_len, "q_len"), (kv_len, "kv_len"), (len8, "len8")))
+    B, T_max, Hq, D, sb, stt = _rows(q, "q", "Hq")
+    ql, kl, l8 = _per_seq(q_len, "q_len", B, dev), _per_seq(kv_len, "kv_len", B, dev), _per_seq(len8, "len8", B, dev)
     _cache_covers(kv, B, D)
     _both_caches(kv8, kv, B)
     if kv.k.device != dev:
         raise ValueError(f"the KV cache is on {kv.k.device}, q on {dev}")
-    par = None
-    if parent is not None:
-        _need(parent, "parent", torch.int32, dev)
-        if tuple(parent.shape) != (B, T_max):
-            raise ValueError("parent must be [B, T_max]")
-        par = parent.data_ptr()
+    par = None if parent is None else _given(parent, "parent", torch.int32, dev, (B, T_max))
     if out is None:
         out = _new((B, T_max, Hq, D), torch.bfloat16, dev, stream)
+        to = out.data_ptr()
     else:
-        _need(out, "out", torch.bfloat16, dev)
-        if out.shape != q.shape:
-            raise ValueError("out must have q's shape")
-    if lse is None:
-        if want_lse:
-            lse = _new((B, T_max, Hq), torch.float32, dev, stream)
+        to = _given(out, "out", torch.bfloat16, dev, (B, T_max, Hq, D))
+    if lse is not None:
+        to_lse = _given(lse, "lse", torch.float32, dev, (B, T_max, Hq))
+    elif want_lse:
+        lse = _new((B, T_max, Hq), torch.float32, dev, stream)
+        to_lse = lse.data_ptr()
     else:
-        _need(lse, "lse", torch.float32, dev)
-        if lse.shape != q.shape[:3]:
-            raise ValueError("lse must be [B, T_max, Hq]")
+        to_lse = None
     _launch("dreams_kv8_attention", dev, stream, q.data_ptr(), sb, stt, ctypes.byref(kv8._c8), ctypes.byref(kv._c),
             layer, par, ql, kl, l8, B, T_max, Hq, float(scale), 2 ** 31 - 1 if window is None else window, sinks,
-            out.data_ptr(), None if lse is None else lse.data_ptr(), _status(status, dev))
+            to, to_lse, None if status is None else _status(status, dev))
     return out, lse
 
 
