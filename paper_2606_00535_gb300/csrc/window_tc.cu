@@ -100,7 +100,9 @@ struct Cfg {
   // next Q K^T can start once the scores are in registers; with 128 P goes over S.
   static constexpr bool BESIDE = D == 64;
   static constexpr uint32_t P_COL = BESIDE ? 128 : 0, O_COL = BESIDE ? 192 : 128;
-  static constexpr int NST = D == 64 ? 8 : 5;
+  // (Six stages for single blocks over 8-bit pages, whose two slots hold four: 512 blocks on
+  // 1500 to 6000 tokens 279 us, 305 with five; one tree on 7808 47.2, 49.2.)
+  static constexpr int NST = D == 64 ? 8 : EIGHT && !PAIR ? 6 : 5;
   // EIGHT: where a stage's codes land, two pages HALF bytes apart. With head dim 128 a row's
   // lie in the stage itself, where its first 64 dimensions come to lie, so that a warp
   // writes over its own rows' alone; with 64 there is room beside it.
@@ -573,8 +575,13 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
   __shared__ uint32_t s_other;    // of the other CTA, 1: gave up, 2: done again row by row
   __shared__ int8_t s_par[8][64];
   __shared__ Slot s_slot[8];
-  __shared__ float2 s_ml[2][ROWS];                                           // !PAIR: (m, l) of the slots' parts
-  __shared__ struct { int off, t; unsigned long long anc; } s_row[PAIR ? 1 : ROWS];
+  // !PAIR: (m, l) of the slots' parts, and what the rows are (EIGHT: where Q was, once all is done)
+  struct RowDesc {
+    int off, t;
+    unsigned long long anc;
+  };
+  __shared__ float2 s_ml[2][PAIR || EIGHT ? 1 : ROWS];
+  __shared__ RowDesc s_row[PAIR || EIGHT ? 1 : ROWS];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t base = smem_u32(smem);
@@ -728,7 +735,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     return false;
   };
 
-  // CLUSTER: this thread's row at the item's end
+  // CLUSTER, and EIGHT without PAIR: this thread's row at the item's end
   Row kept{-1, 0ull};
   int kept_t = 0;
   float2 kept_ml = make_float2(-INFINITY, 0.f);
@@ -1022,6 +1029,10 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
           }
         }
         tc::fence_before_sync();  // O may be overwritten once this warpgroup's next P has arrived
+      } else if constexpr (EIGHT) {
+        kept = Row{tree_ok ? r.off : -1, r.anc};
+        kept_t = t;
+        if (any && live) kept_ml = make_float2(m_ref, l);
       } else {
         // what the rows are, and the slot's (m, l), for the join below
         if (w == 0) {
@@ -1487,10 +1498,17 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     const int rows_blk = it.nb > 0 ? (it.tl0 - it.t00 + 1) * p.G : 0;
     constexpr int CH = D / 4;  // 16-byte columns of a part's row, swizzled by the row
     float *part = reinterpret_cast<float *>(smem + C::NQ * C::Q_BYTES);
+    auto *mls = EIGHT ? reinterpret_cast<float2(*)[ROWS]>(smem) : reinterpret_cast<float2(*)[ROWS]>(&s_ml[0][0]);
+    RowDesc *descs = EIGHT ? reinterpret_cast<RowDesc *>(smem + 2 * ROWS * sizeof(float2)) : s_row;
+    static_assert(!EIGHT || C::Q_BYTES >= ROWS * (2 * sizeof(float2) + sizeof(RowDesc)), "they fit");
     if (warp < 8) {
       const int w = warp >> 2, row = 32 * (warp & 3) + lane;
       const bool has = w < m && s_abort == 0;
-      if (!has) s_ml[w][row] = make_float2(-INFINITY, 0.f);
+      if (EIGHT) {
+        mls[w][row] = kept_ml;
+        if (w == 0) descs[row] = RowDesc{kept.off, kept_t, kept.anc};
+      }
+      if (!has) mls[w][row] = make_float2(-INFINITY, 0.f);
       if (has && 32 * (warp & 3) < rows_blk) {
         const uint32_t tl = tmem + (uint32_t(32 * (warp & 3)) << 16) + 256u * w;
 #pragma unroll 1
@@ -1510,7 +1528,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
     if (nsplit > 1) cluster_sync();
     else __syncthreads();
     const int parts = 2 * nsplit;
-    const uint32_t ml_a = smem_u32(&s_ml[0][0]), part_a = smem_u32(part), ab_a = smem_u32(&s_abort), dirty_a = smem_u32(&s_dirty[0]);
+    const uint32_t ml_a = smem_u32(mls), part_a = smem_u32(part), ab_a = smem_u32(&s_abort), dirty_a = smem_u32(&s_dirty[0]);
     // part i: slot i & 1 of CTA i >> 1
     int state = 0;  // 1: a CTA gave up, 2: done again row by row
     if (lane < nsplit) {
@@ -1531,11 +1549,11 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
       for (int row = split * WARPS + warp; row < rows_blk; row += joiners * WARPS) {
         const float2 ml = next;
         next = sums(row + joiners * WARPS);
-        const int off = s_row[row].off, t = s_row[row].t;
+        const int off = descs[row].off, t = descs[row].t;
         if (off < 0) continue;  // a malformed tree
         const int h = it.g * p.G + row - (t - it.t00) * p.G;
         if (again || __any_sync(0xffffffffu, ml.y > MOST_SUM)) {
-          slow_row<D, EIGHT>(P, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
+          slow_row<D, EIGHT>(P, it.b, it.g, it.L, t, h, off, descs[row].anc, &s_beat);
           continue;
         }
         const uint32_t some = __ballot_sync(0xffffffffu, ml.y != 0.f);
@@ -1572,7 +1590,7 @@ __global__ void __launch_bounds__(Cfg<D, PAIR, EIGHT>::THREADS, 1) window_tc_ker
           // (a sum of 0 x O is zero, or NaN)
           const float odd = 0.f * acc.x + 0.f * acc.y + 0.f * acc.z + 0.f * acc.w;
           if (__any_sync(0xffffffffu, odd != 0.f)) {  // (also where it is NaN)
-            slow_row<D, EIGHT>(P, it.b, it.g, it.L, t, h, off, s_row[row].anc, &s_beat);
+            slow_row<D, EIGHT>(P, it.b, it.g, it.L, t, h, off, descs[row].anc, &s_beat);
             continue;
           }
         }
