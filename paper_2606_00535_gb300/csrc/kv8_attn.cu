@@ -3,25 +3,31 @@
 // Many rows of a KV head go to window_tc.cu: more than 32, with head dim 64 more than 64.
 // Up to there they are blocks of 16 rows, each with a list of keys of its own, which the
 // second block finds in L2. 8 sequences of 1000 to 8000 tokens, 8 KV heads, in us, here and
-// there: 20 rows 53.4 and 79.0, 48 rows 72.2 and 80.2 (all of 4000 tokens: 86.0 and 46.1), 64
-// rows 88.0 and 80.1; head dim 64, 48 rows 46.7 and 58.0, 64 rows 57.4 and 57.9. (One CTA
-// for both blocks of 32 rows, K and V read once: 59.5 against 55.0.)
+// there (in brackets: all of 4000): 20 rows 43.2 and 65.9 (42.6 and 40.9), 48 rows 55.1 and
+// 67.4 (67.9 and 43.1), 64 rows 68.2 and 67.3; head dim 64, 48 rows 40.3 and 59.1 (49.2 and
+// 36.6), 64 rows 50.4 and 59.1, 80 rows 70.4 and 60.2. (One CTA for both blocks of 32 rows, K
+// and V read once: 59.5 against 55.0, before scores were f16 products.)
 //
 // Few rows (single tokens, short drafts), bound by reading K and V once. As in window.cu, a
 // CTA takes part of the keys of a sequence and KV head, its warps take tiles in turn, each
 // with its own ring of cp.async stages, scores and P V run on m16n8k16 tensor
 // instructions, and a cluster's CTAs join their parts in shared memory. What differs is
-// the tiles. Keys come in runs, the sinks and the window, each
-// of them first in 8 bits, then in bf16; a tile is 32 codes' or 16 bf16 keys, which take
-// the same bytes of a stage, lies in one page, and has one power of K and one of V.
-//   Scores of codes are e4m3 products (32 dimensions an instruction), Q being two codes:
-//   its value and 2^5 times what that leaves, which with at most 8 rows (FOLD) is the
-//   other half of the instruction's 16. Two codes hold bf16's eight bits whole down to
-//   2^-7 of a row's largest value, and anything to 2^-24 of it, so K is not converted.
-//   P V are f16 products: one instruction makes two codes of V f16, exactly, and P is
-//   f16, 11 bits of it, lifted by 2^14 so that it reaches 2^-38. The power of K goes into
-//   the scale of the scores; that of V, which f16 has no room for, scales each tile's own
-//   product as it joins the row's f32 sums.
+// the tiles. Keys come in runs, the sinks and the window, each of them first in 8 bits,
+// then in bf16; a tile is 32 codes' or 16 bf16 keys, which take the same bytes of a stage,
+// lies in one page, and has one power of K and one of V.
+//   Scores are f16 products, K's codes made f16 two by one instruction, exactly, and Q
+//   f16 times a power of two of its row, which holds bf16's eight bits whole down to 2^-24 of
+//   the row's largest value.
+//   With at most 8 rows (FOLD) they are e4m3 products (32 dimensions an instruction), Q
+//   being two codes: its value and 2^5 times what that leaves, the other half of the
+//   instruction's 16 rows. Two codes hold bf16's eight bits whole down to 2^-7 of a row's
+//   largest value, and anything to 2^-24 of it. An e4m3 product takes about as long as two of
+//   f16, 34 clocks, but half of those would be rows that there are not: 64 sequences of 1500 to
+//   32768 tokens 345 us with one token and e4m3 (f16: 362), 371 with four and f16 (e4m3: 481).
+//   P V are f16 products, V's codes made f16 likewise; P is f16, 11 bits of it, lifted by
+//   2^14 so that it reaches 2^-38. The power of K goes into the scale of the scores; that of
+//   V, which f16 has no room for, scales each tile's own product as it joins the row's f32
+//   sums.
 //   A 16-byte piece of ldmatrix holds dimensions 4 c .. 4 c + 3 for thread c of four
 //   where bf16 rows give 2 c, 2 c + 1; bf16 tiles read K eight bytes at a time to match
 //   Q's loads. P V's columns are dimensions 16 j + 2 r and 16 j + 2 r + 1 in two
@@ -29,8 +35,8 @@
 //   its sums change places once.
 // In bf16 tiles P is one bf16, or two with FOLD, as in window.cu.
 // Bound by HBM when the GPU is full: 38 sequences of 16384 tokens, 8 KV heads of 128
-// dimensions, 206 us, 93% of the copy rate (253 us with both operands made bf16 by integer
-// instructions, which kept the ALU busy 47% of the time). 64 of 1500 to 32768, 351 us, 97%.
+// dimensions, 204 us, 94% of the copy rate (253 us with both operands made bf16 by integer
+// instructions, which kept the ALU busy 47% of the time). 64 of 1500 to 32768, 345 us, 98%.
 #include <limits.h>
 #include <math.h>
 
@@ -102,13 +108,13 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, int byt
 }
 
 __device__ __forceinline__ void mma_codes(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -315,8 +321,9 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
   const int my8 = ::min(my, j0 + warp < tl.n8 ? (tl.n8 - j0 - warp + WARPS - 1) / WARPS : 0);
   int i = 0;
   if (my8 > 0) {
-    uint32_t qh[D / 32][4], ql[FOLD ? 1 : D / 32][4];  // FOLD: what is left is rows 8 .. 15 of qh
-    float rq[H];                                       // scale of a row's scores
+    // FOLD: codes, rows 8 .. 15 what is left; else f16
+    uint32_t qf[FOLD ? D / 32 : D / 16][4];
+    float rq[H];  // scale of a row's scores
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const __nv_bfloat16 *from = src(h);
@@ -334,16 +341,20 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
       const int ex = ::max(int(bits >> 7), 8);
       const float up = bits >= 0x7f80u ? 0.f : __uint_as_float(uint32_t(261 - ex) << 23);
       rq[h] = bits >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float(uint32_t(ex - 7) << 23) * p.scale_log2;
+      if constexpr (FOLD) {
 #pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk) {
-        uint32_t a0, a1, b0, b1;
-        split_q(w[2 * kk], up, a0, b0);
-        split_q(w[2 * kk + 1], up, a1, b1);
-        if (FOLD) {
-          qh[kk][0] = a0, qh[kk][1] = b0, qh[kk][2] = a1, qh[kk][3] = b1;
-        } else {
-          qh[kk][h] = a0, qh[kk][h + 2] = a1, ql[kk][h] = b0, ql[kk][h + 2] = b1;
+        for (int kk = 0; kk < D / 32; ++kk) {
+          split_q(w[2 * kk], up, qf[kk][0], qf[kk][1]);
+          split_q(w[2 * kk + 1], up, qf[kk][2], qf[kk][3]);
         }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t u = e == 0 ? w[kk].x : w[kk].y;
+            qf[kk][2 * e + h] = pack_f16x2(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up);
+          }
       }
     }
 #pragma unroll 1
@@ -354,16 +365,23 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
       const uint32_t w = s_exp[warp][at];
       float s[4][2 * H];
       {
-        float x[4][4] = {}, y[FOLD ? 1 : 4][4] = {};
+        float x[4][4] = {};
+        if constexpr (FOLD) {
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
-          uint32_t k0[4], k1[4];  // 8 keys each
-          ldsm4(st + (((2 * kk) ^ swz) << 4), k0);
-          ldsm4(st + (((2 * kk + 1) ^ swz) << 4), k1);
+          for (int kk = 0; kk < D / 32; ++kk) {
+            uint32_t k0[4], k1[4];  // 8 keys each
+            ldsm4(st + (((2 * kk) ^ swz) << 4), k0);
+            ldsm4(st + (((2 * kk + 1) ^ swz) << 4), k1);
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            mma_codes(x[n], qh[kk], k0[n], k1[n]);
-            if constexpr (!FOLD) mma_codes(y[n], ql[kk], k0[n], k1[n]);
+            for (int n = 0; n < 4; ++n) mma_codes(x[n], qf[kk], k0[n], k1[n]);
+          }
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            uint32_t k[4];  // 8 keys each
+            ldsm4(st + ((kk ^ swz) << 4), k);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) mma_f16(x[n], qf[kk], codes_to_f16x2(k[n]), codes_to_f16x2(k[n] >> 16));
           }
         }
         const float pk = power(k_exp(w));
@@ -376,7 +394,7 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               if constexpr (FOLD) s[n][e] = fmaf(x[n][2 + e], 0.03125f, x[n][e]) * f;
-              else s[n][2 * h + e] = fmaf(y[n][2 * h + e], 0.03125f, x[n][2 * h + e]) * f;
+              else s[n][2 * h + e] = x[n][2 * h + e] * f;
             }
         }
       }
