@@ -693,13 +693,13 @@ __global__ void __launch_bounds__(32 * WARPS, Cfg8<D, FOLD>::PER_SM == 4 ? 4 : 0
 //   lists          8      16       64       64        128        256          512     1024
 //   lengths     8000   1000-     300-    1500-      1500-      1500-        1500-     500-
 //                       8000     4000    32768      32768      32768        32768     8192
-//   1 CTA       72.4   72.1     39.3    283.2      281.6   (r)347.3     (r)351.6 (r)201.8
-//   2           40.9   40.9     23.7    145.7   (r)170.4   (r)185.4     (r)367.1 (r)229.7
-//   4           23.9   23.9     16.7     91.7   (r)103.9   (r)202.7     (r)392.7 (r)284.9
-//   8           14.6   15.1  (r)19.0  (r)61.6   (r)119.4   (r)236.7     (r)460.3 (r)406.4
-//   16          11.8   16.4  (r)40.7  (r)92.5   (r)181.2   (r)360.6     (r)707.2 (r)791.0
+//   1 CTA       69.5   69.2     37.7    269.6      270.0   (r)327.4     (r)348.4 (r)197.0
+//   2           39.4   39.5     23.2    140.0   (r)163.5   (r)180.2     (r)358.1 (r)226.4
+//   4           23.3   23.3     16.3     88.0   (r)101.3   (r)198.2     (r)385.5 (r)283.5
+//   8           14.3   14.7  (r)19.2  (r)59.9   (r)117.0   (r)234.0     (r)455.4 (r)410.5
+//   16          11.8   16.4  (r)40.5  (r)91.1   (r)180.1   (r)362.8     (r)709.1 (r)795.7
 // The price: lists of equal length that a split makes more than fit (19 sequences of 16384:
-// 147 us for 108). The ranks cost every CTA a pass over the lengths and B comparisons for
+// 144 us for 108). The ranks cost every CTA a pass over the lengths and B comparisons for
 // each of them, nothing where the lengths are alike: 128 sequences at most.
 constexpr int MAX_SPLIT = 16;
 int split_of(int64_t fit, int B, int64_t lists, int64_t keys) {
