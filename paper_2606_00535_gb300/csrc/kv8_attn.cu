@@ -63,7 +63,7 @@ struct AttnParams {
 template <int D, bool FOLD>
 struct Cfg8 {
   // CTAs of an SM. With head dim 64 a tile is half the bytes for the same softmax, and one row
-  // to a thread leaves room for four: 64 sequences of 1500 to 32768 tokens 212 us, 264 with two.
+  // to a thread leaves room for four: 64 sequences of 1500 to 32768 tokens 203 us, 264 with two.
   // (With two rows: 326 and 327, and 38 equal ones 236 and 189.)
   static constexpr int PER_SM = D == 64 && FOLD ? 4 : 2;
   static constexpr int STAGES = D == 128 || FOLD ? 3 : 6;
@@ -253,14 +253,29 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
         const int64_t row = has ? int64_t(npage) * 64 + (next.slot & 63) : 0;
         const uint8_t *kp = P.c.k + (row * p.Hkv + g) * D + ch * 16, *vp = P.c.v + (row * p.Hkv + g) * D + ch * 16;
         if (lane == 0) cp_async4(exps + 4 * stage, P.c.exps + (has ? int64_t(npage) * p.Hkv + g : 0), has ? 4 : 0);
+        // All of its keys: no looking at each. (64 sequences of 1500 to 32768 tokens, one token,
+        // head dim 64: 203 us for 212; four, head dim 128: 363 for 371. But with one token and
+        // head dim 128, where the copies are the bound, 352 for 345, of instructions in between.)
+        if ((D == 64 || !FOLD) && has && next.slot >= next.lo && next.slot + 32 <= next.hi) {
+          const uint32_t dst = st + k0 * C::ROW8 + ((ch ^ (D == 128 ? k0 : k0 >> 1)) << 4);
+          const int64_t rows = (32 / CH) * pitch;
+          kp += k0 * pitch, vp += k0 * pitch;
 #pragma unroll
-        for (int it = 0; it < CH; ++it) {
-          const int key = it * (32 / CH) + k0;
-          const int bytes = has && next.slot + key >= next.lo && next.slot + key < next.hi ? 16 : 0;
-          const uint32_t dst = st + key * C::ROW8 + ((ch ^ (D == 128 ? key & 7 : (key >> 1) & 3)) << 4);
-          const int64_t e = bytes != 0 ? key * pitch : 0;
-          cp_async16(dst, kp + e, bytes);
-          cp_async16(dst + C::TILE, vp + e, bytes);
+          for (int it = 0; it < CH; ++it) {
+            const uint32_t to = (D == 128 && (it & 1) ? dst ^ 64u : dst) + it * (32 / CH) * C::ROW8;
+            cp_async16(to, kp + it * rows, 16);
+            cp_async16(to + C::TILE, vp + it * rows, 16);
+          }
+        } else {
+#pragma unroll
+          for (int it = 0; it < CH; ++it) {
+            const int key = it * (32 / CH) + k0;
+            const int bytes = has && next.slot + key >= next.lo && next.slot + key < next.hi ? 16 : 0;
+            const uint32_t dst = st + key * C::ROW8 + ((ch ^ (D == 128 ? key & 7 : (key >> 1) & 3)) << 4);
+            const int64_t e = bytes != 0 ? key * pitch : 0;
+            cp_async16(dst, kp + e, bytes);
+            cp_async16(dst + C::TILE, vp + e, bytes);
+          }
         }
       } else {
         constexpr int CH = D / 8;
