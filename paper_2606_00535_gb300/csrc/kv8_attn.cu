@@ -15,19 +15,17 @@
 // the tiles. Keys come in runs, the sinks and the window, each of them first in 8 bits,
 // then in bf16; a tile is 32 codes' or 16 bf16 keys, which take the same bytes of a stage,
 // lies in one page, and has one power of K and one of V.
-//   Scores are f16 products, K's codes made f16 two by one instruction, exactly, and Q
-//   f16 times a power of two of its row, which holds bf16's eight bits whole down to 2^-24 of
-//   the row's largest value.
-//   With at most 8 rows (FOLD) they are e4m3 products (32 dimensions an instruction), Q
-//   being two codes: its value and 2^5 times what that leaves, the other half of the
-//   instruction's 16 rows. Two codes hold bf16's eight bits whole down to 2^-7 of a row's
-//   largest value, and anything to 2^-24 of it. An e4m3 product takes about as long as two of
-//   f16, 34 clocks, but half of those would be rows that there are not: 64 sequences of 1500 to
-//   32768 tokens 345 us with one token and e4m3 (f16: 362), 371 with four and f16 (e4m3: 481).
-//   P V are f16 products, V's codes made f16 likewise; P is f16, 11 bits of it, lifted by
-//   2^14 so that it reaches 2^-38. The power of K goes into the scale of the scores; that of
-//   V, which f16 has no room for, scales each tile's own product as it joins the row's f32
-//   sums.
+//   Both products are f16. One instruction makes two codes f16, exactly. Q is f16 times a
+//   power of two of its row, which holds bf16's eight bits whole down to 2^-24 of the row's
+//   largest value; P is f16, 11 bits of it, lifted by 2^14 so that it reaches 2^-38. The power
+//   of K goes into the scale of the scores; that of V, which f16 has no room for, scales each
+//   tile's own product as it joins the row's f32 sums.
+//   With at most 8 rows (FOLD) the products are transposed, K Q^T and V^T P^T: keys, then
+//   dimensions are the instruction's 16 rows and the rows its 8 columns, so none of it is
+//   idle; P^T is turned over on the way (movmatrix). 64 sequences of 1500 to 32768 tokens 340
+//   us, 362 with rows as rows; head dim 64 190, 203. (e4m3 products for the scores, Q being
+//   two codes, 345 and 212; with 16 rows they take as long as two of f16 each, 34 clocks, and
+//   64 sequences of four tokens 481 us, 359 now.)
 //   A 16-byte piece of ldmatrix holds dimensions 4 c .. 4 c + 3 for thread c of four
 //   where bf16 rows give 2 c, 2 c + 1; bf16 tiles read K eight bytes at a time to match
 //   Q's loads. P V's columns are dimensions 16 j + 2 r and 16 j + 2 r + 1 in two
@@ -36,7 +34,7 @@
 // In bf16 tiles P is one bf16, or two with FOLD, as in window.cu.
 // Bound by HBM when the GPU is full: 38 sequences of 16384 tokens, 8 KV heads of 128
 // dimensions, 204 us, 94% of the copy rate (253 us with both operands made bf16 by integer
-// instructions, which kept the ALU busy 47% of the time). 64 of 1500 to 32768, 345 us, 98%.
+// instructions, which kept the ALU busy 47% of the time). 64 of 1500 to 32768, 340 us, 99%.
 #include <limits.h>
 #include <math.h>
 
@@ -63,8 +61,8 @@ struct AttnParams {
 template <int D, bool FOLD>
 struct Cfg8 {
   // CTAs of an SM. With head dim 64 a tile is half the bytes for the same softmax, and one row
-  // to a thread leaves room for four: 64 sequences of 1500 to 32768 tokens 203 us, 264 with two.
-  // (With two rows: 326 and 327, and 38 equal ones 236 and 189.)
+  // to a thread leaves room for four: 64 sequences of 1500 to 32768 tokens 190 us, 246 with two.
+  // (With two rows: 326 and 327, and 38 equal ones 236 and 189, before scores were f16 products.)
   static constexpr int PER_SM = D == 64 && FOLD ? 4 : 2;
   static constexpr int STAGES = D == 128 || FOLD ? 3 : 6;
   static constexpr int ROW8 = D, ROW16 = 2 * D;  // bytes of a key
@@ -107,12 +105,6 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, int byt
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-__device__ __forceinline__ void mma_codes(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -129,25 +121,11 @@ __device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t codes) {  // of the 
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(uint16_t(codes)));
   return r;
 }
-__device__ __forceinline__ uint32_t to_codes_x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// An 8 x 8 matrix of 16-bit values, a row to four threads, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
-}
-
-// Four values of a row of Q as codes, and 2^5 times what those leave. Values are below
-// 2^8. A code has four significant bits of bf16's eight, so the two hold a value whole
-// down to 2^-7 of the row's largest, and any to 2^-24 of that.
-__device__ __forceinline__ void split_q(uint2 w, float up, uint32_t &hi, uint32_t &lo) {
-  hi = lo = 0;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t u = i == 0 ? w.x : w.y;
-    const float x = __uint_as_float(u << 16) * up, y = __uint_as_float(u & 0xffff0000u) * up;
-    const uint32_t q = to_codes_x2(x, y);
-    hi |= q << (16 * i);
-    lo |= to_codes_x2((x - code_value(q & 0xffu)) * 32.f, (y - code_value(q >> 8)) * 32.f) << (16 * i);
-  }
 }
 
 // The sums of a warp from the codes' columns (two products of 16 dimensions hold 16 j +
@@ -172,6 +150,31 @@ __device__ __forceinline__ void to_order(float (&o)[D / 8][W]) {
       x0 = __shfl_sync(0xffffffffu, b0, high), x1 = __shfl_sync(0xffffffffu, b1, high);
       o[j + 1][h + 1] = odd ? x1 : x0;
     }
+}
+
+// FOLD: from the transposed products' order (thread c of four has rows 2 c and 2 c + 1,
+// dimensions 16 j + 2 r and 16 j + 2 r + 1) to row r, dimensions 8 j' + 2 c and + 1.
+template <int D>
+__device__ __forceinline__ void to_rows(float (&o)[D / 8][2], float (&m2)[2], float (&l2)[2], float &m, float &l) {
+  const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3, from = 4 * c + (r >> 1);
+  const bool odd = r & 1;
+#pragma unroll
+  for (int j = 0; j < D / 8; j += 2) {
+    float x[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float a = __shfl_sync(0xffffffffu, o[j + e][0], from + 16 * h), b = __shfl_sync(0xffffffffu, o[j + e][1], from + 16 * h);
+        x[h][e] = odd ? b : a;
+      }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) o[j][e] = x[0][e], o[j + 1][e] = x[1][e];
+  }
+  const float m0 = __shfl_sync(0xffffffffu, m2[0], r >> 1), m1 = __shfl_sync(0xffffffffu, m2[1], r >> 1);
+  const float l0 = __shfl_sync(0xffffffffu, l2[0], r >> 1), l1 = __shfl_sync(0xffffffffu, l2[1], r >> 1);
+  m = odd ? m1 : m0;
+  l = c == 0 ? (odd ? l1 : l0) : 0.f;
 }
 
 // P = 2^(s - m) is scaled by 2^LIFT: f16 then holds it down to 2^-38 of a row's largest.
@@ -253,10 +256,9 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
         const int64_t row = has ? int64_t(npage) * 64 + (next.slot & 63) : 0;
         const uint8_t *kp = P.c.k + (row * p.Hkv + g) * D + ch * 16, *vp = P.c.v + (row * p.Hkv + g) * D + ch * 16;
         if (lane == 0) cp_async4(exps + 4 * stage, P.c.exps + (has ? int64_t(npage) * p.Hkv + g : 0), has ? 4 : 0);
-        // All of its keys: no looking at each. (64 sequences of 1500 to 32768 tokens, one token,
-        // head dim 64: 203 us for 212; four, head dim 128: 363 for 371. But with one token and
-        // head dim 128, where the copies are the bound, 352 for 345, of instructions in between.)
-        if ((D == 64 || !FOLD) && has && next.slot >= next.lo && next.slot + 32 <= next.hi) {
+        // All of its keys: no looking at each (64 sequences of 1500 to 32768 tokens, one token, head
+        // dim 64: 190 us for 200; four, head dim 128: 359 for 371).
+        if (has && next.slot >= next.lo && next.slot + 32 <= next.hi) {
           const uint32_t dst = st + k0 * C::ROW8 + ((ch ^ (D == 128 ? k0 : k0 >> 1)) << 4);
           const int64_t rows = (32 / CH) * pitch;
           kp += k0 * pitch, vp += k0 * pitch;
@@ -335,10 +337,10 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
   // tiles in 8 bits come first
   const int my8 = ::min(my, j0 + warp < tl.n8 ? (tl.n8 - j0 - warp + WARPS - 1) / WARPS : 0);
   int i = 0;
+  float m2[2] = {-INFINITY, -INFINITY}, l2[2] = {0.f, 0.f};  // FOLD: of rows 2 c and 2 c + 1
   if (my8 > 0) {
-    // FOLD: codes, rows 8 .. 15 what is left; else f16
-    uint32_t qf[FOLD ? D / 32 : D / 16][4];
-    float rq[H];  // scale of a row's scores
+    uint32_t qf[D / 16][2 * H];  // f16
+    float rq[H];                 // scale of a row's scores
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const __nv_bfloat16 *from = src(h);
@@ -356,41 +358,123 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
       const int ex = ::max(int(bits >> 7), 8);
       const float up = bits >= 0x7f80u ? 0.f : __uint_as_float(uint32_t(261 - ex) << 23);
       rq[h] = bits >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float(uint32_t(ex - 7) << 23) * p.scale_log2;
-      if constexpr (FOLD) {
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
-          split_q(w[2 * kk], up, qf[kk][0], qf[kk][1]);
-          split_q(w[2 * kk + 1], up, qf[kk][2], qf[kk][3]);
+      for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t u = e == 0 ? w[kk].x : w[kk].y;
+          qf[kk][H * e + h] = pack_f16x2(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up);
         }
-      } else {
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t u = e == 0 ? w[kk].x : w[kk].y;
-            qf[kk][2 * e + h] = pack_f16x2(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up);
-          }
-      }
     }
+    // FOLD: the scales of rows 2 c and 2 c + 1
+    const float rq2[2] = {__shfl_sync(0xffffffffu, rq[0], 8 * c), __shfl_sync(0xffffffffu, rq[0], 8 * c + 4)};
 #pragma unroll 1
     for (; i < my8; ++i) {
       step(i);
       const Tile t = tile_of(tl, j0 + warp + i * WARPS);
       const uint32_t st = ring + at * 2 * C::TILE + lane * C::ROW8, swz = D == 128 ? lane & 7 : (lane >> 1) & 3;
       const uint32_t w = s_exp[warp][at];
-      float s[4][2 * H];
-      {
-        float x[4][4] = {};
-        if constexpr (FOLD) {
+      if constexpr (FOLD) {
+        // K Q^T: e of group n is key 16 n + 8 (e >> 1) + r0 and row 2 c + (e & 1)
+        float x[2][2][4] = {}, s[2][4];
 #pragma unroll
-          for (int kk = 0; kk < D / 32; ++kk) {
-            uint32_t k0[4], k1[4];  // 8 keys each
-            ldsm4(st + (((2 * kk) ^ swz) << 4), k0);
-            ldsm4(st + (((2 * kk + 1) ^ swz) << 4), k1);
+        for (int kk = 0; kk < D / 16; ++kk) {
+          uint32_t k[4];
+          ldsm4(st + ((kk ^ swz) << 4), k);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) mma_codes(x[n], qf[kk], k0[n], k1[n]);
+          for (int n = 0; n < 2; ++n) {
+            const uint32_t a[4] = {codes_to_f16x2(k[2 * n]), codes_to_f16x2(k[2 * n + 1]), codes_to_f16x2(k[2 * n] >> 16), codes_to_f16x2(k[2 * n + 1] >> 16)};
+            mma_f16(x[n][kk & 1], a, qf[kk][0], qf[kk][1]);
           }
-        } else {
+        }
+        const float pk = power(k_exp(w)), fv = power(v_exp(w));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float f = rq2[h] * pk;
+          if (f > 3.4e38f) f = 3.4e38f;  // (0 times infinity is a NaN)
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = h; e < 4; e += 2) s[n][e] = (x[n][0][e] + x[n][1][e]) * f;
+        }
+        if (!(t.slot >= t.lo && t.slot + 32 <= t.hi && (t.sink || int64_t(L) + (p.parent != nullptr ? T - 1 : off_max) - t.slot < p.window))) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const RowInfo ri = sh.row[2 * c + h];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int e = h; e < 4; e += 2) {
+                const int slot = t.slot + 16 * n + 8 * (e >> 1) + r0;
+                if (slot < t.lo || slot >= t.hi || ri.off < 0 || !sees(p, L, ri.off, ri.anc, slot)) s[n][e] = -INFINITY;
+              }
+          }
+        }
+        float mx[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][h], s[0][2 + h]), fmaxf(s[1][h], s[1][2 + h]));
+#pragma unroll
+        for (int k = 4; k < 32; k <<= 1)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], k));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(m2[h], mx[h]);
+        if (__any_sync(0xffffffffu, mx[0] > m2[0] || mx[1] > m2[1])) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float corr = mx[h] == m2[h] ? 1.f : tc::ex2(m2[h] - mx[h]);  // (also where both are -inf)
+            m2[h] = mx[h];
+            l2[h] *= corr;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) o[n][h] *= corr;
+          }
+        }
+        uint32_t pt[2][2];  // P, a key of the first 8 or the others to a row, transposed
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float nm = m2[h] == -INFINITY ? 0.f : LIFT - m2[h];
+          float sum = 0.f;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = h; e < 4; e += 2) {
+              s[n][e] = tc::ex2(s[n][e] + nm);
+              sum += s[n][e];
+            }
+          if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
+            // the rows that see some of the page become NaN; the others stay as they are, whatever the codes
+#pragma unroll
+            for (int k = 4; k < 32; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+            if (sum != 0.f) sum = fv;
+          }
+          l2[h] += sum;
+        }
+        if (__builtin_expect(v_exp(w) != DREAMS_KV8_NOT_FINITE, 1)) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) pt[n][e] = transposed(pack_f16x2(s[n][2 * e], s[n][2 * e + 1]));
+#pragma unroll
+          for (int n = 0; n < D / 8; n += 2) {  // V^T P^T
+            uint32_t vb[4], a[2][4];
+            ldsm4t(st + C::TILE + (((n >> 1) ^ swz) << 4), vb);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t y = __byte_perm(vb[k], 0u, 0x3120);  // two keys of one dimension, and of the next
+              a[k >> 1][2 * (k & 1)] = codes_to_f16x2(y);
+              a[k >> 1][2 * (k & 1) + 1] = codes_to_f16x2(y >> 16);
+            }
+            float z[4] = {};
+            mma_f16(z, a[0], pt[0][0], pt[0][1]);
+            mma_f16(z, a[1], pt[1][0], pt[1][1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n + (e >> 1)][e & 1] = fmaf(z[e], fv, o[n + (e >> 1)][e & 1]);
+          }
+        }
+      } else {
+        float s[4][2 * H];
+        {
+          float x[4][4] = {};
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             uint32_t k[4];  // 8 keys each
@@ -398,82 +482,86 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
 #pragma unroll
             for (int n = 0; n < 4; ++n) mma_f16(x[n], qf[kk], codes_to_f16x2(k[n]), codes_to_f16x2(k[n] >> 16));
           }
+          const float pk = power(k_exp(w));
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            float f = rq[h] * pk;
+            if (f > 3.4e38f) f = 3.4e38f;  // (0 times infinity is a NaN)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) s[n][2 * h + e] = x[n][2 * h + e] * f;
+          }
         }
-        const float pk = power(k_exp(w));
+        // does every row see every key of the tile?
+        if (!(t.slot >= t.lo && t.slot + 32 <= t.hi && (t.sink || int64_t(L) + (p.parent != nullptr ? T - 1 : off_max) - t.slot < p.window))) {
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-          float f = rq[h] * pk;
-          if (f > 3.4e38f) f = 3.4e38f;  // (0 times infinity is a NaN)
+          for (int h = 0; h < H; ++h) {
+            const RowInfo ri = info(h);
 #pragma unroll
-          for (int n = 0; n < 4; ++n)
+            for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              if constexpr (FOLD) s[n][e] = fmaf(x[n][2 + e], 0.03125f, x[n][e]) * f;
-              else s[n][2 * h + e] = x[n][2 * h + e] * f;
-            }
+              for (int e = 0; e < 2; ++e) {
+                const int slot = t.slot + n * 8 + 2 * c + e;
+                if (slot < t.lo || slot >= t.hi || ri.off < 0 || !sees(p, L, ri.off, ri.anc, slot)) s[n][2 * h + e] = -INFINITY;
+              }
+          }
         }
-      }
-      // does every row see every key of the tile?
-      if (!(t.slot >= t.lo && t.slot + 32 <= t.hi && (t.sink || int64_t(L) + (p.parent != nullptr ? T - 1 : off_max) - t.slot < p.window))) {
+        soften<D, 4, H>(s, m, l, o);
+        const float fv = power(v_exp(w));
+        if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
+          // the rows that see some of the page become NaN; the others stay as they are, whatever the codes
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-          const RowInfo ri = info(h);
+          for (int h = 0; h < H; ++h) {
+            float any = 0.f;
 #pragma unroll
-          for (int n = 0; n < 4; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int slot = t.slot + n * 8 + 2 * c + e;
-              if (slot < t.lo || slot >= t.hi || ri.off < 0 || !sees(p, L, ri.off, ri.anc, slot)) s[n][2 * h + e] = -INFINITY;
-            }
+            for (int n = 0; n < 4; ++n) any += s[n][2 * h] + s[n][2 * h + 1];
+            any += __shfl_xor_sync(0xffffffffu, any, 1);
+            any += __shfl_xor_sync(0xffffffffu, any, 2);
+            if (any != 0.f) l[h] = fv;
+          }
+          at = at + 1 == C::STAGES ? 0 : at + 1;
+          continue;
         }
-      }
-      soften<D, 4, H>(s, m, l, o);
-      const float fv = power(v_exp(w));
-      if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
-        // the rows that see some of the page become NaN; the others stay as they are, whatever the codes
+        uint32_t p0[4], p1[4];
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-          float any = 0.f;
-#pragma unroll
-          for (int n = 0; n < 4; ++n) any += s[n][2 * h] + s[n][2 * h + 1];
-          any += __shfl_xor_sync(0xffffffffu, any, 1);
-          any += __shfl_xor_sync(0xffffffffu, any, 2);
-          if (any != 0.f) l[h] = fv;
+        for (int h = 0; h < 2; ++h) {
+          p0[h] = h < H ? pack_f16x2(s[0][2 * (h % H)], s[0][2 * (h % H) + 1]) : 0u;
+          p0[h + 2] = h < H ? pack_f16x2(s[1][2 * (h % H)], s[1][2 * (h % H) + 1]) : 0u;
+          p1[h] = h < H ? pack_f16x2(s[2][2 * (h % H)], s[2][2 * (h % H) + 1]) : 0u;
+          p1[h + 2] = h < H ? pack_f16x2(s[3][2 * (h % H)], s[3][2 * (h % H) + 1]) : 0u;
         }
-        at = at + 1 == C::STAGES ? 0 : at + 1;
-        continue;
-      }
-      uint32_t p0[4], p1[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        p0[h] = h < H ? pack_f16x2(s[0][2 * (h % H)], s[0][2 * (h % H) + 1]) : 0u;
-        p0[h + 2] = h < H ? pack_f16x2(s[1][2 * (h % H)], s[1][2 * (h % H) + 1]) : 0u;
-        p1[h] = h < H ? pack_f16x2(s[2][2 * (h % H)], s[2][2 * (h % H) + 1]) : 0u;
-        p1[h + 2] = h < H ? pack_f16x2(s[3][2 * (h % H)], s[3][2 * (h % H) + 1]) : 0u;
-      }
+        for (int n = 0; n < D / 8; n += 2) {
+          uint32_t vb[4], y[4];
+          ldsm4t(st + C::TILE + (((n >> 1) ^ swz) << 4), vb);
 #pragma unroll
-      for (int n = 0; n < D / 8; n += 2) {
-        uint32_t vb[4], y[4];
-        ldsm4t(st + C::TILE + (((n >> 1) ^ swz) << 4), vb);
+          for (int k = 0; k < 4; ++k) y[k] = __byte_perm(vb[k], 0u, 0x3120);  // two keys of one dimension, and of the next
+          float a0[4] = {}, a1[4] = {};
+          mma_f16(a0, p0, codes_to_f16x2(y[0]), codes_to_f16x2(y[1]));
+          mma_f16(a1, p0, codes_to_f16x2(y[0] >> 16), codes_to_f16x2(y[1] >> 16));
+          mma_f16(a0, p1, codes_to_f16x2(y[2]), codes_to_f16x2(y[3]));
+          mma_f16(a1, p1, codes_to_f16x2(y[2] >> 16), codes_to_f16x2(y[3] >> 16));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = __byte_perm(vb[k], 0u, 0x3120);  // two keys of one dimension, and of the next
-        float a0[4] = {}, a1[4] = {};
-        mma_f16(a0, p0, codes_to_f16x2(y[0]), codes_to_f16x2(y[1]));
-        mma_f16(a1, p0, codes_to_f16x2(y[0] >> 16), codes_to_f16x2(y[1] >> 16));
-        mma_f16(a0, p1, codes_to_f16x2(y[2]), codes_to_f16x2(y[3]));
-        mma_f16(a1, p1, codes_to_f16x2(y[2] >> 16), codes_to_f16x2(y[3] >> 16));
-#pragma unroll
-        for (int e = 0; e < 2 * H; ++e) {
-          o[n][e] = fmaf(a0[e], fv, o[n][e]);
-          o[n + 1][e] = fmaf(a1[e], fv, o[n + 1][e]);
+          for (int e = 0; e < 2 * H; ++e) {
+            o[n][e] = fmaf(a0[e], fv, o[n][e]);
+            o[n + 1][e] = fmaf(a1[e], fv, o[n + 1][e]);
+          }
         }
       }
       at = at + 1 == C::STAGES ? 0 : at + 1;
     }
   }
   const bool ordered = my > my8;  // o's columns, in the end
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int k = 4; k < 32; k <<= 1)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) l2[h] += __shfl_xor_sync(0xffffffffu, l2[h], k);
+  }
   if (ordered) {
-    to_order<D, 2 * H>(o);
+    if constexpr (FOLD) to_rows<D>(o, m2, l2, m[0], l[0]);
+    else to_order<D, 2 * H>(o);
     uint32_t qf[D / 16][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -592,6 +680,17 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
   __syncthreads();  // the stages are free
 
   float *so = reinterpret_cast<float *>(smem);
+  if (FOLD && !ordered) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = 2 * c + h;
+      if (r0 == 0) sh.ml[warp][r] = make_float2(m2[h] - LIFT, l2[h]);
+#pragma unroll
+      for (int n = 0; n < D / 8; n += 2) *reinterpret_cast<float2 *>(so + (warp * RB + r) * D + n * 8 + 2 * r0) = make_float2(o[n][h], o[n + 1][h]);
+    }
+    __syncthreads();
+    return;
+  }
 #pragma unroll
   for (int h = 0; h < H; ++h) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
