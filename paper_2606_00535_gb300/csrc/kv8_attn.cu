@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(32 * WARPS, Cfg8<D, FOLD>::PER_SM == 4 ? 4 : 0
 }
 
 // ------------------------------------------------------------------ host side
-// CTAs of a list, and the order of the lists. One CTA takes 9 us for 1000 keys whatever
+// CTAs of a list, and the order of the lists. One CTA takes 8 us for 1000 keys whatever
 // else runs, and with all places taken the copies are bound by HBM, so lists are split
 // while all CTAs (`fit` places) still run at the same time, 16 to a list only while each
 // has an SM of its own, and once more for several sequences of which each part keeps
@@ -807,13 +807,13 @@ __global__ void __launch_bounds__(32 * WARPS, Cfg8<D, FOLD>::PER_SM == 4 ? 4 : 0
 //   lists          8      16       64       64        128        256          512     1024
 //   lengths     8000   1000-     300-    1500-      1500-      1500-        1500-     500-
 //                       8000     4000    32768      32768      32768        32768     8192
-//   1 CTA       69.5   69.2     37.7    269.6      270.0   (r)327.4     (r)348.4 (r)197.0
-//   2           39.4   39.5     23.2    140.0   (r)163.5   (r)180.2     (r)358.1 (r)226.4
-//   4           23.3   23.3     16.3     88.0   (r)101.3   (r)198.2     (r)385.5 (r)283.5
-//   8           14.3   14.7  (r)19.2  (r)59.9   (r)117.0   (r)234.0     (r)455.4 (r)410.5
-//   16          11.8   16.4  (r)40.5  (r)91.1   (r)180.1   (r)362.8     (r)709.1 (r)795.7
+//   1 CTA       64.4   63.6     34.9    247.9      247.3   (r)274.4     (r)342.5 (r)189.9
+//   2           37.2   37.2     21.9    129.5   (r)144.1   (r)178.6     (r)350.4 (r)225.8
+//   4           22.2   22.0     15.4     77.5    (r)96.3   (r)193.7     (r)380.8 (r)278.8
+//   8           14.0   14.4  (r)18.9  (r)56.7   (r)114.2   (r)228.2     (r)451.1 (r)386.3
+//   16          11.2   16.4  (r)40.6  (r)84.9   (r)168.6   (r)335.2     (r)651.0 (r)777.1
 // The price: lists of equal length that a split makes more than fit (19 sequences of 16384:
-// 144 us for 108). The ranks cost every CTA a pass over the lengths and B comparisons for
+// 142 us for 108). The ranks cost every CTA a pass over the lengths and B comparisons for
 // each of them, nothing where the lengths are alike: 128 sequences at most.
 constexpr int MAX_SPLIT = 16;
 int split_of(int64_t fit, int B, int64_t lists, int64_t keys) {
