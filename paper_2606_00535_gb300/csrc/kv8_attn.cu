@@ -301,10 +301,7 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
   look(0);
 
   const int r0 = lane >> 2, c = lane & 3;  // this thread's rows: r0 and (H = 2) r0 + 8
-  // (in registers where they have room: 64 sequences of up to 32768 tokens 352 us with one
-  // row, 392 from shared memory; with two rows 523 and 481)
-  const RowInfo own = FOLD ? sh.row[r0] : RowInfo{};
-  auto info = [&](int h) { return FOLD ? own : sh.row[r0 + 8 * h]; };
+  auto info = [&](int h) { return sh.row[r0 + 8 * h]; };
   // its part of Q: dimensions 4 c .. 4 c + 3 of each 16
   auto src = [&](int h) -> const __nv_bfloat16 * {
     const int r = first + r0 + 8 * h, t = r / p.G;
@@ -758,10 +755,10 @@ __device__ __noinline__ int by_length(const WinParams &p, int r) {
   return s_at;
 }
 
-// (0 CTAs in the bounds: none are asked for. Asking for two changes the code of head dim
-// 128, and a batch of 64 takes 402 us for 347.)
+// (With head dim 128 the bounds ask for no CTAs beside it, which changes the code: 64
+// sequences of 1500 to 32768 tokens, four new ones, 356 us for 364. Head dim 64: 270 for 261.)
 template <int D, bool FOLD>
-__global__ void __launch_bounds__(32 * WARPS, Cfg8<D, FOLD>::PER_SM == 4 ? 4 : 0) kv8_rows_kernel(const AttnParams P) {
+__global__ void __launch_bounds__(32 * WARPS, D == 128 ? 0 : Cfg8<D, FOLD>::PER_SM) kv8_rows_kernel(const AttnParams P) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ RowsShared sh;
   __shared__ uint32_t s_exp[WARPS][6];
