@@ -180,10 +180,11 @@ __device__ __forceinline__ void to_rows(float (&o)[D / 8][2], float (&m2)[2], fl
 // P = 2^(s - m) is scaled by 2^LIFT: f16 then holds it down to 2^-38 of a row's largest.
 constexpr float LIFT = 14.f;
 
-// New maxima of NB blocks of 8 keys' scores, s in place of P, and its sums. s is scaled
-// already, -inf where a row does not see a key.
+// New maxima of NB blocks of 8 keys' scores, P in place of s, and its sums; mt: these keys'
+// own maxima, -inf for a row that sees none of them. s is scaled already, -inf where a row
+// does not see a key.
 template <int D, int NB, int H>
-__device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], float (&l)[H], float (&o)[D / 8][2 * H]) {
+__device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], float (&l)[H], float (&o)[D / 8][2 * H], float (&mt)[H]) {
   float mx[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) {
@@ -196,7 +197,10 @@ __device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], flo
 #pragma unroll
     for (int h = 0; h < H; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], k));
 #pragma unroll
-  for (int h = 0; h < H; ++h) mx[h] = fmaxf(m[h], mx[h]);
+  for (int h = 0; h < H; ++h) {
+    mt[h] = mx[h];
+    mx[h] = fmaxf(m[h], mx[h]);
+  }
   if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[H - 1] > m[H - 1])) {
 #pragma unroll
     for (int h = 0; h < H; ++h) {
@@ -407,15 +411,15 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
               }
           }
         }
-        float mx[2];
+        float mt[2], mx[2];  // of the tile's keys, -inf for a row that sees none of them; with those before
 #pragma unroll
-        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][h], s[0][2 + h]), fmaxf(s[1][h], s[1][2 + h]));
+        for (int h = 0; h < 2; ++h) mt[h] = fmaxf(fmaxf(s[0][h], s[0][2 + h]), fmaxf(s[1][h], s[1][2 + h]));
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], k));
+          for (int h = 0; h < 2; ++h) mt[h] = fmaxf(mt[h], __shfl_xor_sync(0xffffffffu, mt[h], k));
 #pragma unroll
-        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(m2[h], mx[h]);
+        for (int h = 0; h < 2; ++h) mx[h] = fmaxf(m2[h], mt[h]);
         if (__any_sync(0xffffffffu, mx[0] > m2[0] || mx[1] > m2[1])) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -438,12 +442,9 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
               s[n][e] = tc::ex2(s[n][e] + nm);
               sum += s[n][e];
             }
-          if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
-            // the rows that see some of the page become NaN; the others stay as they are, whatever the codes
-#pragma unroll
-            for (int k = 4; k < 32; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-            if (sum != 0.f) sum = fv;
-          }
+          // the rows that see some of the page become NaN, however little it weighs; the others stay as they
+          // are, whatever the codes
+          if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0) && mt[h] != -INFINITY) sum = fv;
           l2[h] += sum;
         }
         if (__builtin_expect(v_exp(w) != DREAMS_KV8_NOT_FINITE, 1)) {
@@ -504,19 +505,15 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
               }
           }
         }
-        soften<D, 4, H>(s, m, l, o);
+        float mt[H];
+        soften<D, 4, H>(s, m, l, o, mt);
         const float fv = power(v_exp(w));
         if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
-          // the rows that see some of the page become NaN; the others stay as they are, whatever the codes
+          // the rows that see some of the page become NaN, however little it weighs; the others stay as they
+          // are, whatever the codes
 #pragma unroll
-          for (int h = 0; h < H; ++h) {
-            float any = 0.f;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) any += s[n][2 * h] + s[n][2 * h + 1];
-            any += __shfl_xor_sync(0xffffffffu, any, 1);
-            any += __shfl_xor_sync(0xffffffffu, any, 2);
-            if (any != 0.f) l[h] = fv;
-          }
+          for (int h = 0; h < H; ++h)
+            if (mt[h] != -INFINITY) l[h] = fv;
           at = at + 1 == C::STAGES ? 0 : at + 1;
           continue;
         }
@@ -625,7 +622,8 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
             }
         }
       }
-      soften<D, 2, H>(s, m, l, o);
+      float mt[H];
+      soften<D, 2, H>(s, m, l, o, mt);
       uint32_t pf[4];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
