@@ -17,9 +17,11 @@
 // lies in one page, and has one power of K and one of V.
 //   Both products are f16. One instruction makes two codes f16, exactly. Q is f16 times a
 //   power of two of its row, which holds bf16's eight bits whole down to 2^-24 of the row's
-//   largest value; P is f16, 11 bits of it, lifted by 2^14 so that it reaches 2^-38. The power
-//   of K goes into the scale of the scores; that of V, which f16 has no room for, scales each
-//   tile's own product as it joins the row's f32 sums.
+//   largest value; P is f16, 11 bits of it, against the tile's own largest score and lifted by
+//   2^14, so that it reaches 2^-38 of the tile's largest probability. The power of K goes into the
+//   scale of the scores. That of V, and what the tile's largest probability is of the row's, which
+//   f16 has no room for, scale each tile's own product as it joins the row's f32 sums: a page that
+//   weighs 2^-60 counts like any other where its V is 2^80 times the others'.
 //   With at most 8 rows (FOLD) the products are transposed, K Q^T and V^T P^T: keys, then
 //   dimensions are the instruction's 16 rows and the rows its 8 columns, so none of it is
 //   idle; P^T is turned over on the way (movmatrix). 64 sequences of 1500 to 32768 tokens 340
@@ -177,13 +179,16 @@ __device__ __forceinline__ void to_rows(float (&o)[D / 8][2], float (&m2)[2], fl
   l = c == 0 ? (odd ? l1 : l0) : 0.f;
 }
 
-// P = 2^(s - m) is scaled by 2^LIFT: f16 then holds it down to 2^-38 of a row's largest.
+// P = 2^(s - m) is scaled by 2^LIFT: f16 then holds it down to 2^-38 of the largest.
 constexpr float LIFT = 14.f;
 
+// What P against a tile's own maximum mt counts against the row's, m.
+__device__ __forceinline__ float share(float mt, float m) { return mt == -INFINITY ? 1.f : tc::ex2(mt - m); }
+
 // New maxima of NB blocks of 8 keys' scores, P in place of s, and its sums; mt: these keys'
-// own maxima, -inf for a row that sees none of them. s is scaled already, -inf where a row
-// does not see a key.
-template <int D, int NB, int H>
+// own maxima, -inf for a row that sees none of them, which P goes by with OWN. s is scaled
+// already, -inf where a row does not see a key.
+template <int D, int NB, int H, bool OWN>
 __device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], float (&l)[H], float (&o)[D / 8][2 * H], float (&mt)[H]) {
   float mx[H];
 #pragma unroll
@@ -216,13 +221,15 @@ __device__ __forceinline__ void soften(float (&s)[NB][2 * H], float (&m)[H], flo
   }
 #pragma unroll
   for (int h = 0; h < H; ++h) {
-    const float nm = m[h] == -INFINITY ? 0.f : LIFT - m[h];
+    const float ref = OWN ? mt[h] : m[h], nm = ref == -INFINITY ? 0.f : LIFT - ref;
+    float sum = OWN ? 0.f : l[h];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       s[n][2 * h] = tc::ex2(s[n][2 * h] + nm);
       s[n][2 * h + 1] = tc::ex2(s[n][2 * h + 1] + nm);
-      l[h] += s[n][2 * h] + s[n][2 * h + 1];
+      sum += s[n][2 * h] + s[n][2 * h + 1];
     }
+    l[h] = OWN ? fmaf(sum, share(mt[h], m[h]), l[h]) : sum;
   }
 }
 
@@ -431,9 +438,10 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           }
         }
         uint32_t pt[2][2];  // P, a key of the first 8 or the others to a row, transposed
+        float of[2];        // what it counts, with V's power
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float nm = m2[h] == -INFINITY ? 0.f : LIFT - m2[h];
+          const float nm = mt[h] == -INFINITY ? 0.f : LIFT - mt[h];
           float sum = 0.f;
 #pragma unroll
           for (int n = 0; n < 2; ++n)
@@ -445,7 +453,9 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           // the rows that see some of the page become NaN, however little it weighs; the others stay as they
           // are, whatever the codes
           if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0) && mt[h] != -INFINITY) sum = fv;
-          l2[h] += sum;
+          const float sh = share(mt[h], m2[h]);
+          of[h] = fv * sh;
+          l2[h] = fmaf(sum, sh, l2[h]);
         }
         if (__builtin_expect(v_exp(w) != DREAMS_KV8_NOT_FINITE, 1)) {
 #pragma unroll
@@ -466,7 +476,7 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
             mma_f16(z, a[0], pt[0][0], pt[0][1]);
             mma_f16(z, a[1], pt[1][0], pt[1][1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[n + (e >> 1)][e & 1] = fmaf(z[e], fv, o[n + (e >> 1)][e & 1]);
+            for (int e = 0; e < 4; ++e) o[n + (e >> 1)][e & 1] = fmaf(z[e], of[e & 1], o[n + (e >> 1)][e & 1]);
           }
         }
       } else {
@@ -506,7 +516,7 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           }
         }
         float mt[H];
-        soften<D, 4, H>(s, m, l, o, mt);
+        soften<D, 4, H, true>(s, m, l, o, mt);
         const float fv = power(v_exp(w));
         if (__builtin_expect(v_exp(w) == DREAMS_KV8_NOT_FINITE, 0)) {
           // the rows that see some of the page become NaN, however little it weighs; the others stay as they
@@ -517,6 +527,9 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           at = at + 1 == C::STAGES ? 0 : at + 1;
           continue;
         }
+        float of[H];  // what P counts, with V's power
+#pragma unroll
+        for (int h = 0; h < H; ++h) of[h] = fv * share(mt[h], m[h]);
         uint32_t p0[4], p1[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -538,8 +551,8 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
           mma_f16(a1, p1, codes_to_f16x2(y[2] >> 16), codes_to_f16x2(y[3] >> 16));
 #pragma unroll
           for (int e = 0; e < 2 * H; ++e) {
-            o[n][e] = fmaf(a0[e], fv, o[n][e]);
-            o[n + 1][e] = fmaf(a1[e], fv, o[n + 1][e]);
+            o[n][e] = fmaf(a0[e], of[e >> 1], o[n][e]);
+            o[n + 1][e] = fmaf(a1[e], of[e >> 1], o[n + 1][e]);
           }
         }
       }
@@ -623,7 +636,7 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
         }
       }
       float mt[H];
-      soften<D, 2, H>(s, m, l, o, mt);
+      soften<D, 2, H, false>(s, m, l, o, mt);
       uint32_t pf[4];
 #pragma unroll
       for (int n = 0; n < 2; ++n) {

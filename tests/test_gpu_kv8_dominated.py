@@ -1,11 +1,12 @@
 """kv8_attention where a page weighs next to nothing beside others that the same warp has
-read: a page marked as not finite still makes the rows that see it NaN (0 x NaN is a NaN).
-Enough lists that each is one CTA's, so that its warps walk over several tiles; 4, 16, 36
+read: a page marked as not finite still makes the rows that see it NaN (0 x NaN is a NaN),
+and one whose V is that much larger still decides the result. Enough lists that each is one CTA's, so that its warps walk over several tiles; 4, 16, 36
 and 80 rows of a KV head, on both sides of every change of kernel."""
 import numpy as np
 import pytest
 import torch
 
+from oracle import rotary_kv8 as R
 from oracle import serving as S
 from test_gpu_kv8 import Case, U
 
@@ -64,3 +65,31 @@ def test_marked_pages_of_no_weight(dreams, T, D, j):
     ref = S.window_rows(c.q[3].double().numpy(), lambda s, g: (K[s, g], V[s, g]), LONG, c.scale, c.window, 0, lambda h: h // 4, None, sel)
     for (t, h), (o, a, z) in zip(sel, ref):
         assert (np.abs(out[3, t, h].double().cpu().numpy() - o) <= 1.02 * U * (np.abs(o) + a) + (2e-4 + 2 * e) * a + 1e-6).all()
+
+
+@pytest.mark.parametrize("T", [1, 4, 9, 20])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("weight", [10, 30, 45, 60, 90])
+def test_pages_of_little_weight_and_large_values(dreams, T, D, weight):
+    """Probabilities of some 2^-weight of the others' on pages whose V is 2^124 times theirs: first, in the middle, last, two
+    of one sequence. The bound is that of test_gpu_kv8.py: it goes by the magnitudes that add up to the result."""
+    c = case(T + D + weight, D, T, kscale=0.25)
+    heavy = {(0, 0), (1, 3), (2, 6), (3, 1), (3, 4)}
+    c.q[..., 0] = 8.0
+    depth = weight / (8.0 * c.scale * 1.4427)  # dimension 0 of those pages' keys: scores lower by weight ln 2
+    c.k[..., 0] = 0.0
+    c.vals[0, ..., 0] = 0.0
+    for b in range(4):
+        for e in range(END // 64):
+            z, at = int(c.table8[b, e]), slice(64 * e, 64 * e + 64)
+            c.k8[0, z, :, :, 0] = 0
+            if (b, e) in heavy:
+                for h in range(8):
+                    k = c.vals[0, 0, b, at, h]
+                    k[:, 0] = -depth
+                    code, es = R.quantize_page(k[:, None])
+                    c.k8[0, z, :, h], c.exps[0, z, h, 0] = torch.tensor(code[:, 0]), int(es[0])
+                    c.vals[0, 0, b, at, h] = R.decode(code[:, 0], es[0])
+            scale_page(c, 1, b, e, 84 if (b, e) in heavy else -40)
+    scale_tail(c, 1, -40)
+    c.check(c.run(dreams), n=6)
