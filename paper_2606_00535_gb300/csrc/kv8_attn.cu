@@ -16,7 +16,7 @@
 // then in bf16; a tile is 32 codes' or 16 bf16 keys, which take the same bytes of a stage,
 // lies in one page, and has one power of K and one of V.
 //   Both products are f16. One instruction makes two codes f16, exactly. Q is f16 times a
-//   power of two of its row, which holds bf16's eight bits whole down to 2^-24 of the row's
+//   power of two of its row, which holds bf16's eight bits whole down to 2^-31 of the row's
 //   largest value; P is f16, 11 bits of it, against the tile's own largest score and lifted by
 //   2^14, so that it reaches 2^-38 of the tile's largest probability. The power of K goes into the
 //   scale of the scores. That of V, and what the tile's largest probability is of the row's, which
@@ -362,10 +362,10 @@ __device__ __forceinline__ void stream_tiles(const AttnParams &P, RowsShared &sh
       bits = ::max(bits & 0xffffu, bits >> 16);
       bits = ::max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
       bits = ::max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
-      // the largest magnitude comes to lie in [2^7, 2^8); an infinity or a NaN makes the row's scores NaN
-      const int ex = ::max(int(bits >> 7), 8);
-      const float up = bits >= 0x7f80u ? 0.f : __uint_as_float(uint32_t(261 - ex) << 23);
-      rq[h] = bits >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float(uint32_t(ex - 7) << 23) * p.scale_log2;
+      // the largest magnitude comes to lie in [2^14, 2^15); an infinity or a NaN makes the row's scores NaN
+      const int ex = ::max(int(bits >> 7), 15);
+      const float up = bits >= 0x7f80u ? 0.f : __uint_as_float(uint32_t(268 - ex) << 23);
+      rq[h] = bits >= 0x7f80u ? __uint_as_float(0x7fffffffu) : __uint_as_float(uint32_t(ex - 14) << 23) * p.scale_log2;
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll

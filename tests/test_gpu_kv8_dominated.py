@@ -1,6 +1,7 @@
 """kv8_attention where a page weighs next to nothing beside others that the same warp has
 read: a page marked as not finite still makes the rows that see it NaN (0 x NaN is a NaN),
-and one whose V is that much larger still decides the result. Enough lists that each is one CTA's, so that its warps walk over several tiles; 4, 16, 36
+and one whose V is that much larger still decides the result. And where dimensions of Q are
+next to nothing beside others that no key has a part in. Enough lists that each is one CTA's, so that its warps walk over several tiles; 4, 16, 36
 and 80 rows of a KV head, on both sides of every change of kernel."""
 import numpy as np
 import pytest
@@ -92,4 +93,22 @@ def test_pages_of_little_weight_and_large_values(dreams, T, D, weight):
                     c.vals[0, 0, b, at, h] = R.decode(code[:, 0], es[0])
             scale_page(c, 1, b, e, 84 if (b, e) in heavy else -40)
     scale_tail(c, 1, -40)
+    c.check(c.run(dreams), n=6)
+
+
+@pytest.mark.parametrize("T", [1, 4, 9, 20])
+@pytest.mark.parametrize("D", [64, 128])
+def test_small_dimensions_of_q(dreams, T, D):
+    """Eight dimensions of Q that are up to 2^30.6 times the others, where K is zero: the others' eight bits make the scores.
+    (Whole down to 2^-24 of the largest alone, they would have two bits left, and the log-sum-exp be off by some thousandths.)"""
+    c = case(T + D, D, T)
+    c.q = torch.where(c.q < 0, -1.0, 1.0).to(c.q.dtype) * c.q.abs().clamp(min=0.5) * 2.0 ** -15
+    c.q[..., :8] = torch.where(c.q[..., :8] < 0, -1.5, 1.5) * 2.0 ** 14
+    c.k[..., :8] = 0.0
+    c.k8[..., :8] = 0
+    c.vals[0, ..., :8] = 0.0
+    for b in range(4):
+        for e in range(END // 64):
+            scale_page(c, 0, b, e, 15)
+    scale_tail(c, 0, 15)
     c.check(c.run(dreams), n=6)
