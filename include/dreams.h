@@ -496,7 +496,10 @@ dreams_status_t dreams_kv_release(const dreams_page_pool_t *pool, const int32_t 
  * page, and the pages reserved after it, without a copy. parent[i] == -1 empties
  * sequence i. Pages that no sequence holds any more are free afterwards, and may
  * be taken for the copies. new_kv_len[i] = kv_len[parent[i]] (0 when emptied; may
- * alias kv_len). kv is the cache of the pool (same table, page size 64). A call
+ * alias kv_len). kv is the cache of the pool (same table, page size 64), or NULL
+ * for a pool whose pages are all full (those of a dreams_kv8_cache_t): nothing is
+ * copied, a length that is no multiple of 64 is a bad one, and the call is one
+ * launch. A call
  * with a bad parent (BAD_INDEX), a bad length (BAD_KV_LEN), a table entry out of
  * range or missing for a partly filled page (BAD_PAGE) or too few free pages
  * (NO_PAGES) is flagged and changes nothing, with new_kv_len = kv_len. Two
@@ -618,8 +621,8 @@ dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer
  * two cost e4m3 no precision, and the attention works on the very values that are
  * stored). DREAMS_KV8_NOT_FINITE in place of a power: the values held an infinity
  * or a NaN; all 64 rows then count as NaN, whatever the codes. Codes 0x7f and 0xff
- * are not used. The pages have a table and a pool of their own (dreams_kv_reserve,
- * _release and _fork work on it; a fork takes lengths that are multiples of 64).
+ * are not used. The pages have a table and a pool of their own (dreams_kv_reserve
+ * and _release work on it, and _fork without a cache).
  * Slots 0 .. len8[b] - 1 of a sequence are here, len8[b] a multiple of 64; later
  * ones are in its bf16 cache, whose pages for slots below len8[b] can be given back.
  * k, v and layer_stride 16-byte aligned, exps 4-byte aligned.

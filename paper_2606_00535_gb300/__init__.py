@@ -313,8 +313,8 @@ class KV8Cache:
     ``exps`` int16 ``[num_pages, Hkv, 2]`` (likewise), the powers of two of K and
     V of each page and head, and their ``page_table`` int32 ``[B, pages_per_seq]``.
     A cached value is code * 2^exp; an exp of KV8_NOT_FINITE marks 64 rows that held
-    an infinity or a NaN. ``PagePool`` takes it like a ``KVCache``, with lengths in
-    multiples of 64."""
+    an infinity or a NaN. ``PagePool`` takes it like a ``KVCache``; ``kv_fork`` takes
+    lengths in multiples of 64 there."""
     k: torch.Tensor
     v: torch.Tensor
     exps: torch.Tensor
@@ -907,18 +907,21 @@ def kv_fork(pool: PagePool, parent: torch.Tensor, kv_len: torch.Tensor, new_kv_l
             stream=None) -> torch.Tensor:
     """Sequence i becomes a copy of what sequence parent[i] was (-1: empty),
     for all at once: full pages are shared, the partly filled last page is copied
-    in all layers. Returns the new lengths."""
+    in all layers. The pages of a ``KV8Cache`` are full: a length that is no multiple
+    of 64 is flagged there (DATA_BAD_KV_LEN) and changes nothing. Returns the new
+    lengths."""
     dev = pool.refcount.device
     par, kl = _per_seq(parent, "parent", pool.B, dev), _per_seq(kv_len, "kv_len", pool.B, dev)
     if new_kv_len is None:
         new_kv_len = _new(pool.B, torch.int32, dev, stream)
     ws, ws_bytes = _scratch(pool, workspace, dev, stream)
-    _launch("dreams_kv_fork", dev, stream, ctypes.byref(pool.kv._c), ctypes.byref(pool._c), par, kl,
+    cache = ctypes.byref(pool.kv._c) if isinstance(pool.kv, KVCache) else None
+    _launch("dreams_kv_fork", dev, stream, cache, ctypes.byref(pool._c), par, kl,
             _per_seq(new_kv_len, "new_kv_len", pool.B, dev), ws, ws_bytes, _status(status, dev))
     return new_kv_len
 
 
-KV_FORK_LAUNCHES = 2  # the table and counts, then the copies of partly filled pages
+KV_FORK_LAUNCHES = 2  # the table and counts, then the copies of partly filled pages (none of a KV8Cache)
 
 
 def kv_append(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, kv_len: torch.Tensor, n_new: torch.Tensor,

@@ -225,7 +225,7 @@ __device__ __forceinline__ void cluster_sync() {
 template <int CTAS>
 __global__ void __launch_bounds__(BOOK_THREADS)
     kv_fork_table_kernel(const Pool p, const int32_t *parent, const int32_t *kv_len, int32_t *new_kv_len,
-                         const ForkState f, int32_t *status) {
+                         const ForkState f, bool full_pages, int32_t *status) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   after_previous();
   __shared__ int s_warp[32], s_bad;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(BOOK_THREADS)
         q = -1;
       }
       const int L = q < 0 ? 0 : __ldcg(kv_len + q);
-      if (L < 0 || L > int64_t(p.P) * PAGE) bad |= DREAMS_DATA_BAD_KV_LEN;
+      if (L < 0 || L > int64_t(p.P) * PAGE || (full_pages && L % PAGE != 0)) bad |= DREAMS_DATA_BAD_KV_LEN;
       if (q >= 0) atomicMin(first + q, i);
       len[i] = L;
       par[i] = q;
@@ -673,18 +673,19 @@ extern "C" dreams_status_t dreams_kv_fork(const dreams_kv_cache_t *kv, const dre
                                           dreams_stream_t stream) {
   Pool p;
   Cache c;
-  if (!pool_ok(pool, p) || !cache_ok(kv, c) || parent == nullptr || kv_len == nullptr || new_kv_len == nullptr ||
+  const bool full_pages = kv == nullptr;  // there is nothing to copy
+  if (!pool_ok(pool, p) || (!full_pages && !cache_ok(kv, c)) || parent == nullptr || kv_len == nullptr || new_kv_len == nullptr ||
       !aligned4(parent) || !aligned4(kv_len) || !aligned4(new_kv_len))
     return DREAMS_ERR_INVALID_ARG;
-  if (c.table != p.table || c.P != p.P || c.num_pages != p.num_pages) return DREAMS_ERR_INVALID_ARG;
+  if (!full_pages && (c.table != p.table || c.P != p.P || c.num_pages != p.num_pages)) return DREAMS_ERR_INVALID_ARG;
   if (workspace == nullptr || !aligned16(workspace) || workspace_bytes < dreams_kv_fork_workspace_size(pool))
     return DREAMS_ERR_WORKSPACE;
   ForkState f;
   fork_layout(p, static_cast<uint8_t *>(workspace), &f);
   const bool one = int64_t(p.B) * p.P <= FORK_ONE_CELLS;
   const dreams_status_t st = launch(early_launch(), one ? kv_fork_table_kernel<1> : kv_fork_table_kernel<FORK_CTAS>, dim3(one ? 1 : FORK_CTAS), BOOK_THREADS, 0,
-                                    one ? 1 : FORK_CTAS, stream, p, parent, kv_len, new_kv_len, f, status_word);
-  if (st != DREAMS_OK) return st;
+                                    one ? 1 : FORK_CTAS, stream, p, parent, kv_len, new_kv_len, f, full_pages, status_word);
+  if (st != DREAMS_OK || full_pages) return st;
   const int pieces = (PAGE * c.row16 + COPY_PIECE - 1) / COPY_PIECE;
   const int64_t most = int64_t(p.B) * c.n_layers * 2 * pieces;
   return launch(early_launch(), kv_fork_copy_kernel, dim3(unsigned(std::min<int64_t>(most, int64_t(num_sms()) * 8))), 256, 0, 1, stream, c, f, pieces);
