@@ -343,10 +343,6 @@ class KV8Cache:
         self._c8 = _KV8Cache(self.k.data_ptr(), self.v.data_ptr(), self.exps.data_ptr(), self.n_layers,
                              self.layer_stride, self.Hkv, self.D, self.page_table.data_ptr(), self.pages_per_seq,
                              self.num_pages)
-        # the same pages as kv_fork takes them: rows of half as many 16-bit values
-        self._c = _KVCache(self.k.data_ptr(), self.v.data_ptr(), self.n_layers, self.layer_stride // 2, self.Hkv,
-                           self.D // 2, self.capacity, self.page_table.data_ptr(), 64, self.pages_per_seq,
-                           self.num_pages)
 
 
 KV8_NOT_FINITE = 32767  # in place of a power: the page's values of that head held an infinity or a NaN
@@ -411,8 +407,10 @@ VERIFY_STEP_SAMPLED_LAUNCHES = 3  # draw statistics, draw selection, walk + comp
 
 
 def _cache_covers(kv: "KVCache", B: int, D: Optional[int] = None) -> None:
-    """The cache holds (at least) the B sequences a call reads or writes, with
-    head dim D when given."""
+    """The cache is one of bf16 rows and holds (at least) the B sequences a call reads
+    or writes, with head dim D when given."""
+    if not isinstance(kv, KVCache):
+        raise TypeError(f"the call takes a KVCache, got {type(kv).__name__}")
     if kv.B < B:
         raise ValueError(f"the KV cache holds {kv.B} sequences, the call addresses {B}")
     if D is not None and kv.D != D:
@@ -1174,6 +1172,8 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
 
 
 def _both_caches(kv8: KV8Cache, kv: KVCache, B: int) -> None:
+    if not isinstance(kv8, KV8Cache):
+        raise TypeError(f"the call takes a KV8Cache, got {type(kv8).__name__}")
     if kv8.k.device != kv.k.device:
         raise ValueError(f"the 8-bit cache is on {kv8.k.device}, the bf16 one on {kv.k.device}")
     if kv8.n_layers != kv.n_layers or kv8.Hkv != kv.Hkv or kv8.D != kv.D:
