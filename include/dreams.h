@@ -648,7 +648,7 @@ typedef struct dreams_kv8_cache {
  * power with max |x| <= 448 * 2^exp, not below -96 nor above 119 (above 448 * 2^119
  * values become that), and a code is x / 2^exp rounded to nearest even. Pages of kv8 for
  * them have to be there (dreams_kv_reserve) and belong to the sequence alone. new_len8[b]
- * (not the same array as begin or end) = the end of the last page done, begin[b] where
+ * (an array that overlaps neither begin nor end) = the end of the last page done, begin[b] where
  * there is none. begin[b] < 0 or no multiple of 64, end[b] < begin[b] or beyond either
  * cache flags BAD_KV_LEN, skips the sequence and gives new_len8 = begin. A page that is
  * missing in either cache is flagged BAD_PAGE and skipped; new_len8[b] then ends before

@@ -173,6 +173,13 @@ __global__ void __launch_bounds__(THREADS, RESIDENT<D>) kv_quantize_kernel(const
   }
 }
 
+// Blocks read begin and end while others write new lengths: read twice, an overwritten
+// begin would lead behind the table's row.
+bool apart(const int32_t *x, const int32_t *y, int n) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y), bytes = uintptr_t(n) * 4;
+  return a + bytes <= b || b + bytes <= a;
+}
+
 }  // namespace
 }  // namespace dreams
 
@@ -182,7 +189,7 @@ extern "C" dreams_status_t dreams_kv_quantize(const dreams_kv_cache_t *kv, const
                                               const int32_t *end, int32_t *new_len8, int32_t *status_word, dreams_stream_t stream) {
   Cache c;
   if (!cache_ok(kv, c) || !kv8_ok(kv8) || B < 1 || B > 65535 || begin == nullptr || end == nullptr || new_len8 == nullptr || !aligned4(begin) ||
-      !aligned4(end) || !aligned4(new_len8) || new_len8 == begin || new_len8 == end || kv8->n_layers != kv->n_layers || kv8->Hkv != kv->Hkv ||
+      !aligned4(end) || !aligned4(new_len8) || !apart(new_len8, begin, B) || !apart(new_len8, end, B) || kv8->n_layers != kv->n_layers || kv8->Hkv != kv->Hkv ||
       kv8->D != kv->D)
     return DREAMS_ERR_INVALID_ARG;
   // (a block counts the pages of THREADS sequences in 32 bits)
