@@ -1013,10 +1013,13 @@ class Rotary:
         ``factor`` times as long:
           none, linear   f, f / factor (positions interpolated)
           ntk            the base times factor^(rot_dim / (rot_dim - 2)): the fastest
-                         pair as it was, the slowest ``factor`` times slower
+                         pair as it was, the slowest ``factor`` times slower (not with
+                         ``frequencies``, which have no base)
           yarn           pairs that turn more than ``fast`` times over ``original``
                          positions keep f, those below ``slow`` take f / factor,
-                         linearly between; cos and sin times 0.1 ln(factor) + 1
+                         linearly in the turns between (a checkpoint whose ramp is
+                         linear in the pair's index: its own ``frequencies``, with
+                         ``gain``); cos and sin times 0.1 ln(factor) + 1
         ``gain`` sets that multiplier of cos and sin instead."""
         if rot_dim < 2 or rot_dim % 2:
             raise ValueError("rot_dim must be even and positive")
@@ -1030,6 +1033,8 @@ class Rotary:
             raise ValueError("yarn needs original > 0 and fast > slow")
         n = rot_dim // 2
         if scaling == "ntk":
+            if frequencies is not None:
+                raise ValueError("ntk scales the base: with frequencies it has nothing to scale")
             if rot_dim == 2:
                 raise ValueError("ntk needs more than one pair")
             base = base * factor ** (rot_dim / (rot_dim - 2))
