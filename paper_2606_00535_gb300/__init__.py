@@ -1093,6 +1093,24 @@ def _positions(positions: torch.Tensor, B: int, T: int, dev) -> Tuple[int, int]:
     return positions.data_ptr(), s[0]
 
 
+class _Rope(torch.autograd.Function):
+    """rope of an x that takes part in autograd: the gradient is the transposed turn. What the
+    turn depends on is saved, so that autograd notices where torch has changed it since."""
+
+    @staticmethod
+    def forward(ctx, x, rotary, positions, start, transpose, status, stream):
+        ctx.save_for_backward(positions, start, rotary.phase, rotary.axis)
+        ctx.rotary, ctx.transpose = rotary, transpose
+        return rope(x, rotary, positions, start, transpose, None, status, stream)
+
+    @staticmethod
+    def backward(ctx, g):
+        positions, start, _, _ = ctx.saved_tensors
+        if g.stride(-1) != 1:  # (a sum's gradient is one value, spread)
+            g = g.contiguous()
+        return rope(g, ctx.rotary, positions, start, not ctx.transpose), None, None, None, None, None, None
+
+
 def rope(x: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = None,
          start: Optional[torch.Tensor] = None, transpose: bool = False, out: Optional[torch.Tensor] = None,
          status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -1100,9 +1118,15 @@ def rope(x: torch.Tensor, rotary: Rotary, positions: Optional[torch.Tensor] = No
     rows) by their positions: ``positions`` (int32 [B, T] or [n_axes, B, T]), or
     ``start`` (int32 [B]) + t, or t. ``transpose``: by the transposed map, which is
     the gradient with respect to x of an output's (and with factor 1 the inverse).
-    Returns ``out``, which may be ``x``."""
+    Returns ``out``, which may be ``x``. Where x requires a gradient the result has one,
+    and ``out`` is refused: it takes no part in autograd (nor do the results of the
+    calls on the cache)."""
     if not isinstance(x, torch.Tensor) or x.dim() != 4 or (dtype := x.dtype) not in _ROPE_TYPES:
         raise TypeError("x must be a 4-D bfloat16 or float32 tensor [B, T, H, D]")
+    if x.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            raise ValueError("x requires a gradient, which does not go through out: call without it, or under torch.no_grad()")
+        return _Rope.apply(x, rotary, positions, start, transpose, status, stream)
     dev = x.device
     B, T, H, D = x.shape
     sb, stt, sh, sd = x.stride()
