@@ -3,7 +3,6 @@
 #include <atomic>
 #include <mutex>
 #include <map>
-#include <set>
 #include <utility>
 
 #include "common.cuh"
@@ -16,7 +15,6 @@ std::mutex g_sm_mutex;
 int g_sm_count[64] = {0};
 std::mutex g_attr_mutex;
 std::map<std::pair<const void *, int>, int> g_attr_done;  // (kernel, device) -> the largest limit set
-std::set<std::pair<const void *, int>> g_wide_done;       // (kernel, device) that may launch wide clusters
 constexpr uint64_t DEFAULT_WAIT_NS = 2000000000ull;
 std::atomic<int32_t> g_stall_kernels{0};
 std::atomic<int32_t> g_stall_at{-1};
@@ -63,22 +61,6 @@ dreams_status_t ensure_max_dynamic_smem(const void *func, int bytes) {
     return DREAMS_ERR_CUDA;
   }
   g_attr_done[{func, dev}] = bytes;
-  return DREAMS_OK;
-}
-
-dreams_status_t ensure_wide_clusters(const void *func) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) {
-    std::lock_guard<std::mutex> lock(g_attr_mutex);
-    if (g_wide_done.count({func, dev}) != 0) return DREAMS_OK;
-    e = cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) g_wide_done.insert({func, dev});
-  }
-  if (e != cudaSuccess) {
-    set_last_cuda_error(e);
-    return DREAMS_ERR_CUDA;
-  }
   return DREAMS_OK;
 }
 

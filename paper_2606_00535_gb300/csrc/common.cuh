@@ -21,10 +21,6 @@ int num_sms();
 // to call from several host threads.
 dreams_status_t ensure_max_dynamic_smem(const void *func, int bytes);
 
-// Lets a kernel be launched on the current device in clusters of 16 CTAs (asked for
-// once per kernel and device); safe to call from several host threads.
-dreams_status_t ensure_wide_clusters(const void *func);
-
 // The stall test hook (dreams_test_set_stall) as it applies to one kernel
 // family: the index of the first withheld copy (-1: none) and the limit of
 // every pipeline wait (2 s unless the hook shortens it).

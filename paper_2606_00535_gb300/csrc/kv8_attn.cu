@@ -838,7 +838,7 @@ dreams_status_t launch_rows(AttnParams P, cudaStream_t stream) {
   const int64_t fit = int64_t(Cfg8<D, FOLD>::PER_SM) * num_sms();
   P.p.nsplit = split_of(fit, P.p.B, lists, std::min<int64_t>(P.p.capacity, int64_t(P.p.window) - 1 + P.p.T_max + P.p.sinks));
   P.ranked = P.p.B > 1 && P.p.B <= MAX_RANKED && lists * P.p.nsplit > fit;
-  return launch_lists(early_launch(), kv8_rows_kernel<D, FOLD>, Cfg8<D, FOLD>::SMEM, lists, P.p.nsplit, stream, P);
+  return launch_lists<kv8_rows_kernel<D, FOLD>>(early_launch(), Cfg8<D, FOLD>::SMEM, lists, P.p.nsplit, stream, P);
 }
 
 }  // namespace

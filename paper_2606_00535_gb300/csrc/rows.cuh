@@ -169,13 +169,26 @@ __device__ __forceinline__ void finish_rows(const WinParams &p, RowsShared &sh, 
 
 // ------------------------------------------------------------------ host side
 // One CTA, or a cluster of nsplit, to each of `lists` key lists.
-template <typename Params>
-dreams_status_t launch_lists(cudaLaunchAttribute first, void (*kernel)(const Params), int smem, int64_t lists, int nsplit, cudaStream_t stream, Params p) {
-  const dreams_status_t st = ensure_max_dynamic_smem(reinterpret_cast<const void *>(kernel), smem);
+template <auto KERNEL, typename Params>
+dreams_status_t launch_lists(cudaLaunchAttribute first, int smem, int64_t lists, int nsplit, cudaStream_t stream, Params p) {
+  const void *kernel = reinterpret_cast<const void *>(KERNEL);
+  const dreams_status_t st = ensure_max_dynamic_smem(kernel, smem);
   if (st != DREAMS_OK) return st;
-  // clusters of 16 have to be asked for
-  const dreams_status_t wide = ensure_wide_clusters(reinterpret_cast<const void *>(kernel));
-  if (wide != DREAMS_OK) return wide;
+  if (nsplit > 8) {
+    // clusters of 16 have to be asked for, once per device; without a lock, as single tokens'
+    // calls are bound by the host
+    static std::atomic<uint64_t> wide{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev >= 64 || !((wide.load() >> dev) & 1u))) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e == cudaSuccess && dev < 64) wide.fetch_or(uint64_t(1) << dev);
+    }
+    if (e != cudaSuccess) {
+      set_last_cuda_error(e);
+      return DREAMS_ERR_CUDA;
+    }
+  }
   if (lists * nsplit > INT_MAX) return DREAMS_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(lists * nsplit));
@@ -189,7 +202,7 @@ dreams_status_t launch_lists(cudaLaunchAttribute first, void (*kernel)(const Par
   cfg.attrs = attr;
   cfg.numAttrs = nsplit > 1 ? 2 : 1;
   void *args[] = {&p};
-  const cudaError_t e = cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(kernel), args);
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, args);
   if (e != cudaSuccess) {
     set_last_cuda_error(e);
     return DREAMS_ERR_CUDA;

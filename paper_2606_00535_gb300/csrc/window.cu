@@ -359,7 +359,7 @@ int split_of(int64_t lists, int64_t keys) {
 template <int D, bool FOLD>
 dreams_status_t launch_rows(WinParams p, cudaStream_t stream) {
   p.nsplit = split_of(int64_t(p.B) * p.Hkv, std::min<int64_t>(p.capacity, int64_t(p.window) - 1 + p.T_max + p.sinks));
-  return launch_lists(early_launch(), window_rows_kernel<D, FOLD>, RowsCfg<D>::SMEM, int64_t(p.B) * p.Hkv, p.nsplit, stream, p);
+  return launch_lists<window_rows_kernel<D, FOLD>>(early_launch(), RowsCfg<D>::SMEM, int64_t(p.B) * p.Hkv, p.nsplit, stream, p);
 }
 
 }  // namespace
