@@ -552,8 +552,10 @@ dreams_status_t dreams_kv_prune(const dreams_kv_cache_t *kv, int32_t B, const in
  *            angle at any position is then one integer product, exact however far
  *            the position; scalings for long contexts are other phases.
  *   axis     device [n_pairs], or NULL (all 0): which of a call's position axes a
- *            pair goes by (visual tokens: time, row, column). A value that is no
- *            axis of the call is flagged DREAMS_DATA_BAD_INDEX and counts as 0.
+ *            pair goes by (visual tokens: time, row, column). Looked at where a call
+ *            has positions (without them a token has one position on all axes): a
+ *            value that is no axis of the call is flagged DREAMS_DATA_BAD_INDEX and
+ *            counts as 0.
  *   layout   DREAMS_ROPE_HALF: pair i is dimensions (i, i + n_pairs);
  *            DREAMS_ROPE_INTERLEAVED: (2 i, 2 i + 1)
  *   factor   finite; the cosines and sines are multiplied by it
@@ -600,7 +602,9 @@ dreams_status_t dreams_rope(const void *x, int64_t x_stride_b, int64_t x_stride_
  * q itself where q is dense. All are 16-byte aligned and overlap neither the cache
  * nor, but for that, each other. Positions: positions ([n_axes, B, T_max]); or
  * parent ([B, T_max], T_max <= 64): the rows are the nodes of a draft tree, node t
- * at kv_len[b] + its depth; or neither (both NULL, n_axes 1): kv_len[b] + t.
+ * at kv_len[b] + its depth; or neither (both NULL, n_axes 1): kv_len[b] + t. Where a
+ * token's position is not its slot (after dreams_kv_prune, or behind a prompt with
+ * several axes) positions have to be given, those of a tree's nodes too.
  * kv->D any multiple of 8 up to 512. Rows t >= n_new[b] of q_out are left
  * untouched. Bad lengths (BAD_KV_LEN) or a bad tree (BAD_PARENT; its first n_new[b]
  * entries) skip the sequence; a slot whose page is missing is skipped (BAD_PAGE),
@@ -621,7 +625,7 @@ dreams_status_t dreams_kv_append_rope(const dreams_kv_cache_t *kv, int32_t layer
  * two cost e4m3 no precision, and the attention works on the very values that are
  * stored). DREAMS_KV8_NOT_FINITE in place of a power: the values held an infinity
  * or a NaN; all 64 rows then count as NaN, whatever the codes. Codes 0x7f and 0xff
- * are not used. The pages have a table and a pool of their own (dreams_kv_reserve
+ * are in such pages alone. The pages have a table and a pool of their own (dreams_kv_reserve
  * and _release work on it, and _fork without a cache).
  * Slots 0 .. len8[b] - 1 of a sequence are here, len8[b] a multiple of 64; later
  * ones are in its bf16 cache, whose pages for slots below len8[b] can be given back.
@@ -664,10 +668,13 @@ dreams_status_t dreams_kv_quantize(const dreams_kv_cache_t *kv, const dreams_kv8
  * s < len8[b] is read from kv8, any other from kv (contiguous or paged). Everything
  * else is as there: causal queries and draft trees, window (INT32_MAX: every slot is
  * seen) and sinks, lengths, bad data and untouched rows, finite values up to 2^87 in
- * magnitude, the roundings. len8[b] < 0, no multiple of 64, above kv_len[b] or above
+ * magnitude, the roundings; but up to 32 rows of a KV head (64 with D 64) probabilities
+ * enter P V over 8-bit pages with 11 bits, and Q loses bits below 2^-31 of a row's
+ * largest value. len8[b] < 0, no multiple of 64, above kv_len[b] or above
  * kv8's capacity flags BAD_KV_LEN and skips the sequence. A visible slot whose page
  * is missing in the cache that holds it is flagged BAD_PAGE and reads as zeros. Rows
- * that see a page marked DREAMS_KV8_NOT_FINITE become NaN, others do not. One launch,
+ * that see a page marked DREAMS_KV8_NOT_FINITE become NaN, however little it weighs,
+ * others do not. One launch,
  * no workspace.
  */
 dreams_status_t dreams_kv8_attention(const void *q, int64_t q_stride_b, int64_t q_stride_t,

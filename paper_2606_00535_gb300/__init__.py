@@ -979,7 +979,7 @@ class Rotary:
     number): how far a pair turns per position, in turns times 2^64; ``layout``
     ROPE_HALF (pairs (i, i + n_pairs)) or ROPE_INTERLEAVED ((2 i, 2 i + 1));
     ``factor`` multiplies the cosines and sines; ``axis`` (int32 [n_pairs], or
-    None): the position axis each pair goes by. ``Rotary.make`` works the phases out."""
+    None): the position axis each pair goes by where positions are given. ``Rotary.make`` works the phases out."""
     phase: torch.Tensor
     layout: int = ROPE_HALF
     factor: float = 1.0
@@ -1161,7 +1161,9 @@ def kv_append_rope(kv: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, rotary
     go to slots kv_len .. kv_len + n_new - 1 of one layer, and turned rows of ``q``
     (bf16 [B, T_max, Hq, D]) to ``q_out`` (dense; may be ``q``), which is returned.
     Positions: ``positions`` (int32 [B, T_max] or [n_axes, B, T_max]); or
-    ``parent`` (int32 [B, T_max]): kv_len + a tree node's depth; or kv_len + t."""
+    ``parent`` (int32 [B, T_max]): kv_len + a tree node's depth; or kv_len + t. Where a
+    token's position is not its slot (after ``kv_prune``, or behind a prompt with several
+    axes) ``positions`` have to be given, those of a tree's nodes too."""
     dev = kv.k.device
     B, T_max, Hkv, D, kb, kt = _rows(k_new, "k_new", "Hkv")
     vB, vT, vH, vD, vb, vt = _rows(v_new, "v_new", "Hkv")

@@ -6,8 +6,9 @@
 
 namespace dreams {
 
-// Powers that are used: below the lowest a value counts as zero, above the highest
-// bf16 would end. (P 2^exp still is a normal number for probabilities down to 2^-30.)
+// Powers that are used. A code, 2^-9 to 448, times its power is a normal and finite bf16 at
+// both ends, as the kernel for blocks makes it. A page of smaller values loses those below
+// half of 2^-9 2^EXP_MIN; larger ones become 448 2^EXP_MAX.
 constexpr int EXP_MIN = -96, EXP_MAX = 119;
 
 struct Kv8 {

@@ -5,7 +5,8 @@
 // second block finds in L2. 8 sequences of 1000 to 8000 tokens, 8 KV heads, in us, here and
 // there (in brackets: all of 4000): 20 rows 43.2 and 65.9 (42.6 and 40.9), 48 rows 55.1 and
 // 67.4 (67.9 and 43.1), 64 rows 68.2 and 67.3; head dim 64, 48 rows 40.3 and 59.1 (49.2 and
-// 36.6), 64 rows 50.4 and 59.1, 80 rows 70.4 and 60.2. (One CTA for both blocks of 32 rows, K
+// 36.6), 64 rows 50.4 and 59.1, 80 rows 70.4 and 60.2: the border lies where spread lengths gain more than
+// equal ones lose. (One CTA for both blocks of 32 rows, K
 // and V read once: 59.5 against 55.0, before scores were f16 products.)
 //
 // Few rows (single tokens, short drafts), bound by reading K and V once. As in window.cu, a
@@ -821,7 +822,9 @@ __global__ void __launch_bounds__(32 * WARPS, D == 128 ? 0 : Cfg8<D, FOLD>::PER_
 //   8           14.0   14.4  (r)18.9  (r)56.7   (r)114.2   (r)228.2     (r)451.1 (r)386.3
 //   16          11.2   16.4  (r)40.6  (r)84.9   (r)168.6   (r)335.2     (r)651.0 (r)777.1
 // The price: lists of equal length that a split makes more than fit (19 sequences of 16384:
-// 142 us for 108). The ranks cost every CTA a pass over the lengths and B comparisons for
+// 142 us for 108). And keys are counted by the tables' capacity, as the lengths are on the
+// device: 16 sequences of 500 tokens, 8 KV heads, take 10.7 us in tables of their length and
+// 17.3 in tables of 32768 slots (one sequence of 2000 7.1 in both). The ranks cost every CTA a pass over the lengths and B comparisons for
 // each of them, nothing where the lengths are alike: 128 sequences at most.
 constexpr int MAX_SPLIT = 16;
 int split_of(int64_t fit, int B, int64_t lists, int64_t keys) {

@@ -3,8 +3,9 @@
 //
 // Pair (u, v) of a head's dimensions is turned by the angle a = 2 pi p f of its
 // token's position p. f comes as a 64-bit fraction of a turn, so p f modulo one turn
-// is one integer product, whose upper 32 bits give a within 2^-31 pi at any position;
-// a position times an f32 frequency is off by 0.06 radians at a million. cos and sin are
+// is one integer product, whose upper 32 bits, rounded to f32, give a within 2^-25 pi at
+// any position (24 bits of up to half a turn); a position times an f32 frequency is off by
+// 0.06 radians at a million. cos and sin are
 // sincospif of it, f32 like the products, and the result is rounded once.
 //
 // Bound by HBM (each row read and written once), or by latency for few tokens. A
@@ -15,7 +16,8 @@
 // 3392 tokens of 32 heads of 128 dimensions, bf16: 11.3 us, 74% of the copy rate (from L2,
 // which holds both sides, and with launch, angles and tail in it); rows of 16 chunks of up
 // to 2048 tokens with 32 and 8 heads on their way into the cache: 94.6 us, 95% of it; one
-// token of 28 heads 1.6 us, appended 2.3 us.
+// token of 28 heads 1.6 us, appended 2.3 us. Rows that are no whole 16-byte pieces go value by
+// value: the same 3392 tokens with 24 of 96 dimensions turned 11.6 us, 32 of 96 9.6.
 #include <limits.h>
 #include <math.h>
 
